@@ -18,6 +18,9 @@
  *   ordermoe_local_moe_forward  execution of the selected (server, expert)
  *                               pairs of one server (Algorithm 2, "execute
  *                               token q on S_m* by expert k*")
+ *   ordermoe_cache_write, ordermoe_cache_read, ordermoe_draft_attention
+ *                               the attention half of a decode step, over a
+ *                               quantised paged cache
  *
  * Conventions
  *   - Every entry point returns ORDERMOE_OK (0) or a negative status code and
@@ -471,6 +474,118 @@ int ordermoe_pack_gate_up(int32_t dtype, int32_t n, int32_t f, int32_t d, const 
                           const void* w_up, void* out, void* stream);
 int ordermoe_pack_down(int32_t dtype, int32_t n, int32_t d, int32_t f, const void* w_down, void* out,
                        void* stream);
+
+/* ------------------------------------------------------------------------
+ * Attention half of a decode step: a quantised, paged cache of keys and values,
+ * the step's rows written to it, rows read back, and the attention of drafted
+ * tokens over it.
+ *
+ * The cache holds 8-bit codes and one fp32 scale per (slot, head); an element
+ * stands for code * scale.  Page p holds slots [p page_size, (p + 1) page_size),
+ * for every head the rows of its slots side by side.
+ *   INT8  two's complement codes in [-127, 127], scale = largest |x| / 127
+ *   FP8   e4m3 codes (4 exponent bits, bias 7, 3 fraction bits, largest 448),
+ *         scale = largest |x| / 448
+ * code = x / scale rounded to nearest, ties to even, both in fp32 with IEEE
+ * division.  A row whose largest magnitude is below 2^-100 is stored as zeros
+ * (codes and scale), a row with an infinity or a NaN as codes 0 with scale NaN:
+ * no written code is a NaN, so what one row holds never reaches another.
+ */
+#define ORDERMOE_CACHE_INT8 0
+#define ORDERMOE_CACHE_FP8 1
+#define ORDERMOE_MAX_DRAFT 64     /* drafted tokens of one sequence in one call */
+
+typedef struct {
+    int32_t format;         /* ORDERMOE_CACHE_INT8 or ORDERMOE_CACHE_FP8 */
+    int32_t n_kv;           /* key/value heads, >= 1 */
+    int32_t head_dim;       /* 64, 128 or 256 */
+    int32_t page_size;      /* slots of a page: a power of two from 16 to 1024 */
+    int64_t n_pages;
+    uint8_t* k_codes;       /* dev [n_pages][n_kv][page_size][head_dim], 16-byte aligned */
+    uint8_t* v_codes;       /* dev, the same */
+    float* k_scale;         /* dev [n_pages][n_kv][page_size], 16-byte aligned */
+    float* v_scale;         /* dev, the same */
+} ordermoe_cache;
+
+typedef struct {
+    int32_t dtype;          /* storage of q, k, v, q_out and the norm weights */
+    int32_t n_q;            /* query heads, a multiple of the cache's n_kv */
+    int32_t rotary_dim;     /* leading elements of a head that are turned: 0 to head_dim, a multiple of head_dim / 8 */
+    int32_t interleaved;    /* 1: elements 2i and 2i + 1 turn together; 0: i and i + rotary_dim / 2 */
+    int64_t max_pos;        /* rows of cos_sin */
+    float eps;              /* of the norms, >= 0 */
+    const void* q_norm;     /* dev [head_dim] weights of the query norm, or NULL: no query norm */
+    const void* k_norm;     /* dev [head_dim] weights of the key norm, or NULL: no key norm */
+    const float* cos_sin;   /* dev [max_pos][rotary_dim]: per position the cosines of the rotary_dim / 2
+                               angles, then their sines; NULL if rotary_dim = 0 */
+} ordermoe_heads;
+
+/* Rows of T new tokens: the RMS norm of every query and key head, the rotation
+ * by the token's position, and the keys and values quantised into the cache, in
+ * one pass.  Per head row x, in fp32:
+ *   n = x / sqrt(mean(x^2) + eps) * weight        (where the norm has weights)
+ *   (a, b) -> (a cos - b sin, b cos + a sin)      for each turned pair
+ * The queries are rounded once to the storage type, the keys go from fp32 to
+ * their codes; values are neither normed nor turned.
+ *   q, k, v   dev: head h of token t starts at t * stride + h * head_dim elements
+ *             (n_q, n_kv, n_kv heads; parts of one array of QKV rows, or arrays of
+ *             their own).  16-byte aligned, strides multiples of 16 bytes and
+ *             at least the heads' elements.
+ *   pos       dev [T] int32 position of each token (NULL if rotary_dim = 0); one
+ *             outside [0, max_pos) makes the token's queries and keys NaN
+ *   slots     dev [T] int64 cache slot of each token, distinct; a token whose slot is
+ *             outside [0, n_pages * page_size) is not written (its queries are)
+ *   q_out     dev [T][n_q][head_dim], may not overlap the inputs
+ * T >= 0 with T * (n_q + 2 n_kv) < 2^31.  No workspace; the work is ordered on
+ * `stream`.  EINVAL, EDTYPE as above. */
+int ordermoe_cache_write(const ordermoe_cache* C, const ordermoe_heads* H, const void* q, int64_t q_stride,
+                         const void* k, int64_t k_stride, const void* v, int64_t v_stride, int64_t T,
+                         const int32_t* pos, const int64_t* slots, void* q_out, void* stream);
+
+/* Rows of the cache as the values they stand for: k_out, v_out dev
+ * [n][n_kv][head_dim] of storage `dtype`, 16-byte aligned, row i from slots[i]
+ * (dev int64; any order, repeats allowed; zeros for a slot outside the cache);
+ * code * scale in fp32, rounded once.  n >= 0 with 2 n n_kv < 2^31. */
+int ordermoe_cache_read(const ordermoe_cache* C, int32_t dtype, const int64_t* slots, int64_t n, void* k_out,
+                        void* v_out, void* stream);
+
+/* Attention of drafted tokens over the cache.  Sequence b holds tokens
+ * [q_start[b], q_start[b + 1]) of q, n_b of them (0 to max_q), and ctx_len[b]
+ * cached tokens before them.  Position p of the sequence lies in slot
+ * page_table[b][p / page_size] * page_size + p % page_size; the n_b new tokens
+ * have positions ctx_len[b] .. ctx_len[b] + n_b - 1 and are in the cache too
+ * (ordermoe_cache_write).  Query head h reads key/value head h / (n_q / n_kv).
+ * Token i of a sequence sees position p if p < ctx_len, or if bit p - ctx_len of
+ * its word in `tree` is set (no bit is implied, its own included); with tree =
+ * NULL the tokens are a chain and token i sees ctx_len .. ctx_len + i.  Then
+ *   s_p = scale * q . k_p,   out = sum_p exp(s_p) v_p / sum_p exp(s_p),
+ *   lse = log sum_p exp(s_p)                          over the seen positions;
+ * a token that sees nothing gets out = 0 and lse = -infinity.  What the cache
+ * holds at unseen positions, and past a sequence's end, has no effect.
+ * bf16: q times the codes with fp32 sums, statistics in fp32, the weights
+ * exp(s - max) * v_scale rounded to bf16 for the product with the codes of V,
+ * fp32 sums, rounded once.  fp32: fp32 throughout.
+ *   q        dev [T][n_q][head_dim] of storage `dtype`, 16-byte aligned (as out)
+ *   q_start  dev [B + 1] int32, not decreasing, within [0, T]
+ *   ctx_len  dev [B] int32, >= 0
+ *   page_table dev [B][max_pages] int32; entries past a sequence's pages are not
+ *            read; positions in a page outside [0, n_pages), or past the table,
+ *            are unseen
+ *   tree     dev [T] uint64, or NULL
+ *   out      dev [T][n_q][head_dim]; lse dev [T][n_q] fp32, or NULL.  Rows of
+ *            tokens in no sequence, or past a sequence's first max_q, are not written.
+ *   ws       dev, of the size below: partial results of sequences whose cache is
+ *            split over workgroups (joined in a fixed order: results are the same
+ *            on every run); in use until the stream passes the call
+ * 1 <= max_q <= ORDERMOE_MAX_DRAFT (an upper bound of n_b), 0 <= B <= 65535,
+ * max_pages >= 1, max_pages * page_size < 2^31, n_q <= 1024, scale finite.  The lengths are
+ * read on the device; the call does not synchronise. */
+size_t ordermoe_draft_attention_workspace_size(const ordermoe_cache* C, int32_t dtype, int32_t n_q, int32_t B,
+                                               int32_t max_q);
+int ordermoe_draft_attention(const ordermoe_cache* C, int32_t dtype, int32_t n_q, const void* q, int64_t T, int32_t B,
+                             int32_t max_q, const int32_t* q_start, const int32_t* ctx_len,
+                             const int32_t* page_table, int32_t max_pages, const uint64_t* tree, float scale,
+                             void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * Kernel timing (measurement support, off by default).

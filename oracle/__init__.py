@@ -16,6 +16,8 @@ Modules and the passages they follow:
                  per-step cost (eq 37-38), transitions and look-ahead (eq 41-42)
   layer       -- per-token selection (eq 36-44, Alg. 2 for one layer, in
                  select.c), dispatch list (eq 13-14), one server's output
+  attention   -- the quantised cache and the drafted tokens' attention (no passage
+                 of the paper: the other half of a decoder layer)
 Precision: fp64 for every real-valued quantity, except the selection's
 decision arithmetic, which is fp32 as the runtime tables are fp32.
 
@@ -32,4 +34,4 @@ Parity unpinned: the paper prints no worked numeric example (no Sim values,
 groups, placements or per-token decisions), so no value here is checked
 against a number printed in the paper.
 """
-from . import layer, placement, route, similarity, tables  # noqa: F401
+from . import attention, layer, placement, route, similarity, tables  # noqa: F401

@@ -160,6 +160,63 @@ int launch_transitions_device(int32_t N, int32_t E, int64_t T_cal, const int32_t
                               void* stream);
 int launch_lookahead_device(const LookaheadDeviceArgs& d, void* stream);
 
+// quantised paged cache and the attention over it (cache.hip, draft_attention.hip)
+struct CacheArgs {
+    int format, n_kv, head_dim, page_shift;
+    int64_t n_pages;
+    uint8_t* k_codes;
+    uint8_t* v_codes;
+    float* k_scale;
+    float* v_scale;
+};
+struct CacheWriteArgs {
+    CacheArgs cache;
+    int dtype, n_q, rot, interleaved;
+    float eps;
+    int64_t max_pos;
+    const void* q_norm;
+    const void* k_norm;
+    const float* cos_sin;
+    const void* q;
+    const void* k;
+    const void* v;
+    int64_t q_stride, k_stride, v_stride, T;
+    const int32_t* pos;
+    const int64_t* slots;
+    void* q_out;
+};
+int launch_cache_write(const CacheWriteArgs& a, void* stream);
+struct CacheReadArgs {
+    CacheArgs cache;
+    int dtype;
+    const int64_t* slots;
+    int64_t n;
+    void* k_out;
+    void* v_out;
+};
+int launch_cache_read(const CacheReadArgs& a, void* stream);
+
+struct DraftArgs {
+    CacheArgs cache;
+    int dtype, n_q, B, max_q, max_pages;
+    int64_t T;
+    const void* q;
+    const int32_t* q_start;
+    const int32_t* ctx_len;
+    const int32_t* page_table;
+    const uint64_t* tree;
+    float scale;
+    void* out;
+    float* lse;
+    // workspace
+    int32_t* plan;         // [B][2] first work item of each sequence, its pieces
+    float* part_ml;        // [items][n_kv][rows][2] maximum and sum of each piece's rows
+    float* part_o;         // [items][n_kv][rows][head_dim] its sums
+};
+// work items (sequence, piece of its cache) that a batch has at most
+int64_t draft_items(int n_q, int n_kv, int head_dim, int dtype, int B, int max_q);
+int launch_draft_attention(const DraftArgs& a, void* stream);
+
 int launch_pack_gate_up(int dtype, int n, int f, int d, const void* g, const void* u, void* out,
                         void* stream);
 int launch_pack_down(int dtype, int n, int d, int f, const void* w, void* out, void* stream);

@@ -1,0 +1,609 @@
+// Attention of drafted tokens over the quantised paged cache.
+//
+//   draft_attention_kernel  one workgroup per (work item, key/value head, block of
+//                           16 RT query rows).  A work item is a piece of one
+//                           sequence's cache; its 32-token tiles go round the
+//                           workgroup's waves, every wave with a running maximum,
+//                           sum and output of its own, joined in LDS at the end.
+//   draft_join_kernel       sequences of several pieces: the pieces' sums added in
+//                           order, relative to their largest maximum
+// The query rows of a key/value head are its n_b tokens times the n_q / n_kv query
+// heads that share it, so that one read of the codes serves them all.
+//
+// A tile (bf16; v_mfma_f32_16x16x32_bf16, c = lane % 16, g = lane / 16):
+//   S^T = K Q^T   rows: 16 tokens, columns: 16 query rows.  The inner index may be
+//                 taken in any order common to both sides, so lane (c, g) reads the
+//                 D/4 neighbouring codes [g D/4, (g + 1) D/4) of token c, and Q in the
+//                 same order.
+//   O^T = V^T P^T rows: 16 elements of the head, columns: 16 query rows.  Two S^T
+//                 blocks leave lane (c, g) the weights of query row c for tokens
+//                 4g .. 4g + 3 of each: exactly the 8 inner indexes of its P^T operand
+//                 when V^T's lanes hold the same tokens.  So the weights never leave
+//                 their registers, and neither do maximum and sum: they belong to a
+//                 column, that is to a lane.
+//   V             lane (c, g) reads D/16 neighbouring codes of its 8 tokens; matrix
+//                 instruction j takes element c D/16 + j of each, whose codes are
+//                 paired across tokens by byte permutes.
+// Keys' scales multiply the scores, values' scales the weights, so codes enter the
+// matrix unit as they are (8-bit codes are exact in bf16).  fp32 runs the same tile
+// with v_mfma_f32_16x16x4_f32.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "common.hpp"
+#include "kv_codes.hpp"
+
+namespace ordermoe {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int DA_WAVES = 4;
+constexpr int DA_THREADS = 64 * DA_WAVES;
+constexpr int DA_TILE = 32;                          // tokens of a tile
+constexpr int DA_ROUND = DA_WAVES * DA_TILE;         // pieces are whole rounds of tiles
+constexpr int DA_MIN_PIECE = 4 * DA_ROUND;           // tokens of a piece, at least
+constexpr int DA_TARGET = 1024;                      // workgroups that a large batch is split into
+
+// 16-row tiles of query rows per workgroup
+__host__ __device__ inline int row_tiles(int dtype, int head_dim, int rows) {
+    const int most = dtype == ORDERMOE_BF16 ? (head_dim == 256 ? 2 : 4) : 1;
+    return rows <= 16 ? 1 : rows <= 32 && most >= 2 ? 2 : most;
+}
+__host__ __device__ inline int row_blocks(int rows, int rt) { return (rows + 16 * rt - 1) / (16 * rt); }
+
+struct SeqInfo {
+    int first, n, ctx, len;     // first token, drafted tokens, cached tokens before them, positions
+};
+__device__ inline SeqInfo sequence(const DraftArgs& a, int b) {
+    SeqInfo s;
+    const int T = (int)a.T, cap = a.max_pages << a.cache.page_shift;
+    int s0 = a.q_start[b], s1 = a.q_start[b + 1], ctx = a.ctx_len[b];
+    s0 = s0 < 0 ? 0 : s0 > T ? T : s0;
+    s1 = s1 < s0 ? s0 : s1 > T ? T : s1;
+    ctx = ctx < 0 ? 0 : ctx > cap ? cap : ctx;
+    s.first = s0;
+    s.n = s1 - s0 < a.max_q ? s1 - s0 : a.max_q;
+    s.ctx = ctx;
+    s.len = s.n < cap - ctx ? ctx + s.n : cap;
+    return s;
+}
+
+// The pieces of the batch, by one wave: tokens of a piece, so that the pieces times
+// `units` (workgroups per piece) come to about DA_TARGET: at most
+// DA_TARGET / units + B pieces, since every sequence ends in at most one short one.
+__device__ inline int piece_tokens(const DraftArgs& a, int units, int lane) {
+    int64_t total = 0;
+    for (int b = lane; b < a.B; b += 64) {
+        const SeqInfo s = sequence(a, b);
+        total += s.n > 0 ? s.len : 0;
+    }
+    if (a.B > 1) {
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o);
+    } else {
+        total = __shfl(total, 0);
+    }
+    const int64_t p = (total * units + DA_TARGET - 1) / DA_TARGET;
+    const int64_t whole = (p + DA_ROUND - 1) / DA_ROUND * DA_ROUND;
+    return (int)(whole < DA_MIN_PIECE ? DA_MIN_PIECE : whole);
+}
+__device__ inline int pieces_of(const SeqInfo& s, int piece) {
+    // a sequence without positions still writes its rows (zeros)
+    return s.n <= 0 ? 0 : s.len <= piece ? 1 : (s.len + piece - 1) / piece;
+}
+// sequence and piece of a work item, by one wave; b < 0: none.  write_plan: every
+// sequence's first item and pieces to a.plan.
+__device__ inline void find_item(const DraftArgs& a, int piece, int item, int lane, bool write_plan, int& b, int& j) {
+    int base = 0;
+    b = -1;
+    j = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        int cnt = 0;
+        if (b0 + lane < a.B) cnt = pieces_of(sequence(a, b0 + lane), piece);
+        int inc = cnt;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(inc, o);
+            if (lane >= o) inc += v;
+        }
+        const int first = base + inc - cnt;
+        if (write_plan && b0 + lane < a.B) {
+            a.plan[2 * (b0 + lane)] = first;
+            a.plan[2 * (b0 + lane) + 1] = cnt;
+        }
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(item >= first && item < first + cnt);
+        if (hit) {
+            const int l = __builtin_ctzll(hit);
+            b = b0 + l;
+            j = item - __builtin_amdgcn_readlane(first, l);
+            if (!write_plan) return;
+        }
+        base += __builtin_amdgcn_readlane(inc, 63);
+    }
+}
+
+// one 32-token tile as read: codes of K (lane: token c of each 16-token block,
+// elements [g D/4, (g+1) D/4)) and of V (lane: tokens 4g .. 4g+3 of each block,
+// elements [c D/16, (c+1) D/16)), and the scales of those four tokens
+template <int D>
+struct Tile {
+    u32x4 k[2][D / 64];
+    uint32_t v[8][D / 64];
+    f32x4 ks[2], vs[2];
+    bool ok[2];                 // uniform: the block's page is in the cache
+};
+
+template <int D>
+__device__ inline void load_tile(const DraftArgs& a, const int32_t* table, int kvh, int t0, int len, int lane, Tile<D>& t) {
+    const int c = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) {
+        const int p = t0 + 16 * tb;
+        const int sh = a.cache.page_shift;
+        const int pid = p < len ? table[p >> sh] : -1;
+        t.ok[tb] = pid >= 0 && pid < a.cache.n_pages;
+        // 16 tokens never cross a page; a block without one reads page 0
+        const int64_t row = t.ok[tb] ? ((((int64_t)pid * a.cache.n_kv + kvh) << sh) + (p & ((1 << sh) - 1))) : 0;
+        const uint8_t* kc = a.cache.k_codes + row * D;
+        const uint8_t* vc = a.cache.v_codes + row * D;
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) t.k[tb][i] = *(const u32x4*)(kc + (uint32_t)(c * D + g * (D / 4) + 16 * i));
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const uint8_t* s = vc + (uint32_t)((4 * g + u) * D + c * (D / 16));
+            uint32_t* o = t.v[4 * tb + u];
+            if constexpr (D == 64) {
+                o[0] = *(const uint32_t*)s;
+            } else if constexpr (D == 128) {
+                const u32x2 v = *(const u32x2*)s;
+                o[0] = v[0]; o[1] = v[1];
+            } else {
+                const u32x4 v = *(const u32x4*)s;
+                o[0] = v[0]; o[1] = v[1]; o[2] = v[2]; o[3] = v[3];
+            }
+        }
+        t.ks[tb] = *(const f32x4*)(a.cache.k_scale + row + 4 * g);
+        t.vs[tb] = *(const f32x4*)(a.cache.v_scale + row + 4 * g);
+    }
+}
+
+// The running state of a wave: per row tile, lane (c, g) has row c's maximum (in
+// units of log 2; a shared reference that may lag behind the true one, see
+// below) and its own tokens' share of the sum; o[j] holds rows' elements
+// (4g + i) D/16 + j, i = 0 .. 3.
+template <int D, int RT>
+struct State {
+    float m[RT], l[RT];
+    f32x4 o[D / 16][RT];
+};
+// A maximum is taken over only when some score passes it by 8 (a factor of 256 in
+// the weights, which fp32 sums and bf16 weights hold as well as 1): most tiles then
+// need no exchange between lanes and no rescaling of the outputs.
+constexpr float DA_LAG = 8.0f;
+
+template <int N>
+struct Queries { bf16x8 b[N]; };
+
+template <bool BF, int D, int FMT, int RT>
+__device__ inline void attend_tile(Tile<D>& t, const void* qv, const uint64_t* word,
+                                   int t0, const SeqInfo& s, float scale2, int lane, State<D, RT>& st) {
+    const int g = lane >> 4;
+    // the tokens past the end and in no page: their codes of V must be numbers
+    if (t0 + DA_TILE > s.len || !t.ok[0] || !t.ok[1]) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const bool in = t.ok[u >> 2] && t0 + 16 * (u >> 2) + 4 * g + (u & 3) < s.len;
+#pragma unroll
+            for (int w = 0; w < D / 64; ++w) t.v[u][w] = in ? t.v[u][w] : 0u;
+        }
+    }
+    f32x4 sc[2][RT];
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) sc[tb][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+            if constexpr (BF) {
+                const Queries<RT * D / 32>& q = *(const Queries<RT * D / 32>*)qv;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    u32x4 kf;
+                    kf[0] = kv_to_bf16x2<FMT, 0>(t.k[tb][i][2 * h]);
+                    kf[1] = kv_to_bf16x2<FMT, 1>(t.k[tb][i][2 * h]);
+                    kf[2] = kv_to_bf16x2<FMT, 0>(t.k[tb][i][2 * h + 1]);
+                    kf[3] = kv_to_bf16x2<FMT, 1>(t.k[tb][i][2 * h + 1]);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r)
+                        sc[tb][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf),
+                                                                            q.b[r * (D / 32) + 2 * i + h], sc[tb][r], 0, 0, 0);
+                }
+            } else {
+                const float* q = (const float*)qv;
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const uint32_t w = t.k[tb][i][h];
+                    const float kf[4] = {kv_to_f32<FMT, 0>(w), kv_to_f32<FMT, 1>(w), kv_to_f32<FMT, 2>(w), kv_to_f32<FMT, 3>(w)};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        sc[tb][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], q[16 * i + 4 * h + e], sc[tb][0], 0, 0, 0);
+                }
+            }
+        }
+    }
+    const float ninf = -__builtin_inff();
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) {
+        const f32x4 ks = t.ks[tb] * scale2;
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc[tb][r][i] *= ks[i];
+    }
+    const bool edge = t0 + DA_TILE > s.ctx || !t.ok[0] || !t.ok[1];
+    uint32_t hidden[RT];                                         // the lane's 8 tokens, a bit each
+    if (edge) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            hidden[r] = 0u;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int p = t0 + 16 * (u >> 2) + 4 * g + (u & 3), j = p - s.ctx;
+                const bool seen = t.ok[u >> 2] && p < s.len && (j < 0 || ((word[r] >> (j & 63)) & 1));
+                hidden[r] |= (uint32_t)!seen << u;
+                sc[u >> 2][r][u & 3] = seen ? sc[u >> 2][r][u & 3] : ninf;
+            }
+        }
+    }
+    float top[RT];
+    bool past = false;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        top[r] = ninf;
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top[r] = fmaxf(top[r], sc[tb][r][i]);
+        past |= top[r] > st.m[r] + DA_LAG;
+    }
+    if (__builtin_amdgcn_ballot_w64(past)) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            float x = fmaxf(top[r], __shfl_xor(top[r], 16));
+            x = fmaxf(x, __shfl_xor(x, 32));
+            const float m = x > st.m[r] + DA_LAG ? x : st.m[r];      // by the row alone, whatever the others do
+            const float al = st.m[r] == m ? 1.0f : __builtin_amdgcn_exp2f(st.m[r] - m);
+            st.m[r] = m;
+            st.l[r] *= al;
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) st.o[j][r] = st.o[j][r] * al;
+        }
+    }
+    // weights exp2(score - maximum), 0 where nothing has been seen yet
+    float pw[RT][8];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const float m = st.m[r] == ninf ? 0.f : st.m[r];
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float p = __builtin_amdgcn_exp2f(sc[tb][r][i] - m);
+                st.l[r] += p;
+                pw[r][4 * tb + i] = p * t.vs[tb][i];
+            }
+    }
+    if (edge) {
+        // an unseen token's scale may be no number
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) pw[r][u] = (hidden[r] >> u) & 1 ? 0.f : pw[r][u];
+    }
+    if constexpr (BF) {
+        bf16x8 pf[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) pf[r][u] = (__bf16)pw[r][u];
+#pragma unroll
+        for (int w = 0; w < D / 64; ++w) {
+            u32x4 vf[4];                                         // elements 4w .. 4w + 3, tokens in pairs
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                // bytes b of tokens 2u and 2u + 1 side by side: b = 0, 1 and b = 2, 3
+                const uint32_t lo = __builtin_amdgcn_perm(t.v[2 * u + 1][w], t.v[2 * u][w], 0x05010400u);
+                const uint32_t hi = __builtin_amdgcn_perm(t.v[2 * u + 1][w], t.v[2 * u][w], 0x07030602u);
+                vf[0][u] = kv_to_bf16x2<FMT, 0>(lo);
+                vf[1][u] = kv_to_bf16x2<FMT, 1>(lo);
+                vf[2][u] = kv_to_bf16x2<FMT, 0>(hi);
+                vf[3][u] = kv_to_bf16x2<FMT, 1>(hi);
+            }
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+                    st.o[4 * w + b][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[b]), pf[r],
+                                                                                 st.o[4 * w + b][r], 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+        for (int w = 0; w < D / 64; ++w)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const uint32_t x = t.v[u][w];
+                const float vf[4] = {kv_to_f32<FMT, 0>(x), kv_to_f32<FMT, 1>(x), kv_to_f32<FMT, 2>(x), kv_to_f32<FMT, 3>(x)};
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    st.o[4 * w + b][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[b], pw[0][u], st.o[4 * w + b][0], 0, 0, 0);
+            }
+    }
+}
+
+// out = sum / l (0 where nothing was seen), N elements of a row
+template <bool BF, int N>
+__device__ inline void write_row(void* out, int64_t at, const float* x, float l) {
+    const float r = l == 0.f ? 0.f : 1.0f / l;
+    if constexpr (BF) {
+        __bf16* o = (__bf16*)out + at;
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            kv_bf16x2 u, v;
+            u[0] = (__bf16)(x[i] * r); u[1] = (__bf16)(x[i + 1] * r);
+            v[0] = (__bf16)(x[i + 2] * r); v[1] = (__bf16)(x[i + 3] * r);
+            *(u32x2*)(o + i) = u32x2{__builtin_bit_cast(uint32_t, u), __builtin_bit_cast(uint32_t, v)};
+        }
+    } else {
+        float* o = (float*)out + at;
+#pragma unroll
+        for (int i = 0; i < N; i += 4) *(f32x4*)(o + i) = f32x4{x[i] * r, x[i + 1] * r, x[i + 2] * r, x[i + 3] * r};
+    }
+}
+constexpr float LN2 = 0.69314718055994531f;
+__device__ inline float row_lse(float m, float l) {
+    return l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * LN2;
+}
+
+template <bool BF, int D, int FMT, int RT>
+__global__ void __launch_bounds__(DA_THREADS) draft_attention_kernel(const DraftArgs a, int items, int rb_n) {
+    constexpr int LD = D + 4;
+    __shared__ __attribute__((aligned(16))) float s_o[DA_WAVES][16][LD];
+    __shared__ float s_m[DA_WAVES][RT * 16], s_l[DA_WAVES][RT * 16];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    // the row blocks of one piece and head on one XCD, where its codes are in L2
+    const int idx = blockIdx.x, jx = idx >> 3;
+    const int unit = (jx / rb_n) * 8 + (idx & 7), rb = jx % rb_n;
+    const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
+    if (unit >= items * n_kv) return;
+    const int item = unit / n_kv, kvh = unit - item * n_kv;
+    const int piece = piece_tokens(a, n_kv * rb_n, lane);
+    int b, j;
+    find_item(a, piece, item, lane, blockIdx.x == 0 && wave == 0, b, j);
+    b = __builtin_amdgcn_readfirstlane(b);
+    j = __builtin_amdgcn_readfirstlane(j);
+    if (b < 0) return;
+    SeqInfo s = sequence(a, b);
+    s.first = __builtin_amdgcn_readfirstlane(s.first);
+    s.n = __builtin_amdgcn_readfirstlane(s.n);
+    s.ctx = __builtin_amdgcn_readfirstlane(s.ctx);
+    s.len = __builtin_amdgcn_readfirstlane(s.len);
+    const int rows = s.n * G, row0 = rb * 16 * RT;
+    if (row0 >= rows) return;
+    const int pieces = pieces_of(s, piece);
+    const int t_lo = j * piece, t_hi = t_lo + piece < s.len ? t_lo + piece : s.len;
+    const int32_t* table = a.page_table + (int64_t)b * a.max_pages;
+
+    // query rows: row = token * G + head; rows past the end are zeros and see nothing
+    constexpr int NQ = BF ? RT * D / 32 : 1;
+    Queries<NQ> qb;
+    float qf[BF ? 1 : D / 4];
+    uint64_t word[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const int row = row0 + 16 * r + c;
+        const bool in = row < rows;
+        const int i = in ? row / G : 0, h = kvh * G + (in ? row - i * G : 0);
+        const int64_t at = ((int64_t)(s.first + i) * a.n_q + h) * D + g * (D / 4);
+        // a chain's word: bits 0 .. i
+        word[r] = !in ? 0ull : a.tree ? a.tree[s.first + i] : ~0ull >> (63 - i);
+        if constexpr (BF) {
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) {
+                bf16x8 v = {};
+                if (in) v = *(const bf16x8*)((const __bf16*)a.q + at + 8 * e);
+                qb.b[r * (D / 32) + e] = v;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < D / 16; ++e) {
+                f32x4 v = {0.f, 0.f, 0.f, 0.f};
+                if (in) v = *(const f32x4*)((const float*)a.q + at + 4 * e);
+#pragma unroll
+                for (int f = 0; f < 4; ++f) qf[4 * e + f] = v[f];
+            }
+        }
+    }
+    const void* qv = BF ? (const void*)&qb : (const void*)qf;
+    State<D, RT> st;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        st.m[r] = -__builtin_inff();
+        st.l[r] = 0.f;
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) st.o[e][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const float scale2 = a.scale * 1.44269504088896341f;        // scores in units of log 2
+    Tile<D> t[2];
+    int p = t_lo + wave * DA_TILE;
+    if (p < t_hi) load_tile<D>(a, table, kvh, p, s.len, lane, t[0]);
+    while (p < t_hi) {
+        if (p + DA_ROUND < t_hi) load_tile<D>(a, table, kvh, p + DA_ROUND, s.len, lane, t[1]);
+        attend_tile<BF, D, FMT, RT>(t[0], qv, word, p, s, scale2, lane, st);
+        p += DA_ROUND;
+        if (p >= t_hi) break;
+        if (p + DA_ROUND < t_hi) load_tile<D>(a, table, kvh, p + DA_ROUND, s.len, lane, t[0]);
+        attend_tile<BF, D, FMT, RT>(t[1], qv, word, p, s, scale2, lane, st);
+        p += DA_ROUND;
+    }
+
+    // the waves' states joined, a row tile at a time
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        float l = st.l[r];
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if (g == 0) { s_m[wave][16 * r + c] = st.m[r]; s_l[wave][16 * r + c] = l; }
+    }
+    __syncthreads();
+    const int64_t prow = ((int64_t)item * n_kv + kvh) * (a.max_q * G);
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        if (row0 + 16 * r >= rows) break;
+        float m = s_m[0][16 * r + c];
+#pragma unroll
+        for (int w = 1; w < DA_WAVES; ++w) m = fmaxf(m, s_m[w][16 * r + c]);
+        const float f = st.m[r] == m ? 1.0f : __builtin_amdgcn_exp2f(st.m[r] - m);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < D / 16; e += 4)
+                *(f32x4*)&s_o[wave][c][(4 * g + i) * (D / 16) + e] =
+                    f32x4{st.o[e][r][i], st.o[e + 1][r][i], st.o[e + 2][r][i], st.o[e + 3][r][i]} * f;
+        __syncthreads();
+        // 16 threads a row, D / 16 elements each
+        const int row = tid >> 4, rr = row0 + 16 * r + row, d0 = (tid & 15) * (D / 16);
+        if (rr < rows) {
+            float mm = s_m[0][16 * r + row], l = 0.f;
+#pragma unroll
+            for (int w = 1; w < DA_WAVES; ++w) mm = fmaxf(mm, s_m[w][16 * r + row]);
+#pragma unroll
+            for (int w = 0; w < DA_WAVES; ++w) {
+                const float mw = s_m[w][16 * r + row];
+                l += s_l[w][16 * r + row] * (mw == mm ? 1.0f : __builtin_amdgcn_exp2f(mw - mm));
+            }
+            float x[D / 16];
+#pragma unroll
+            for (int e = 0; e < D / 16; e += 4) {
+                f32x4 v = *(const f32x4*)&s_o[0][row][d0 + e];
+#pragma unroll
+                for (int w = 1; w < DA_WAVES; ++w) v += *(const f32x4*)&s_o[w][row][d0 + e];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[e + k] = v[k];
+            }
+            if (pieces > 1) {
+                float* po = a.part_o + (prow + rr) * D + d0;
+#pragma unroll
+                for (int e = 0; e < D / 16; e += 4) *(f32x4*)(po + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+                if ((tid & 15) == 0) {
+                    a.part_ml[2 * (prow + rr)] = mm;
+                    a.part_ml[2 * (prow + rr) + 1] = l;
+                }
+            } else {
+                const int i = rr / G, h = kvh * G + rr - i * G;
+                const int64_t at = (int64_t)(s.first + i) * a.n_q + h;
+                write_row<BF, D / 16>(a.out, at * D + d0, x, l);
+                if (a.lse && (tid & 15) == 0) a.lse[at] = row_lse(mm, l);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// one block per 16 (token, head) rows of a sequence, 16 lanes a row
+template <bool BF, int D>
+__global__ void __launch_bounds__(256) draft_join_kernel(const DraftArgs a, int rows_n) {
+    const int b = blockIdx.x / rows_n;
+    const int pieces = a.plan[2 * b + 1];
+    if (pieces <= 1) return;
+    const SeqInfo s = sequence(a, b);
+    const int r = (blockIdx.x - b * rows_n) * 16 + (threadIdx.x >> 4);
+    if (r >= s.n * a.n_q) return;
+    const int item = a.plan[2 * b], n_kv = a.cache.n_kv, G = a.n_q / n_kv;
+    const int i = r / a.n_q, h = r - i * a.n_q, kvh = h / G;
+    const int64_t stride = (int64_t)n_kv * a.max_q * G;          // rows of a piece
+    const int64_t row = ((int64_t)item * n_kv + kvh) * (a.max_q * G) + i * G + (h - kvh * G);
+    const int d0 = (threadIdx.x & 15) * (D / 16);
+    float m = -__builtin_inff();
+    for (int p = 0; p < pieces; ++p) m = fmaxf(m, a.part_ml[2 * (row + p * stride)]);
+    float l = 0.f, x[D / 16] = {};
+    for (int p = 0; p < pieces; ++p) {
+        const float mp = a.part_ml[2 * (row + p * stride)];
+        const float f = mp == m ? 1.0f : __builtin_amdgcn_exp2f(mp - m);
+        l += a.part_ml[2 * (row + p * stride) + 1] * f;
+        const float* po = a.part_o + (row + p * stride) * D + d0;
+#pragma unroll
+        for (int e = 0; e < D / 16; e += 4) {
+            const f32x4 v = *(const f32x4*)(po + e);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[e + k] += v[k] * f;
+        }
+    }
+    const int64_t at = (int64_t)(s.first + i) * a.n_q + h;
+    write_row<BF, D / 16>(a.out, at * D + d0, x, l);
+    if (a.lse && (threadIdx.x & 15) == 0) a.lse[at] = row_lse(m, l);
+}
+
+template <bool BF, int D, int FMT, int RT>
+int launch_rows(const DraftArgs& a, int rt_rows, hipStream_t st) {
+    const int rb = row_blocks(rt_rows, RT);
+    const int64_t items = draft_items(a.n_q, a.cache.n_kv, D, a.dtype, a.B, a.max_q);
+    const int64_t units = (items * a.cache.n_kv + 7) / 8 * 8;
+    {
+        KernelTimer kt_("draft_attention", st);
+        draft_attention_kernel<BF, D, FMT, RT><<<dim3((unsigned)(units * rb)), dim3(DA_THREADS), 0, st>>>(a, (int)items, rb);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return (int)e;
+    }
+    // no sequence can be longer than the table: nothing is split
+    if (((int64_t)a.max_pages << a.cache.page_shift) <= DA_MIN_PIECE) return 0;
+    const int rows_n = (a.max_q * a.n_q + 15) / 16;
+    KernelTimer kt_("draft_join", st);
+    draft_join_kernel<BF, D><<<dim3((unsigned)((int64_t)a.B * rows_n)), dim3(256), 0, st>>>(a, rows_n);
+    return (int)hipGetLastError();
+}
+
+template <bool BF, int D, int FMT>
+int launch_type(const DraftArgs& a, hipStream_t st) {
+    const int rows = a.max_q * (a.n_q / a.cache.n_kv);
+    const int rt = row_tiles(a.dtype, D, rows);
+    if constexpr (BF) {
+        if (rt == 2) return launch_rows<BF, D, FMT, 2>(a, rows, st);
+        if constexpr (D != 256)
+            if (rt == 4) return launch_rows<BF, D, FMT, 4>(a, rows, st);
+    }
+    return launch_rows<BF, D, FMT, 1>(a, rows, st);
+}
+template <bool BF, int D>
+int launch_fmt(const DraftArgs& a, hipStream_t st) {
+    return a.cache.format == ORDERMOE_CACHE_INT8 ? launch_type<BF, D, ORDERMOE_CACHE_INT8>(a, st)
+                                                 : launch_type<BF, D, ORDERMOE_CACHE_FP8>(a, st);
+}
+template <bool BF>
+int launch_dim(const DraftArgs& a, hipStream_t st) {
+    return a.cache.head_dim == 64    ? launch_fmt<BF, 64>(a, st)
+           : a.cache.head_dim == 128 ? launch_fmt<BF, 128>(a, st)
+                                     : launch_fmt<BF, 256>(a, st);
+}
+
+}  // namespace
+
+int64_t draft_items(int n_q, int n_kv, int head_dim, int dtype, int B, int max_q) {
+    const int rows = max_q * (n_q / n_kv);
+    const int64_t units = (int64_t)n_kv * row_blocks(rows, row_tiles(dtype, head_dim, rows));
+    return (DA_TARGET + units - 1) / units + B;
+}
+
+int launch_draft_attention(const DraftArgs& a, void* stream) {
+    if (a.B == 0 || a.T == 0) return 0;
+    return a.dtype == ORDERMOE_BF16 ? launch_dim<true>(a, (hipStream_t)stream) : launch_dim<false>(a, (hipStream_t)stream);
+}
+
+}  // namespace ordermoe

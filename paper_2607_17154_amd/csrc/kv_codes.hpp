@@ -1,0 +1,54 @@
+// Codes of the quantised cache: 8-bit elements and the conversions between
+// them and the compute types.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "common.hpp"
+
+namespace ordermoe {
+
+typedef __bf16 kv_bf16x2 __attribute__((ext_vector_type(2)));
+
+template <int FMT>
+constexpr float kv_code_max() { return FMT == ORDERMOE_CACHE_INT8 ? 127.f : 448.f; }
+
+// rows of a smaller largest magnitude are stored as zeros: well above where
+// the scale would lose bits to fp32's smallest exponent
+constexpr float KV_TINY = 0x1p-100f;
+
+// byte B of w as fp32
+template <int FMT, int B>
+__device__ inline float kv_to_f32(uint32_t w) {
+    if constexpr (FMT == ORDERMOE_CACHE_INT8) return (float)(int8_t)(w >> (8 * B));
+    else return __builtin_amdgcn_cvt_f32_fp8((int)w, B);
+}
+
+// bytes 2H and 2H + 1 of w as a pair of bf16 (every code is a bf16 value)
+template <int FMT, int H>
+__device__ inline uint32_t kv_to_bf16x2(uint32_t w) {
+    kv_bf16x2 r;
+    if constexpr (FMT == ORDERMOE_CACHE_INT8) {
+        r[0] = (__bf16)kv_to_f32<FMT, 2 * H>(w);
+        r[1] = (__bf16)kv_to_f32<FMT, 2 * H + 1>(w);
+    } else {
+        r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, H != 0);
+    }
+    return __builtin_bit_cast(uint32_t, r);
+}
+
+// four values in [-max, max] to codes
+template <int FMT>
+__device__ inline uint32_t kv_to_codes(float a, float b, float c, float d) {
+    if constexpr (FMT == ORDERMOE_CACHE_INT8) {
+        return ((uint32_t)(int)rintf(a) & 255u) | ((uint32_t)(int)rintf(b) & 255u) << 8 |
+               ((uint32_t)(int)rintf(c) & 255u) << 16 | (uint32_t)(int)rintf(d) << 24;
+    } else {
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+    }
+}
+
+}  // namespace ordermoe

@@ -21,6 +21,7 @@ OK, EINVAL, EDTYPE, ECAPACITY, EHIP, EWORKSPACE = 0, -1, -2, -3, -4, -5
 F32, BF16 = 0, 1
 MAX_SERVERS, MAX_EXPERTS, MAX_TOPK, MAX_SUBS, MAX_LOCAL = 32, 256, 8, 15, 64
 NOALLOC_SCRATCH_BYTES = 8 << 20
+CACHE_INT8, CACHE_FP8, MAX_DRAFT = 0, 1, 64
 MARGIN_FLAG = 1.0e-4
 CNT_LOCAL_EXACT, CNT_LOCAL_SUB, CNT_REMOTE_EXACT, CNT_REMOTE_SUB = 0, 1, 2, 3
 CNT_FLAGGED, CNT_TRANSFERS, CNT_REMOTE_SLOTS, CNT_INVALID, NUM_COUNTERS = 4, 5, 6, 7, 8
@@ -34,7 +35,9 @@ EXPORTS = ("ordermoe_last_error", "ordermoe_similarity_workspace_size", "ordermo
            "ordermoe_estimate_transitions", "ordermoe_theta_layer", "ordermoe_adapt_weights",
            "ordermoe_place_random", "ordermoe_simulate_delay", "ordermoe_lookahead_device_workspace_size",
            "ordermoe_build_lookahead_device", "ordermoe_transitions_device_workspace_size",
-           "ordermoe_estimate_transitions_device", "ordermoe_route_select_noalloc")
+           "ordermoe_estimate_transitions_device", "ordermoe_route_select_noalloc",
+           "ordermoe_cache_write", "ordermoe_cache_read", "ordermoe_draft_attention_workspace_size",
+           "ordermoe_draft_attention")
 TIMING_NAME = 64
 
 
@@ -64,6 +67,16 @@ class Experts(ctypes.Structure):
     _fields_ = [("dtype", _I32), ("d", _I32), ("f", _I32), ("E", _I32), ("n_local", _I32),
                 ("n_shared", _I32), ("local_experts", _P), ("w_gate_up", _P), ("w_down", _P),
                 ("w_shared_gate_up", _P), ("w_shared_down", _P)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("format", _I32), ("n_kv", _I32), ("head_dim", _I32), ("page_size", _I32), ("n_pages", _I64),
+                ("k_codes", _P), ("v_codes", _P), ("k_scale", _P), ("v_scale", _P)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("dtype", _I32), ("n_q", _I32), ("rotary_dim", _I32), ("interleaved", _I32), ("max_pos", _I64),
+                ("eps", _F32), ("q_norm", _P), ("k_norm", _P), ("cos_sin", _P)]
 
 
 _lib = None
@@ -131,6 +144,16 @@ def lib() -> ctypes.CDLL:
     L.ordermoe_pack_gate_up.argtypes = [_I32, _I32, _I32, _I32, _P, _P, _P, _P]
     L.ordermoe_pack_down.restype = ctypes.c_int
     L.ordermoe_pack_down.argtypes = [_I32, _I32, _I32, _I32, _P, _P, _P]
+    L.ordermoe_cache_write.restype = ctypes.c_int
+    L.ordermoe_cache_write.argtypes = [ctypes.POINTER(Cache), ctypes.POINTER(Heads), _P, _I64, _P, _I64, _P, _I64, _I64,
+                                       _P, _P, _P, _P]
+    L.ordermoe_cache_read.restype = ctypes.c_int
+    L.ordermoe_cache_read.argtypes = [ctypes.POINTER(Cache), _I32, _P, _I64, _P, _P, _P]
+    L.ordermoe_draft_attention_workspace_size.restype = _SZ
+    L.ordermoe_draft_attention_workspace_size.argtypes = [ctypes.POINTER(Cache), _I32, _I32, _I32, _I32]
+    L.ordermoe_draft_attention.restype = ctypes.c_int
+    L.ordermoe_draft_attention.argtypes = [ctypes.POINTER(Cache), _I32, _I32, _P, _I64, _I32, _I32, _P, _P, _P, _I32, _P,
+                                           _F32, _P, _P, _P, _SZ, _P]
     L.ordermoe_timing_enable.restype = ctypes.c_int
     L.ordermoe_timing_enable.argtypes = [_I32]
     L.ordermoe_timing_read.restype = ctypes.c_int
@@ -530,6 +553,109 @@ def ordermoe_pack_down(w_down, out, stream=None):
     code = BF16 if w_down.dtype == torch.bfloat16 else F32
     _check(lib().ordermoe_pack_down(code, n, d, f, _dev(w_down), _dev(out, w_down.dtype, n * d * f),
                                     _stream(stream)))
+
+
+# ---------------------------------------------------------------- decode step
+def _dtype_code(t) -> int:
+    import torch
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("expected float32 or bfloat16, got %s" % t.dtype)
+    return BF16 if t.dtype == torch.bfloat16 else F32
+
+
+def make_cache(format: int, k_codes, v_codes, k_scale, v_scale) -> Cache:
+    """ordermoe_cache of codes [n_pages, n_kv, page_size, head_dim] uint8 and
+    scales [n_pages, n_kv, page_size] float32; keeps the tensors alive."""
+    import torch
+    n_pages, n_kv, page, D = k_codes.shape
+    n = n_pages * n_kv * page
+    c = Cache(format=format, n_kv=n_kv, head_dim=D, page_size=page, n_pages=n_pages,
+              k_codes=_dev(k_codes, torch.uint8, n * D), v_codes=_dev(v_codes, torch.uint8, n * D),
+              k_scale=_dev(k_scale, torch.float32, n), v_scale=_dev(v_scale, torch.float32, n))
+    c._tensors = (k_codes, v_codes, k_scale, v_scale)
+    return c
+
+
+def alloc_cache(format: int, n_pages: int, n_kv: int, page_size: int, head_dim: int, device) -> Cache:
+    """An ordermoe_cache with memory of its own (contents undefined)."""
+    import torch
+    codes = [torch.empty((n_pages, n_kv, page_size, head_dim), dtype=torch.uint8, device=device) for _ in range(2)]
+    scale = [torch.empty((n_pages, n_kv, page_size), dtype=torch.float32, device=device) for _ in range(2)]
+    return make_cache(format, *codes, *scale)
+
+
+def rotary_table(max_pos: int, rotary_dim: int, base: float = 10000.0) -> np.ndarray:
+    """Host float32 [max_pos, rotary_dim] for make_heads: cosines, then sines, of
+    pos * base^(-2i / rotary_dim), i < rotary_dim / 2, formed in float64."""
+    i = np.arange(rotary_dim // 2, dtype=np.float64)
+    a = np.arange(max_pos, dtype=np.float64)[:, None] * np.power(float(base), -2.0 * i / max(rotary_dim, 1))[None, :]
+    return np.concatenate([np.cos(a), np.sin(a)], axis=1).astype(np.float32)
+
+
+def make_heads(dtype: int, n_q: int, head_dim: int, q_norm=None, k_norm=None, cos_sin=None, interleaved: int = 0,
+               eps: float = 1e-6) -> Heads:
+    """ordermoe_heads; cos_sin float32 [max_pos, rotary_dim] (rotary_table), None
+    for no rotation; keeps the tensors alive."""
+    import torch
+    max_pos, rot = cos_sin.shape if cos_sin is not None else (0, 0)
+    h = Heads(dtype=dtype, n_q=n_q, rotary_dim=rot, interleaved=interleaved, max_pos=max_pos, eps=eps,
+              q_norm=_dev(q_norm, _torch_dtype(dtype), head_dim) or None,
+              k_norm=_dev(k_norm, _torch_dtype(dtype), head_dim) or None,
+              cos_sin=(_dev(cos_sin, torch.float32) or None) if rot else None)
+    h._tensors = (q_norm, k_norm, cos_sin)
+    return h
+
+
+def _rows(t, dtype, T: int, heads: int, D: int):
+    """(address, stride) of [T, heads, D] whose tokens may lie apart."""
+    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != (T, heads, D):
+        raise ValueError("expected a %s device tensor [%d, %d, %d]" % (dtype, T, heads, D))
+    if T > 0 and (t.stride(2) != 1 or t.stride(1) != D):
+        raise ValueError("the heads of a token must lie side by side")
+    return t.data_ptr(), (t.stride(0) if T > 1 else heads * D)
+
+
+def ordermoe_cache_write(cache: Cache, heads: Heads, q, k, v, pos, slots, q_out, stream=None):
+    """q [T, n_q, D], k, v [T, n_kv, D] (tokens may lie apart, as in one array of QKV
+    rows), pos int32 [T] (None without rotation), slots int64 [T], q_out [T, n_q, D]."""
+    import torch
+    T, D, dt = q.shape[0], cache.head_dim, _torch_dtype(heads.dtype)
+    (qp, qs), (kp, ks), (vp, vs) = _rows(q, dt, T, heads.n_q, D), _rows(k, dt, T, cache.n_kv, D), _rows(v, dt, T, cache.n_kv, D)
+    _check(lib().ordermoe_cache_write(ctypes.byref(cache), ctypes.byref(heads), qp, qs, kp, ks, vp, vs, T,
+                                      _dev(pos, torch.int32, T), _dev(slots, torch.int64, T),
+                                      _dev(q_out, dt, T * heads.n_q * D), _stream(stream)))
+
+
+def ordermoe_cache_read(cache: Cache, slots, k_out, v_out, stream=None):
+    """k_out, v_out [n, n_kv, D] (float32 or bfloat16) from slots int64 [n]."""
+    import torch
+    n = slots.numel()
+    m = n * cache.n_kv * cache.head_dim
+    code = _dtype_code(k_out)
+    _check(lib().ordermoe_cache_read(ctypes.byref(cache), code, _dev(slots, torch.int64, n), n, _dev(k_out, None, m),
+                                     _dev(v_out, k_out.dtype, m), _stream(stream)))
+
+
+def ordermoe_draft_attention_workspace_size(cache: Cache, dtype: int, n_q: int, B: int, max_q: int) -> int:
+    return int(lib().ordermoe_draft_attention_workspace_size(ctypes.byref(cache), dtype, n_q, B, max_q))
+
+
+def ordermoe_draft_attention(cache: Cache, q, q_start, ctx_len, page_table, max_q: int, scale: float, out, workspace,
+                             tree=None, lse=None, stream=None):
+    """q, out [T, n_q, D]; q_start int32 [B + 1], ctx_len int32 [B], page_table int32
+    [B, max_pages]; tree int64 [T] (the bits of each token's word) or None for
+    chains; lse float32 [T, n_q] or None."""
+    import torch
+    T, n_q, D = q.shape
+    B, max_pages = page_table.shape
+    if D != cache.head_dim:
+        raise ValueError("q has heads of %d, the cache of %d" % (D, cache.head_dim))
+    code = _dtype_code(q)
+    _check(lib().ordermoe_draft_attention(
+        ctypes.byref(cache), code, n_q, _dev(q), T, B, max_q, _dev(q_start, torch.int32, B + 1),
+        _dev(ctx_len, torch.int32, B), _dev(page_table, torch.int32), max_pages, _dev(tree, torch.int64, T), scale,
+        _dev(out, q.dtype, T * n_q * D), _dev(lse, torch.float32, T * n_q), _dev(workspace), workspace.numel(),
+        _stream(stream)))
 
 
 def ordermoe_timing_enable(on: bool = True):
