@@ -18,6 +18,7 @@
  *   ordermoe_local_moe_forward  execution of the selected (server, expert)
  *                               pairs of one server (Algorithm 2, "execute
  *                               token q on S_m* by expert k*")
+ *   ordermoe_few_moe_layer      the two together for a few tokens
  *   ordermoe_cache_write, ordermoe_cache_read, ordermoe_draft_attention
  *                               the attention half of a decode step, over a
  *                               quantised paged cache
@@ -586,6 +587,23 @@ int ordermoe_draft_attention(const ordermoe_cache* C, int32_t dtype, int32_t n_q
                              int32_t max_q, const int32_t* q_start, const int32_t* ctx_len,
                              const int32_t* page_table, int32_t max_pages, const uint64_t* tree, float scale,
                              void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * The whole MoE layer of one server for a few tokens (1 to ORDERMOE_MAX_FEW of
+ * them: a decode step of a few users, a drafted tree) in two kernels:
+ * ordermoe_route_select, then ordermoe_local_moe_forward on its decisions, with
+ * their arguments, requirements and results, but for
+ *   - out->dispatch, whose T * k entries are all written (-1 past the last);
+ *   - bf16 y: the activation times the row's gate weight is rounded to bf16 before
+ *     the down projection, whose products over all of a token's rows are summed in
+ *     fp32 and rounded once (instead of once per row and once more).
+ * L and W must agree in dtype, d and E; 0 <= T <= ORDERMOE_MAX_FEW.  ws: dev, of the size
+ * below, in use until the stream passes the call; needs no initial contents. */
+#define ORDERMOE_MAX_FEW 16
+size_t ordermoe_few_workspace_size(const ordermoe_layer* L, const ordermoe_experts* W, int64_t T);
+int ordermoe_few_moe_layer(const ordermoe_layer* L, const ordermoe_experts* W, const void* x, int64_t T,
+                           const uint8_t* loc_in, const float* qhat_in, int32_t server,
+                           const ordermoe_route_out* out, void* y, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * Kernel timing (measurement support, off by default).

@@ -217,10 +217,9 @@ extern "C" int ordermoe_route_select_noalloc(const ordermoe_layer* L, const void
     return run_route(L, x, T, loc_in, qhat_in, out, ws, stream, "route_select_noalloc launch");
 }
 
-static int run_route(const ordermoe_layer* L, const void* x, int64_t T, const uint8_t* loc_in,
-                     const float* qhat_in, const ordermoe_route_out* out, void* ws, void* stream,
-                     const char* who) {
-    RouteArgs a{};
+static void fill_route(const ordermoe_layer* L, const void* x, int64_t T, const uint8_t* loc_in, const float* qhat_in,
+                       const ordermoe_route_out* out, RouteArgs* r) {
+    RouteArgs& a = *r;
     a.dtype = L->dtype; a.d = L->d; a.E = L->E; a.k = L->k; a.M = L->M; a.gmax = L->gmax;
     a.pin = L->pin_local_exact; a.allow_sub = L->allow_sub; a.renorm = L->renorm;
     a.Qbar = L->Qbar;
@@ -228,6 +227,13 @@ static int run_route(const ordermoe_layer* L, const void* x, int64_t T, const ui
     a.w_router = L->w_router; a.t1_k = L->t1_k; a.t1_q = L->t1_q; a.t1_n = L->t1_n;
     a.srvmask = L->srvmask; a.S = L->S;
     a.x = x; a.T = T; a.loc_in = loc_in; a.qhat_in = qhat_in; a.out = *out;
+}
+
+static int run_route(const ordermoe_layer* L, const void* x, int64_t T, const uint8_t* loc_in,
+                     const float* qhat_in, const ordermoe_route_out* out, void* ws, void* stream,
+                     const char* who) {
+    RouteArgs a{};
+    fill_route(L, x, T, loc_in, qhat_in, out, &a);
     Carver c(ws);
     route_ws(T, L->k, L->M, c, &a);
     int e = launch_route_select(a, stream);
@@ -363,6 +369,62 @@ extern "C" int ordermoe_local_moe_forward(const ordermoe_experts* W, const void*
     fwd_ws(W, T, k, gemms, c, &a);
     const int e = launch_local_forward(a, stream);
     if (e) return hip_fail(e, "local_moe_forward launch");
+    clear_error();
+    return ORDERMOE_OK;
+}
+
+// ------------------------------------------------------------ the layer for a few tokens
+static size_t few_ws(const ordermoe_experts* W, Carver& c, FewArgs* a) {
+    const size_t esz = W->dtype == ORDERMOE_BF16 ? 2 : 4;
+    float* lg = c.take<float>((size_t)ORDERMOE_MAX_FEW * ORDERMOE_MAX_EXPERTS);
+    int32_t* ct = c.take<int32_t>(2);
+    char* ar = c.take<char>((size_t)W->n_local * ORDERMOE_MAX_FEW * W->f * esz);
+    char* as = c.take<char>((size_t)W->n_shared * ORDERMOE_MAX_FEW * W->f * esz);
+    if (a) { a->logits = lg; a->ctr = ct; a->act_r = ar; a->act_s = as; }
+    return c.size();
+}
+
+static int check_few(const ordermoe_layer* L, const ordermoe_experts* W, int64_t T) {
+    const int rc = check_experts(W);
+    if (rc) return rc;
+    if (!L) return fail(ORDERMOE_EINVAL, "few_moe_layer: null layer");
+    if (T < 0 || T > ORDERMOE_MAX_FEW)
+        return fail(ORDERMOE_EINVAL, "few_moe_layer: T must lie in [0, " + std::to_string(ORDERMOE_MAX_FEW) + "]");
+    if (L->dtype != W->dtype || L->d != W->d || L->E != W->E)
+        return fail(ORDERMOE_EINVAL, "few_moe_layer: layer and experts must agree in dtype, d and E");
+    if (!operands_fit_31_bits(W, ORDERMOE_MAX_FEW))
+        return fail(ORDERMOE_EINVAL, "few_moe_layer: 2*f*d and 2*n_shared*f*d elements must each span fewer than 2^31 bytes");
+    return ORDERMOE_OK;
+}
+
+extern "C" size_t ordermoe_few_workspace_size(const ordermoe_layer* L, const ordermoe_experts* W, int64_t T) {
+    if (check_few(L, W, T) != ORDERMOE_OK) return 0;
+    Carver c(nullptr);
+    return few_ws(W, c, nullptr);
+}
+
+extern "C" int ordermoe_few_moe_layer(const ordermoe_layer* L, const ordermoe_experts* W, const void* x, int64_t T,
+                                      const uint8_t* loc_in, const float* qhat_in, int32_t server,
+                                      const ordermoe_route_out* out, void* y, void* ws, size_t ws_bytes, void* stream) {
+    int rc = check_few(L, W, T);
+    if (rc) return rc;
+    if ((rc = check_route_args(L, x, T, loc_in, qhat_in, out))) return rc;
+    if (server < 0 || server >= ORDERMOE_MAX_SERVERS) return fail(ORDERMOE_EINVAL, "few_moe_layer: server out of range");
+    if (T > 0 && (!y || !aligned16(y))) return fail(ORDERMOE_EINVAL, "few_moe_layer: y must be a 16-byte aligned pointer");
+    const size_t need = ordermoe_few_workspace_size(L, W, T);
+    if (!ws || ws_bytes < need)
+        return fail(ORDERMOE_EWORKSPACE, "few_moe_layer: workspace needs " + std::to_string(need) + " bytes");
+    FewArgs a{};
+    fill_route(L, x, T, loc_in, qhat_in, out, &a.r);
+    a.f = W->f; a.n_local = W->n_local; a.n_shared = W->n_shared; a.server = server;
+    for (int i = 0; i < ORDERMOE_MAX_EXPERTS; ++i) a.lidx[i] = -1;
+    for (int i = 0; i < W->n_local; ++i) a.lidx[W->local_experts[i]] = i;
+    a.w_gu = W->w_gate_up; a.w_dn = W->w_down; a.w_sh_gu = W->w_shared_gate_up; a.w_sh_dn = W->w_shared_down;
+    a.y = y;
+    Carver c(ws);
+    few_ws(W, c, &a);
+    const int e = launch_few_layer(a, stream);
+    if (e) return hip_fail(e, "few_moe_layer launch");
     clear_error();
     return ORDERMOE_OK;
 }

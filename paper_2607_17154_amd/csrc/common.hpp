@@ -115,6 +115,26 @@ int forward_gemms(int dtype, int64_t T, int k, int E, int f, int n_shared, int64
 size_t forward_split_counters();
 size_t forward_split_floats(int gemms);
 
+// the whole layer for a few tokens (few_moe.hip)
+struct FewArgs {
+    RouteArgs r;           // layer, batch and outputs of the routing (its workspace unused)
+    int f, n_local, n_shared, server;
+    int32_t lidx[ORDERMOE_MAX_EXPERTS];  // expert id -> local slot, -1 if not held
+    const void* w_gu;
+    const void* w_dn;
+    const void* w_sh_gu;
+    const void* w_sh_dn;
+    void* y;
+    // workspace
+    float* logits;         // [ORDERMOE_MAX_FEW][Epad]
+    int32_t* ctr;          // [2] next work item, finished activation tiles
+    void* act_r;           // [n_local][ORDERMOE_MAX_FEW][f] weighted activations
+    void* act_s;           // [ORDERMOE_MAX_FEW][n_shared * f]
+};
+int launch_few_layer(const FewArgs& a, void* stream);
+// K slices of the split router of a small batch: nblk 16-token blocks, nb 16-expert blocks
+int route_ksplit(int nblk, int nb, int d);
+
 struct SimArgs {
     int dtype, d, E, k;
     const void* x_cal;

@@ -34,6 +34,7 @@
 
 #include "common.hpp"
 #include "logits_f64.hpp"
+#include "token_pick.hpp"
 
 namespace ordermoe {
 namespace {
@@ -47,62 +48,6 @@ constexpr int RT_SLOTS = 4;      // partial-sum slots of the wave reduction
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-// order-preserving map of fp32 onto uint32
-__device__ inline uint32_t f2ord(float v) {
-    uint32_t u = __float_as_uint(v);
-    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
-__device__ inline float ord2f(uint32_t o) {
-    uint32_t u = (o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o;
-    return __uint_as_float(u);
-}
-
-// Reductions over each row of 16 lanes (one token's lanes) with DPP row
-// rotations by 8, 4, 2, 1: after the four steps every lane of the row holds
-// the result.  Max and min are exact in any order; of a float sum of several
-// terms only lane 0's is used.
-template <int CTRL>
-__device__ inline uint32_t dpp_u32(uint32_t v) {
-    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false);
-}
-template <int CTRL>
-__device__ inline uint64_t dpp_u64(uint64_t v) {
-    const uint32_t lo = dpp_u32<CTRL>((uint32_t)v), hi = dpp_u32<CTRL>((uint32_t)(v >> 32));
-    return ((uint64_t)hi << 32) | lo;
-}
-constexpr int DPP_ROR8 = 0x128, DPP_ROR4 = 0x124, DPP_ROR2 = 0x122, DPP_ROR1 = 0x121;
-__device__ inline uint32_t row_max_u32(uint32_t v) {
-    uint32_t o;
-    o = dpp_u32<DPP_ROR8>(v); v = o > v ? o : v;
-    o = dpp_u32<DPP_ROR4>(v); v = o > v ? o : v;
-    o = dpp_u32<DPP_ROR2>(v); v = o > v ? o : v;
-    o = dpp_u32<DPP_ROR1>(v); v = o > v ? o : v;
-    return v;
-}
-__device__ inline uint32_t row_min_u32(uint32_t v) {
-    uint32_t o;
-    o = dpp_u32<DPP_ROR8>(v); v = o < v ? o : v;
-    o = dpp_u32<DPP_ROR4>(v); v = o < v ? o : v;
-    o = dpp_u32<DPP_ROR2>(v); v = o < v ? o : v;
-    o = dpp_u32<DPP_ROR1>(v); v = o < v ? o : v;
-    return v;
-}
-__device__ inline uint64_t row_min_u64(uint64_t v) {
-    uint64_t o;
-    o = dpp_u64<DPP_ROR8>(v); v = o < v ? o : v;
-    o = dpp_u64<DPP_ROR4>(v); v = o < v ? o : v;
-    o = dpp_u64<DPP_ROR2>(v); v = o < v ? o : v;
-    o = dpp_u64<DPP_ROR1>(v); v = o < v ? o : v;
-    return v;
-}
-__device__ inline float row_sum_f32(float v) {
-    v += __uint_as_float(dpp_u32<DPP_ROR8>(__float_as_uint(v)));
-    v += __uint_as_float(dpp_u32<DPP_ROR4>(__float_as_uint(v)));
-    v += __uint_as_float(dpp_u32<DPP_ROR2>(__float_as_uint(v)));
-    v += __uint_as_float(dpp_u32<DPP_ROR1>(__float_as_uint(v)));
-    return v;
-}
 
 // Raw buffer loads: the hardware range check returns zeros for offsets at or
 // past the resource's size, so rows and experts outside the batch need no
@@ -603,160 +548,18 @@ route_select_kernel(const RouteArgs a) {
     const bool valid = t < a.T;
     const float* lg = s_logit + tr * Epad;
 
-    // top-(k+1) selection by (logit desc, index asc); this lane's logits (experts
-    // j + 16 i) are read once and kept as order-preserving keys
-    const int kk1 = (k + 1 < E) ? k + 1 : E;
-    // (reads at clamped addresses and selects instead of branches, so that the
-    // LDS reads issue together and no per-element branch splits the wave)
-    // Each rank takes the row's largest key with 32-bit maxima, then the lowest
-    // expert that has it (64-bit (logit, expert) keys took 900 cycles a rank, this
-    // about 300); a taken key becomes 0, below every key in play (at least 1).
-    uint32_t okey[NBT];
-#pragma unroll
-    for (int i = 0; i < NBT; ++i) {
-        const int e = j + 16 * i;
-        const uint32_t o = f2ord(lg[e < E ? e : E - 1]);
-        okey[i] = e < E ? (o > 1u ? o : 1u) : 0u;
-    }
-    int sel_e[KM + 1];
-    float sel_v[KM + 1];
-#pragma unroll
-    for (int r = 0; r < KM + 1; ++r) {
-        if (r < kk1) {
-            uint32_t mx = okey[0];
-#pragma unroll
-            for (int i = 1; i < NBT; ++i) mx = okey[i] > mx ? okey[i] : mx;
-            mx = row_max_u32(mx);
-            uint32_t e = 0xFFFFu;
-#pragma unroll
-            for (int i = NBT - 1; i >= 0; --i) e = okey[i] == mx ? (uint32_t)(j + 16 * i) : e;
-            e = row_min_u32(e);
-            sel_e[r] = (int)e;
-            sel_v[r] = ord2f(mx);
-#pragma unroll
-            for (int i = 0; i < NBT; ++i) okey[i] = e == (uint32_t)(j + 16 * i) ? 0u : okey[i];
-        }
-    }
-    float mg = __builtin_inff();
-#pragma unroll
-    for (int r = 0; r < KM; ++r) {
-        if (r + 1 < kk1) {
-            float gap = sel_v[r] - sel_v[r + 1];
-            mg = gap < mg ? gap : mg;
-        }
-    }
-    // gates: softmax renormalised over the top-k, or over all experts
-    float den = 0.f;
-    if (a.renorm) {
-#pragma unroll
-        for (int r = 0; r < KM; ++r)
-            if (r < k) den += expf(sel_v[r] - sel_v[0]);
-    } else {
-        for (int e = j; e < E; e += 16) den += expf(lg[e] - sel_v[0]);
-        // (the rotations add in another order in every lane: all take lane 0's sum)
-        den = __shfl(row_sum_f32(den), 0, 16);
-    }
-
-    // server-expert selection.  Lane j holds candidate j of every slot: j = 0
-    // the exact target, j >= 1 its (j-1)-th substitute in the LDS-staged table.
-    // The search does not depend on the budget, so it runs for all slots at
-    // once: each lane keeps, per slot, the smallest 64-bit key (J, position,
-    // remote, server, expert) over the servers holding its expert.  Then the
-    // slots are taken in rank order: the budget test of eq (40) masks the
-    // substitutes, a min over the row picks (m*, k*) (eq 43) and the budget is
-    // updated as eq (44).
-    const int s_loc = loc_pre;
-    const bool loc_ok = s_loc < M;
-    float qhat = qhat_pre;
-    const bool subs_on = a.allow_sub && a.Qbar > 0.f;
-    const uint32_t mmask = M >= 32 ? 0xFFFFFFFFu : ((1u << M) - 1u);   // servers that exist
-    const int jm1 = j >= 1 ? j - 1 : 0;
-    int ke[KM];
-    float qe[KM];
-    uint32_t msv[KM];
-    uint64_t key[KM];
-    bool search[KM];
-    // every slot's table reads are issued (slots past k read slot 0's entries,
-    // discarded), then masked, so that no per-slot branch serialises them
-#pragma unroll
-    for (int slot = 0; slot < KM; ++slot) {
-        const bool on = slot < k;
-        const int r = sel_e[on ? slot : 0];
-        const uint32_t rmask = s_mask[r];
-        const int nsub = s_t1n[r];
-        const int tk = s_t1k[r * a.gmax + jm1];
-        const float tq = s_t1q[r * a.gmax + jm1];
-        // uniform over the token's row: the reductions below read only lanes of the row
-        search[slot] = on && loc_ok && !(a.pin && ((rmask >> s_loc) & 1u));
-        const bool sub = j >= 1 && subs_on && j - 1 < nsub;
-        int kc = j == 0 ? r : (sub ? tk : -1);
-        if (!on || kc < 0 || kc >= E) kc = -1;
-        ke[slot] = kc;
-        qe[slot] = on && sub ? tq : 0.f;
-        key[slot] = ~0ull;
-    }
-    // the servers holding each candidate (a substitute only on the token's
-    // server in the Local Substitute Only mode)
-    const uint32_t lmask = a.allow_sub == 2 && j >= 1 ? 1u << (s_loc & 31) : ~0u;
-#pragma unroll
-    for (int slot = 0; slot < KM; ++slot) {
-        const uint32_t hm = s_mask[ke[slot] >= 0 ? ke[slot] : 0];
-        msv[slot] = search[slot] && ke[slot] >= 0 ? hm & mmask & lmask : 0u;
-    }
-    // servers holding each candidate, one per round for every slot together
-    for (;;) {
-        uint32_t any = 0;
-#pragma unroll
-        for (int slot = 0; slot < KM; ++slot) any |= msv[slot];
-        if (!__builtin_amdgcn_ballot_w64(any != 0)) break;
-#pragma unroll
-        for (int slot = 0; slot < KM; ++slot) {
-            if (msv[slot]) {
-                const int m = __builtin_ctz(msv[slot]);
-                msv[slot] &= msv[slot] - 1;
-                const float J = fmaf(a.cq, qe[slot], Stab[((int64_t)s_loc * M + m) * E + ke[slot]]);
-                // J's order as a float (negative costs included; -0 counts as +0)
-                const uint64_t cand = ((uint64_t)f2ord(J == 0.f ? 0.f : J) << 32) | ((uint32_t)j << 16) |
-                                      ((uint32_t)(m != s_loc) << 15) | ((uint32_t)m << 8) |
-                                      (uint32_t)ke[slot];
-                key[slot] = cand < key[slot] ? cand : key[slot];
-            }
-        }
-    }
-    // Only the choice is serial over the slots; lane j keeps slot j's, and the
-    // lanes write the token's slots together (lane 0 writing them one after the
-    // other took 5.6 of 19 us at 64 tokens of 128 experts, top-8).
-    int first_m = s_loc, my_r = 0, my_k = 0, my_m = s_loc;
-    float my_v = 0.f;
-    uint32_t dstmask = 0;
-#pragma unroll
-    for (int slot = 0; slot < KM; ++slot) {
-        if (slot >= k) break;
-        const int r = sel_e[slot];
-        int km = r, mm = s_loc;
-        float qsel = 0.f;
-        if (search[slot]) {
-            // eq (40): a substitute must fit the remaining budget; the exact target always does
-            uint64_t kk = (j == 0 || qhat + qe[slot] <= a.Qbar) ? key[slot] : ~0ull;
-            kk = row_min_u64(kk);
-            const int pos = (int)((kk >> 16) & 15u);
-            mm = (int)((kk >> 8) & 31u);
-            km = (int)(kk & 0xFFu);
-            // the chosen candidate's loss, from its lane (a sum of one term: exact)
-            qsel = row_sum_f32(j == pos ? qe[slot] : 0.f);
-        }
-        qhat = qhat + qsel;
-        if (slot == 0) first_m = mm;
-        if (mm != s_loc) dstmask |= 1u << mm;
-        if (j == slot) { my_r = r; my_k = km; my_m = mm; my_v = sel_v[slot]; }
-    }
+    const TokenPick pk_ = pick_token<NBT, KM>(a, lg, s_t1k, s_t1q, s_t1n, s_mask, Stab, j, loc_pre, qhat_pre);
+    const int s_loc = loc_pre, my_r = pk_.r, my_k = pk_.k, my_m = pk_.m, first_m = pk_.first_m;
+    const float my_v = pk_.v, den = pk_.den, mg = pk_.margin, qhat = pk_.qhat;
+    const uint32_t dstmask = pk_.dstmask;
+    const bool loc_ok = pk_.loc_ok;
     const bool mine = valid && j < k, placed = mine && loc_ok;
     const bool remote = my_m != s_loc;
     const int c = ((int)remote << 1) | (int)(my_k != my_r);
     if (mine) {
         const int64_t o = t * k + j;
         a.out.idx[o] = my_r;
-        a.out.w[o] = expf(my_v - sel_v[0]) / den;
+        a.out.w[o] = expf(my_v - pk_.top) / den;
         a.out.exec_k[o] = loc_ok ? my_k : -1;
         a.out.exec_m[o] = loc_ok ? (uint8_t)my_m : 255;
         a.out.cls[o] = loc_ok ? (uint8_t)c : 255;
@@ -973,6 +776,14 @@ size_t route_split_buffer_floats(int64_t T) {
     return (size_t)(rows > 0 ? rows : 1) * ORDERMOE_MAX_EXPERTS;
 }
 
+// enough waves to cover the CUs, K slices a multiple of 32
+int route_ksplit(int nblk, int nb, int d) {
+    int ks = 256 / (nblk * nb);
+    ks = ks < 1 ? 1 : (ks > RT_SPLIT_MAX_K ? RT_SPLIT_MAX_K : ks);
+    while (ks > 1 && d % (32 * ks) != 0) --ks;
+    return ks;
+}
+
 int launch_route_select(const RouteArgs& a, void* stream) {
     hipStream_t st = (hipStream_t)stream;
     const int nb = (a.E + 15) / 16;
@@ -1001,11 +812,7 @@ int launch_route_select(const RouteArgs& a, void* stream) {
         const size_t smem = route_smem(tb, a.E, a.gmax, a.M, b.S_in_lds != 0, b.x_lds);
         b.ksplit = 0;
         if (split) {
-            // enough waves to cover the CUs, K slices a multiple of 32
-            int ks = 256 / (b.nblk * nb);
-            ks = ks < 1 ? 1 : (ks > RT_SPLIT_MAX_K ? RT_SPLIT_MAX_K : ks);
-            while (ks > 1 && a.d % (32 * ks) != 0) --ks;
-            b.ksplit = ks;
+            const int ks = b.ksplit = route_ksplit(b.nblk, nb, a.d);
             KernelTimer kt_("router_split", st);
             router_split_kernel<<<dim3((unsigned)b.nblk, (unsigned)nb, (unsigned)ks), dim3(64), 0, st>>>(b);
             hipError_t e = hipGetLastError();

@@ -21,7 +21,7 @@ OK, EINVAL, EDTYPE, ECAPACITY, EHIP, EWORKSPACE = 0, -1, -2, -3, -4, -5
 F32, BF16 = 0, 1
 MAX_SERVERS, MAX_EXPERTS, MAX_TOPK, MAX_SUBS, MAX_LOCAL = 32, 256, 8, 15, 64
 NOALLOC_SCRATCH_BYTES = 8 << 20
-CACHE_INT8, CACHE_FP8, MAX_DRAFT = 0, 1, 64
+CACHE_INT8, CACHE_FP8, MAX_DRAFT, MAX_FEW = 0, 1, 64, 16
 MARGIN_FLAG = 1.0e-4
 CNT_LOCAL_EXACT, CNT_LOCAL_SUB, CNT_REMOTE_EXACT, CNT_REMOTE_SUB = 0, 1, 2, 3
 CNT_FLAGGED, CNT_TRANSFERS, CNT_REMOTE_SLOTS, CNT_INVALID, NUM_COUNTERS = 4, 5, 6, 7, 8
@@ -37,7 +37,7 @@ EXPORTS = ("ordermoe_last_error", "ordermoe_similarity_workspace_size", "ordermo
            "ordermoe_build_lookahead_device", "ordermoe_transitions_device_workspace_size",
            "ordermoe_estimate_transitions_device", "ordermoe_route_select_noalloc",
            "ordermoe_cache_write", "ordermoe_cache_read", "ordermoe_draft_attention_workspace_size",
-           "ordermoe_draft_attention")
+           "ordermoe_draft_attention", "ordermoe_few_workspace_size", "ordermoe_few_moe_layer")
 TIMING_NAME = 64
 
 
@@ -154,6 +154,11 @@ def lib() -> ctypes.CDLL:
     L.ordermoe_draft_attention.restype = ctypes.c_int
     L.ordermoe_draft_attention.argtypes = [ctypes.POINTER(Cache), _I32, _I32, _P, _I64, _I32, _I32, _P, _P, _P, _I32, _P,
                                            _F32, _P, _P, _P, _SZ, _P]
+    L.ordermoe_few_workspace_size.restype = _SZ
+    L.ordermoe_few_workspace_size.argtypes = [ctypes.POINTER(Layer), ctypes.POINTER(Experts), _I64]
+    L.ordermoe_few_moe_layer.restype = ctypes.c_int
+    L.ordermoe_few_moe_layer.argtypes = [ctypes.POINTER(Layer), ctypes.POINTER(Experts), _P, _I64, _P, _P, _I32,
+                                         ctypes.POINTER(RouteOut), _P, _P, _SZ, _P]
     L.ordermoe_timing_enable.restype = ctypes.c_int
     L.ordermoe_timing_enable.argtypes = [_I32]
     L.ordermoe_timing_read.restype = ctypes.c_int
@@ -656,6 +661,27 @@ def ordermoe_draft_attention(cache: Cache, q, q_start, ctx_len, page_table, max_
         _dev(ctx_len, torch.int32, B), _dev(page_table, torch.int32), max_pages, _dev(tree, torch.int64, T), scale,
         _dev(out, q.dtype, T * n_q * D), _dev(lse, torch.float32, T * n_q), _dev(workspace), workspace.numel(),
         _stream(stream)))
+
+
+def ordermoe_few_workspace_size(layer: Layer, experts: Experts, T: int) -> int:
+    return int(lib().ordermoe_few_workspace_size(ctypes.byref(layer), ctypes.byref(experts), T))
+
+
+def ordermoe_few_moe_layer(layer: Layer, experts: Experts, x, T: int, loc_in, qhat_in, server: int, out: Dict, y,
+                           workspace, stream=None, out_struct: Optional[RouteOut] = None):
+    """The whole layer for T <= MAX_FEW tokens: the route outputs into `out`
+    (alloc_route_out), the server's part of the layer's output into y [T, d]."""
+    import torch
+    s = out_struct if out_struct is not None else route_out_struct(out)
+    if T > 0:
+        _dev(x, _torch_dtype(layer.dtype), T * layer.d)
+        _dev(y, _torch_dtype(layer.dtype), T * layer.d)
+        _dev(loc_in, torch.uint8, T)
+        _dev(qhat_in, torch.float32, T)
+    ptr = (lambda t: t.data_ptr() if T > 0 else 0)
+    _check(lib().ordermoe_few_moe_layer(ctypes.byref(layer), ctypes.byref(experts), ptr(x), T, ptr(loc_in), ptr(qhat_in),
+                                        server, ctypes.byref(s), ptr(y), _dev(workspace), workspace.numel(),
+                                        _stream(stream)))
 
 
 def ordermoe_timing_enable(on: bool = True):

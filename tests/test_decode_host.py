@@ -108,3 +108,46 @@ def test_rotary_table():
     np.testing.assert_allclose(t[3], np.concatenate([np.cos(3 * 100.0 ** (-np.arange(4) / 4)), np.sin(3 * 100.0 ** (-np.arange(4) / 4))]),
                                rtol=1e-6)
     assert om.rotary_table(4, 0).shape == (4, 0)
+
+
+def _few_structs(layer=None, experts=None):
+    ids = np.array([0, 3], np.int32)
+    la = dict(dtype=om.BF16, d=256, E=8, k=2, M=2, gmax=3, pin_local_exact=1, allow_sub=1, renorm=1, Qbar=0.25, omega_Q=0.5,
+              w_router=P, t1_k=P, t1_q=P, t1_n=P, srvmask=P, S=P)
+    ea = dict(dtype=om.BF16, d=256, f=128, E=8, n_local=2, n_shared=1, local_experts=ids.ctypes.data, w_gate_up=P, w_down=P,
+              w_shared_gate_up=P, w_shared_down=P)
+    la.update(layer or {})
+    ea.update(experts or {})
+    e = om.Experts(**ea)
+    e._ids = ids
+    return om.Layer(**la), e, om.RouteOut(**{n: P for n, _ in om.RouteOut._fields_})
+
+
+def _few(L, E, out, x=P, T=4, loc=P, qhat=P, server=0, y=P, ws=P, ws_bytes=1 << 40):
+    r = ctypes.byref
+    return om.lib().ordermoe_few_moe_layer(r(L) if L else None, r(E) if E else None, x, T, loc, qhat, server, r(out) if out else None,
+                                           y, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("layer,experts,args,code", [
+    (dict(dtype=7), {}, {}, om.EINVAL), ({}, dict(dtype=7), {}, om.EDTYPE), (dict(d=512), {}, {}, om.EINVAL),
+    (dict(E=9), {}, {}, om.EINVAL), (dict(dtype=om.F32), {}, {}, om.EINVAL), (dict(d=100), dict(d=100), {}, om.EINVAL),
+    ({}, dict(f=100), {}, om.EINVAL), ({}, dict(n_local=9), {}, om.EINVAL), ({}, dict(w_gate_up=P + 8), {}, om.EINVAL),
+    (dict(k=9), {}, {}, om.EINVAL), (dict(M=0), {}, {}, om.EINVAL), (dict(gmax=16), {}, {}, om.EINVAL), (dict(S=None), {}, {}, om.EINVAL),
+    (dict(w_router=P + 2), {}, {}, om.EINVAL), ({}, {}, dict(T=-1), om.EINVAL), ({}, {}, dict(T=17), om.EINVAL),
+    ({}, {}, dict(x=0), om.EINVAL), ({}, {}, dict(x=P + 8), om.EINVAL), ({}, {}, dict(loc=0), om.EINVAL),
+    ({}, {}, dict(qhat=0), om.EINVAL), ({}, {}, dict(y=0), om.EINVAL), ({}, {}, dict(y=P + 4), om.EINVAL),
+    ({}, {}, dict(server=32), om.EINVAL), ({}, {}, dict(server=-1), om.EINVAL), ({}, {}, dict(ws=0), om.EWORKSPACE),
+    ({}, {}, dict(ws_bytes=64), om.EWORKSPACE),
+])
+def test_few_layer_refusals(layer, experts, args, code):
+    L, E, out = _few_structs(layer, experts)
+    assert _few(L, E, out, **args) == code
+    assert om.last_error()
+
+
+def test_few_layer_null_structs_and_sizes():
+    L, E, out = _few_structs()
+    assert _few(None, E, out) == om.EINVAL and _few(L, None, out) == om.EINVAL and _few(L, E, None) == om.EINVAL
+    size = lambda T: om.lib().ordermoe_few_workspace_size(ctypes.byref(L), ctypes.byref(E), T)  # noqa: E731
+    assert size(1) > 0 and size(16) > 0 and size(17) == 0 and size(-1) == 0
