@@ -377,10 +377,11 @@ extern "C" int ordermoe_local_moe_forward(const ordermoe_experts* W, const void*
 static size_t few_ws(const ordermoe_experts* W, Carver& c, FewArgs* a) {
     const size_t esz = W->dtype == ORDERMOE_BF16 ? 2 : 4;
     float* lg = c.take<float>((size_t)ORDERMOE_MAX_FEW * ORDERMOE_MAX_EXPERTS);
-    int32_t* ct = c.take<int32_t>(2);
+    int32_t* ct = c.take<int32_t>(few_counters(W->d));
+    float* pt = c.take<float>((size_t)W->d * 16 * ORDERMOE_MAX_FEW);
     char* ar = c.take<char>((size_t)W->n_local * ORDERMOE_MAX_FEW * W->f * esz);
     char* as = c.take<char>((size_t)W->n_shared * ORDERMOE_MAX_FEW * W->f * esz);
-    if (a) { a->logits = lg; a->ctr = ct; a->act_r = ar; a->act_s = as; }
+    if (a) { a->logits = lg; a->ctr = ct; a->part = pt; a->act_r = ar; a->act_s = as; }
     return c.size();
 }
 

@@ -127,11 +127,13 @@ struct FewArgs {
     void* y;
     // workspace
     float* logits;         // [ORDERMOE_MAX_FEW][Epad]
-    int32_t* ctr;          // [2] next work item, finished activation tiles
+    int32_t* ctr;          // [few_counters(d)] work counters
+    float* part;           // [d / 64][16][ORDERMOE_MAX_FEW][64] sums of the pieces
     void* act_r;           // [n_local][ORDERMOE_MAX_FEW][f] weighted activations
     void* act_s;           // [ORDERMOE_MAX_FEW][n_shared * f]
 };
 int launch_few_layer(const FewArgs& a, void* stream);
+size_t few_counters(int d);
 // K slices of the split router of a small batch: nblk 16-token blocks, nb 16-expert blocks
 int route_ksplit(int nblk, int nb, int d);
 

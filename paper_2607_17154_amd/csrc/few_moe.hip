@@ -8,11 +8,12 @@
 //                      them; the first one writes the routing's outputs), which tells it
 //                      the experts in use and their tokens.  Then the workgroups draw
 //                      work items from a counter:
-//     activation tiles   16 FFN columns of one expert: gate and up rows times the
+//     activation tiles   32 FFN columns of one expert: gate and up rows times the
 //                        tokens, silu(g) u w -> the weighted activations (memory)
-//     output tiles       16 output columns: the down rows of every expert in use times
+//     output tiles       64 output columns: the down rows of every expert in use times
 //                        its weighted activations, summed over the experts in one
-//                        accumulator -> y
+//                        accumulator, in up to 16 pieces along the experts' columns whose
+//                        sums the last one to finish adds in order -> y
 // An output tile needs all activations.  Items are drawn in order, activation tiles
 // first, and one never waits: whoever draws an output tile knows that every
 // activation tile is in the hands of a running workgroup, so its wait ends without
@@ -39,11 +40,21 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int FW = ORDERMOE_MAX_FEW;
 static_assert(FW == 16, "the tokens are the columns of one matrix instruction");
-constexpr int FW_THREADS = 256, FW_WAVES = 4;
-constexpr int FW_PER_CU = 2;                      // workgroups per CU
+constexpr int FW_WAVES = 8, FW_THREADS = 64 * FW_WAVES;
+constexpr int FW_PER_CU = 1;                      // workgroups per CU
+constexpr int FW_ITEMS = 256 * FW_PER_CU;         // output items wished for
+constexpr int FW_PIECES = 16;                     // pieces of an output tile, at most
+constexpr int FW_XCDS = 8;
+constexpr int FW_SHARES = 256 * FW_PER_CU;        // shares of the work, at most
+// Counters, each in a cache line of its own: atomics on one line take turns, 50 ns each here (drawing every
+// item from one counter cost 24 us with 768 workgroups).  Per XCD: shares drawn, shares whose activations are
+// done, the signal that all are; then the XCDs that are done, and the finished pieces of each output tile.
+constexpr int LINE = 16;
+constexpr int CTR_DRAWN = 0, CTR_DONE = FW_XCDS, CTR_ALL = 2 * FW_XCDS, CTR_XCDS = 3 * FW_XCDS, CTR_TILE = 3 * FW_XCDS + 1;
 constexpr int FW_SLICES = 16;                     // K slices of the router, at most
 constexpr uint32_t OOR = 0x80000000u;             // past every buffer: reads zeros
 constexpr int NT = 2;                             // buffer load cache bit nt: non-temporal
+constexpr int SC1 = 16;                           // buffer store cache bit sc1: through to where every XCD reads
 // a layer of this many bytes of gate/up weights outgrows the caches: its weights go
 // past them (as in the grouped GEMMs)
 constexpr int64_t FW_STREAM_BYTES = (int64_t)64 << 20;
@@ -77,7 +88,8 @@ __global__ void __launch_bounds__(FW_SLICES * 64) few_router_kernel(const FewArg
     const int r16 = lane & 15, g = lane >> 4;
     const int E = a.r.E, d = a.r.d, T = (int)a.r.T;
     const int Epad = (E + 15) & ~15;
-    if (blockIdx.x == 0 && tid < 2) a.ctr[tid] = 0;
+    if (blockIdx.x == 0)
+        for (int i = tid; i < (CTR_TILE + d / 64) * LINE; i += FW_SLICES * 64) a.ctr[i] = 0;
     const int kc = d / ks;                                   // a multiple of 32
     const int e = blockIdx.x * 16 + r16;
     const bool bf = a.r.dtype == ORDERMOE_BF16;
@@ -151,17 +163,25 @@ __device__ inline float silu(float g) {
     else return g / (1.0f + expf(-g));
 }
 
-// A matrix [N][K] of weights as the packed layout has it: byte offset of the 16
-// rows that start at row0 (a multiple of 16), of lane (r = lane % 16, g = lane / 16),
-// and of a step of 64 (bf16) or 32 (fp32) columns; a step is two reads 64 bytes apart.
+// A matrix [N][K] of weights as the packed layout has it, read in steps of 64 (bf16)
+// or 32 (fp32) columns, 128 bytes of a row: one read of a wave covers 8 rows, whole
+// cache lines (lane: row lane / 8, 16 bytes at 16 (lane % 8)).  Byte offset of the
+// lane's part of the 8 rows from row0 (a multiple of 8), and of a step.
 template <bool BF>
 __device__ inline uint32_t rows_offset(int row0, int K, int lane) {
-    const uint32_t r = (uint32_t)(row0 + (lane & 15)), g = (uint32_t)(lane >> 4);
-    if constexpr (BF) return (r / 256u) * (uint32_t)(K / 64) * 32768u + (r % 256u) * 128u + g * 16u;
-    else return r * (uint32_t)K * 4u + g * 16u;
+    const uint32_t r = (uint32_t)(row0 + (lane >> 3)), ch = (uint32_t)(lane & 7);
+    if constexpr (BF) return (r / 256u) * (uint32_t)(K / 64) * 32768u + (r % 256u) * 128u + ch * 16u;
+    else return r * (uint32_t)K * 4u + ch * 16u;
 }
 template <bool BF>
 constexpr uint32_t STEP_BYTES = BF ? 32768u : 128u;
+
+// From that order to the operand's (lane: row lane % 16, 16 bytes at 16 (lane / 16)
+// of either half of the row's 128) through the wave's own LDS rows, padded so that
+// 8 rows' reads fall on distinct banks.  (Reading memory in the operand's order asks
+// for half a line at a time, and a CU has so many requests in flight: 16 tokens of the
+// 128-expert layer took 312 us.)
+constexpr int ROW_LD = 144;
 
 // the routing's outputs that need all tokens, by the first workgroup: dispatch
 // list (rank of a slot: earlier destinations, then earlier slots), totals
@@ -187,7 +207,7 @@ __device__ inline void write_route_totals(const FewArgs& a, const int8_t* dst, c
 }
 
 template <bool BF, int NBT, int AUX>
-__global__ void __launch_bounds__(FW_THREADS, FW_PER_CU) few_layer_kernel(const FewArgs a) {
+__global__ void __launch_bounds__(FW_THREADS) few_layer_kernel(const FewArgs a) {
     constexpr int U = 4;                                     // steps per set of reads; two sets in turn
     constexpr int SK = BF ? 64 : 32;                         // columns of a step
     constexpr uint32_t ES = BF ? 2 : 4;
@@ -198,16 +218,23 @@ __global__ void __launch_bounds__(FW_THREADS, FW_PER_CU) few_layer_kernel(const 
     __shared__ int32_t s_grp[ORDERMOE_MAX_LOCAL + 1];        // the groups in use, the shared one first
     __shared__ int8_t s_dst[FW * ORDERMOE_MAX_TOPK];
     __shared__ int32_t s_cnt[ORDERMOE_NUM_COUNTERS];
-    __shared__ __attribute__((aligned(16))) float s_red[FW_WAVES][2][16][17];
+    __shared__ __attribute__((aligned(16))) float s_red[FW_WAVES][4][16][17];
+    __shared__ __attribute__((aligned(16))) char s_stage[FW_WAVES][64 * ROW_LD];
     __shared__ int32_t s_item;
+    __shared__ int32_t s_share[FW_SHARES];                   // shares of this workgroup: XCD << 16 | number
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15, g16 = lane >> 4;
     const int T = (int)a.r.T, E = a.r.E, k = a.r.k, d = a.r.d, n_local = a.n_local;
     const int Epad = (E + 15) & ~15;
     const bool first = blockIdx.x == 0;
-    int next = 0;
-    if (tid == 0) next = __hip_atomic_fetch_add(a.ctr, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    auto add = [&](int c) { return __hip_atomic_fetch_add(a.ctr + c * LINE, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+    auto look = [&](int c) { return __hip_atomic_load(a.ctr + c * LINE, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+    // this workgroup's share, drawn among those of its XCD (workgroups go to the XCDs in turn; where they do not,
+    // only locality is lost)
+    const int grid = (int)gridDim.x, per_xcd = grid / FW_XCDS;
+    int drawn = 0;
+    if (tid == 0) drawn = add(CTR_DRAWN + (int)(blockIdx.x % FW_XCDS));
 
     // ---- token stage: lanes 16 t .. 16 t + 15 of the block hold token t
     const int t = tid >> 4, j = tid & 15;
@@ -284,127 +311,194 @@ __global__ void __launch_bounds__(FW_THREADS, FW_PER_CU) few_layer_kernel(const 
         if (lane == 0 && sh) s_grp[0] = n_local;
         if ((used >> lane) & 1) s_grp[sh + __popcll(used & ((1ull << lane) - 1ull))] = lane;
     }
-    const int per = a.f / 16, per_sh = sh * a.n_shared * per;
-    const int n_act = per_sh + nu * per, n_items = T > 0 ? n_act + d / 16 : 0;
+    const int per = a.f / 32, per_sh = sh * a.n_shared * per;
+    const int n_r = a.f / SK, n_s = a.n_shared * n_r;        // steps of a routed group's down rows, of the shared one's
+    const int total = sh * n_s + nu * n_r;
+    // output tiles are cut into pieces along the groups' columns, enough for the chip but of FW_WAVES steps at least
+    const int tiles = d / 64;
+    const int n_act = per_sh + nu * per;
+    int pieces = FW_ITEMS / tiles;
+    pieces = pieces > FW_PIECES ? FW_PIECES : pieces;
+    pieces = pieces > total / FW_WAVES ? total / FW_WAVES : pieces;
+    pieces = pieces < 1 ? 1 : pieces;
+    const int n_out = T > 0 ? tiles * pieces : 0;
     const __amdgpu_buffer_rsrc_t rx = make_rsrc(a.r.x, (uint32_t)T * (uint32_t)d * ES);
-    bool ready = false;
+    char* const put = s_stage[wave] + (lane >> 3) * ROW_LD + (lane & 7) * 16;
+    const char* const get = s_stage[wave] + r16 * ROW_LD + g16 * 16;
+    // item `round` of share (x, j) among n: every XCD's shares get neighbouring items; the last, partial round is
+    // spread evenly over the XCDs
+    auto item_of = [&](int x, int j, int round, int n) {
+        const int left = n - round * grid;
+        if (left >= grid) return round * grid + x * per_xcd + j;
+        const int lo = x * (left > 0 ? left : 0) / FW_XCDS, hi = (x + 1) * (left > 0 ? left : 0) / FW_XCDS;
+        return j < hi - lo ? round * grid + lo + j : -1;
+    };
+    // Activation tiles of this workgroup's share, then of shares that nobody has drawn (their workgroups have not
+    // started: they will find no share left and leave).  So when a workgroup begins to wait, every share is in the
+    // hands of a running workgroup that finishes its activation tiles before it waits for anything: all waits end,
+    // whatever else runs on the GPU.
+    int own = 0;
+    if (tid == 0) s_item = drawn < per_xcd ? (int)(blockIdx.x % FW_XCDS) << 16 | drawn : -1;
+    __syncthreads();
+    int share = __builtin_amdgcn_readfirstlane(s_item);
     for (;;) {
-        __syncthreads();
-        if (tid == 0) s_item = next;
-        __syncthreads();
-        const int item = __builtin_amdgcn_readfirstlane(s_item);
-        if (item >= n_items) break;
-        // the following item is drawn now, its latency behind this one
-        if (tid == 0) next = __hip_atomic_fetch_add(a.ctr, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (item < n_act) {
-            // ---- activation tile: FFN columns c0 .. c0 + 15 of group grp
+        if (share >= 0) {
+            if (tid == 0) s_share[own] = share;
+            ++own;
+            const int sx = share >> 16, sj = share & 0xFFFF;
+            int item = item_of(sx, sj, 0, n_act);
+            const bool some = item >= 0;
+            for (int round = 1; item >= 0; item = item_of(sx, sj, round++, n_act)) {
+            // ---- activation tile: FFN columns c0 .. c0 + 31 of group grp
+            constexpr int UA = 1;                            // steps per set of reads
             const bool shared = item < per_sh;
             const int q = shared ? 0 : (item - per_sh) / per;
-            const int c0 = 16 * (shared ? item : item - per_sh - q * per);
+            const int c0 = 32 * (shared ? item : item - per_sh - q * per);
             const int grp = __builtin_amdgcn_readfirstlane(shared ? n_local : s_grp[sh + q]);
             const int F = shared ? a.n_shared * a.f : a.f;
             const char* W = shared ? (const char*)a.w_sh_gu : (const char*)a.w_gu + (size_t)grp * 2 * a.f * d * ES;
             const __amdgpu_buffer_rsrc_t rw = make_rsrc(W, (uint32_t)((size_t)2 * F * d * ES));
             // packed rows: gate columns in blocks of 32, each followed by its up columns
-            const int row0 = 64 * (c0 / 32) + c0 % 32;
-            const uint32_t wg = rows_offset<BF>(row0, d, lane), wu = rows_offset<BF>(row0 + 32, d, lane);
+            uint32_t wo[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) wo[i] = rows_offset<BF>(2 * c0 + 8 * i, d, lane);
             const uint32_t msk = s_msk[grp];
             const uint32_t xo = (msk >> r16) & 1 ? (uint32_t)r16 * (uint32_t)d * ES + 16u * g16 : OOR;
             const int n = d / SK, ns = (n - wave + FW_WAVES - 1) / FW_WAVES;     // steps wave, wave + 4, ...
-            u32x4 vg[2][U][2], vu[2][U][2], vx[2][U][2];
+            u32x4 vw[2][UA][8], vx[2][UA][2];
             auto load = [&](int b, int i0) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
+                for (int u = 0; u < UA; ++u) {
                     const uint32_t past = i0 + u < ns ? 0u : OOR;
                     const uint32_t s = (uint32_t)(i0 + u < ns ? wave + FW_WAVES * (i0 + u) : 0);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        vg[b][u][h] = load16<AUX>(rw, wg | past, s * STEP_BYTES<BF> + 64u * h);
-                        vu[b][u][h] = load16<AUX>(rw, wu | past, s * STEP_BYTES<BF> + 64u * h);
-                        vx[b][u][h] = load16(rx, xo | past, s * 128u + 64u * h);
-                    }
+                    for (int i = 0; i < 8; ++i) vw[b][u][i] = load16<AUX>(rw, wo[i] | past, s * STEP_BYTES<BF>);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) vx[b][u][h] = load16(rx, xo | past, s * 128u + 64u * h);
                 }
             };
-            f32x4 ag = {0.f, 0.f, 0.f, 0.f}, au = {0.f, 0.f, 0.f, 0.f};
+            f32x4 acc[4] = {};                               // gate columns 0-15, 16-31, up columns 0-15, 16-31
             auto mul = [&](int b) {
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+                for (int u = 0; u < UA; ++u) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        ag = mma<BF>(vg[b][u][h], vx[b][u][h], ag);
-                        au = mma<BF>(vu[b][u][h], vx[b][u][h], au);
-                    }
+                    for (int i = 0; i < 8; ++i) *(u32x4*)(put + 8 * i * ROW_LD) = vw[b][u][i];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            acc[r] = mma<BF>(*(const u32x4*)(get + 16 * r * ROW_LD + 64 * h), vx[b][u][h], acc[r]);
+                }
             };
             load(0, 0);
-            for (int i = 0; i < ns; i += 2 * U) {
-                load(1, i + U);
+            for (int i = 0; i < ns; i += 2 * UA) {
+                load(1, i + UA);
                 __builtin_amdgcn_sched_barrier(0);
                 mul(0);
                 __builtin_amdgcn_sched_barrier(0);
-                load(0, i + 2 * U);
+                load(0, i + 2 * UA);
                 __builtin_amdgcn_sched_barrier(0);
                 mul(1);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            // element i of a lane: column 4 g16 + i of the tile, token r16
+            // element i of a lane: column 4 g16 + i of the 16, token r16
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s_red[wave][0][4 * g16 + i][r16] = ag[i];
-                s_red[wave][1][4 * g16 + i][r16] = au[i];
-            }
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s_red[wave][r][4 * g16 + i][r16] = acc[r][i];
             __syncthreads();
-            const int col = tid & 15, tok = tid >> 4;
+            const __amdgpu_buffer_rsrc_t ra = make_rsrc(shared ? (char*)a.act_s : (char*)a.act_r + (size_t)grp * FW * F * ES,
+                                                        (uint32_t)FW * (uint32_t)F * ES);
+            const int col = tid & 15, r = (tid >> 4) & 1, tok = tid >> 5;
             if ((msk >> tok) & 1) {
                 float gv = 0.f, uv = 0.f;
 #pragma unroll
-                for (int w = 0; w < FW_WAVES; ++w) { gv += s_red[w][0][col][tok]; uv += s_red[w][1][col][tok]; }
+                for (int w = 0; w < FW_WAVES; ++w) { gv += s_red[w][r][col][tok]; uv += s_red[w][2 + r][col][tok]; }
                 const float v = silu<BF>(gv) * uv * s_w[grp][tok];
-                const size_t o = shared ? (size_t)tok * F + c0 + col : ((size_t)grp * FW + tok) * F + c0 + col;
-                if constexpr (BF) ((__bf16*)(shared ? a.act_s : a.act_r))[o] = (__bf16)v;
-                else ((float*)(shared ? a.act_s : a.act_r))[o] = v;
+                const uint32_t o = ((uint32_t)tok * (uint32_t)F + c0 + 16 * r + col) * ES;
+                if constexpr (BF)
+                    __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (__bf16)v), ra, (int)o, 0, SC1);
+                else
+                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), ra, (int)o, 0, SC1);
             }
-            // every wave's activations are in memory for every XCD before the tile counts as finished
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+            // every wave's stores have been acknowledged before the tile counts as finished
+            // (written through: a release fence would write back the whole L2 for them)
+            __builtin_amdgcn_s_waitcnt(0x0f70);              // vmcnt(0)
             __syncthreads();
-            if (tid == 0) __hip_atomic_fetch_add(a.ctr + 1, 1, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT);
-            continue;
+            }
+            if (some && tid == 0) {
+                // shares of the XCD that have activation tiles
+                auto with = [&](int x) { return n_act >= grid ? per_xcd : (x + 1) * n_act / FW_XCDS - x * n_act / FW_XCDS; };
+                if (add(CTR_DONE + sx) == with(sx) - 1) {
+                    int xcds = 0;
+                    for (int x = 0; x < FW_XCDS; ++x) xcds += with(x) > 0;
+                    if (add(CTR_XCDS) == xcds - 1)
+                        for (int x = 0; x < FW_XCDS; ++x)
+                            __hip_atomic_store(a.ctr + (CTR_ALL + x) * LINE, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                }
+            }
         }
-        // ---- output tile: columns d0 .. d0 + 15 of y
-        const int d0 = 16 * (item - n_act), ng = sh + nu;
-        const int n_r = a.f / SK, n_s = a.n_shared * n_r;    // steps of a routed group, of the shared one
-        // this wave's steps wave, wave + 4, ... of the groups' steps one after the other
-        struct Pos { int q, s; };                            // group (of those in use), step in it
+        // a share that nobody has drawn
+        __syncthreads();
+        if (wave == 0) {
+            const uint64_t open = __builtin_amdgcn_ballot_w64(lane < FW_XCDS && look(CTR_DRAWN + (lane < FW_XCDS ? lane : 0)) < per_xcd);
+            int f = open ? -2 : -1;
+            if (open && lane == 0) {
+                const int x = __builtin_ctzll(open), t = add(CTR_DRAWN + x);
+                if (t < per_xcd) f = x << 16 | t;
+            }
+            if (lane == 0) s_item = f;
+        }
+        __syncthreads();
+        share = __builtin_amdgcn_readfirstlane(s_item);
+        if (share == -1) break;                              // (-2: another workgroup was first, look again)
+    }
+    bool ready = n_act == 0;
+    for (int o = 0; o < own; ++o) {
+      const int sh_o = __builtin_amdgcn_readfirstlane(s_share[o]);
+      // (from the other end: shares without activation tiles take output items first)
+      const int ox = sh_o >> 16, oj = per_xcd - 1 - (sh_o & 0xFFFF);
+      int item = item_of(ox, oj, 0, n_out);
+      for (int round = 1; item >= 0; item = item_of(ox, oj, round++, n_out)) {
+        // ---- output tile: columns d0 .. d0 + 63 of y, piece sp of the groups' steps one after the other
+        constexpr int UD = 1;
+        const int tile = item % tiles, sp = item / tiles;
+        const int d0 = 64 * tile;
+        const int lo = (int)((int64_t)total * sp / pieces), hi = (int)((int64_t)total * (sp + 1) / pieces);
+        const int ns = (hi - lo - wave + FW_WAVES - 1) / FW_WAVES;               // steps lo + wave, lo + wave + 4, ...
+        struct Pos { int q, s, left; };                      // group (of those in use), step in it, steps left
         auto norm = [&](Pos& p) {
-            while (p.q < ng) {
+            while (p.left > 0) {
                 const int n = p.q < sh ? n_s : n_r;
                 if (p.s < n) break;
                 p.s -= n;
                 ++p.q;
             }
         };
-        u32x4 vw[2][U][2], va[2][U][2];
-        Pos pw{0, wave}, pa{0, wave};
+        u32x4 vw[2][UD][8], va[2][UD][2];
+        Pos pw{0, lo + wave, ns}, pa = pw;
         auto load_w = [&](int b) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
+            for (int u = 0; u < UD; ++u) {
                 norm(pw);
-                const bool in = pw.q < ng;
+                const bool in = pw.left > 0;
                 const int grp = __builtin_amdgcn_readfirstlane(s_grp[in ? pw.q : 0]);
                 const bool shared = in && pw.q < sh;
                 const int F = shared ? a.n_shared * a.f : a.f;
                 const char* W = shared ? (const char*)a.w_sh_dn : (const char*)a.w_dn + (size_t)(in ? grp : 0) * a.f * d * ES;
                 const __amdgpu_buffer_rsrc_t rw = make_rsrc(W, (uint32_t)((size_t)F * d * ES));
-                const uint32_t wo = in ? rows_offset<BF>(d0, F, lane) : OOR;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) vw[b][u][h] = load16<AUX>(rw, wo, (uint32_t)(in ? pw.s : 0) * STEP_BYTES<BF> + 64u * h);
+                for (int i = 0; i < 8; ++i)
+                    vw[b][u][i] = load16<AUX>(rw, in ? rows_offset<BF>(d0 + 8 * i, F, lane) : OOR, (uint32_t)(in ? pw.s : 0) * STEP_BYTES<BF>);
                 pw.s += FW_WAVES;
+                --pw.left;
             }
         };
         auto load_a = [&](int b) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
+            for (int u = 0; u < UD; ++u) {
                 norm(pa);
-                const bool in = pa.q < ng;
+                const bool in = pa.left > 0;
                 const int grp = __builtin_amdgcn_readfirstlane(s_grp[in ? pa.q : 0]);
                 const bool shared = in && pa.q < sh;
                 const int F = shared ? a.n_shared * a.f : a.f;
@@ -415,30 +509,34 @@ __global__ void __launch_bounds__(FW_THREADS, FW_PER_CU) few_layer_kernel(const 
 #pragma unroll
                 for (int h = 0; h < 2; ++h) va[b][u][h] = load16(ra, ao, (uint32_t)(in ? pa.s : 0) * 128u + 64u * h);
                 pa.s += FW_WAVES;
+                --pa.left;
             }
         };
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        f32x4 acc[4] = {};
         auto mul = [&](int b) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+            for (int u = 0; u < UD; ++u) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) acc = mma<BF>(vw[b][u][h], va[b][u][h], acc);
+                for (int i = 0; i < 8; ++i) *(u32x4*)(put + 8 * i * ROW_LD) = vw[b][u][i];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        acc[r] = mma<BF>(*(const u32x4*)(get + 16 * r * ROW_LD + 64 * h), va[b][u][h], acc[r]);
+            }
         };
-        const int total = sh * n_s + nu * n_r, ns = (total - wave + FW_WAVES - 1) / FW_WAVES;
         load_w(0);
         load_w(1);
         if (!ready) {
-            // all activation tiles have been drawn by running workgroups (they precede
-            // this item on the counter) and wait for nothing: this ends
             if (tid == 0) {
-                while (__hip_atomic_load(a.ctr + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < n_act) __builtin_amdgcn_s_sleep(1);
+                while (look(CTR_ALL + (int)(blockIdx.x % FW_XCDS)) == 0) __builtin_amdgcn_s_sleep(8);
                 __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
             }
             __syncthreads();
             ready = true;
         }
         load_a(0);
-        for (int i = 0; i < ns; i += 2 * U) {
+        for (int i = 0; i < ns; i += 2 * UD) {
             load_a(1);
             __builtin_amdgcn_sched_barrier(0);
             mul(0);
@@ -450,18 +548,60 @@ __global__ void __launch_bounds__(FW_THREADS, FW_PER_CU) few_layer_kernel(const 
             __builtin_amdgcn_sched_barrier(0);
             load_w(1);
         }
+        __syncthreads();                                     // (the sums of the item before have been read)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s_red[wave][0][4 * g16 + i][r16] = acc[i];
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s_red[wave][r][4 * g16 + i][r16] = acc[r][i];
         __syncthreads();
-        const int col = tid & 15, tok = tid >> 4;
-        if (tok < T) {
-            float v = 0.f;
+        // two of the 64 columns per thread, 32 apart
+        const int col = tid & 31, tok = tid >> 5;
+        float v[2];
 #pragma unroll
-            for (int w = 0; w < FW_WAVES; ++w) v += s_red[w][0][col][tok];
-            const size_t o = (size_t)tok * d + d0 + col;
-            if constexpr (BF) ((__bf16*)a.y)[o] = (__bf16)v;
-            else ((float*)a.y)[o] = v;
+        for (int r = 0; r < 2; ++r) {
+            v[r] = 0.f;
+#pragma unroll
+            for (int w = 0; w < FW_WAVES; ++w) v[r] += s_red[w][2 * r + (col >> 4)][col & 15][tok];
         }
+        if (pieces > 1) {
+            // the pieces' sums meet in memory; the last piece to arrive adds them in order
+            const __amdgpu_buffer_rsrc_t rp = make_rsrc(a.part + (size_t)tile * FW_PIECES * FW * 64, FW_PIECES * FW * 64 * 4);
+            const uint32_t at = (uint32_t)(tok * 64 + col) * 4u;
+            if (tok < T)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[r]), rp, (int)(at + 128u * r), sp * FW * 64 * 4, SC1);
+            __builtin_amdgcn_s_waitcnt(0x0f70);              // vmcnt(0)
+            __syncthreads();
+            if (tid == 0) s_item = add(CTR_TILE + tile);
+            __syncthreads();
+            if (s_item != pieces - 1) continue;
+            if (tok < T) {
+                float pv[FW_PIECES][2];
+#pragma unroll
+                for (int p = 0; p < FW_PIECES; ++p)          // (past the pieces: the last one again, not added)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+                        pv[p][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(
+                            rp, (int)(at + 128u * r), (p < pieces ? p : pieces - 1) * FW * 64 * 4, SC1));
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    v[r] = pv[0][r];
+#pragma unroll
+                    for (int p = 1; p < FW_PIECES; ++p)
+                        if (p < pieces) v[r] += pv[p][r];
+                }
+            }
+        }
+        if (tok < T) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const size_t o = (size_t)tok * d + d0 + 32 * r + col;
+                if constexpr (BF) ((__bf16*)a.y)[o] = (__bf16)v[r];
+                else ((float*)a.y)[o] = v[r];
+            }
+        }
+      }
     }
 }
 
@@ -469,11 +609,11 @@ template <bool BF, int NBT, int AUX>
 int launch_layer(const FewArgs& a, hipStream_t st) {
     // never more workgroups than items: a tile of every group that can be in use
     const int64_t groups = a.r.T * (a.r.k < a.n_local ? a.r.k : a.n_local);
-    const int64_t act = ((groups < a.n_local ? groups : a.n_local) + a.n_shared) * (a.f / 16);
-    const int64_t items = a.r.T > 0 ? act + a.r.d / 16 : 1;
-    const int64_t most = 256 * FW_PER_CU;
+    const int64_t act = ((groups < a.n_local ? groups : a.n_local) + a.n_shared) * (a.f / 32);
+    const int64_t items = a.r.T > 0 ? act + a.r.d / 64 * FW_PIECES : 1;
+    const int64_t most = FW_SHARES, shares = (items + FW_XCDS - 1) / FW_XCDS * FW_XCDS;
     KernelTimer kt_("few_layer", st);
-    few_layer_kernel<BF, NBT, AUX><<<dim3((unsigned)(items < most ? items : most)), dim3(FW_THREADS), 0, st>>>(a);
+    few_layer_kernel<BF, NBT, AUX><<<dim3((unsigned)(shares < most ? shares : most)), dim3(FW_THREADS), 0, st>>>(a);
     return (int)hipGetLastError();
 }
 
@@ -487,6 +627,8 @@ int launch_experts(const FewArgs& a, hipStream_t st) {
 }
 
 }  // namespace
+
+size_t few_counters(int d) { return (size_t)(CTR_TILE + d / 64) * LINE; }
 
 int launch_few_layer(const FewArgs& a, void* stream) {
     hipStream_t st = (hipStream_t)stream;
