@@ -128,49 +128,66 @@ __device__ inline void find_item(const DraftArgs& a, int piece, int item, int la
     }
 }
 
-// one 32-token tile as read: codes of K (lane: token c of each 16-token block,
-// elements [g D/4, (g+1) D/4)) and of V (lane: tokens 4g .. 4g+3 of each block,
-// elements [c D/16, (c+1) D/16)), and the scales of those four tokens
+// A tile's codes and scales on their way: whole cache lines, 16 bytes a lane (a
+// 16-token block is 16 D bytes in a row), and one scale a lane (K's of the 32 tokens,
+// then V's).  They go through the wave's own LDS rows into the lane order of the
+// operands; rows PITCH = D + 32 bytes apart put the reads of both on distinct banks.
 template <int D>
 struct Tile {
-    u32x4 k[2][D / 64];
-    uint32_t v[8][D / 64];
-    f32x4 ks[2], vs[2];
+    u32x4 k[2][D / 64], v[2][D / 64];
+    float s;
     bool ok[2];                 // uniform: the block's page is in the cache
 };
-
 template <int D>
-__device__ inline void load_tile(const DraftArgs& a, const int32_t* table, int kvh, int t0, int len, int lane, Tile<D>& t) {
-    const int c = lane & 15, g = lane >> 4;
+constexpr int PITCH = D + 32;
+template <int D>
+constexpr int STAGE = 64 * PITCH<D> + 64 * 4;        // bytes of a wave: 32 rows of K, 32 of V, 64 scales
+
+// pages of the tile's two 16-token blocks (16 tokens never cross a page), -1: none; uniform, through the
+// scalar cache
+struct Pages { int p[2]; };
+__device__ inline Pages tile_pages(const DraftArgs& a, const int32_t* table, int t0, int len) {
+    const __attribute__((address_space(4))) int32_t* t = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)table;
+    Pages r;
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
         const int p = t0 + 16 * tb;
-        const int sh = a.cache.page_shift;
-        const int pid = p < len ? table[p >> sh] : -1;
-        t.ok[tb] = pid >= 0 && pid < a.cache.n_pages;
-        // 16 tokens never cross a page; a block without one reads page 0
-        const int64_t row = t.ok[tb] ? ((((int64_t)pid * a.cache.n_kv + kvh) << sh) + (p & ((1 << sh) - 1))) : 0;
-        const uint8_t* kc = a.cache.k_codes + row * D;
-        const uint8_t* vc = a.cache.v_codes + row * D;
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) t.k[tb][i] = *(const u32x4*)(kc + (uint32_t)(c * D + g * (D / 4) + 16 * i));
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const uint8_t* s = vc + (uint32_t)((4 * g + u) * D + c * (D / 16));
-            uint32_t* o = t.v[4 * tb + u];
-            if constexpr (D == 64) {
-                o[0] = *(const uint32_t*)s;
-            } else if constexpr (D == 128) {
-                const u32x2 v = *(const u32x2*)s;
-                o[0] = v[0]; o[1] = v[1];
-            } else {
-                const u32x4 v = *(const u32x4*)s;
-                o[0] = v[0]; o[1] = v[1]; o[2] = v[2]; o[3] = v[3];
-            }
-        }
-        t.ks[tb] = *(const f32x4*)(a.cache.k_scale + row + 4 * g);
-        t.vs[tb] = *(const f32x4*)(a.cache.v_scale + row + 4 * g);
+        r.p[tb] = p < len ? t[p >> a.cache.page_shift] : -1;
     }
+    return r;
+}
+
+template <int D>
+__device__ inline void load_tile(const DraftArgs& a, const Pages& pg, int kvh, int t0, int lane, Tile<D>& t) {
+    const int sh = a.cache.page_shift;
+    int64_t row[2];
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) {
+        const int pid = pg.p[tb];
+        t.ok[tb] = pid >= 0 && pid < a.cache.n_pages;
+        // a block without a page reads page 0
+        row[tb] = t.ok[tb] ? ((((int64_t)pid * a.cache.n_kv + kvh) << sh) + ((t0 + 16 * tb) & ((1 << sh) - 1))) : 0;
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+            t.k[tb][i] = *(const u32x4*)(a.cache.k_codes + row[tb] * D + (uint32_t)(lane * 16 + 1024 * i));
+            t.v[tb][i] = *(const u32x4*)(a.cache.v_codes + row[tb] * D + (uint32_t)(lane * 16 + 1024 * i));
+        }
+    }
+    const float* sc = lane < 32 ? a.cache.k_scale : a.cache.v_scale;
+    t.s = sc[(lane & 16 ? row[1] : row[0]) + (lane & 15)];
+}
+template <int D>
+__device__ inline void stage_tile(const Tile<D>& t, char* st, int lane) {
+    constexpr int CH = D / 16;                       // 16-byte chunks of a row
+    char* p = st + (lane / CH) * PITCH<D> + (lane % CH) * 16;
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+            *(u32x4*)(p + (16 * tb + 64 / CH * i) * PITCH<D>) = t.k[tb][i];
+            *(u32x4*)(p + (32 + 16 * tb + 64 / CH * i) * PITCH<D>) = t.v[tb][i];
+        }
+    *(float*)(st + 64 * PITCH<D> + 4 * lane) = t.s;
 }
 
 // The running state of a wave: per row tile, lane (c, g) has row c's maximum (in
@@ -191,16 +208,32 @@ template <int N>
 struct Queries { bf16x8 b[N]; };
 
 template <bool BF, int D, int FMT, int RT>
-__device__ inline void attend_tile(Tile<D>& t, const void* qv, const uint64_t* word,
+__device__ inline void attend_tile(const char* stage, const bool* ok, const void* qv, const uint64_t* word,
                                    int t0, const SeqInfo& s, float scale2, int lane, State<D, RT>& st) {
-    const int g = lane >> 4;
+    const int c = lane & 15, g = lane >> 4;
+    // V: tokens 4g .. 4g + 3 of each block, elements [c D/16, (c + 1) D/16)
+    uint32_t v[8][D / 64];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        const char* r = stage + (32 + 16 * (u >> 2) + 4 * g + (u & 3)) * PITCH<D> + c * (D / 16);
+        if constexpr (D == 64) {
+            v[u][0] = *(const uint32_t*)r;
+        } else if constexpr (D == 128) {
+            const u32x2 w = *(const u32x2*)r;
+            v[u][0] = w[0]; v[u][1] = w[1];
+        } else {
+            const u32x4 w = *(const u32x4*)r;
+            v[u][0] = w[0]; v[u][1] = w[1]; v[u][2] = w[2]; v[u][3] = w[3];
+        }
+    }
+    const f32x4* scales = (const f32x4*)(stage + 64 * PITCH<D>) + g;     // of tokens 4g .. 4g + 3
     // the tokens past the end and in no page: their codes of V must be numbers
-    if (t0 + DA_TILE > s.len || !t.ok[0] || !t.ok[1]) {
+    if (t0 + DA_TILE > s.len || !ok[0] || !ok[1]) {
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            const bool in = t.ok[u >> 2] && t0 + 16 * (u >> 2) + 4 * g + (u & 3) < s.len;
+            const bool in = ok[u >> 2] && t0 + 16 * (u >> 2) + 4 * g + (u & 3) < s.len;
 #pragma unroll
-            for (int w = 0; w < D / 64; ++w) t.v[u][w] = in ? t.v[u][w] : 0u;
+            for (int w = 0; w < D / 64; ++w) v[u][w] = in ? v[u][w] : 0u;
         }
     }
     f32x4 sc[2][RT];
@@ -210,15 +243,17 @@ __device__ inline void attend_tile(Tile<D>& t, const void* qv, const uint64_t* w
         for (int r = 0; r < RT; ++r) sc[tb][r] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) {
+            // K: token c, elements 64 i + 16 g .. + 15
+            const u32x4 kc = *(const u32x4*)(stage + (16 * tb + c) * PITCH<D> + 64 * i + 16 * g);
             if constexpr (BF) {
                 const Queries<RT * D / 32>& q = *(const Queries<RT * D / 32>*)qv;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     u32x4 kf;
-                    kf[0] = kv_to_bf16x2<FMT, 0>(t.k[tb][i][2 * h]);
-                    kf[1] = kv_to_bf16x2<FMT, 1>(t.k[tb][i][2 * h]);
-                    kf[2] = kv_to_bf16x2<FMT, 0>(t.k[tb][i][2 * h + 1]);
-                    kf[3] = kv_to_bf16x2<FMT, 1>(t.k[tb][i][2 * h + 1]);
+                    kf[0] = kv_to_bf16x2<FMT, 0>(kc[2 * h]);
+                    kf[1] = kv_to_bf16x2<FMT, 1>(kc[2 * h]);
+                    kf[2] = kv_to_bf16x2<FMT, 0>(kc[2 * h + 1]);
+                    kf[3] = kv_to_bf16x2<FMT, 1>(kc[2 * h + 1]);
 #pragma unroll
                     for (int r = 0; r < RT; ++r)
                         sc[tb][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf),
@@ -228,7 +263,7 @@ __device__ inline void attend_tile(Tile<D>& t, const void* qv, const uint64_t* w
                 const float* q = (const float*)qv;
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
-                    const uint32_t w = t.k[tb][i][h];
+                    const uint32_t w = kc[h];
                     const float kf[4] = {kv_to_f32<FMT, 0>(w), kv_to_f32<FMT, 1>(w), kv_to_f32<FMT, 2>(w), kv_to_f32<FMT, 3>(w)};
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
@@ -240,13 +275,13 @@ __device__ inline void attend_tile(Tile<D>& t, const void* qv, const uint64_t* w
     const float ninf = -__builtin_inff();
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
-        const f32x4 ks = t.ks[tb] * scale2;
+        const f32x4 ks = scales[4 * tb] * scale2;
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int i = 0; i < 4; ++i) sc[tb][r][i] *= ks[i];
     }
-    const bool edge = t0 + DA_TILE > s.ctx || !t.ok[0] || !t.ok[1];
+    const bool edge = t0 + DA_TILE > s.ctx || !ok[0] || !ok[1];
     uint32_t hidden[RT];                                         // the lane's 8 tokens, a bit each
     if (edge) {
 #pragma unroll
@@ -255,7 +290,7 @@ __device__ inline void attend_tile(Tile<D>& t, const void* qv, const uint64_t* w
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 const int p = t0 + 16 * (u >> 2) + 4 * g + (u & 3), j = p - s.ctx;
-                const bool seen = t.ok[u >> 2] && p < s.len && (j < 0 || ((word[r] >> (j & 63)) & 1));
+                const bool seen = ok[u >> 2] && p < s.len && (j < 0 || ((word[r] >> (j & 63)) & 1));
                 hidden[r] |= (uint32_t)!seen << u;
                 sc[u >> 2][r][u & 3] = seen ? sc[u >> 2][r][u & 3] : ninf;
             }
@@ -291,13 +326,15 @@ __device__ inline void attend_tile(Tile<D>& t, const void* qv, const uint64_t* w
     for (int r = 0; r < RT; ++r) {
         const float m = st.m[r] == ninf ? 0.f : st.m[r];
 #pragma unroll
-        for (int tb = 0; tb < 2; ++tb)
+        for (int tb = 0; tb < 2; ++tb) {
+            const f32x4 vs = scales[8 + 4 * tb];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float p = __builtin_amdgcn_exp2f(sc[tb][r][i] - m);
                 st.l[r] += p;
-                pw[r][4 * tb + i] = p * t.vs[tb][i];
+                pw[r][4 * tb + i] = p * vs[i];
             }
+        }
     }
     if (edge) {
         // an unseen token's scale may be no number
@@ -318,8 +355,8 @@ __device__ inline void attend_tile(Tile<D>& t, const void* qv, const uint64_t* w
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 // bytes b of tokens 2u and 2u + 1 side by side: b = 0, 1 and b = 2, 3
-                const uint32_t lo = __builtin_amdgcn_perm(t.v[2 * u + 1][w], t.v[2 * u][w], 0x05010400u);
-                const uint32_t hi = __builtin_amdgcn_perm(t.v[2 * u + 1][w], t.v[2 * u][w], 0x07030602u);
+                const uint32_t lo = __builtin_amdgcn_perm(v[2 * u + 1][w], v[2 * u][w], 0x05010400u);
+                const uint32_t hi = __builtin_amdgcn_perm(v[2 * u + 1][w], v[2 * u][w], 0x07030602u);
                 vf[0][u] = kv_to_bf16x2<FMT, 0>(lo);
                 vf[1][u] = kv_to_bf16x2<FMT, 1>(lo);
                 vf[2][u] = kv_to_bf16x2<FMT, 0>(hi);
@@ -337,7 +374,7 @@ __device__ inline void attend_tile(Tile<D>& t, const void* qv, const uint64_t* w
         for (int w = 0; w < D / 64; ++w)
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                const uint32_t x = t.v[u][w];
+                const uint32_t x = v[u][w];
                 const float vf[4] = {kv_to_f32<FMT, 0>(x), kv_to_f32<FMT, 1>(x), kv_to_f32<FMT, 2>(x), kv_to_f32<FMT, 3>(x)};
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
@@ -373,7 +410,9 @@ __device__ inline float row_lse(float m, float l) {
 template <bool BF, int D, int FMT, int RT>
 __global__ void __launch_bounds__(DA_THREADS) draft_attention_kernel(const DraftArgs a, int items, int rb_n) {
     constexpr int LD = D + 4;
-    __shared__ __attribute__((aligned(16))) float s_o[DA_WAVES][16][LD];
+    constexpr int SUMS = DA_WAVES * 16 * LD * 4;
+    __shared__ __attribute__((aligned(16))) char s_mem[DA_WAVES * STAGE<D> > SUMS ? DA_WAVES * STAGE<D> : SUMS];
+    float (*const s_o)[16][LD] = (float (*)[16][LD])s_mem;
     __shared__ float s_m[DA_WAVES][RT * 16], s_l[DA_WAVES][RT * 16];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -411,21 +450,22 @@ __global__ void __launch_bounds__(DA_THREADS) draft_attention_kernel(const Draft
         const int row = row0 + 16 * r + c;
         const bool in = row < rows;
         const int i = in ? row / G : 0, h = kvh * G + (in ? row - i * G : 0);
-        const int64_t at = ((int64_t)(s.first + i) * a.n_q + h) * D + g * (D / 4);
+        // lane group g holds elements 16 g .. 16 g + 15 of every 64
+        const int64_t at = ((int64_t)(s.first + i) * a.n_q + h) * D + 16 * g;
         // a chain's word: bits 0 .. i
         word[r] = !in ? 0ull : a.tree ? a.tree[s.first + i] : ~0ull >> (63 - i);
         if constexpr (BF) {
 #pragma unroll
             for (int e = 0; e < D / 32; ++e) {
                 bf16x8 v = {};
-                if (in) v = *(const bf16x8*)((const __bf16*)a.q + at + 8 * e);
+                if (in) v = *(const bf16x8*)((const __bf16*)a.q + at + 64 * (e >> 1) + 8 * (e & 1));
                 qb.b[r * (D / 32) + e] = v;
             }
         } else {
 #pragma unroll
             for (int e = 0; e < D / 16; ++e) {
                 f32x4 v = {0.f, 0.f, 0.f, 0.f};
-                if (in) v = *(const f32x4*)((const float*)a.q + at + 4 * e);
+                if (in) v = *(const f32x4*)((const float*)a.q + at + 64 * (e >> 2) + 4 * (e & 3));
 #pragma unroll
                 for (int f = 0; f < 4; ++f) qf[4 * e + f] = v[f];
             }
@@ -441,19 +481,30 @@ __global__ void __launch_bounds__(DA_THREADS) draft_attention_kernel(const Draft
         for (int e = 0; e < D / 16; ++e) st.o[e][r] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     const float scale2 = a.scale * 1.44269504088896341f;        // scores in units of log 2
+    // two tiles are on their way while one is attended to
     Tile<D> t[2];
+    char* const stage = s_mem + wave * STAGE<D>;
     int p = t_lo + wave * DA_TILE;
-    if (p < t_hi) load_tile<D>(a, table, kvh, p, s.len, lane, t[0]);
+    Pages pg = tile_pages(a, table, p, t_hi);
+    load_tile<D>(a, pg, kvh, p, lane, t[0]);
+    pg = tile_pages(a, table, p + DA_ROUND, t_hi);
+    load_tile<D>(a, pg, kvh, p + DA_ROUND, lane, t[1]);
+    pg = tile_pages(a, table, p + 2 * DA_ROUND, t_hi);
+    auto step = [&](Tile<D>& u) __attribute__((always_inline)) {
+        const bool ok[2] = {u.ok[0], u.ok[1]};
+        stage_tile<D>(u, stage, lane);
+        load_tile<D>(a, pg, kvh, p + 2 * DA_ROUND, lane, u);
+        pg = tile_pages(a, table, p + 3 * DA_ROUND, t_hi);
+        attend_tile<BF, D, FMT, RT>(stage, ok, qv, word, p, s, scale2, lane, st);
+        p += DA_ROUND;
+    };
     while (p < t_hi) {
-        if (p + DA_ROUND < t_hi) load_tile<D>(a, table, kvh, p + DA_ROUND, s.len, lane, t[1]);
-        attend_tile<BF, D, FMT, RT>(t[0], qv, word, p, s, scale2, lane, st);
-        p += DA_ROUND;
+        step(t[0]);
         if (p >= t_hi) break;
-        if (p + DA_ROUND < t_hi) load_tile<D>(a, table, kvh, p + DA_ROUND, s.len, lane, t[0]);
-        attend_tile<BF, D, FMT, RT>(t[1], qv, word, p, s, scale2, lane, st);
-        p += DA_ROUND;
+        step(t[1]);
     }
 
+    __syncthreads();                                 // the staging rows become the place of the sums
     // the waves' states joined, a row tile at a time
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
