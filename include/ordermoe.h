@@ -579,7 +579,7 @@ int ordermoe_cache_read(const ordermoe_cache* C, int32_t dtype, const int64_t* s
  *            split over workgroups (joined in a fixed order: results are the same
  *            on every run); in use until the stream passes the call
  * 1 <= max_q <= ORDERMOE_MAX_DRAFT (an upper bound of n_b), 0 <= B <= 65535,
- * max_pages >= 1, max_pages * page_size < 2^31, n_q <= 1024, scale finite.  The lengths are
+ * max_pages >= 1, max_pages * page_size <= 2^30, n_q <= 1024, scale finite.  The lengths are
  * read on the device; the call does not synchronise. */
 size_t ordermoe_draft_attention_workspace_size(const ordermoe_cache* C, int32_t dtype, int32_t n_q, int32_t B,
                                                int32_t max_q);

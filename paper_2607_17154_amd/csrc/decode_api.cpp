@@ -143,8 +143,8 @@ extern "C" int ordermoe_draft_attention(const ordermoe_cache* C, int32_t dtype, 
     const int rc = check_draft_sizes(C, dtype, n_q, B, max_q);
     if (rc) return rc;
     if (T < 0 || T > ((int64_t)1 << 31) - 1) return fail(ORDERMOE_EINVAL, "draft_attention: T out of range");
-    if (max_pages < 1 || (int64_t)max_pages * C->page_size >= (int64_t)1 << 31)
-        return fail(ORDERMOE_EINVAL, "draft_attention: max_pages * page_size must lie in [1, 2^31)");
+    if (max_pages < 1 || (int64_t)max_pages * C->page_size > (int64_t)1 << 30)
+        return fail(ORDERMOE_EINVAL, "draft_attention: max_pages * page_size must lie in [1, 2^30]");
     if (!std::isfinite(scale)) return fail(ORDERMOE_EINVAL, "draft_attention: scale must be finite");
     if (T > 0 && B > 0 && (!q || !q_start || !ctx_len || !page_table || !out))
         return fail(ORDERMOE_EINVAL, "draft_attention: null pointer");

@@ -42,18 +42,22 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int DA_WAVES = 4;
-constexpr int DA_THREADS = 64 * DA_WAVES;
+constexpr int DA_WAVES = 4, DA_WAVES_WIDE = 8;       // waves of a workgroup (wide: see launch_type)
 constexpr int DA_TILE = 32;                          // tokens of a tile
-constexpr int DA_ROUND = DA_WAVES * DA_TILE;         // pieces are whole rounds of tiles
-constexpr int DA_MIN_PIECE = 4 * DA_ROUND;           // tokens of a piece, at least
-constexpr int DA_TARGET = 1024;                      // workgroups that a large batch is split into
+constexpr int DA_MIN_PIECE = 1024;                   // tokens of a piece, at least
+constexpr int DA_WIDE_MAX = 2048;                    // tokens of a table that wide workgroups take whole
+// workgroups that a large batch is split into: of the 512 that run together, two
+// rounds where the memory sets the pace and any two pieces take the same time (64
+// tokens over 200-8000: 512 111 us, 1024 105, 2048 104 and 2 more to join), four where row blocks of unequal
+// number do (trees of 64 over 30000-100000: 404, 360, 334)
+constexpr int DA_TARGET = 1024, DA_TARGET_BLOCKS = 2048;
 
 // 16-row tiles of query rows per workgroup
 __host__ __device__ inline int row_tiles(int dtype, int head_dim, int rows) {
-    const int most = dtype == ORDERMOE_BF16 ? (head_dim == 256 ? 2 : 4) : 1;
-    return rows <= 16 ? 1 : rows <= 32 && most >= 2 ? 2 : most;
+    const int most = dtype == ORDERMOE_BF16 ? (head_dim == 256 ? 1 : 2) : 1;
+    return rows <= 16 ? 1 : most;
 }
 __host__ __device__ inline int row_blocks(int rows, int rt) { return (rows + 16 * rt - 1) / (16 * rt); }
 
@@ -74,38 +78,53 @@ __device__ inline SeqInfo sequence(const DraftArgs& a, int b) {
     return s;
 }
 
-// The pieces of the batch, by one wave: tokens of a piece, so that the pieces times
-// `units` (workgroups per piece) come to about DA_TARGET: at most
-// DA_TARGET / units + B pieces, since every sequence ends in at most one short one.
-__device__ inline int piece_tokens(const DraftArgs& a, int units, int lane) {
-    int64_t total = 0;
+// The pieces of the batch, by one wave.  A workgroup's work is a piece of one
+// sequence's tokens for one key/value head and one block of its rows; pieces have as
+// many tokens, a multiple of `round`, as give about `target` workgroups in all, but at
+// least half of what the batch would ask for with every sequence at max_q: that bounds
+// the pieces by 2 target / (n_kv rb_n) + B, since each sequence ends in one short one.
+__device__ inline int piece_tokens(const DraftArgs& a, int rb_n, int rt, int round, int target, int min_piece, const SeqInfo& mine,
+                                   int lane) {
+    const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
+    int64_t total = 0, blocks = 0;
     for (int b = lane; b < a.B; b += 64) {
-        const SeqInfo s = sequence(a, b);
+        const SeqInfo s = b < 64 ? mine : sequence(a, b);
         total += s.n > 0 ? s.len : 0;
+        blocks += s.n > 0 ? (int64_t)s.len * row_blocks(s.n * G, rt) : 0;
     }
     if (a.B > 1) {
 #pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o);
+        for (int o = 32; o >= 1; o >>= 1) {
+            total += __shfl_xor(total, o);
+            if (rb_n > 1) blocks += __shfl_xor(blocks, o);
+        }
     } else {
         total = __shfl(total, 0);
+        blocks = __shfl(blocks, 0);
     }
-    const int64_t p = (total * units + DA_TARGET - 1) / DA_TARGET;
-    const int64_t whole = (p + DA_ROUND - 1) / DA_ROUND * DA_ROUND;
-    return (int)(whole < DA_MIN_PIECE ? DA_MIN_PIECE : whole);
+    if (rb_n == 1) blocks = total;
+    int64_t p = (blocks * n_kv + target - 1) / target;
+    const int64_t least = (total * n_kv * rb_n + 2 * target - 1) / (2 * target);
+    p = p < least ? least : p;
+    p = (p + round - 1) / round * round;
+    return (int)(p < min_piece ? min_piece : p > (1 << 30) ? 1 << 30 : p);
 }
 __device__ inline int pieces_of(const SeqInfo& s, int piece) {
     // a sequence without positions still writes its rows (zeros)
     return s.n <= 0 ? 0 : s.len <= piece ? 1 : (s.len + piece - 1) / piece;
 }
-// sequence and piece of a work item, by one wave; b < 0: none.  write_plan: every
-// sequence's first item and pieces to a.plan.
-__device__ inline void find_item(const DraftArgs& a, int piece, int item, int lane, bool write_plan, int& b, int& j) {
+// sequence (of number b, < 0: none) and piece j of a work item, by one wave.
+// write_plan: every sequence's first item and pieces to a.plan.
+__device__ inline SeqInfo find_item(const DraftArgs& a, int piece, int item, int lane, bool write_plan, const SeqInfo& mine, int& b,
+                                    int& j) {
+    SeqInfo found = {0, 0, 0, 0};
     int base = 0;
     b = -1;
     j = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
-        int cnt = 0;
-        if (b0 + lane < a.B) cnt = pieces_of(sequence(a, b0 + lane), piece);
+        SeqInfo s = mine;
+        if (b0 > 0 && b0 + lane < a.B) s = sequence(a, b0 + lane);
+        const int cnt = b0 + lane < a.B ? pieces_of(s, piece) : 0;
         int inc = cnt;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -122,10 +141,13 @@ __device__ inline void find_item(const DraftArgs& a, int piece, int item, int la
             const int l = __builtin_ctzll(hit);
             b = b0 + l;
             j = item - __builtin_amdgcn_readlane(first, l);
-            if (!write_plan) return;
+            found = SeqInfo{__builtin_amdgcn_readlane(s.first, l), __builtin_amdgcn_readlane(s.n, l),
+                            __builtin_amdgcn_readlane(s.ctx, l), __builtin_amdgcn_readlane(s.len, l)};
+            if (!write_plan) break;
         }
         base += __builtin_amdgcn_readlane(inc, 63);
     }
+    return found;
 }
 
 // A tile's codes and scales on their way: whole cache lines, 16 bytes a lane (a
@@ -157,7 +179,14 @@ __device__ inline Pages tile_pages(const DraftArgs& a, const int32_t* table, int
     return r;
 }
 
-template <int D>
+// NTL: past the caches, where no other workgroup reads the codes
+template <bool NTL>
+__device__ inline u32x4 load_codes(const uint8_t* p) {
+    if constexpr (NTL) return __builtin_nontemporal_load((const u32x4*)p);
+    else return *(const u32x4*)p;
+}
+
+template <int D, bool NTL>
 __device__ inline void load_tile(const DraftArgs& a, const Pages& pg, int kvh, int t0, int lane, Tile<D>& t) {
     const int sh = a.cache.page_shift;
     int64_t row[2];
@@ -169,8 +198,8 @@ __device__ inline void load_tile(const DraftArgs& a, const Pages& pg, int kvh, i
         row[tb] = t.ok[tb] ? ((((int64_t)pid * a.cache.n_kv + kvh) << sh) + ((t0 + 16 * tb) & ((1 << sh) - 1))) : 0;
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) {
-            t.k[tb][i] = *(const u32x4*)(a.cache.k_codes + row[tb] * D + (uint32_t)(lane * 16 + 1024 * i));
-            t.v[tb][i] = *(const u32x4*)(a.cache.v_codes + row[tb] * D + (uint32_t)(lane * 16 + 1024 * i));
+            t.k[tb][i] = load_codes<NTL>(a.cache.k_codes + row[tb] * D + (uint32_t)(lane * 16 + 1024 * i));
+            t.v[tb][i] = load_codes<NTL>(a.cache.v_codes + row[tb] * D + (uint32_t)(lane * 16 + 1024 * i));
         }
     }
     const float* sc = lane < 32 ? a.cache.k_scale : a.cache.v_scale;
@@ -211,31 +240,7 @@ template <bool BF, int D, int FMT, int RT>
 __device__ inline void attend_tile(const char* stage, const bool* ok, const void* qv, const uint64_t* word,
                                    int t0, const SeqInfo& s, float scale2, int lane, State<D, RT>& st) {
     const int c = lane & 15, g = lane >> 4;
-    // V: tokens 4g .. 4g + 3 of each block, elements [c D/16, (c + 1) D/16)
-    uint32_t v[8][D / 64];
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-        const char* r = stage + (32 + 16 * (u >> 2) + 4 * g + (u & 3)) * PITCH<D> + c * (D / 16);
-        if constexpr (D == 64) {
-            v[u][0] = *(const uint32_t*)r;
-        } else if constexpr (D == 128) {
-            const u32x2 w = *(const u32x2*)r;
-            v[u][0] = w[0]; v[u][1] = w[1];
-        } else {
-            const u32x4 w = *(const u32x4*)r;
-            v[u][0] = w[0]; v[u][1] = w[1]; v[u][2] = w[2]; v[u][3] = w[3];
-        }
-    }
     const f32x4* scales = (const f32x4*)(stage + 64 * PITCH<D>) + g;     // of tokens 4g .. 4g + 3
-    // the tokens past the end and in no page: their codes of V must be numbers
-    if (t0 + DA_TILE > s.len || !ok[0] || !ok[1]) {
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const bool in = ok[u >> 2] && t0 + 16 * (u >> 2) + 4 * g + (u & 3) < s.len;
-#pragma unroll
-            for (int w = 0; w < D / 64; ++w) v[u][w] = in ? v[u][w] : 0u;
-        }
-    }
     f32x4 sc[2][RT];
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
@@ -343,6 +348,31 @@ __device__ inline void attend_tile(const char* stage, const bool* ok, const void
 #pragma unroll
             for (int u = 0; u < 8; ++u) pw[r][u] = (hidden[r] >> u) & 1 ? 0.f : pw[r][u];
     }
+    __builtin_amdgcn_sched_barrier(0);               // (V's registers only from here on)
+    // V: tokens 4g .. 4g + 3 of each block, elements [c D/16, (c + 1) D/16)
+    uint32_t v[8][D / 64];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        const char* r = stage + (32 + 16 * (u >> 2) + 4 * g + (u & 3)) * PITCH<D> + c * (D / 16);
+        if constexpr (D == 64) {
+            v[u][0] = *(const uint32_t*)r;
+        } else if constexpr (D == 128) {
+            const u32x2 w = *(const u32x2*)r;
+            v[u][0] = w[0]; v[u][1] = w[1];
+        } else {
+            const u32x4 w = *(const u32x4*)r;
+            v[u][0] = w[0]; v[u][1] = w[1]; v[u][2] = w[2]; v[u][3] = w[3];
+        }
+    }
+    // the tokens past the end and in no page: their codes of V must be numbers
+    if (t0 + DA_TILE > s.len || !ok[0] || !ok[1]) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const bool in = ok[u >> 2] && t0 + 16 * (u >> 2) + 4 * g + (u & 3) < s.len;
+#pragma unroll
+            for (int w = 0; w < D / 64; ++w) v[u][w] = in ? v[u][w] : 0u;
+        }
+    }
     if constexpr (BF) {
         bf16x8 pf[RT];
 #pragma unroll
@@ -407,13 +437,20 @@ __device__ inline float row_lse(float m, float l) {
     return l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * LN2;
 }
 
-template <bool BF, int D, int FMT, int RT>
-__global__ void __launch_bounds__(DA_THREADS) draft_attention_kernel(const DraftArgs a, int items, int rb_n) {
-    constexpr int LD = D + 4;
-    constexpr int SUMS = DA_WAVES * 16 * LD * 4;
-    __shared__ __attribute__((aligned(16))) char s_mem[DA_WAVES * STAGE<D> > SUMS ? DA_WAVES * STAGE<D> : SUMS];
+// waves per SIMD that the registers leave room for (two tiles on their way take 66,
+// the outputs D / 4 per row tile; four row tiles at one wave per SIMD took 932 us where
+// two at two take 360)
+template <int D>
+constexpr int OCC = D == 256 ? 1 : 2;
+
+template <bool BF, int D, int FMT, int RT, int NW>
+__global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const DraftArgs a, int items, int rb_n, int target,
+                                                                           int min_piece) {
+    constexpr int LD = D + 4, ROUND = NW * DA_TILE;
+    constexpr int SUMS = NW * 16 * LD * 4;
+    __shared__ __attribute__((aligned(16))) char s_mem[NW * STAGE<D> > SUMS ? NW * STAGE<D> : SUMS];
     float (*const s_o)[16][LD] = (float (*)[16][LD])s_mem;
-    __shared__ float s_m[DA_WAVES][RT * 16], s_l[DA_WAVES][RT * 16];
+    __shared__ float s_m[NW][RT * 16], s_l[NW][RT * 16];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
@@ -423,21 +460,17 @@ __global__ void __launch_bounds__(DA_THREADS) draft_attention_kernel(const Draft
     const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
     if (unit >= items * n_kv) return;
     const int item = unit / n_kv, kvh = unit - item * n_kv;
-    const int piece = piece_tokens(a, n_kv * rb_n, lane);
+    SeqInfo mine = {0, 0, 0, 0};
+    if (lane < a.B) mine = sequence(a, lane);
+    const int piece = piece_tokens(a, rb_n, RT, ROUND, target, min_piece, mine, lane);
     int b, j;
-    find_item(a, piece, item, lane, blockIdx.x == 0 && wave == 0, b, j);
+    const SeqInfo s = find_item(a, piece, item, lane, blockIdx.x == 0 && wave == 0, mine, b, j);
     b = __builtin_amdgcn_readfirstlane(b);
-    j = __builtin_amdgcn_readfirstlane(j);
     if (b < 0) return;
-    SeqInfo s = sequence(a, b);
-    s.first = __builtin_amdgcn_readfirstlane(s.first);
-    s.n = __builtin_amdgcn_readfirstlane(s.n);
-    s.ctx = __builtin_amdgcn_readfirstlane(s.ctx);
-    s.len = __builtin_amdgcn_readfirstlane(s.len);
     const int rows = s.n * G, row0 = rb * 16 * RT;
     if (row0 >= rows) return;
     const int pieces = pieces_of(s, piece);
-    const int t_lo = j * piece, t_hi = t_lo + piece < s.len ? t_lo + piece : s.len;
+    const int t_lo = j * piece, t_hi = s.len - t_lo < piece ? s.len : t_lo + piece;
     const int32_t* table = a.page_table + (int64_t)b * a.max_pages;
 
     // query rows: row = token * G + head; rows past the end are zeros and see nothing
@@ -482,21 +515,22 @@ __global__ void __launch_bounds__(DA_THREADS) draft_attention_kernel(const Draft
     }
     const float scale2 = a.scale * 1.44269504088896341f;        // scores in units of log 2
     // two tiles are on their way while one is attended to
+    constexpr bool NTL = RT == 1;                     // (with more row tiles, other row blocks may read the codes too)
     Tile<D> t[2];
     char* const stage = s_mem + wave * STAGE<D>;
     int p = t_lo + wave * DA_TILE;
     Pages pg = tile_pages(a, table, p, t_hi);
-    load_tile<D>(a, pg, kvh, p, lane, t[0]);
-    pg = tile_pages(a, table, p + DA_ROUND, t_hi);
-    load_tile<D>(a, pg, kvh, p + DA_ROUND, lane, t[1]);
-    pg = tile_pages(a, table, p + 2 * DA_ROUND, t_hi);
+    load_tile<D, NTL>(a, pg, kvh, p, lane, t[0]);
+    pg = tile_pages(a, table, p + ROUND, t_hi);
+    load_tile<D, NTL>(a, pg, kvh, p + ROUND, lane, t[1]);
+    pg = tile_pages(a, table, p + 2 * ROUND, t_hi);
     auto step = [&](Tile<D>& u) __attribute__((always_inline)) {
         const bool ok[2] = {u.ok[0], u.ok[1]};
         stage_tile<D>(u, stage, lane);
-        load_tile<D>(a, pg, kvh, p + 2 * DA_ROUND, lane, u);
-        pg = tile_pages(a, table, p + 3 * DA_ROUND, t_hi);
+        load_tile<D, NTL>(a, pg, kvh, p + 2 * ROUND, lane, u);
+        pg = tile_pages(a, table, p + 3 * ROUND, t_hi);
         attend_tile<BF, D, FMT, RT>(stage, ok, qv, word, p, s, scale2, lane, st);
-        p += DA_ROUND;
+        p += ROUND;
     };
     while (p < t_hi) {
         step(t[0]);
@@ -520,7 +554,7 @@ __global__ void __launch_bounds__(DA_THREADS) draft_attention_kernel(const Draft
         if (row0 + 16 * r >= rows) break;
         float m = s_m[0][16 * r + c];
 #pragma unroll
-        for (int w = 1; w < DA_WAVES; ++w) m = fmaxf(m, s_m[w][16 * r + c]);
+        for (int w = 1; w < NW; ++w) m = fmaxf(m, s_m[w][16 * r + c]);
         const float f = st.m[r] == m ? 1.0f : __builtin_amdgcn_exp2f(st.m[r] - m);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -531,12 +565,12 @@ __global__ void __launch_bounds__(DA_THREADS) draft_attention_kernel(const Draft
         __syncthreads();
         // 16 threads a row, D / 16 elements each
         const int row = tid >> 4, rr = row0 + 16 * r + row, d0 = (tid & 15) * (D / 16);
-        if (rr < rows) {
+        if (row < 16 && rr < rows) {
             float mm = s_m[0][16 * r + row], l = 0.f;
 #pragma unroll
-            for (int w = 1; w < DA_WAVES; ++w) mm = fmaxf(mm, s_m[w][16 * r + row]);
+            for (int w = 1; w < NW; ++w) mm = fmaxf(mm, s_m[w][16 * r + row]);
 #pragma unroll
-            for (int w = 0; w < DA_WAVES; ++w) {
+            for (int w = 0; w < NW; ++w) {
                 const float mw = s_m[w][16 * r + row];
                 l += s_l[w][16 * r + row] * (mw == mm ? 1.0f : __builtin_amdgcn_exp2f(mw - mm));
             }
@@ -545,7 +579,7 @@ __global__ void __launch_bounds__(DA_THREADS) draft_attention_kernel(const Draft
             for (int e = 0; e < D / 16; e += 4) {
                 f32x4 v = *(const f32x4*)&s_o[0][row][d0 + e];
 #pragma unroll
-                for (int w = 1; w < DA_WAVES; ++w) v += *(const f32x4*)&s_o[w][row][d0 + e];
+                for (int w = 1; w < NW; ++w) v += *(const f32x4*)&s_o[w][row][d0 + e];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) x[e + k] = v[k];
             }
@@ -582,19 +616,30 @@ __global__ void __launch_bounds__(256) draft_join_kernel(const DraftArgs a, int 
     const int64_t stride = (int64_t)n_kv * a.max_q * G;          // rows of a piece
     const int64_t row = ((int64_t)item * n_kv + kvh) * (a.max_q * G) + i * G + (h - kvh * G);
     const int d0 = (threadIdx.x & 15) * (D / 16);
+    const f32x2* ml = (const f32x2*)a.part_ml;
     float m = -__builtin_inff();
-    for (int p = 0; p < pieces; ++p) m = fmaxf(m, a.part_ml[2 * (row + p * stride)]);
+    for (int p = 0; p < pieces; p += 8) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) m = fmaxf(m, ml[row + (p + u < pieces ? p + u : p) * stride][0]);
+    }
     float l = 0.f, x[D / 16] = {};
-    for (int p = 0; p < pieces; ++p) {
-        const float mp = a.part_ml[2 * (row + p * stride)];
-        const float f = mp == m ? 1.0f : __builtin_amdgcn_exp2f(mp - m);
-        l += a.part_ml[2 * (row + p * stride) + 1] * f;
-        const float* po = a.part_o + (row + p * stride) * D + d0;
+    for (int p = 0; p < pieces; p += 4) {                        // four pieces' reads in flight
+        f32x2 q[4];
+        f32x4 v[4][D / 64];
 #pragma unroll
-        for (int e = 0; e < D / 16; e += 4) {
-            const f32x4 v = *(const f32x4*)(po + e);
+        for (int u = 0; u < 4; ++u) {
+            const int64_t r = row + (p + u < pieces ? p + u : p) * stride;
+            q[u] = ml[r];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[e + k] += v[k] * f;
+            for (int e = 0; e < D / 64; ++e) v[u][e] = *(const f32x4*)(a.part_o + r * D + d0 + 4 * e);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (p + u >= pieces) break;
+            const float f = q[u][0] == m ? 1.0f : __builtin_amdgcn_exp2f(q[u][0] - m);
+            l += q[u][1] * f;
+#pragma unroll
+            for (int e = 0; e < D / 16; ++e) x[e] += v[u][e / 4][e % 4] * f;
         }
     }
     const int64_t at = (int64_t)(s.first + i) * a.n_q + h;
@@ -602,19 +647,24 @@ __global__ void __launch_bounds__(256) draft_join_kernel(const DraftArgs a, int 
     if (a.lse && (threadIdx.x & 15) == 0) a.lse[at] = row_lse(m, l);
 }
 
-template <bool BF, int D, int FMT, int RT>
-int launch_rows(const DraftArgs& a, int rt_rows, hipStream_t st) {
-    const int rb = row_blocks(rt_rows, RT);
+int64_t table_tokens(const DraftArgs& a) { return (int64_t)a.max_pages << a.cache.page_shift; }
+
+template <bool BF, int D, int FMT, int RT, int NW>
+int launch_rows(const DraftArgs& a, int rows, hipStream_t st) {
+    const int rb = row_blocks(rows, RT);
+    const int min_piece = NW == DA_WAVES_WIDE ? DA_WIDE_MAX : DA_MIN_PIECE;
     const int64_t items = draft_items(a.n_q, a.cache.n_kv, D, a.dtype, a.B, a.max_q);
     const int64_t units = (items * a.cache.n_kv + 7) / 8 * 8;
     {
         KernelTimer kt_("draft_attention", st);
-        draft_attention_kernel<BF, D, FMT, RT><<<dim3((unsigned)(units * rb)), dim3(DA_THREADS), 0, st>>>(a, (int)items, rb);
+        draft_attention_kernel<BF, D, FMT, RT, NW>
+            <<<dim3((unsigned)(units * rb)), dim3(64 * NW), 0, st>>>(a, (int)items, rb, rb > 1 ? DA_TARGET_BLOCKS : DA_TARGET,
+                                                                     min_piece);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return (int)e;
     }
     // no sequence can be longer than the table: nothing is split
-    if (((int64_t)a.max_pages << a.cache.page_shift) <= DA_MIN_PIECE) return 0;
+    if (table_tokens(a) <= min_piece) return 0;
     const int rows_n = (a.max_q * a.n_q + 15) / 16;
     KernelTimer kt_("draft_join", st);
     draft_join_kernel<BF, D><<<dim3((unsigned)((int64_t)a.B * rows_n)), dim3(256), 0, st>>>(a, rows_n);
@@ -625,12 +675,13 @@ template <bool BF, int D, int FMT>
 int launch_type(const DraftArgs& a, hipStream_t st) {
     const int rows = a.max_q * (a.n_q / a.cache.n_kv);
     const int rt = row_tiles(a.dtype, D, rows);
-    if constexpr (BF) {
-        if (rt == 2) return launch_rows<BF, D, FMT, 2>(a, rows, st);
-        if constexpr (D != 256)
-            if (rt == 4) return launch_rows<BF, D, FMT, 4>(a, rows, st);
-    }
-    return launch_rows<BF, D, FMT, 1>(a, rows, st);
+    if constexpr (BF && D != 256)
+        if (rt == 2) return launch_rows<BF, D, FMT, 2, DA_WAVES>(a, rows, st);
+    // A few sequences that the host knows to be short: eight waves take one whole, which
+    // saves the second kernel (one sequence of 778 tokens: see the kernel times)
+    if (table_tokens(a) <= DA_WIDE_MAX && (int64_t)a.B * a.cache.n_kv * row_blocks(rows, 1) <= 256)
+        return launch_rows<BF, D, FMT, 1, DA_WAVES_WIDE>(a, rows, st);
+    return launch_rows<BF, D, FMT, 1, DA_WAVES>(a, rows, st);
 }
 template <bool BF, int D>
 int launch_fmt(const DraftArgs& a, hipStream_t st) {
@@ -648,8 +699,9 @@ int launch_dim(const DraftArgs& a, hipStream_t st) {
 
 int64_t draft_items(int n_q, int n_kv, int head_dim, int dtype, int B, int max_q) {
     const int rows = max_q * (n_q / n_kv);
-    const int64_t units = (int64_t)n_kv * row_blocks(rows, row_tiles(dtype, head_dim, rows));
-    return (DA_TARGET + units - 1) / units + B;
+    const int rb = row_blocks(rows, row_tiles(dtype, head_dim, rows));
+    const int64_t units = (int64_t)n_kv * rb;
+    return rb > 1 ? (2 * DA_TARGET_BLOCKS + units - 1) / units + B : (DA_TARGET + units - 1) / units + B;
 }
 
 int launch_draft_attention(const DraftArgs& a, void* stream) {
