@@ -48,11 +48,11 @@ constexpr int DA_WAVES = 4, DA_WAVES_WIDE = 8;       // waves of a workgroup (wi
 constexpr int DA_TILE = 32;                          // tokens of a tile
 constexpr int DA_MIN_PIECE = 1024;                   // tokens of a piece, at least
 constexpr int DA_WIDE_MAX = 2048;                    // tokens of a table that wide workgroups take whole
-// workgroups that a large batch is split into: of the 512 that run together, two
-// rounds where the memory sets the pace and any two pieces take the same time (64
-// tokens over 200-8000: 512 111 us, 1024 105, 2048 104 and 2 more to join), four where row blocks of unequal
-// number do (trees of 64 over 30000-100000: 404, 360, 334)
-constexpr int DA_TARGET = 1024, DA_TARGET_BLOCKS = 2048;
+// Workgroups that a large batch is split into: two rounds of the 512 that run together
+// (64 tokens over 200-8000 cached: 512 111 us, 1024 100, 1536 99; trees of 33 over
+// 1-5000, with the second kernel: 1024 50, 1536 52, 2048 55; trees of 64 over
+// 30000-100000: 359, 356, 360)
+constexpr int DA_TARGET = 1024;
 
 // 16-row tiles of query rows per workgroup
 __host__ __device__ inline int row_tiles(int dtype, int head_dim, int rows) {
@@ -80,30 +80,37 @@ __device__ inline SeqInfo sequence(const DraftArgs& a, int b) {
 
 // The pieces of the batch, by one wave.  A workgroup's work is a piece of one
 // sequence's tokens for one key/value head and one block of its rows; pieces have as
-// many tokens, a multiple of `round`, as give about `target` workgroups in all, but at
+// many tokens, a multiple of `round`, as give about DA_TARGET workgroups in all, but at
 // least half of what the batch would ask for with every sequence at max_q: that bounds
-// the pieces by 2 target / (n_kv rb_n) + B, since each sequence ends in one short one.
-__device__ inline int piece_tokens(const DraftArgs& a, int rb_n, int rt, int round, int target, int min_piece, const SeqInfo& mine,
-                                   int lane) {
+// the pieces by 2 DA_TARGET / (n_kv rb_n) + B, since each sequence ends in one short one.
+__device__ inline int piece_tokens(const DraftArgs& a, int rb_n, int rt, int round, int min_piece, const SeqInfo& mine, int lane) {
+    constexpr int target = DA_TARGET;
     const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
     int64_t total = 0, blocks = 0;
+    int ends = 0;                                    // row blocks in all
     for (int b = lane; b < a.B; b += 64) {
         const SeqInfo s = b < 64 ? mine : sequence(a, b);
+        const int rb = s.n > 0 ? row_blocks(s.n * G, rt) : 0;
         total += s.n > 0 ? s.len : 0;
-        blocks += s.n > 0 ? (int64_t)s.len * row_blocks(s.n * G, rt) : 0;
+        blocks += (int64_t)s.len * rb;
+        ends += rb;
     }
     if (a.B > 1) {
 #pragma unroll
         for (int o = 32; o >= 1; o >>= 1) {
             total += __shfl_xor(total, o);
+            ends += __shfl_xor(ends, o);
             if (rb_n > 1) blocks += __shfl_xor(blocks, o);
         }
     } else {
         total = __shfl(total, 0);
         blocks = __shfl(blocks, 0);
+        ends = __shfl(ends, 0);
     }
     if (rb_n == 1) blocks = total;
-    int64_t p = (blocks * n_kv + target - 1) / target;
+    // (a sequence's last piece is half a piece on average)
+    const int64_t half = (int64_t)ends * n_kv / 2, want = half < target / 2 ? target - half : target / 2;
+    int64_t p = (blocks * n_kv + want - 1) / want;
     const int64_t least = (total * n_kv * rb_n + 2 * target - 1) / (2 * target);
     p = p < least ? least : p;
     p = (p + round - 1) / round * round;
@@ -206,7 +213,7 @@ __device__ inline void load_tile(const DraftArgs& a, const Pages& pg, int kvh, i
     t.s = sc[(lane & 16 ? row[1] : row[0]) + (lane & 15)];
 }
 template <int D>
-__device__ inline void stage_tile(const Tile<D>& t, char* st, int lane) {
+__device__ inline void stage_tile(const Tile<D>& t, char* st, int lane, float scale2) {
     constexpr int CH = D / 16;                       // 16-byte chunks of a row
     char* p = st + (lane / CH) * PITCH<D> + (lane % CH) * 16;
 #pragma unroll
@@ -216,7 +223,7 @@ __device__ inline void stage_tile(const Tile<D>& t, char* st, int lane) {
             *(u32x4*)(p + (16 * tb + 64 / CH * i) * PITCH<D>) = t.k[tb][i];
             *(u32x4*)(p + (32 + 16 * tb + 64 / CH * i) * PITCH<D>) = t.v[tb][i];
         }
-    *(float*)(st + 64 * PITCH<D> + 4 * lane) = t.s;
+    *(float*)(st + 64 * PITCH<D> + 4 * lane) = lane < 32 ? t.s * scale2 : t.s;   // (K's in units of the scores)
 }
 
 // The running state of a wave: per row tile, lane (c, g) has row c's maximum (in
@@ -238,16 +245,14 @@ struct Queries { bf16x8 b[N]; };
 
 template <bool BF, int D, int FMT, int RT>
 __device__ inline void attend_tile(const char* stage, const bool* ok, const void* qv, const uint64_t* word,
-                                   int t0, const SeqInfo& s, float scale2, int lane, State<D, RT>& st) {
+                                   int t0, const SeqInfo& s, int lane, State<D, RT>& st) {
     const int c = lane & 15, g = lane >> 4;
     const f32x4* scales = (const f32x4*)(stage + 64 * PITCH<D>) + g;     // of tokens 4g .. 4g + 3
-    f32x4 sc[2][RT];
+    f32x4 sc[2][RT] = {};
 #pragma unroll
-    for (int tb = 0; tb < 2; ++tb) {
+    for (int i = 0; i < D / 64; ++i) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r) sc[tb][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
+        for (int tb = 0; tb < 2; ++tb) {
             // K: token c, elements 64 i + 16 g .. + 15
             const u32x4 kc = *(const u32x4*)(stage + (16 * tb + c) * PITCH<D> + 64 * i + 16 * g);
             if constexpr (BF) {
@@ -280,7 +285,7 @@ __device__ inline void attend_tile(const char* stage, const bool* ok, const void
     const float ninf = -__builtin_inff();
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
-        const f32x4 ks = scales[4 * tb] * scale2;
+        const f32x4 ks = scales[4 * tb];
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -444,8 +449,7 @@ template <int D>
 constexpr int OCC = D == 256 ? 1 : 2;
 
 template <bool BF, int D, int FMT, int RT, int NW>
-__global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const DraftArgs a, int items, int rb_n, int target,
-                                                                           int min_piece) {
+__global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const DraftArgs a, int items, int rb_n, int min_piece) {
     constexpr int LD = D + 4, ROUND = NW * DA_TILE;
     constexpr int SUMS = NW * 16 * LD * 4;
     __shared__ __attribute__((aligned(16))) char s_mem[NW * STAGE<D> > SUMS ? NW * STAGE<D> : SUMS];
@@ -462,10 +466,14 @@ __global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const 
     const int item = unit / n_kv, kvh = unit - item * n_kv;
     SeqInfo mine = {0, 0, 0, 0};
     if (lane < a.B) mine = sequence(a, lane);
-    const int piece = piece_tokens(a, rb_n, RT, ROUND, target, min_piece, mine, lane);
+    // (the same in every lane, and in scalar registers from here on: addresses and branches below rest on it)
+    const int piece = __builtin_amdgcn_readfirstlane(piece_tokens(a, rb_n, RT, ROUND, min_piece, mine, lane));
     int b, j;
-    const SeqInfo s = find_item(a, piece, item, lane, blockIdx.x == 0 && wave == 0, mine, b, j);
+    SeqInfo s = find_item(a, piece, item, lane, blockIdx.x == 0 && wave == 0, mine, b, j);
     b = __builtin_amdgcn_readfirstlane(b);
+    j = __builtin_amdgcn_readfirstlane(j);
+    s = SeqInfo{__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.n), __builtin_amdgcn_readfirstlane(s.ctx),
+                __builtin_amdgcn_readfirstlane(s.len)};
     if (b < 0) return;
     const int rows = s.n * G, row0 = rb * 16 * RT;
     if (row0 >= rows) return;
@@ -526,10 +534,10 @@ __global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const 
     pg = tile_pages(a, table, p + 2 * ROUND, t_hi);
     auto step = [&](Tile<D>& u) __attribute__((always_inline)) {
         const bool ok[2] = {u.ok[0], u.ok[1]};
-        stage_tile<D>(u, stage, lane);
+        stage_tile<D>(u, stage, lane, scale2);
         load_tile<D, NTL>(a, pg, kvh, p + 2 * ROUND, lane, u);
         pg = tile_pages(a, table, p + 3 * ROUND, t_hi);
-        attend_tile<BF, D, FMT, RT>(stage, ok, qv, word, p, s, scale2, lane, st);
+        attend_tile<BF, D, FMT, RT>(stage, ok, qv, word, p, s, lane, st);
         p += ROUND;
     };
     while (p < t_hi) {
@@ -658,8 +666,7 @@ int launch_rows(const DraftArgs& a, int rows, hipStream_t st) {
     {
         KernelTimer kt_("draft_attention", st);
         draft_attention_kernel<BF, D, FMT, RT, NW>
-            <<<dim3((unsigned)(units * rb)), dim3(64 * NW), 0, st>>>(a, (int)items, rb, rb > 1 ? DA_TARGET_BLOCKS : DA_TARGET,
-                                                                     min_piece);
+            <<<dim3((unsigned)(units * rb)), dim3(64 * NW), 0, st>>>(a, (int)items, rb, min_piece);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return (int)e;
     }
@@ -701,7 +708,7 @@ int64_t draft_items(int n_q, int n_kv, int head_dim, int dtype, int B, int max_q
     const int rows = max_q * (n_q / n_kv);
     const int rb = row_blocks(rows, row_tiles(dtype, head_dim, rows));
     const int64_t units = (int64_t)n_kv * rb;
-    return rb > 1 ? (2 * DA_TARGET_BLOCKS + units - 1) / units + B : (DA_TARGET + units - 1) / units + B;
+    return (2 * DA_TARGET + units - 1) / units + B;
 }
 
 int launch_draft_attention(const DraftArgs& a, void* stream) {
