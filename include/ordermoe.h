@@ -515,7 +515,7 @@ typedef struct {
     int32_t interleaved;    /* 1: elements 2i and 2i + 1 turn together; 0: i and i + rotary_dim / 2 */
     int64_t max_pos;        /* rows of cos_sin */
     float eps;              /* of the norms, >= 0 */
-    const void* q_norm;     /* dev [head_dim] weights of the query norm, or NULL: no query norm */
+    const void* q_norm;     /* dev [head_dim] weights of the query norm, or NULL: no query norm (all three 16-byte aligned) */
     const void* k_norm;     /* dev [head_dim] weights of the key norm, or NULL: no key norm */
     const float* cos_sin;   /* dev [max_pos][rotary_dim]: per position the cosines of the rotary_dim / 2
                                angles, then their sines; NULL if rotary_dim = 0 */

@@ -22,7 +22,8 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int CW_THREADS = 256;
-constexpr int CW_ROWS = CW_THREADS / 16;     // head rows per block
+constexpr int CW_ROWS = CW_THREADS / 16;     // 16-lane groups per block
+constexpr int64_t CW_MANY = 1 << 16;         // head rows from which a group takes four: twice the chip's waves
 
 // reductions over the 16 lanes of a DPP row, by rotations of 8, 4, 2, 1; every
 // lane ends with the same bits (each step adds the same two values in both lanes)
@@ -44,35 +45,41 @@ __device__ inline uint32_t row_max(uint32_t v) {
     return v;
 }
 
-// N neighbouring elements of storage T as fp32, and back
+// N neighbouring elements of storage T: as read, and as fp32
 template <typename T, int N>
-__device__ inline void load_f32(const T* p, float* x) {
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int i = 0; i < N / 4; ++i) {
-            const u32x4 v = ((const u32x4*)p)[i];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[4 * i + j] = __uint_as_float(v[j]);
-        }
-    } else {
-        uint32_t w[N / 2];
-        if constexpr (N == 4) {
+struct Raw {
+    static constexpr int W = N * (int)sizeof(T) / 4;
+    uint32_t w[W];
+    __device__ inline void load(const T* p) {
+        if constexpr (W == 2) {
             const u32x2 v = *(const u32x2*)p;
             w[0] = v[0]; w[1] = v[1];
         } else {
 #pragma unroll
-            for (int i = 0; i < N / 8; ++i) {
+            for (int i = 0; i < W / 4; ++i) {
                 const u32x4 v = ((const u32x4*)p)[i];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
             }
         }
+    }
+    __device__ inline void f32(float* x) const {
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        for (int i = 0; i < W; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                x[i] = __uint_as_float(w[i]);
+            } else {
+                x[2 * i] = __uint_as_float(w[i] << 16);
+                x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            }
         }
     }
+};
+template <typename T, int N>
+__device__ inline void load_f32(const T* p, float* x) {
+    Raw<T, N> r;
+    r.load(p);
+    r.f32(x);
 }
 template <typename T, int N>
 __device__ inline void store_f32(T* p, const float* x) {
@@ -125,124 +132,198 @@ __device__ inline int64_t cache_row(const CacheArgs& c, int64_t slot, int h) {
     return (((slot >> c.page_shift) * c.n_kv + h) << c.page_shift) + (slot & (((int64_t)1 << c.page_shift) - 1));
 }
 
+// x / b for x of a magnitude of at most 2^30 b, rounded as an IEEE division rounds it
+// where that can matter to the code: with r the correctly rounded 1 / b and q = x r
+// within a unit in the last place, q + r (x - b q) with fused steps is the correctly
+// rounded quotient (Markstein).  (The residual is exact unless x is below 2^-125, whose
+// quotient is below 2^-16: code 0 either way.)  The divisions took a third of the kernel.
+__device__ inline float quotient(float x, float b, float r) {
+    const float q = x * r;
+    return fmaf(fmaf(-q, b, x), r, q);
+}
+
+// row / n for row < 2^31, by a product (n >= 2)
+__device__ inline uint32_t divided(uint32_t row, const Divisor& n) { return __umulhi(row, n.mul) >> n.shift; }
+
+// One head row of N elements per lane, already read (x): all of its work.
 template <typename T, int D, int FMT>
-__global__ void __launch_bounds__(CW_THREADS) cache_write_kernel(const CacheWriteArgs a) {
+__device__ inline void write_head_row(const CacheWriteArgs& a, uint32_t t, int h, int pos, int64_t slot, float* x, int c) {
     constexpr int N = D / 16;                                   // elements per lane
-    const int c = threadIdx.x & 15;
-    const uint32_t heads = (uint32_t)(a.n_q + 2 * a.cache.n_kv);
-    const uint32_t row = blockIdx.x * CW_ROWS + (threadIdx.x >> 4);
-    if (row >= (uint32_t)a.T * heads) return;                   // whole rows leave together
-    const int64_t t = row / heads;
-    const int h = (int)(row - (uint32_t)t * heads);
     const int kind = h < a.n_q ? 0 : h < a.n_q + a.cache.n_kv ? 1 : 2;      // query, key, value
     const int hk = h - a.n_q - (kind == 2 ? a.cache.n_kv : 0);
-    const T* src = kind == 0 ? (const T*)a.q + t * a.q_stride + h * D
-                             : (kind == 1 ? (const T*)a.k + t * a.k_stride : (const T*)a.v + t * a.v_stride) + hk * D;
-    float x[N];
-    load_f32<T, N>(src + c * N, x);
     const T* nw = (const T*)(kind == 0 ? a.q_norm : kind == 1 ? a.k_norm : nullptr);
+    const bool turn = kind != 2 && a.rot;
+    const int half = a.rot / 2;
+    const float* cs = a.cos_sin;
+    bool in = true;
+    // the lane's pairs (interleaved: N / 2 from c N / 2 on; else N, of its own elements or its partner's)
+    const int dl = half / N;
+    const bool lo = c < dl, turned = turn && (a.interleaved ? c * (N / 2) < half : c < 2 * dl);
+    float co[N], si[N];
+    if (turn) {
+        in = pos >= 0 && (int64_t)pos < a.max_pos;
+        cs += (int64_t)(in ? pos : 0) * a.rot;
+        if (a.interleaved) {
+            load_f32<float, N / 2 < 4 ? 4 : N / 2>(cs + (turned ? c * (N / 2) & ~3 : 0), co);
+            load_f32<float, N / 2 < 4 ? 4 : N / 2>(cs + half + (turned ? c * (N / 2) & ~3 : 0), si);
+            if (N == 4 && (c & 1)) {                            // (two pairs a lane, read with the neighbour's)
+                co[0] = co[2]; co[1] = co[3];
+                si[0] = si[2]; si[1] = si[3];
+            }
+        } else {
+            const int i0 = turned ? (lo ? c : c - dl) * N : 0;
+            load_f32<float, N>(cs + i0, co);
+            load_f32<float, N>(cs + half + i0, si);
+        }
+    }
     if (nw) {
         float w[N], s = 0.f;
         load_f32<T, N>(nw + c * N, w);
 #pragma unroll
         for (int i = 0; i < N; ++i) s = fmaf(x[i], x[i], s);
-        const float r = 1.0f / sqrtf(row_sum(s) * (1.0f / D) + a.eps);
+        const float r = __builtin_amdgcn_rsqf(row_sum(s) * (1.0f / D) + a.eps);
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] = x[i] * r * w[i];
     }
-    if (kind != 2 && a.rot) {
-        const int half = a.rot / 2, p = a.pos[t];
-        const bool in = p >= 0 && (int64_t)p < a.max_pos;
-        const float* cs = a.cos_sin + (int64_t)(in ? p : 0) * a.rot;
-        const float nan = __builtin_nanf("");
+    if (turn) {
         if (a.interleaved) {
-            const int i0 = c * (N / 2);                         // first pair of the lane
-            if (i0 < half) {
 #pragma unroll
-                for (int i = 0; i < N / 2; ++i) {
-                    const float co = in ? cs[i0 + i] : nan, si = in ? cs[half + i0 + i] : nan;
-                    const float u = x[2 * i], v = x[2 * i + 1];
-                    x[2 * i] = u * co - v * si;
-                    x[2 * i + 1] = v * co + u * si;
-                }
+            for (int i = 0; i < N / 2; ++i) {
+                const float u = x[2 * i], v = x[2 * i + 1];
+                x[2 * i] = turned ? fmaf(u, co[i], -(v * si[i])) : u;
+                x[2 * i + 1] = turned ? fmaf(v, co[i], u * si[i]) : v;
             }
         } else {
             // the partner of element i is i +- half, `half / N` lanes away (whole lanes, since half is a multiple of N)
-            const int dl = half / N;
-            const bool lo = c < dl, turned = c < 2 * dl;
             const int from = turned ? (lo ? c + dl : c - dl) : c;
-            const int i0 = turned ? (lo ? c : c - dl) * N : 0;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const float o = __shfl(x[i], from, 16);
-                const float co = in ? cs[i0 + i] : nan, si = in ? cs[half + i0 + i] : nan;
-                const float y = lo ? x[i] * co - o * si : x[i] * co + o * si;
+                const float y = fmaf(o, lo ? -si[i] : si[i], x[i] * co[i]);
                 x[i] = turned ? y : x[i];
             }
         }
+        if (!in && turned)                                      // no such position
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = __builtin_nanf("");
     }
     if (kind == 0) {
-        store_f32<T, N>((T*)a.q_out + (t * a.n_q + h) * D + c * N, x);
+        store_f32<T, N>((T*)a.q_out + ((int64_t)t * a.n_q + h) * D + c * N, x);
         return;
     }
     // the largest magnitude on the bits, where a NaN is larger than infinity
     uint32_t big = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const uint32_t b = __float_as_uint(x[i]) & 0x7FFFFFFFu;
+        const uint32_t b = __float_as_uint(x[i]) << 1;          // (without the sign)
         big = b > big ? b : big;
     }
-    big = row_max(big);
+    big = row_max(big) >> 1;
     const bool bad = big >= 0x7F800000u, none = __uint_as_float(big) < KV_TINY;
     const float scale = bad ? __builtin_nanf("") : none ? 0.f : __uint_as_float(big) / kv_code_max<FMT>();
+    const float inv = 1.0f / scale;
     uint32_t w[N / 4];
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
-        w[i] = 0u;
-        if (!bad && !none) {
-            float y[4];
+        float y[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                y[j] = __builtin_amdgcn_fmed3f(x[4 * i + j] / scale, -kv_code_max<FMT>(), kv_code_max<FMT>());
-            w[i] = kv_to_codes<FMT>(y[0], y[1], y[2], y[3]);
-        }
+        for (int j = 0; j < 4; ++j) y[j] = quotient(x[4 * i + j], scale, inv);
+        w[i] = bad || none ? 0u : kv_to_codes<FMT>(y[0], y[1], y[2], y[3]);
     }
-    const int64_t slot = a.slots[t];
     if (slot < 0 || slot >= (a.cache.n_pages << a.cache.page_shift)) return;
     const int64_t at = cache_row(a.cache, slot, hk);
     store_codes<N>((kind == 1 ? a.cache.k_codes : a.cache.v_codes) + at * D + c * N, w);
     if (c == 0) (kind == 1 ? a.cache.k_scale : a.cache.v_scale)[at] = scale;
 }
 
-template <typename T, int D, int FMT>
-__global__ void __launch_bounds__(CW_THREADS) cache_read_kernel(const CacheReadArgs a) {
+// U rows per 16 lanes, all read before the first is worked on: one row a lane leaves
+// too few bytes on their way for a prompt's rows (16001 tokens of 16 + 16 + 16 heads of 128: one row 94 us, four 90);
+// a step's are too few to share four by four.
+template <typename T, int D, int FMT, int U>
+__global__ void __launch_bounds__(CW_THREADS) cache_write_kernel(const CacheWriteArgs a) {
     constexpr int N = D / 16;
     const int c = threadIdx.x & 15;
-    const uint32_t nh = (uint32_t)a.cache.n_kv, per = 2 * nh;
-    const uint32_t row = blockIdx.x * CW_ROWS + (threadIdx.x >> 4);
-    if (row >= (uint32_t)a.n * per) return;
-    const int64_t i = row / per;
-    const int r = (int)(row - (uint32_t)i * per);
-    const bool is_v = r >= (int)nh;
-    const int h = is_v ? r - (int)nh : r;
-    const int64_t slot = a.slots[i];
-    float x[N];
+    const uint32_t heads = (uint32_t)(a.n_q + 2 * a.cache.n_kv), rows = (uint32_t)a.T * heads;
+    const uint32_t row0 = blockIdx.x * (CW_ROWS * U) + (threadIdx.x >> 4);
+    uint32_t t[U];
+    int h[U], pos[U];
+    int64_t slot[U];
+    Raw<T, N> raw[U];
 #pragma unroll
-    for (int j = 0; j < N; ++j) x[j] = 0.f;
-    if (slot >= 0 && slot < (a.cache.n_pages << a.cache.page_shift)) {
-        const int64_t at = cache_row(a.cache, slot, h);
-        uint32_t w[N / 4];
-        load_codes<N>((is_v ? a.cache.v_codes : a.cache.k_codes) + at * D + c * N, w);
-        const float s = (is_v ? a.cache.v_scale : a.cache.k_scale)[at];
+    for (int u = 0; u < U; ++u) {
+        const uint32_t row = row0 + CW_ROWS * u < rows ? row0 + CW_ROWS * u : 0;     // (past the end: read, not worked on)
+        t[u] = divided(row, a.heads);
+        h[u] = (int)(row - t[u] * heads);
+        const int hk = h[u] - a.n_q, hv = hk - a.cache.n_kv;
+        const T* src = hk < 0 ? (const T*)a.q + (int64_t)t[u] * a.q_stride + h[u] * D
+                       : hv < 0 ? (const T*)a.k + (int64_t)t[u] * a.k_stride + hk * D
+                                : (const T*)a.v + (int64_t)t[u] * a.v_stride + hv * D;
+        raw[u].load(src + c * N);
+        pos[u] = hv < 0 && a.rot ? a.pos[t[u]] : 0;
+        slot[u] = hk < 0 ? -1 : a.slots[t[u]];
+    }
 #pragma unroll
-        for (int j = 0; j < N / 4; ++j) {
-            x[4 * j] = kv_to_f32<FMT, 0>(w[j]) * s;
-            x[4 * j + 1] = kv_to_f32<FMT, 1>(w[j]) * s;
-            x[4 * j + 2] = kv_to_f32<FMT, 2>(w[j]) * s;
-            x[4 * j + 3] = kv_to_f32<FMT, 3>(w[j]) * s;
+    for (int u = 0; u < U; ++u) {
+        if (row0 + CW_ROWS * u >= rows) return;                 // whole rows leave together
+        float x[N];
+        raw[u].f32(x);
+        write_head_row<T, D, FMT>(a, t[u], h[u], pos[u], slot[u], x, c);
+    }
+}
+
+// U rows per 16 lanes, their reads in flight together; a store covers 256 neighbouring
+// bytes of a row (lane: 16 bytes of every 256)
+constexpr int CR_U = 4;
+template <typename T, int D, int FMT>
+__global__ void __launch_bounds__(CW_THREADS) cache_read_kernel(const CacheReadArgs a) {
+    constexpr int N = 16 / sizeof(T);                           // elements of 16 bytes
+    constexpr int C = D / (16 * N) > 0 ? D / (16 * N) : 1;      // 256-byte chunks of a row (or less than one)
+    const int c = threadIdx.x & 15;
+    const bool on = D >= 16 * N || c < D / N;                   // lanes with a part of the row
+    const uint32_t nh = (uint32_t)a.cache.n_kv, per = 2 * nh, rows = (uint32_t)a.n * per;
+    const uint32_t row0 = blockIdx.x * (CW_ROWS * CR_U) + (threadIdx.x >> 4);
+    uint32_t i[CR_U], r[CR_U];
+    int64_t slot[CR_U];
+#pragma unroll
+    for (int u = 0; u < CR_U; ++u) {
+        const uint32_t row = row0 + CW_ROWS * u;
+        i[u] = divided(row < rows ? row : 0, a.per);
+        r[u] = (row < rows ? row : 0) - i[u] * per;
+        slot[u] = row < rows ? a.slots[i[u]] : -1;
+    }
+    uint32_t w[CR_U][C][N / 4];
+    float s[CR_U];
+    bool there[CR_U];
+#pragma unroll
+    for (int u = 0; u < CR_U; ++u) {
+        const bool is_v = r[u] >= nh;
+        there[u] = slot[u] >= 0 && slot[u] < (a.cache.n_pages << a.cache.page_shift);
+        const int64_t at = cache_row(a.cache, there[u] ? slot[u] : 0, (int)(is_v ? r[u] - nh : r[u]));
+        const uint8_t* p = (is_v ? a.cache.v_codes : a.cache.k_codes) + at * D + (on ? c * N : 0);
+#pragma unroll
+        for (int k = 0; k < C; ++k) load_codes<N>(p + 16 * N * k, w[u][k]);
+        s[u] = (is_v ? a.cache.v_scale : a.cache.k_scale)[at];
+    }
+#pragma unroll
+    for (int u = 0; u < CR_U; ++u) {
+        if (row0 + CW_ROWS * u >= rows) break;
+        const bool is_v = r[u] >= nh;
+        T* o = (T*)(is_v ? a.v_out : a.k_out) + ((int64_t)i[u] * nh + (is_v ? r[u] - nh : r[u])) * D + c * N;
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            float x[N];
+#pragma unroll
+            for (int j = 0; j < N / 4; ++j) {
+                x[4 * j] = kv_to_f32<FMT, 0>(w[u][k][j]) * s[u];
+                x[4 * j + 1] = kv_to_f32<FMT, 1>(w[u][k][j]) * s[u];
+                x[4 * j + 2] = kv_to_f32<FMT, 2>(w[u][k][j]) * s[u];
+                x[4 * j + 3] = kv_to_f32<FMT, 3>(w[u][k][j]) * s[u];
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) x[j] = there[u] ? x[j] : 0.f;
+            if (on) store_f32<T, N>(o + 16 * N * k, x);
         }
     }
-    store_f32<T, N>((T*)(is_v ? a.v_out : a.k_out) + (i * nh + h) * D + c * N, x);
 }
 
 // calls f<T, D, FMT> for the storage type, head size and format
@@ -260,26 +341,42 @@ int by_type(int dtype, const CacheArgs& c, F f) {
     return dtype == ORDERMOE_BF16 ? with_d(__bf16{}) : with_d(float{});
 }
 
+// with 2^s the power of two from n on: row / n = (row m) / 2^(31 + s) rounded down, m = 2^(31 + s) / n rounded
+// down, plus 1, for every row < 2^31 (m exceeds the quotient by at most 2^-31 of a unit of row)
+Divisor divisor(int n) {
+    int s = 1;
+    while ((1 << s) < n) ++s;
+    return Divisor{(uint32_t)(((uint64_t)1 << (31 + s)) / (uint64_t)n + 1), s - 1};
+}
+
 }  // namespace
 
-int launch_cache_write(const CacheWriteArgs& a, void* stream) {
+int launch_cache_write(const CacheWriteArgs& args, void* stream) {
+    CacheWriteArgs a = args;
+    a.heads = divisor(a.n_q + 2 * a.cache.n_kv);
     const int64_t rows = a.T * (a.n_q + 2 * a.cache.n_kv);
     if (rows == 0) return 0;
     return by_type(a.dtype, a.cache, [&](auto t, auto d, auto f) {
         KernelTimer kt_("cache_write", stream);
-        cache_write_kernel<decltype(t), decltype(d)::value, decltype(f)::value>
-            <<<dim3((unsigned)((rows + CW_ROWS - 1) / CW_ROWS)), dim3(CW_THREADS), 0, (hipStream_t)stream>>>(a);
+        constexpr int D = decltype(d)::value, F = decltype(f)::value;
+        auto blocks = [&](int u) { return dim3((unsigned)((rows + CW_ROWS * u - 1) / (CW_ROWS * u))); };
+        if (rows >= CW_MANY)
+            cache_write_kernel<decltype(t), D, F, 4><<<blocks(4), dim3(CW_THREADS), 0, (hipStream_t)stream>>>(a);
+        else
+            cache_write_kernel<decltype(t), D, F, 1><<<blocks(1), dim3(CW_THREADS), 0, (hipStream_t)stream>>>(a);
         return (int)hipGetLastError();
     });
 }
 
-int launch_cache_read(const CacheReadArgs& a, void* stream) {
+int launch_cache_read(const CacheReadArgs& args, void* stream) {
+    CacheReadArgs a = args;
+    a.per = divisor(2 * a.cache.n_kv);
     const int64_t rows = a.n * 2 * a.cache.n_kv;
     if (rows == 0) return 0;
     return by_type(a.dtype, a.cache, [&](auto t, auto d, auto f) {
         KernelTimer kt_("cache_read", stream);
         cache_read_kernel<decltype(t), decltype(d)::value, decltype(f)::value>
-            <<<dim3((unsigned)((rows + CW_ROWS - 1) / CW_ROWS)), dim3(CW_THREADS), 0, (hipStream_t)stream>>>(a);
+            <<<dim3((unsigned)((rows + CW_ROWS * CR_U - 1) / (CW_ROWS * CR_U))), dim3(CW_THREADS), 0, (hipStream_t)stream>>>(a);
         return (int)hipGetLastError();
     });
 }

@@ -191,8 +191,14 @@ struct CacheArgs {
     float* k_scale;
     float* v_scale;
 };
+// row / n as a product: umulhi(row, mul) >> shift
+struct Divisor {
+    uint32_t mul;
+    int shift;
+};
 struct CacheWriteArgs {
     CacheArgs cache;
+    Divisor heads;         // set by the launcher: of n_q + 2 n_kv
     int dtype, n_q, rot, interleaved;
     float eps;
     int64_t max_pos;
@@ -210,6 +216,7 @@ struct CacheWriteArgs {
 int launch_cache_write(const CacheWriteArgs& a, void* stream);
 struct CacheReadArgs {
     CacheArgs cache;
+    Divisor per;           // set by the launcher: of 2 n_kv
     int dtype;
     const int64_t* slots;
     int64_t n;

@@ -96,8 +96,8 @@ extern "C" int ordermoe_cache_write(const ordermoe_cache* C, const ordermoe_head
         return fail(ORDERMOE_EINVAL, "cache_write: strides must hold the heads and be multiples of 16 bytes");
     if (T > 0 && (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out)))
         return fail(ORDERMOE_EINVAL, "cache_write: q, k, v and q_out must be 16-byte aligned");
-    if ((H->q_norm && !aligned16(H->q_norm)) || (H->k_norm && !aligned16(H->k_norm)))
-        return fail(ORDERMOE_EINVAL, "cache_write: norm weights must be 16-byte aligned");
+    if ((H->q_norm && !aligned16(H->q_norm)) || (H->k_norm && !aligned16(H->k_norm)) || (H->rotary_dim > 0 && !aligned16(H->cos_sin)))
+        return fail(ORDERMOE_EINVAL, "cache_write: norm weights and cos_sin must be 16-byte aligned");
     CacheWriteArgs a{};
     a.cache = cache_args(C);
     a.dtype = H->dtype; a.n_q = H->n_q; a.rot = H->rotary_dim; a.interleaved = H->interleaved;

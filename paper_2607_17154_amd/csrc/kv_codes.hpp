@@ -43,8 +43,11 @@ __device__ inline uint32_t kv_to_bf16x2(uint32_t w) {
 template <int FMT>
 __device__ inline uint32_t kv_to_codes(float a, float b, float c, float d) {
     if constexpr (FMT == ORDERMOE_CACHE_INT8) {
-        return ((uint32_t)(int)rintf(a) & 255u) | ((uint32_t)(int)rintf(b) & 255u) << 8 |
-               ((uint32_t)(int)rintf(c) & 255u) << 16 | (uint32_t)(int)rintf(d) << 24;
+        // 1.5 2^23 + y rounds y to the nearest integer, ties to even, and its low byte is the code
+        const uint32_t m[4] = {__float_as_uint(a + 0x1.8p23f), __float_as_uint(b + 0x1.8p23f), __float_as_uint(c + 0x1.8p23f),
+                               __float_as_uint(d + 0x1.8p23f)};
+        return __builtin_amdgcn_perm(__builtin_amdgcn_perm(m[3], m[2], 0x0c0c0400u), __builtin_amdgcn_perm(m[1], m[0], 0x0c0c0400u),
+                                     0x05040100u);
     } else {
         int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
         return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);

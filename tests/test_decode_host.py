@@ -46,6 +46,7 @@ def test_a_bad_cache_is_refused_everywhere(kw):
     (dict(dtype=5), {}), (dict(n_q=3), {}), (dict(n_q=0), {}), (dict(n_q=1026), {}), (dict(rotary_dim=8), {}),
     (dict(rotary_dim=144), {}), (dict(rotary_dim=-16), {}), (dict(interleaved=2), {}), (dict(eps=-1.0), {}),
     (dict(eps=float("nan")), {}), (dict(eps=float("inf")), {}), (dict(max_pos=0), {}), (dict(cos_sin=None), {}), (dict(q_norm=P + 2), {}),
+    (dict(cos_sin=P + 4), {}),
     ({}, dict(T=-1)), ({}, dict(T=1 << 29)), ({}, dict(q=0)), ({}, dict(k=0)), ({}, dict(v=0)), ({}, dict(pos=0)),
     ({}, dict(slots=0)), ({}, dict(out=0)), ({}, dict(q=P + 8)), ({}, dict(out=P + 4)), ({}, dict(qs=504)), ({}, dict(ks=260)),
     ({}, dict(vs=0)), (dict(dtype=om.F32), dict(ks=258)),
