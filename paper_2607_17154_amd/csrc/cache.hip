@@ -81,7 +81,12 @@ __device__ inline void load_f32(const T* p, float* x) {
     r.load(p);
     r.f32(x);
 }
-template <typename T, int N>
+template <bool NTS>
+__device__ inline void store16(void* p, u32x4 v) {
+    if constexpr (NTS) __builtin_nontemporal_store(v, (u32x4*)p);
+    else *(u32x4*)p = v;
+}
+template <typename T, int N, bool NTS = false>
 __device__ inline void store_f32(T* p, const float* x) {
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
@@ -89,7 +94,7 @@ __device__ inline void store_f32(T* p, const float* x) {
             u32x4 v;
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = __float_as_uint(x[4 * i + j]);
-            ((u32x4*)p)[i] = v;
+            store16<NTS>((u32x4*)p + i, v);
         }
     } else {
         uint32_t w[N / 2];
@@ -104,7 +109,7 @@ __device__ inline void store_f32(T* p, const float* x) {
             *(u32x2*)p = u32x2{w[0], w[1]};
         } else {
 #pragma unroll
-            for (int i = 0; i < N / 8; ++i) ((u32x4*)p)[i] = u32x4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+            for (int i = 0; i < N / 8; ++i) store16<NTS>((u32x4*)p + i, u32x4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]});
         }
     }
 }
@@ -271,10 +276,13 @@ __global__ void __launch_bounds__(CW_THREADS) cache_write_kernel(const CacheWrit
     }
 }
 
-// U rows per 16 lanes, their reads in flight together; a store covers 256 neighbouring
-// bytes of a row (lane: 16 bytes of every 256)
+// CR_U rows per 16 lanes, their reads in flight together; a store covers 256
+// neighbouring bytes of a row (lane: 16 bytes of every 256).  Outputs that outgrow the
+// caches are stored past them: 60001 rows as fp32 118 us (5.3 TB/s; 126 otherwise),
+// 16001 as bf16 38 (44).
 constexpr int CR_U = 4;
-template <typename T, int D, int FMT>
+constexpr int64_t CR_STREAM_BYTES = (int64_t)64 << 20;
+template <typename T, int D, int FMT, bool NTS>
 __global__ void __launch_bounds__(CW_THREADS) cache_read_kernel(const CacheReadArgs a) {
     constexpr int N = 16 / sizeof(T);                           // elements of 16 bytes
     constexpr int C = D / (16 * N) > 0 ? D / (16 * N) : 1;      // 256-byte chunks of a row (or less than one)
@@ -321,7 +329,7 @@ __global__ void __launch_bounds__(CW_THREADS) cache_read_kernel(const CacheReadA
             }
 #pragma unroll
             for (int j = 0; j < N; ++j) x[j] = there[u] ? x[j] : 0.f;
-            if (on) store_f32<T, N>(o + 16 * N * k, x);
+            if (on) store_f32<T, N, NTS>(o + 16 * N * k, x);
         }
     }
 }
@@ -375,8 +383,12 @@ int launch_cache_read(const CacheReadArgs& args, void* stream) {
     if (rows == 0) return 0;
     return by_type(a.dtype, a.cache, [&](auto t, auto d, auto f) {
         KernelTimer kt_("cache_read", stream);
-        cache_read_kernel<decltype(t), decltype(d)::value, decltype(f)::value>
-            <<<dim3((unsigned)((rows + CW_ROWS * CR_U - 1) / (CW_ROWS * CR_U))), dim3(CW_THREADS), 0, (hipStream_t)stream>>>(a);
+        constexpr int D = decltype(d)::value, F = decltype(f)::value;
+        const dim3 blocks((unsigned)((rows + CW_ROWS * CR_U - 1) / (CW_ROWS * CR_U)));
+        if (rows * D * (int64_t)sizeof(t) >= CR_STREAM_BYTES)
+            cache_read_kernel<decltype(t), D, F, true><<<blocks, dim3(CW_THREADS), 0, (hipStream_t)stream>>>(a);
+        else
+            cache_read_kernel<decltype(t), D, F, false><<<blocks, dim3(CW_THREADS), 0, (hipStream_t)stream>>>(a);
         return (int)hipGetLastError();
     });
 }
