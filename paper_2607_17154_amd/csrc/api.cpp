@@ -376,7 +376,7 @@ extern "C" int ordermoe_local_moe_forward(const ordermoe_experts* W, const void*
 // ------------------------------------------------------------ the layer for a few tokens
 static size_t few_ws(const ordermoe_experts* W, Carver& c, FewArgs* a) {
     const size_t esz = W->dtype == ORDERMOE_BF16 ? 2 : 4;
-    float* lg = c.take<float>((size_t)ORDERMOE_MAX_FEW * ORDERMOE_MAX_EXPERTS);
+    char* lg = c.take<char>((size_t)16 * ORDERMOE_MAX_FEW * ORDERMOE_MAX_EXPERTS * (esz == 2 ? sizeof(float) : sizeof(double)));
     int32_t* ct = c.take<int32_t>(few_counters(W->d));
     float* pt = c.take<float>((size_t)W->d * 16 * ORDERMOE_MAX_FEW);
     char* ar = c.take<char>((size_t)W->n_local * ORDERMOE_MAX_FEW * W->f * esz);

@@ -126,7 +126,7 @@ struct FewArgs {
     const void* w_sh_dn;
     void* y;
     // workspace
-    float* logits;         // [ORDERMOE_MAX_FEW][Epad]
+    void* logits;          // [K slices <= 16][ORDERMOE_MAX_FEW][Epad] sums of the router's slices (bf16: fp32, fp32: fp64)
     int32_t* ctr;          // [few_counters(d)] work counters
     float* part;           // [d / 64][16][ORDERMOE_MAX_FEW][64] sums of the pieces
     void* act_r;           // [n_local][ORDERMOE_MAX_FEW][f] weighted activations

@@ -1,27 +1,33 @@
-// The whole MoE layer of one server for at most ORDERMOE_MAX_FEW = 16 tokens.
+// The whole MoE layer of one server for at most ORDERMOE_MAX_FEW = 16 tokens:
+//   l = x W_r^T, the routing decisions of route_select on l, and
+//   y[t] = sum over the slots of t executed here of w (silu(x G^T) * x U^T) D^T
+//          + the shared experts of the tokens that are at home here.
 //
-//   few_router_kernel  logits l = x W_r^T: a workgroup per 16 experts, a wave per K
-//                      slice (the slices of the split router of small batches, added in
-//                      the same order: the same logits); clears the work counters
-//   few_layer_kernel   everything else.  Every workgroup runs the token stage of the
-//                      routing itself (a few microseconds of latency, the same in all of
-//                      them; the first one writes the routing's outputs), which tells it
-//                      the experts in use and their tokens.  Then the workgroups draw
-//                      work items from a counter:
+//   few_router_kernel  sums of l over K slices: a wave per (16 experts, slice), the
+//                      slices of the split router of small batches, so that added in
+//                      the same order they are the same logits; clears the counters
+//   few_layer_kernel   everything else, in at most FW_SHARES workgroups.  Each adds the
+//                      router's slices and runs the token stage of the routing itself (about
+//                      7 us of latency, side by side; the first one writes the routing's
+//                      outputs), which tells it the experts in use and their tokens.
+//                      Then it works through its share of two lists:
 //     activation tiles   32 FFN columns of one expert: gate and up rows times the
 //                        tokens, silu(g) u w -> the weighted activations (memory)
 //     output tiles       64 output columns: the down rows of every expert in use times
 //                        its weighted activations, summed over the experts in one
 //                        accumulator, in up to 16 pieces along the experts' columns whose
 //                        sums the last one to finish adds in order -> y
-// An output tile needs all activations.  Items are drawn in order, activation tiles
-// first, and one never waits: whoever draws an output tile knows that every
-// activation tile is in the hands of a running workgroup, so its wait ends without
-// any assumption on which workgroups run together.  It reads its first weights
-// before it waits, so that the weight stream does not stop in between.
-// The weights in use are read once; they bound the time.  The 16 tokens are the
-// columns of one v_mfma_f32_16x16x32_bf16 (fp32: v_mfma_f32_16x16x4_f32), the
-// weights its rows, straight from memory in the lane order of the operand.
+// An output tile needs all activations.  A workgroup waits for them only after its own
+// share's activation tiles and those of every share that no workgroup has drawn yet,
+// so all waits end whatever else runs on the GPU.  It reads the first weights of its
+// output tile before it waits, so that the weight stream does not stop in between.
+// The 16 tokens are the columns of one v_mfma_f32_16x16x32_bf16 (fp32:
+// v_mfma_f32_16x16x4_f32), the weights its rows, read in whole cache lines and turned
+// into the operand's lane order through LDS.
+// Bound: the weights in use, read once; below some 100 MB of them the latency of router,
+// token stage and hand-over (about 5 + 7 + 3 us).  d 4096, f 1536, bf16, both kernels:
+// 16 tokens with 24 experts in use (906 MB) 167 us, 5.4 TB/s; 1 token with 2
+// (75 MB) 37 us.  route_select and local_moe_forward in turn: 180 and 50 us.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -41,11 +47,11 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 constexpr int FW = ORDERMOE_MAX_FEW;
 static_assert(FW == 16, "the tokens are the columns of one matrix instruction");
 constexpr int FW_WAVES = 8, FW_THREADS = 64 * FW_WAVES;
-constexpr int FW_PER_CU = 1;                      // workgroups per CU
-constexpr int FW_ITEMS = 256 * FW_PER_CU;         // output items wished for
+constexpr int FW_ITEMS = 256;                     // output items wished for
 constexpr int FW_PIECES = 16;                     // pieces of an output tile, at most
 constexpr int FW_XCDS = 8;
-constexpr int FW_SHARES = 256 * FW_PER_CU;        // shares of the work, at most
+// shares of the work, at most: a workgroup of 8 waves per CU (512 of 4 waves: 16 tokens 183 us, these 172)
+constexpr int FW_SHARES = 256;
 // Counters, each in a cache line of its own: atomics on one line take turns, 50 ns each here (drawing every
 // item from one counter cost 24 us with 768 workgroups).  Per XCD: shares drawn, shares whose activations are
 // done, the signal that all are; then the XCDs that are done, and the finished pieces of each output tile.
@@ -82,76 +88,56 @@ __device__ inline f32x4 mma(u32x4 a, u32x4 b, f32x4 acc) {
 }
 
 // ------------------------------------------------------------------ router
-__global__ void __launch_bounds__(FW_SLICES * 64) few_router_kernel(const FewArgs a, int ks) {
-    __shared__ double s_part[FW_SLICES][16][16];             // (bf16: floats in the same place)
-    const int tid = threadIdx.x, lane = tid & 63, z = tid >> 6;
+// Partial logits of 16 experts over the K slice [z kc, (z + 1) kc), by one wave:
+// bf16 v_mfma_f32_16x16x32_bf16 (element i of a lane: token 4 g + i), fp32
+// v_mfma_f64_16x16x4_f64 (token 4 i + g, exact products); expert lane % 16.
+template <bool BF>
+__device__ inline auto router_slice(const FewArgs& a, int eb, int z, int kc, int lane) {
+    constexpr uint32_t ES = BF ? 2 : 4;
+    constexpr int U = BF ? 8 : 4, SK = BF ? 32 : 16;         // steps in flight, columns of a step
     const int r16 = lane & 15, g = lane >> 4;
-    const int E = a.r.E, d = a.r.d, T = (int)a.r.T;
-    const int Epad = (E + 15) & ~15;
-    if (blockIdx.x == 0)
-        for (int i = tid; i < (CTR_TILE + d / 64) * LINE; i += FW_SLICES * 64) a.ctr[i] = 0;
-    const int kc = d / ks;                                   // a multiple of 32
-    const int e = blockIdx.x * 16 + r16;
-    const bool bf = a.r.dtype == ORDERMOE_BF16;
-    const uint32_t esz = bf ? 2 : 4;
-    const __amdgpu_buffer_rsrc_t rx = make_rsrc(a.r.x, (uint32_t)T * (uint32_t)d * esz);
-    const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.r.w_router, (uint32_t)E * (uint32_t)d * esz);
-    const uint32_t xo = r16 < T ? (uint32_t)r16 * (uint32_t)d * esz + 16u * g : OOR;
-    const uint32_t wo = e < E ? (uint32_t)e * (uint32_t)d * esz + 16u * g : OOR;
-    float* pf = (float*)s_part;
-    if (z < ks) {
-        if (bf) {
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-            const int n = kc / 32;
-            for (int s0 = 0; s0 < n; s0 += 8) {
-                u32x4 xv[8], wv[8];
+    const int E = a.r.E, d = a.r.d, T = (int)a.r.T, e = eb * 16 + r16;
+    const __amdgpu_buffer_rsrc_t rx = make_rsrc(a.r.x, (uint32_t)T * (uint32_t)d * ES);
+    const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.r.w_router, (uint32_t)E * (uint32_t)d * ES);
+    const uint32_t xo = r16 < T ? (uint32_t)r16 * (uint32_t)d * ES + 16u * g : OOR;
+    const uint32_t wo = e < E ? (uint32_t)e * (uint32_t)d * ES + 16u * g : OOR;
+    std::conditional_t<BF, f32x4, f64x4> acc = {};
+    const int n = kc / SK;
+    for (int s0 = 0; s0 < n; s0 += U) {
+        u32x4 xv[U], wv[U];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const uint32_t past = s0 + u < n ? 0u : OOR, so = (uint32_t)(z * kc + (s0 + u < n ? s0 + u : 0) * 32) * 2u;
-                    xv[u] = load16(rx, xo | past, so);
-                    wv[u] = load16(rw, wo | past, so);
-                }
+        for (int u = 0; u < U; ++u) {
+            const uint32_t past = s0 + u < n ? 0u : OOR, so = (uint32_t)(z * kc + (s0 + u < n ? s0 + u : 0) * SK) * ES;
+            xv[u] = load16(rx, xo | past, so);
+            wv[u] = load16(rw, wo | past, so);
+        }
 #pragma unroll
-                for (int u = 0; u < 8; ++u) acc = mma<true>(xv[u], wv[u], acc);
+        for (int u = 0; u < U; ++u) {
+            if constexpr (BF) {
+                acc = mma<true>(xv[u], wv[u], acc);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)__uint_as_float(xv[u][i]), (double)__uint_as_float(wv[u][i]),
+                                                               acc, 0, 0, 0);
             }
-            // acc[i]: token 4 g + i, expert r16
-#pragma unroll
-            for (int i = 0; i < 4; ++i) pf[(z * 16 + 4 * g + i) * 16 + r16] = acc[i];
-        } else {
-            f64x4 acc = {0.0, 0.0, 0.0, 0.0};
-            const int n = kc / 16;
-            for (int s0 = 0; s0 < n; s0 += 4) {
-                u32x4 xv[4], wv[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const uint32_t past = s0 + u < n ? 0u : OOR, so = (uint32_t)(z * kc + (s0 + u < n ? s0 + u : 0) * 16) * 4u;
-                    xv[u] = load16(rx, xo | past, so);
-                    wv[u] = load16(rw, wo | past, so);
-                }
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)__uint_as_float(xv[u][i]),
-                                                                   (double)__uint_as_float(wv[u][i]), acc, 0, 0, 0);
-            }
-            // acc[i]: token 4 i + g, expert r16
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s_part[z][4 * i + g][r16] = acc[i];
         }
     }
-    __syncthreads();
-    if (tid < 256) {
-        const int t = tid >> 4, c = tid & 15;
-        float v = 0.f;
-        if (bf) {
-            for (int s = 0; s < ks; ++s) v += pf[(s * 16 + t) * 16 + c];
-        } else {
-            double w = 0.0;
-            for (int s = 0; s < ks; ++s) w += s_part[s][t][c];
-            v = (float)w;
-        }
-        if (t < T) a.logits[t * Epad + blockIdx.x * 16 + c] = v;
+    return acc;
+}
+
+// a wave per (16 experts, slice); workgroup 0 clears the layer kernel's counters
+template <bool BF>
+__global__ void __launch_bounds__(64) few_router_kernel(const FewArgs a, int ks) {
+    using V = std::conditional_t<BF, float, double>;
+    const int lane = threadIdx.x, r16 = lane & 15, g = lane >> 4, Epad = (a.r.E + 15) & ~15;
+    if (blockIdx.x == 0 && blockIdx.y == 0)
+        for (int i = lane; i < (CTR_TILE + a.r.d / 64) * LINE; i += 64) a.ctr[i] = 0;
+    const auto acc = router_slice<BF>(a, blockIdx.x, blockIdx.y, a.r.d / ks, lane);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int t = BF ? 4 * g + i : 4 * i + g;
+        if (t < a.r.T) ((V*)a.logits)[((int)blockIdx.y * FW + t) * Epad + blockIdx.x * 16 + r16] = acc[i];
     }
 }
 
@@ -207,7 +193,7 @@ __device__ inline void write_route_totals(const FewArgs& a, const int8_t* dst, c
 }
 
 template <bool BF, int NBT, int AUX>
-__global__ void __launch_bounds__(FW_THREADS) few_layer_kernel(const FewArgs a) {
+__global__ void __launch_bounds__(FW_THREADS) few_layer_kernel(const FewArgs a, int ks) {
     constexpr int U = 4;                                     // steps per set of reads; two sets in turn
     constexpr int SK = BF ? 64 : 32;                         // columns of a step
     constexpr uint32_t ES = BF ? 2 : 4;
@@ -241,7 +227,17 @@ __global__ void __launch_bounds__(FW_THREADS) few_layer_kernel(const FewArgs a) 
     const bool valid = t < T;
     const int loc = valid ? a.r.loc_in[t] : 0;
     const float qhat = valid ? a.r.qhat_in[t] : 0.f;
-    for (int i = tid; i < T * Epad; i += FW_THREADS) s_logit[i] = a.logits[i];
+    for (int i = tid; i < T * Epad; i += FW_THREADS) {       // logits: the router's slices, added in order
+        using V = std::conditional_t<BF, float, double>;
+        const V* q = (const V*)a.logits + i;
+        V part[FW_SLICES], v = 0;
+#pragma unroll
+        for (int z = 0; z < FW_SLICES; ++z) part[z] = q[(z < ks ? z : 0) * FW * Epad];
+#pragma unroll
+        for (int z = 0; z < FW_SLICES; ++z)
+            if (z < ks) v += part[z];
+        s_logit[i] = (float)v;
+    }
     for (int i = tid; i < E; i += FW_THREADS) s_lidx[i] = a.lidx[i];
     for (int i = tid; i < (ORDERMOE_MAX_LOCAL + 1) * FW; i += FW_THREADS) (&s_w[0][0])[i] = 0.f;
     if (tid <= ORDERMOE_MAX_LOCAL) s_msk[tid] = 0u;
@@ -606,24 +602,24 @@ __global__ void __launch_bounds__(FW_THREADS) few_layer_kernel(const FewArgs a) 
 }
 
 template <bool BF, int NBT, int AUX>
-int launch_layer(const FewArgs& a, hipStream_t st) {
+int launch_layer(const FewArgs& a, int ks, hipStream_t st) {
     // never more workgroups than items: a tile of every group that can be in use
     const int64_t groups = a.r.T * (a.r.k < a.n_local ? a.r.k : a.n_local);
     const int64_t act = ((groups < a.n_local ? groups : a.n_local) + a.n_shared) * (a.f / 32);
     const int64_t items = a.r.T > 0 ? act + a.r.d / 64 * FW_PIECES : 1;
     const int64_t most = FW_SHARES, shares = (items + FW_XCDS - 1) / FW_XCDS * FW_XCDS;
     KernelTimer kt_("few_layer", st);
-    few_layer_kernel<BF, NBT, AUX><<<dim3((unsigned)(shares < most ? shares : most)), dim3(FW_THREADS), 0, st>>>(a);
+    few_layer_kernel<BF, NBT, AUX><<<dim3((unsigned)(shares < most ? shares : most)), dim3(FW_THREADS), 0, st>>>(a, ks);
     return (int)hipGetLastError();
 }
 
 template <bool BF, int AUX>
-int launch_experts(const FewArgs& a, hipStream_t st) {
+int launch_experts(const FewArgs& a, int ks, hipStream_t st) {
     const int nb = (a.r.E + 15) / 16;
-    if (nb <= 1) return launch_layer<BF, 1, AUX>(a, st);
-    if (nb <= 4) return launch_layer<BF, 4, AUX>(a, st);
-    if (nb <= 8) return launch_layer<BF, 8, AUX>(a, st);
-    return launch_layer<BF, 16, AUX>(a, st);
+    if (nb <= 1) return launch_layer<BF, 1, AUX>(a, ks, st);
+    if (nb <= 4) return launch_layer<BF, 4, AUX>(a, ks, st);
+    if (nb <= 8) return launch_layer<BF, 8, AUX>(a, ks, st);
+    return launch_layer<BF, 16, AUX>(a, ks, st);
 }
 
 }  // namespace
@@ -632,16 +628,19 @@ size_t few_counters(int d) { return (size_t)(CTR_TILE + d / 64) * LINE; }
 
 int launch_few_layer(const FewArgs& a, void* stream) {
     hipStream_t st = (hipStream_t)stream;
-    const int nb = (a.r.E + 15) / 16;
+    const bool bf = a.r.dtype == ORDERMOE_BF16;
+    const int nb = (a.r.E + 15) / 16, ks = route_ksplit(1, nb, a.r.d);
     {
         KernelTimer kt_("few_router", st);
-        few_router_kernel<<<dim3((unsigned)nb), dim3(FW_SLICES * 64), 0, st>>>(a, route_ksplit(1, nb, a.r.d));
+        const dim3 blocks((unsigned)nb, (unsigned)ks);
+        if (bf) few_router_kernel<true><<<blocks, dim3(64), 0, st>>>(a, ks);
+        else few_router_kernel<false><<<blocks, dim3(64), 0, st>>>(a, ks);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return (int)e;
     }
-    if (a.r.dtype != ORDERMOE_BF16) return launch_experts<false, 0>(a, st);
+    if (!bf) return launch_experts<false, 0>(a, ks, st);
     const bool stream_w = (int64_t)a.n_local * 2 * a.f * a.r.d * 2 >= FW_STREAM_BYTES;
-    return stream_w ? launch_experts<true, NT>(a, st) : launch_experts<true, 0>(a, st);
+    return stream_w ? launch_experts<true, NT>(a, ks, st) : launch_experts<true, 0>(a, ks, st);
 }
 
 }  // namespace ordermoe

@@ -152,7 +152,7 @@ __device__ inline TokenPick pick_token(const RouteArgs& a, const float* lg, cons
     float qhat = qhat_in;
     const bool subs_on = a.allow_sub && a.Qbar > 0.f;
     const uint32_t mmask = M >= 32 ? 0xFFFFFFFFu : ((1u << M) - 1u);   // servers that exist
-    const int jm1 = j >= 1 ? j - 1 : 0;
+    const int jm1 = j >= 1 && j - 1 < a.gmax ? j - 1 : 0;    // (in the table's row; past its entries it is not used)
     int ke[KM];
     float qe[KM];
     uint32_t msv[KM];
