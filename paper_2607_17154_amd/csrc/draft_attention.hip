@@ -12,9 +12,9 @@
 //
 // A tile (bf16; v_mfma_f32_16x16x32_bf16, c = lane % 16, g = lane / 16):
 //   S^T = K Q^T   rows: 16 tokens, columns: 16 query rows.  The inner index may be
-//                 taken in any order common to both sides, so lane (c, g) reads the
-//                 D/4 neighbouring codes [g D/4, (g + 1) D/4) of token c, and Q in the
-//                 same order.
+//                 taken in any order common to both sides, so lane (c, g) reads, of
+//                 token c, the 16 neighbouring codes from 64 i + 16 g on for i = 0, 1, ..,
+//                 and Q in the same order.
 //   O^T = V^T P^T rows: 16 elements of the head, columns: 16 query rows.  Two S^T
 //                 blocks leave lane (c, g) the weights of query row c for tokens
 //                 4g .. 4g + 3 of each: exactly the 8 inner indexes of its P^T operand
@@ -24,11 +24,22 @@
 //   V             lane (c, g) reads D/16 neighbouring codes of its 8 tokens; matrix
 //                 instruction j takes element c D/16 + j of each, whose codes are
 //                 paired across tokens by byte permutes.
+// Codes come from memory in whole cache lines, 16 bytes a lane, two tiles on their way,
+// and get into these orders through the wave's own LDS rows (read in operand order
+// straight from memory, 64 single tokens took 149 us for 119).
 // Keys' scales multiply the scores, values' scales the weights, so codes enter the
-// matrix unit as they are (8-bit codes are exact in bf16).  fp32 runs the same tile
-// with v_mfma_f32_16x16x4_f32.
+// matrix unit as they are (8-bit codes are exact in bf16).  In bf16 the weights are
+// rounded to bf16 for the second product, as its operands are; sums stay in fp32.
+// fp32 runs the same tile with v_mfma_f32_16x16x4_f32.
+//
+// Bound: one query row block, the codes: 64 sequences of 200-8000 tokens, 32 query and 8
+// key/value heads of 128, 106 us with the join, 5.3 TB/s.  64 drafted tokens (16 rows
+// of 16 a head), the vector instructions of a tile (some 230 a wave next to 40 matrix
+// instructions): 4 sequences of 30000-100000 tokens 355 us, 500 TFLOP/s.  One sequence of 778
+// tokens 10.6 us: a launch, and a chain of five dependent reads.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <type_traits>
 
@@ -46,8 +57,13 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int DA_WAVES = 4, DA_WAVES_WIDE = 8;       // waves of a workgroup (wide: see launch_type)
 constexpr int DA_TILE = 32;                          // tokens of a tile
-constexpr int DA_MIN_PIECE = 1024;                   // tokens of a piece, at least
-constexpr int DA_WIDE_MAX = 2048;                    // tokens of a table that wide workgroups take whole
+// Tokens of a piece.  DA_FULL at least, where that gives DA_ONE_EACH workgroups or more
+// (pieces of 512: trees of 33 over 1-5000, eight sequences, 47 us for 42); else as many
+// fewer as give about that many, but DA_MIN_PIECE at least (one sequence of 8000 tokens:
+// 1024 19.8 us, 512 15.9, 256 15.3, with the second kernel; 128 is one round of the waves).
+constexpr int DA_FULL = 1024, DA_MIN_PIECE = 256, DA_ONE_EACH = 256;
+// Tokens of a table up to which sequences are not split: see launch_type
+constexpr int DA_WHOLE_WIDE = 1024, DA_WHOLE = 512;
 // Workgroups that a large batch is split into: two rounds of the 512 that run together
 // (64 tokens over 200-8000 cached: 512 111 us, 1024 100, 1536 99; trees of 33 over
 // 1-5000, with the second kernel: 1024 50, 1536 52, 2048 55; trees of 64 over
@@ -83,7 +99,7 @@ __device__ inline SeqInfo sequence(const DraftArgs& a, int b) {
 // many tokens, a multiple of `round`, as give about DA_TARGET workgroups in all, but at
 // least half of what the batch would ask for with every sequence at max_q: that bounds
 // the pieces by 2 DA_TARGET / (n_kv rb_n) + B, since each sequence ends in one short one.
-__device__ inline int piece_tokens(const DraftArgs& a, int rb_n, int rt, int round, int min_piece, const SeqInfo& mine, int lane) {
+__device__ inline int piece_tokens(const DraftArgs& a, int rb_n, int rt, int round, const SeqInfo& mine, int lane) {
     constexpr int target = DA_TARGET;
     const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
     int64_t total = 0, blocks = 0;
@@ -110,11 +126,14 @@ __device__ inline int piece_tokens(const DraftArgs& a, int rb_n, int rt, int rou
     if (rb_n == 1) blocks = total;
     // (a sequence's last piece is half a piece on average)
     const int64_t half = (int64_t)ends * n_kv / 2, want = half < target / 2 ? target - half : target / 2;
-    int64_t p = (blocks * n_kv + want - 1) / want;
+    int64_t p = (blocks * n_kv + want - 1) / want, few = (blocks * n_kv + DA_ONE_EACH - 1) / DA_ONE_EACH;
+    p = p < DA_FULL ? DA_FULL : p;
+    few = few < DA_MIN_PIECE ? DA_MIN_PIECE : few;
+    p = p < few ? p : few;
     const int64_t least = (total * n_kv * rb_n + 2 * target - 1) / (2 * target);
     p = p < least ? least : p;
     p = (p + round - 1) / round * round;
-    return (int)(p < min_piece ? min_piece : p > (1 << 30) ? 1 << 30 : p);
+    return (int)(p > (1 << 30) ? 1 << 30 : p);
 }
 __device__ inline int pieces_of(const SeqInfo& s, int piece) {
     // a sequence without positions still writes its rows (zeros)
@@ -449,7 +468,7 @@ template <int D>
 constexpr int OCC = D == 256 ? 1 : 2;
 
 template <bool BF, int D, int FMT, int RT, int NW>
-__global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const DraftArgs a, int items, int rb_n, int min_piece) {
+__global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const DraftArgs a, int items, int rb_n, int whole) {
     constexpr int LD = D + 4, ROUND = NW * DA_TILE;
     constexpr int SUMS = NW * 16 * LD * 4;
     __shared__ __attribute__((aligned(16))) char s_mem[NW * STAGE<D> > SUMS ? NW * STAGE<D> : SUMS];
@@ -464,12 +483,17 @@ __global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const 
     const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
     if (unit >= items * n_kv) return;
     const int item = unit / n_kv, kvh = unit - item * n_kv;
-    SeqInfo mine = {0, 0, 0, 0};
-    if (lane < a.B) mine = sequence(a, lane);
-    // (the same in every lane, and in scalar registers from here on: addresses and branches below rest on it)
-    const int piece = __builtin_amdgcn_readfirstlane(piece_tokens(a, rb_n, RT, ROUND, min_piece, mine, lane));
-    int b, j;
-    SeqInfo s = find_item(a, piece, item, lane, blockIdx.x == 0 && wave == 0, mine, b, j);
+    int piece = 1 << 30, b = item, j = 0;
+    SeqInfo s;
+    if (whole) {
+        s = sequence(a, b);                          // every sequence is one piece
+    } else {
+        SeqInfo mine = {0, 0, 0, 0};
+        if (lane < a.B) mine = sequence(a, lane);
+        // (the same in every lane, and in scalar registers from here on: addresses and branches below rest on it)
+        piece = __builtin_amdgcn_readfirstlane(piece_tokens(a, rb_n, RT, ROUND, mine, lane));
+        s = find_item(a, piece, item, lane, blockIdx.x == 0 && wave == 0, mine, b, j);
+    }
     b = __builtin_amdgcn_readfirstlane(b);
     j = __builtin_amdgcn_readfirstlane(j);
     s = SeqInfo{__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.n), __builtin_amdgcn_readfirstlane(s.ctx),
@@ -610,85 +634,134 @@ __global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const 
     }
 }
 
-// one block per 16 (token, head) rows of a sequence, 16 lanes a row
-template <bool BF, int D>
+// 16 / S (token, head) rows of a sequence per workgroup, S sets of 16 lanes a row: set z
+// adds pieces z, z + S, .., and the sets' sums are added in order
+template <bool BF, int D, int S>
 __global__ void __launch_bounds__(256) draft_join_kernel(const DraftArgs a, int rows_n) {
+    constexpr int R = 16 / S, U = 4;                             // rows; pieces whose reads are in flight
+    __shared__ __attribute__((aligned(16))) float s_x[16][D + 4];
+    __shared__ float s_m[16], s_l[16];
     const int b = blockIdx.x / rows_n;
     const int pieces = a.plan[2 * b + 1];
     if (pieces <= 1) return;
     const SeqInfo s = sequence(a, b);
-    const int r = (blockIdx.x - b * rows_n) * 16 + (threadIdx.x >> 4);
-    if (r >= s.n * a.n_q) return;
+    const int slot = threadIdx.x >> 4, z = slot % S, rows = s.n * a.n_q;
+    const int r = (blockIdx.x - b * rows_n) * R + slot / S;
     const int item = a.plan[2 * b], n_kv = a.cache.n_kv, G = a.n_q / n_kv;
     const int i = r / a.n_q, h = r - i * a.n_q, kvh = h / G;
     const int64_t stride = (int64_t)n_kv * a.max_q * G;          // rows of a piece
     const int64_t row = ((int64_t)item * n_kv + kvh) * (a.max_q * G) + i * G + (h - kvh * G);
     const int d0 = (threadIdx.x & 15) * (D / 16);
     const f32x2* ml = (const f32x2*)a.part_ml;
-    float m = -__builtin_inff();
-    for (int p = 0; p < pieces; p += 8) {
+    float m = -__builtin_inff(), l = 0.f, x[D / 16] = {};
+    for (int p = r < rows ? z : pieces; p < pieces; p += U * S) {
+        f32x2 q[U];
+        f32x4 v[U][D / 64];
+        float top = m;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) m = fmaxf(m, ml[row + (p + u < pieces ? p + u : p) * stride][0]);
-    }
-    float l = 0.f, x[D / 16] = {};
-    for (int p = 0; p < pieces; p += 4) {                        // four pieces' reads in flight
-        f32x2 q[4];
-        f32x4 v[4][D / 64];
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = row + (p + u * S < pieces ? p + u * S : p) * stride;
+            q[u] = ml[at];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int64_t r = row + (p + u < pieces ? p + u : p) * stride;
-            q[u] = ml[r];
-#pragma unroll
-            for (int e = 0; e < D / 64; ++e) v[u][e] = *(const f32x4*)(a.part_o + r * D + d0 + 4 * e);
+            for (int e = 0; e < D / 64; ++e) v[u][e] = *(const f32x4*)(a.part_o + at * D + d0 + 4 * e);
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (p + u >= pieces) break;
+        for (int u = 0; u < U; ++u) top = fmaxf(top, q[u][0]);
+        const float al = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+        m = top;
+        l *= al;
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) x[e] *= al;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (p + u * S >= pieces) break;
             const float f = q[u][0] == m ? 1.0f : __builtin_amdgcn_exp2f(q[u][0] - m);
             l += q[u][1] * f;
 #pragma unroll
             for (int e = 0; e < D / 16; ++e) x[e] += v[u][e / 4][e % 4] * f;
         }
     }
+    if constexpr (S > 1) {
+        if ((threadIdx.x & 15) == 0) { s_m[slot] = m; s_l[slot] = l; }
+#pragma unroll
+        for (int e = 0; e < D / 16; e += 4) *(f32x4*)&s_x[slot][d0 + e] = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+        __syncthreads();
+        if (z != 0) return;
+        float mm = m;
+#pragma unroll
+        for (int u = 1; u < S; ++u) mm = fmaxf(mm, s_m[slot + u]);
+        const float al = m == mm ? 1.0f : __builtin_amdgcn_exp2f(m - mm);
+        m = mm;
+        l *= al;
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) x[e] *= al;
+        for (int u = 1; u < S && u < pieces; ++u) {
+            const float f = s_m[slot + u] == m ? 1.0f : __builtin_amdgcn_exp2f(s_m[slot + u] - m);
+            l += s_l[slot + u] * f;
+#pragma unroll
+            for (int e = 0; e < D / 16; ++e) x[e] += s_x[slot + u][d0 + e] * f;
+        }
+    }
+    if (r >= rows) return;
     const int64_t at = (int64_t)(s.first + i) * a.n_q + h;
     write_row<BF, D / 16>(a.out, at * D + d0, x, l);
     if (a.lse && (threadIdx.x & 15) == 0) a.lse[at] = row_lse(m, l);
 }
 
+// rows (of all sequences) up to which a row gets 16 sets of lanes, or 4: 40 pieces of
+// 32 rows 16 sets 7 us, one 21; 6 of 8192 rows 4 sets 9 us, one 12
+constexpr int64_t JOIN_16 = 1024, JOIN_4 = 16384;
+
 int64_t table_tokens(const DraftArgs& a) { return (int64_t)a.max_pages << a.cache.page_shift; }
 
 template <bool BF, int D, int FMT, int RT, int NW>
-int launch_rows(const DraftArgs& a, int rows, hipStream_t st) {
+int launch_rows(const DraftArgs& a, int rows, bool whole, hipStream_t st) {
     const int rb = row_blocks(rows, RT);
-    const int min_piece = NW == DA_WAVES_WIDE ? DA_WIDE_MAX : DA_MIN_PIECE;
-    const int64_t items = draft_items(a.n_q, a.cache.n_kv, D, a.dtype, a.B, a.max_q);
+    // (workgroups without a piece are not free: a sequence has no more of them than its table holds)
+    const int64_t most = whole ? a.B : (int64_t)a.B * ((table_tokens(a) + DA_MIN_PIECE - 1) / DA_MIN_PIECE);
+    const int64_t items = std::min(most, draft_items(a.n_q, a.cache.n_kv, D, a.dtype, a.B, a.max_q));
     const int64_t units = (items * a.cache.n_kv + 7) / 8 * 8;
     {
         KernelTimer kt_("draft_attention", st);
         draft_attention_kernel<BF, D, FMT, RT, NW>
-            <<<dim3((unsigned)(units * rb)), dim3(64 * NW), 0, st>>>(a, (int)items, rb, min_piece);
+            <<<dim3((unsigned)(units * rb)), dim3(64 * NW), 0, st>>>(a, (int)items, rb, whole);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return (int)e;
     }
-    // no sequence can be longer than the table: nothing is split
-    if (table_tokens(a) <= min_piece) return 0;
-    const int rows_n = (a.max_q * a.n_q + 15) / 16;
+    if (whole) return 0;
     KernelTimer kt_("draft_join", st);
-    draft_join_kernel<BF, D><<<dim3((unsigned)((int64_t)a.B * rows_n)), dim3(256), 0, st>>>(a, rows_n);
+    const int64_t all = (int64_t)a.B * a.max_q * a.n_q;
+    auto join = [&](auto sets) {
+        constexpr int S = decltype(sets)::value;
+        const int rows_n = (a.max_q * a.n_q + 16 / S - 1) / (16 / S);
+        draft_join_kernel<BF, D, S><<<dim3((unsigned)((int64_t)a.B * rows_n)), dim3(256), 0, st>>>(a, rows_n);
+    };
+    if (all <= JOIN_16) join(std::integral_constant<int, 16>{});
+    else if (all <= JOIN_4) join(std::integral_constant<int, 4>{});
+    else join(std::integral_constant<int, 1>{});
     return (int)hipGetLastError();
 }
 
 template <bool BF, int D, int FMT>
 int launch_type(const DraftArgs& a, hipStream_t st) {
-    const int rows = a.max_q * (a.n_q / a.cache.n_kv);
-    const int rt = row_tiles(a.dtype, D, rows);
-    if constexpr (BF && D != 256)
-        if (rt == 2) return launch_rows<BF, D, FMT, 2, DA_WAVES>(a, rows, st);
-    // A few sequences that the host knows to be short: eight waves take one whole, which
-    // saves the second kernel (one sequence of 778 tokens: see the kernel times)
-    if (table_tokens(a) <= DA_WIDE_MAX && (int64_t)a.B * a.cache.n_kv * row_blocks(rows, 1) <= 256)
-        return launch_rows<BF, D, FMT, 1, DA_WAVES_WIDE>(a, rows, st);
-    return launch_rows<BF, D, FMT, 1, DA_WAVES>(a, rows, st);
+    const int rows = a.max_q * (a.n_q / a.cache.n_kv), rt = row_tiles(a.dtype, D, rows);
+    const int64_t table = table_tokens(a);
+    // Sequences that the host knows to be short are not split, which saves the second
+    // kernel.  With a workgroup per compute unit all the same: those of a whole piece; else
+    // as long as one workgroup takes less time than pieces and join (one sequence, whole and
+    // split: bf16 500 tokens 9.3 and 12.8 us, 1000 13.0 and 12.7; fp32 500 17.4 and 16.8;
+    // heads of 256, 500 15.9 and 16.3; trees of 33, 470 12.3 and 15.3, 900 17.8 and 15.4).
+    const bool many = (int64_t)a.B * a.cache.n_kv * row_blocks(rows, rt) >= DA_ONE_EACH;
+    if (many || rt > 1 || D == 256) {
+        const bool whole = table <= (many ? DA_FULL : DA_WHOLE);
+        if constexpr (BF && D != 256)
+            if (rt == 2) return launch_rows<BF, D, FMT, 2, DA_WAVES>(a, rows, whole, st);
+        return launch_rows<BF, D, FMT, 1, DA_WAVES>(a, rows, whole, st);
+    }
+    // one row tile, eight waves (not with heads of 256, whose registers eight waves do not have)
+    if constexpr (D != 256)
+        if (table <= (BF ? DA_WHOLE_WIDE : DA_WHOLE)) return launch_rows<BF, D, FMT, 1, DA_WAVES_WIDE>(a, rows, true, st);
+    return launch_rows<BF, D, FMT, 1, DA_WAVES>(a, rows, false, st);
 }
 template <bool BF, int D>
 int launch_fmt(const DraftArgs& a, hipStream_t st) {

@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(FW_THREADS) few_layer_kernel(const FewArgs a, 
             for (int i = 0; i < 8; ++i) wo[i] = rows_offset<BF>(2 * c0 + 8 * i, d, lane);
             const uint32_t msk = s_msk[grp];
             const uint32_t xo = (msk >> r16) & 1 ? (uint32_t)r16 * (uint32_t)d * ES + 16u * g16 : OOR;
-            const int n = d / SK, ns = (n - wave + FW_WAVES - 1) / FW_WAVES;     // steps wave, wave + 4, ...
+            const int n = d / SK, ns = (n - wave + FW_WAVES - 1) / FW_WAVES;     // steps wave, wave + 8, ...
             u32x4 vw[2][UA][8], vx[2][UA][2];
             auto load = [&](int b, int i0) {
 #pragma unroll

@@ -428,3 +428,22 @@ def test_captured_calls_follow_their_lengths():
         k, v = ca.rows(np.array(slot_of[:p + 1]))
         want, _, mag = oa.draft_attention(_host(q), k, v, p, [1], D ** -0.5)
         assert (np.abs(_host(out) - want) <= (2.0 ** -7 + 1e-4) * mag).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ctx,n,hq,hkv,D,page", [
+    ([20000], [1], 4, 2, 64, 16),                           # some eighty pieces of four rows
+    ([3000, 40, 1500], [40, 2, 7], 16, 2, 128, 32),         # a few pieces of some thousand rows
+    ([2500] + [3] * 39, [1] * 40, 8, 2, 64, 16),            # a long sequence among many short ones
+    ([400], [33], 8, 8, 128, 64),                           # short tables: in one piece
+    ([500], [1], 2, 2, 256, 16),
+    ([900, 20], [2, 1], 4, 1, 128, 32),
+    ([1000] * 40, [1] * 40, 8, 8, 64, 16),
+])
+def test_sequences_split_into_few_and_many_pieces(dtype, ctx, n, hq, hkv, D, page):
+    b = _Batch(np.random.default_rng(len(ctx) + D), "fp8", dtype, ctx, n, hq, hkv, D, page, False)
+    got = b.run()
+    b.check(got)
+    again, _ = b.run()
+    np.testing.assert_array_equal(again, got[0])
+    b.check(b.run(max_q=64))

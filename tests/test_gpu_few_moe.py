@@ -236,3 +236,29 @@ def test_captured_layer_follows_its_tokens():
         np.testing.assert_array_equal(got[1], host(y2))
         for n in got[0]:
             np.testing.assert_array_equal(got[0][n], host(o2[n]), err_msg=n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_workgroups_than_the_chip_holds(dtype):
+    """Six calls of 256 workgroups at once, one of which fills a compute unit: some
+    start when others of their call have long begun to wait."""
+    cfg = wl.C4.with_(T=16, d=1024, f=512, T_cal=2048, n_shared=1, dtype=dtype)
+    case = build_case(cfg)
+    dl = DeviceLayer(case, library_tables(case))
+    x, loc, qh = dl.inputs()
+    xs = [x.roll(i, 0).contiguous() for i in range(6)]
+    want = [_few(dl, v, loc, qh, 16) for v in xs]
+    need = om.ordermoe_few_workspace_size(dl.layer, dl.experts, 16)
+    bufs = [(om.alloc_route_out(16, cfg.k, cfg.M, "cuda"), torch.empty(need, dtype=torch.uint8, device="cuda"),
+             torch.zeros_like(x)) for _ in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for v, (o, ws, y), s in zip(xs, bufs, streams):
+            _few(dl, v, loc, qh, 16, stream=s, out=o, ws=ws, y=y)
+    torch.cuda.synchronize()
+    for (o, _, y), (wo, wy) in zip(bufs, want):
+        np.testing.assert_array_equal(host(y), host(wy))
+        for n in PER_TOKEN:
+            np.testing.assert_array_equal(host(o[n]), host(wo[n]), err_msg=n)
+    _check_y(case, want[0][0], want[0][1], 16, cfg.m0)
