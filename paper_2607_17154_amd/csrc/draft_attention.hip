@@ -262,6 +262,15 @@ constexpr float DA_LAG = 8.0f;
 template <int N>
 struct Queries { bf16x8 b[N]; };
 
+// and over the 16 lanes of a DPP row, by rotations of 8, 4, 2, 1
+__device__ inline uint32_t row_and(uint32_t v) {
+    v &= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xF, 0xF, false);
+    v &= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xF, 0xF, false);
+    v &= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xF, 0xF, false);
+    v &= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xF, 0xF, false);
+    return v;
+}
+
 template <bool BF, int D, int FMT, int RT>
 __device__ inline void attend_tile(const char* stage, const bool* ok, const void* qv, const uint64_t* word,
                                    int t0, const SeqInfo& s, int lane, State<D, RT>& st) {
@@ -388,14 +397,17 @@ __device__ inline void attend_tile(const char* stage, const bool* ok, const void
             v[u][0] = w[0]; v[u][1] = w[1]; v[u][2] = w[2]; v[u][3] = w[3];
         }
     }
-    // the tokens past the end and in no page: their codes of V must be numbers
-    if (t0 + DA_TILE > s.len || !ok[0] || !ok[1]) {
+    // tokens that no row sees, past the end, in no page or drafted, may never have been written: a
+    // weight of 0 would not keep codes that are no numbers out of the sums
+    if (edge) {
+        uint32_t none = hidden[0];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const bool in = ok[u >> 2] && t0 + 16 * (u >> 2) + 4 * g + (u & 3) < s.len;
+        for (int r = 1; r < RT; ++r) none &= hidden[r];
+        none = row_and(none);                                    // (the 16 lanes of a group have the same tokens)
 #pragma unroll
-            for (int w = 0; w < D / 64; ++w) v[u][w] = in ? v[u][w] : 0u;
-        }
+        for (int u = 0; u < 8; ++u)
+#pragma unroll
+            for (int w = 0; w < D / 64; ++w) v[u][w] = (none >> u) & 1 ? 0u : v[u][w];
     }
     if constexpr (BF) {
         bf16x8 pf[RT];

@@ -331,6 +331,29 @@ def test_what_is_not_seen_has_no_effect(fmt, bad):
         t += m
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("hq,D", [(4, 128), (2, 64), (8, 256)])
+def test_drafted_places_that_nothing_was_written_to(dtype, fmt, hq, D):
+    """A padded place of a tree has no row in the cache; no token sees it, and whatever
+    its slot holds (codes that are no numbers, a scale that is none) changes nothing."""
+    rng = np.random.default_rng(12)
+    b = _Batch(rng, fmt, dtype, [50, 0, 900], [12, 3, 33], hq, 2, D, 16, True)
+    pads = [(s, int(j)) for s, m in enumerate(b.n) for j in rng.permutation(m)[:1 + m // 6]]
+    for s, j in pads:
+        b.words[s] = [w & ~(1 << j) for w in b.words[s]]
+    b.tree = _dev(np.array([w for ws in b.words for w in ws], np.uint64).view(np.int64))
+    clean = b.run()
+    b.check(clean)
+    for s, j in pads:
+        slot = int(b.slots[s][b.ctx[s] + j])
+        for codes, scale in zip(b.ca.codes, b.ca.scale):
+            codes[slot // 16, :, slot % 16] = 0x7F if j % 2 else 0xFF
+            scale[slot // 16, :, slot % 16] = float("nan")
+    for got, want in zip(b.run(), clean):
+        np.testing.assert_array_equal(got, want)
+
+
 def test_pages_outside_the_cache_and_positions_past_the_table_are_unseen():
     rng = np.random.default_rng(7)
     b = _Batch(rng, "int8", "bf16", [100, 40], [2, 3], 2, 1, 64, 16, False)
