@@ -564,7 +564,8 @@ int ordermoe_cache_read(const ordermoe_cache* C, int32_t dtype, const int64_t* s
  * a token that sees nothing gets out = 0 and lse = -infinity.  What the cache
  * holds at unseen positions, and past a sequence's end, has no effect.
  * bf16: q times the codes with fp32 sums, statistics in fp32, the weights
- * exp(s - max) * v_scale rounded to bf16 for the product with the codes of V,
+ * exp(s - max) * v_scale rounded to bf16 for the product with the codes of V (in
+ * two parts, 16 bits together, for head_dim 256 or max_q * n_q / n_kv <= 16 rows),
  * fp32 sums, rounded once.  fp32: fp32 throughout.
  *   q        dev [T][n_q][head_dim] of storage `dtype`, 16-byte aligned (as out)
  *   q_start  dev [B + 1] int32, not decreasing, within [0, T]

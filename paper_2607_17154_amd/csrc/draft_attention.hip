@@ -29,13 +29,16 @@
 // straight from memory, 64 single tokens took 149 us for 119).
 // Keys' scales multiply the scores, values' scales the weights, so codes enter the
 // matrix unit as they are (8-bit codes are exact in bf16).  In bf16 the weights are
-// rounded to bf16 for the second product, as its operands are; sums stay in fp32.
+// rounded to bf16 for the second product, as its operands are; with one row tile what the
+// rounding leaves out goes through it as well (one token over 777 cached: error 0.0028 of
+// the output's size without, 0.0017 with, which is the output's own rounding; 64 single
+// tokens 100 -> 101 us).  Sums stay in fp32.
 // fp32 runs the same tile with v_mfma_f32_16x16x4_f32.
 //
 // Bound: one query row block, the codes: 64 sequences of 200-8000 tokens, 32 query and 8
-// key/value heads of 128, 106 us with the join, 5.3 TB/s.  64 drafted tokens (16 rows
+// key/value heads of 128, 101 us with the join, 5.5 TB/s.  64 drafted tokens (16 rows
 // of 16 a head), the vector instructions of a tile (some 230 a wave next to 40 matrix
-// instructions): 4 sequences of 30000-100000 tokens 355 us, 500 TFLOP/s.  One sequence of 778
+// instructions): 4 sequences of 30000-100000 tokens 330 us, 540 TFLOP/s.  One sequence of 778
 // tokens 10.6 us: a launch, and a chain of five dependent reads.
 #include <hip/hip_runtime.h>
 
@@ -410,11 +413,16 @@ __device__ inline void attend_tile(const char* stage, const bool* ok, const void
             for (int w = 0; w < D / 64; ++w) v[u][w] = (none >> u) & 1 ? 0u : v[u][w];
     }
     if constexpr (BF) {
-        bf16x8 pf[RT];
+        // one row tile: what the rounding of the weights leaves out goes through the matrix unit too, which has
+        // the time there (the codes' reads bound it); more: the rounded weights alone
+        bf16x8 pf[RT], pl = {};
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int u = 0; u < 8; ++u) pf[r][u] = (__bf16)pw[r][u];
+            for (int u = 0; u < 8; ++u) {
+                pf[r][u] = (__bf16)pw[r][u];
+                if constexpr (RT == 1) pl[u] = (__bf16)(pw[r][u] - (float)pf[r][u]);
+            }
 #pragma unroll
         for (int w = 0; w < D / 64; ++w) {
             u32x4 vf[4];                                         // elements 4w .. 4w + 3, tokens in pairs
@@ -429,11 +437,15 @@ __device__ inline void attend_tile(const char* stage, const bool* ok, const void
                 vf[3][u] = kv_to_bf16x2<FMT, 1>(hi);
             }
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
+            for (int b = 0; b < 4; ++b) {
 #pragma unroll
                 for (int r = 0; r < RT; ++r)
                     st.o[4 * w + b][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[b]), pf[r],
                                                                                  st.o[4 * w + b][r], 0, 0, 0);
+                if constexpr (RT == 1)
+                    st.o[4 * w + b][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[b]), pl,
+                                                                                 st.o[4 * w + b][0], 0, 0, 0);
+            }
         }
     } else {
 #pragma unroll

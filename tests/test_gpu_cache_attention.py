@@ -282,6 +282,20 @@ def test_attention(dtype, fmt, shape):
     b.check(b.run(max_q=64))
 
 
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("ctx,n,hq,hkv,D,page", [
+    ([777, 3, 2600], [1, 1, 1], 32, 8, 128, 64), ([5000], [4], 4, 1, 64, 16), ([900, 31], [5, 1], 6, 2, 256, 32)])
+def test_few_rows_keep_the_weights_bits(fmt, ctx, n, hq, hkv, D, page):
+    """Up to 16 rows a head (or heads of 256): the output's rounding, 2^-8 of it, and of the terms'
+    sum 2^-17 for the weights in two parts and 2^-24 D |score| (|score| < 5) for the scores."""
+    b = _Batch(np.random.default_rng(21), fmt, "bf16", ctx, n, hq, hkv, D, page, False)
+    out, _ = b.run()
+    want, _, mag = b.want()
+    tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -17 + 5 * D * 2.0 ** -24 + 2e-6) * mag
+    over = np.abs(out - want) - tol
+    assert (over <= 0).all(), over.max()
+
+
 @pytest.mark.parametrize("spread", [0.0, 1e-3, 12.0])
 def test_scores_from_all_equal_to_far_apart(spread):
     """Weights that are all 1/len, and ones where a few keys take everything (the
