@@ -8,7 +8,7 @@
 //                      the same order they are the same logits; clears the counters
 //   few_layer_kernel   everything else, in at most FW_SHARES workgroups.  Each adds the
 //                      router's slices and runs the token stage of the routing itself (about
-//                      7 us of latency, side by side; the first one writes the routing's
+//                      5 us of latency, side by side; the first one writes the routing's
 //                      outputs), which tells it the experts in use and their tokens.
 //                      Then it works through its share of two lists:
 //     activation tiles   32 FFN columns of one expert: gate and up rows times the
@@ -25,9 +25,10 @@
 // v_mfma_f32_16x16x4_f32), the weights its rows, read in whole cache lines and turned
 // into the operand's lane order through LDS.
 // Bound: the weights in use, read once; below some 100 MB of them the latency of router,
-// token stage and hand-over (about 5 + 7 + 3 us).  d 4096, f 1536, bf16, both kernels:
-// 16 tokens with 24 experts in use (906 MB) 167 us, 5.4 TB/s; 1 token with 2
-// (75 MB) 37 us.  route_select and local_moe_forward in turn: 180 and 50 us.
+// token stage and hand-over (about 5 + 5 + 3 us) and of the weight stream's start.  d 4096,
+// f 1536, bf16, both kernels: 16 tokens with 24 experts in use (906 MB) 167 us, 5.4 TB/s; 1
+// token with 2 (75 MB) 36.5 us: 2.6 router, 2.4 logits, 5.3 token stage, 16 the gate/up weights,
+// 4 to 8 the down weights.  route_select and local_moe_forward in turn: 180 and 50 us.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -169,6 +170,98 @@ constexpr uint32_t STEP_BYTES = BF ? 32768u : 128u;
 // 128-expert layer took 312 us.)
 constexpr int ROW_LD = 144;
 
+// The candidate tables in LDS, in the place of the staging rows, which are not in use yet: the selection reads them in
+// a chain (an expert's row, its substitutes' servers, each server's cost).
+constexpr int TAB_T1 = ORDERMOE_MAX_EXPERTS * ORDERMOE_MAX_SUBS, TAB_S = 8192;      // words of t1_k, t1_q; of S at most
+constexpr int TAB_READS = (TAB_T1 / 4 + FW_THREADS - 1) / FW_THREADS, TAB_S_READS = TAB_S / 4 / FW_THREADS;
+static_assert((2 * TAB_T1 + 2 * ORDERMOE_MAX_EXPERTS + TAB_S) * 4 <= FW_WAVES * 64 * ROW_LD, "the tables fit in the staging rows");
+// where the selection reads them: there or in memory
+struct Tables {
+    const int32_t* k;
+    const float* q;
+    const int32_t* n;
+    const uint32_t* mask;
+    const float* S;
+};
+
+// pick_token's decisions, bit for bit, in loops that are not unrolled and with the slots' searches side by side: the
+// kernel runs this code once, so that fetching its instructions counts (one token of 128 experts, top-8: pick_token,
+// 20 KB of instructions, 7.6 us; this, with the tables in LDS, 5.3).  Three parts, with the workgroup's barriers
+// between them: targets, searches, and the choice (in the kernel).
+struct FewPick {
+    int r;                   // lane j: slot j's target
+    float v, top, den, margin;
+};
+// by the 16 lanes of a token: the targets in rank order, gates and margin
+template <int NBT>
+__device__ inline FewPick few_top(const RouteArgs& a, const float* lg, int j) {
+    const int E = a.E, k = a.k, kk1 = k + 1 < E ? k + 1 : E;
+    uint32_t okey[NBT];
+#pragma unroll
+    for (int i = 0; i < NBT; ++i) {
+        const int e = j + 16 * i;
+        const uint32_t o = f2ord(lg[e < E ? e : E - 1]);
+        okey[i] = e < E ? (o > 1u ? o : 1u) : 0u;
+    }
+    FewPick p{0, 0.f, 0.f, 0.f, __builtin_inff()};
+    float last = 0.f;
+#pragma unroll 1
+    for (int r = 0; r < kk1; ++r) {
+        uint32_t mx = okey[0];
+#pragma unroll
+        for (int i = 1; i < NBT; ++i) mx = okey[i] > mx ? okey[i] : mx;
+        mx = row_max_u32(mx);
+        uint32_t e = 0xFFFFu;
+#pragma unroll
+        for (int i = NBT - 1; i >= 0; --i) e = okey[i] == mx ? (uint32_t)(j + 16 * i) : e;
+        e = row_min_u32(e);
+#pragma unroll
+        for (int i = 0; i < NBT; ++i) okey[i] = e == (uint32_t)(j + 16 * i) ? 0u : okey[i];
+        const float v = ord2f(mx);
+        if (r == 0) p.top = v;
+        else p.margin = last - v < p.margin ? last - v : p.margin;
+        last = v;
+        if (r < k && a.renorm) p.den += expf(v - p.top);
+        if (j == r) { p.r = (int)e; p.v = v; }
+    }
+    if (!a.renorm) {
+#pragma unroll 1
+        for (int e = j; e < E; e += 16) p.den += expf(lg[e] - p.top);
+        p.den = __shfl(row_sum_f32(p.den), 0, 16);
+    }
+    return p;
+}
+// by 16 lanes per (token, slot): the best server of each candidate (lane j: candidate j) of target r; false: no search,
+// the target runs where the token is
+__device__ inline bool few_search(const RouteArgs& a, const Tables& tb, int r, int loc, int j, uint64_t& key, float& q) {
+    const int E = a.E, M = a.M;
+    const bool subs_on = a.allow_sub && a.Qbar > 0.f;
+    const uint32_t mmask = M >= 32 ? 0xFFFFFFFFu : ((1u << M) - 1u);
+    const int jm1 = j >= 1 && j - 1 < a.gmax ? j - 1 : 0;
+    const uint32_t rmask = tb.mask[r];
+    const int nsub = tb.n[r], tk = tb.k[r * a.gmax + jm1];
+    const float tq = tb.q[r * a.gmax + jm1];
+    const bool search = loc < M && !(a.pin && ((rmask >> loc) & 1u)), sub = j >= 1 && subs_on && j - 1 < nsub;
+    int kc = j == 0 ? r : (sub ? tk : -1);
+    if (kc < 0 || kc >= E) kc = -1;
+    q = sub ? tq : 0.f;
+    key = ~0ull;
+    const uint32_t lmask = a.allow_sub == 2 && j >= 1 ? 1u << (loc & 31) : ~0u;
+    uint32_t on = search && kc >= 0 ? tb.mask[kc] & mmask & lmask : 0u;
+#pragma unroll 1
+    while (__builtin_amdgcn_ballot_w64(on != 0)) {
+        if (on) {
+            const int m = __builtin_ctz(on);
+            on &= on - 1;
+            const float J = fmaf(a.cq, q, tb.S[((int64_t)loc * M + m) * E + kc]);
+            const uint64_t cand = ((uint64_t)f2ord(J == 0.f ? 0.f : J) << 32) | ((uint32_t)j << 16) | ((uint32_t)(m != loc) << 15) |
+                                  ((uint32_t)m << 8) | (uint32_t)kc;
+            key = cand < key ? cand : key;
+        }
+    }
+    return search;
+}
+
 // the routing's outputs that need all tokens, by the first workgroup: dispatch
 // list (rank of a slot: earlier destinations, then earlier slots), totals
 __device__ inline void write_route_totals(const FewArgs& a, const int8_t* dst, const int32_t* cnt, int tid) {
@@ -193,8 +286,7 @@ __device__ inline void write_route_totals(const FewArgs& a, const int8_t* dst, c
 }
 
 template <bool BF, int NBT, int AUX>
-__global__ void __launch_bounds__(FW_THREADS) few_layer_kernel(const FewArgs a, int ks) {
-    constexpr int U = 4;                                     // steps per set of reads; two sets in turn
+__global__ void __launch_bounds__(FW_THREADS) few_layer_kernel(const FewArgs a, int ks, int tables) {
     constexpr int SK = BF ? 64 : 32;                         // columns of a step
     constexpr uint32_t ES = BF ? 2 : 4;
     __shared__ float s_logit[FW * NBT * 16];
@@ -227,6 +319,28 @@ __global__ void __launch_bounds__(FW_THREADS) few_layer_kernel(const FewArgs a, 
     const bool valid = t < T;
     const int loc = valid ? a.r.loc_in[t] : 0;
     const float qhat = valid ? a.r.qhat_in[t] : 0.f;
+    // tables: 16-byte reads of each (tables & 2: of S too), on their way while the logits are added
+    const int n_t1 = E * a.r.gmax, n_S = tables & 2 ? a.r.M * a.r.M * E : 0;
+    u32x4 vk[TAB_READS] = {}, vq[TAB_READS] = {}, vS[TAB_S_READS] = {}, vn = {}, vm = {};
+    if (tables) {
+#pragma unroll
+        for (int u = 0; u < TAB_READS; ++u) {
+            const int i = 4 * (tid + FW_THREADS * u);
+            if (i < n_t1) {
+                vk[u] = *(const u32x4*)(a.r.t1_k + i);
+                vq[u] = *(const u32x4*)(a.r.t1_q + i);
+            }
+        }
+        if (4 * tid < E) {
+            vn = *(const u32x4*)(a.r.t1_n + 4 * tid);
+            vm = *(const u32x4*)(a.r.srvmask + 4 * tid);
+        }
+#pragma unroll
+        for (int u = 0; u < TAB_S_READS; ++u) {
+            const int i = 4 * (tid + FW_THREADS * u);
+            if (i < n_S) vS[u] = *(const u32x4*)(a.r.S + i);
+        }
+    }
     for (int i = tid; i < T * Epad; i += FW_THREADS) {       // logits: the router's slices, added in order
         using V = std::conditional_t<BF, float, double>;
         const V* q = (const V*)a.logits + i;
@@ -242,10 +356,82 @@ __global__ void __launch_bounds__(FW_THREADS) few_layer_kernel(const FewArgs a, 
     for (int i = tid; i < (ORDERMOE_MAX_LOCAL + 1) * FW; i += FW_THREADS) (&s_w[0][0])[i] = 0.f;
     if (tid <= ORDERMOE_MAX_LOCAL) s_msk[tid] = 0u;
     if (tid < ORDERMOE_NUM_COUNTERS) s_cnt[tid] = 0;
+    Tables tb{a.r.t1_k, a.r.t1_q, a.r.t1_n, a.r.srvmask, a.r.S};
+    if (tables) {
+        int32_t* const l_k = (int32_t*)&s_stage[0][0];
+        float* const l_q = (float*)(l_k + TAB_T1);
+        int32_t* const l_n = (int32_t*)(l_q + TAB_T1);
+        uint32_t* const l_m = (uint32_t*)(l_n + ORDERMOE_MAX_EXPERTS);
+        float* const l_S = (float*)(l_m + ORDERMOE_MAX_EXPERTS);
+#pragma unroll
+        for (int u = 0; u < TAB_READS; ++u) {
+            const int i = 4 * (tid + FW_THREADS * u);
+            if (i < n_t1) {
+                *(u32x4*)(l_k + i) = vk[u];
+                *(u32x4*)(l_q + i) = vq[u];
+            }
+        }
+        if (4 * tid < E) {
+            *(u32x4*)(l_n + 4 * tid) = vn;
+            *(u32x4*)(l_m + 4 * tid) = vm;
+        }
+#pragma unroll
+        for (int u = 0; u < TAB_S_READS; ++u) {
+            const int i = 4 * (tid + FW_THREADS * u);
+            if (i < n_S) *(u32x4*)(l_S + i) = vS[u];
+        }
+        tb = Tables{l_k, l_q, l_n, l_m, tables & 2 ? l_S : a.r.S};
+    }
+    // (targets, and what the searches find, in the place of the partial sums)
+    uint64_t* const s_key = (uint64_t*)&s_red[0][0][0][0];       // [slot of a token][16]
+    float* const s_q = (float*)(s_key + FW * ORDERMOE_MAX_TOPK * 16);
+    int32_t* const s_sel = (int32_t*)(s_q + FW * ORDERMOE_MAX_TOPK * 16);
+    uint8_t* const s_try = (uint8_t*)(s_sel + FW * ORDERMOE_MAX_TOPK);
+    uint8_t* const s_loc = s_try + FW * ORDERMOE_MAX_TOPK;
+    static_assert(FW * ORDERMOE_MAX_TOPK * (16 * 12 + 5) + FW <= (int)sizeof(s_red), "the searches fit");
+    __syncthreads();
+    FewPick f{};
+    if (4 * wave < T) {
+        f = few_top<NBT>(a.r, s_logit + (valid ? t : 0) * Epad, j);
+        if (valid && j < k) s_sel[t * k + j] = f.r;
+        if (valid && j == 0) s_loc[t] = (uint8_t)loc;
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int i = t; i < T * k; i += FW_THREADS / 16) {
+        uint64_t key;
+        float q;
+        const bool search = few_search(a.r, tb, s_sel[i], s_loc[i / k], j, key, q);
+        s_key[i * 16 + j] = key;
+        s_q[i * 16 + j] = q;
+        if (j == 0) s_try[i] = search;
+    }
     __syncthreads();
     if (4 * wave < T) {
-        const TokenPick p = pick_token<NBT, ORDERMOE_MAX_TOPK>(a.r, s_logit + (valid ? t : 0) * Epad, a.r.t1_k, a.r.t1_q,
-                                                               a.r.t1_n, a.r.srvmask, a.r.S, j, loc, qhat);
+        TokenPick p;
+        p.r = f.r; p.k = 0; p.m = loc;
+        p.v = f.v; p.top = f.top; p.den = f.den; p.margin = f.margin;
+        p.qhat = qhat; p.first_m = loc; p.dstmask = 0; p.loc_ok = loc < a.r.M;
+        // the slots in rank order: eq (40)'s budget, the choice of eq (43), the update of eq (44)
+#pragma unroll 1
+        for (int slot = 0; slot < k; ++slot) {
+            const int i = (valid ? t : 0) * k + slot;
+            int km = __shfl(f.r, slot, 16), mm = loc;
+            float qsel = 0.f;
+            if (s_try[i]) {
+                const float q = s_q[i * 16 + j];
+                uint64_t kk = (j == 0 || p.qhat + q <= a.r.Qbar) ? s_key[i * 16 + j] : ~0ull;
+                kk = row_min_u64(kk);
+                const int pos = (int)((kk >> 16) & 15u);
+                mm = (int)((kk >> 8) & 31u);
+                km = (int)(kk & 0xFFu);
+                qsel = row_sum_f32(j == pos ? q : 0.f);
+            }
+            p.qhat += qsel;
+            if (slot == 0) p.first_m = mm;
+            if (mm != loc) p.dstmask |= 1u << mm;
+            if (j == slot) { p.k = km; p.m = mm; }
+        }
         const bool mine = valid && j < k;
         const float w = expf(p.v - p.top) / p.den;
         // the slots that run here; those of one expert merged, weights added in slot order
@@ -608,8 +794,13 @@ int launch_layer(const FewArgs& a, int ks, hipStream_t st) {
     const int64_t act = ((groups < a.n_local ? groups : a.n_local) + a.n_shared) * (a.f / 32);
     const int64_t items = a.r.T > 0 ? act + a.r.d / 64 * FW_PIECES : 1;
     const int64_t most = FW_SHARES, shares = (items + FW_XCDS - 1) / FW_XCDS * FW_XCDS;
+    // (tables of other sizes and alignments are read where they are)
+    auto vec = [](const void* p, int64_t n) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && n % 4 == 0; };
+    const int64_t n_t1 = (int64_t)a.r.E * a.r.gmax, n_S = (int64_t)a.r.M * a.r.M * a.r.E;
+    int tables = vec(a.r.t1_k, n_t1) && vec(a.r.t1_q, n_t1) && vec(a.r.t1_n, a.r.E) && vec(a.r.srvmask, a.r.E) ? 1 : 0;
+    if (tables && vec(a.r.S, n_S) && n_S <= TAB_S) tables |= 2;
     KernelTimer kt_("few_layer", st);
-    few_layer_kernel<BF, NBT, AUX><<<dim3((unsigned)(shares < most ? shares : most)), dim3(FW_THREADS), 0, st>>>(a, ks);
+    few_layer_kernel<BF, NBT, AUX><<<dim3((unsigned)(shares < most ? shares : most)), dim3(FW_THREADS), 0, st>>>(a, ks, tables);
     return (int)hipGetLastError();
 }
 
