@@ -1,6 +1,6 @@
-// The token stage of the routing, shared by the routing kernel and the layer
-// kernel for a few tokens: top-k, gates, margin and server-expert selection of one
-// token by 16 lanes (one DPP row).
+// The token stage of the routing: top-k, gates, margin and server-expert selection of
+// one token by 16 lanes (one DPP row).  The layer kernel for a few tokens shares the
+// order of logits, the reductions and the result, and makes the same decisions in loops.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -192,6 +192,29 @@ def test_a_token_that_is_no_number_leaves_the_others_alone():
     assert np.isnan(host(y)[3]).all()
 
 
+@pytest.mark.parametrize("k,M,allow_sub,renorm", [(8, 8, 1, 1), (3, 8, 2, 0), (8, 16, 1, 1), (1, 2, 0, 0)])
+def test_tables_at_any_address(k, M, allow_sub, renorm):
+    """Tables that 16-byte reads cannot take, and costs too large to be kept on the chip
+    (16 servers x 16 x 64 experts), give the decisions of the routing."""
+    case, dl = _layer(k=k, M=M, capacity=wl._cap(M, max(8, 64 // M)), allow_sub=allow_sub, renorm=renorm)
+    x, loc, qh = dl.inputs()
+    cfg = dl.cfg
+    ref = dl.route(x, loc, qh, 16)
+    first, y = _few(dl, x, loc, qh, 16)
+    _check_route(dl, first, ref, 16)
+    moved = {}
+    for n, v in dl.tabs_dev.items():
+        room = torch.empty(v.numel() + 1, dtype=v.dtype, device="cuda")
+        room[1:] = v.reshape(-1)
+        moved[n] = room[1:]
+        assert moved[n].data_ptr() % 16 == 4
+    dl.layer = om.make_layer(dl.code, cfg.d, cfg.E, cfg.k, cfg.M, 15, dl.w_router, moved, dl.Qbar, cfg.omega_Q, cfg.pin_local_exact,
+                             cfg.allow_sub, cfg.renorm)
+    out, y2 = _few(dl, x, loc, qh, 16)
+    _check_route(dl, out, ref, 16)
+    np.testing.assert_array_equal(host(y2), host(y))
+
+
 def test_two_streams_and_shared_weights():
     case, dl = _layer(n_shared=2)
     x, loc, qh = dl.inputs()
