@@ -23,7 +23,7 @@
 //                 column, that is to a lane.
 //   V             lane (c, g) reads D/16 neighbouring codes of its 8 tokens; matrix
 //                 instruction j takes element c D/16 + j of each, whose codes are
-//                 paired across tokens by byte permutes.
+//                 paired across tokens (e4m3: by byte permutes).
 // Codes come from memory in whole cache lines, 16 bytes a lane, two tiles on their way,
 // and get into these orders through the wave's own LDS rows (read in operand order
 // straight from memory, 64 single tokens took 149 us for 119).
@@ -38,7 +38,7 @@
 // Bound: one query row block, the codes: 64 sequences of 200-8000 tokens, 32 query and 8
 // key/value heads of 128, 101 us with the join, 5.5 TB/s.  64 drafted tokens (16 rows
 // of 16 a head), the vector instructions of a tile (some 230 a wave next to 40 matrix
-// instructions): 4 sequences of 30000-100000 tokens 330 us, 540 TFLOP/s.  One sequence of 778
+// instructions): 4 sequences of 30000-100000 tokens 312 us, 570 TFLOP/s.  One sequence of 778
 // tokens 10.6 us: a launch, and a chain of five dependent reads.
 #include <hip/hip_runtime.h>
 
@@ -274,8 +274,9 @@ __device__ inline uint32_t row_and(uint32_t v) {
     return v;
 }
 
-template <bool BF, int D, int FMT, int RT>
-__device__ inline void attend_tile(const char* stage, const bool* ok, const void* qv, const uint64_t* word,
+// FINE: the second product takes what the rounding of the weights to bf16 leaves out as well
+template <bool BF, int D, int FMT, int RT, bool FINE>
+__device__ inline __attribute__((always_inline)) void attend_tile(const char* stage, const bool* ok, const void* qv, const uint64_t* word,
                                    int t0, const SeqInfo& s, int lane, State<D, RT>& st) {
     const int c = lane & 15, g = lane >> 4;
     const f32x4* scales = (const f32x4*)(stage + 64 * PITCH<D>) + g;     // of tokens 4g .. 4g + 3
@@ -413,28 +414,34 @@ __device__ inline void attend_tile(const char* stage, const bool* ok, const void
             for (int w = 0; w < D / 64; ++w) v[u][w] = (none >> u) & 1 ? 0u : v[u][w];
     }
     if constexpr (BF) {
-        // one row tile: what the rounding of the weights leaves out goes through the matrix unit too, which has
-        // the time there (the codes' reads bound it); more: the rounded weights alone
+        // a kernel of one row tile has the matrix unit's time for it (the codes' reads bound it)
         bf16x8 pf[RT], pl = {};
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 pf[r][u] = (__bf16)pw[r][u];
-                if constexpr (RT == 1) pl[u] = (__bf16)(pw[r][u] - (float)pf[r][u]);
+                if constexpr (FINE) pl[u] = (__bf16)(pw[r][u] - (float)pf[r][u]);
             }
 #pragma unroll
         for (int w = 0; w < D / 64; ++w) {
             u32x4 vf[4];                                         // elements 4w .. 4w + 3, tokens in pairs
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                // bytes b of tokens 2u and 2u + 1 side by side: b = 0, 1 and b = 2, 3
-                const uint32_t lo = __builtin_amdgcn_perm(v[2 * u + 1][w], v[2 * u][w], 0x05010400u);
-                const uint32_t hi = __builtin_amdgcn_perm(v[2 * u + 1][w], v[2 * u][w], 0x07030602u);
-                vf[0][u] = kv_to_bf16x2<FMT, 0>(lo);
-                vf[1][u] = kv_to_bf16x2<FMT, 1>(lo);
-                vf[2][u] = kv_to_bf16x2<FMT, 0>(hi);
-                vf[3][u] = kv_to_bf16x2<FMT, 1>(hi);
+                if constexpr (FMT == ORDERMOE_CACHE_INT8) {
+                    vf[0][u] = kv_bf16_pair(kv_to_f32<FMT, 0>(v[2 * u][w]), kv_to_f32<FMT, 0>(v[2 * u + 1][w]));
+                    vf[1][u] = kv_bf16_pair(kv_to_f32<FMT, 1>(v[2 * u][w]), kv_to_f32<FMT, 1>(v[2 * u + 1][w]));
+                    vf[2][u] = kv_bf16_pair(kv_to_f32<FMT, 2>(v[2 * u][w]), kv_to_f32<FMT, 2>(v[2 * u + 1][w]));
+                    vf[3][u] = kv_bf16_pair(kv_to_f32<FMT, 3>(v[2 * u][w]), kv_to_f32<FMT, 3>(v[2 * u + 1][w]));
+                } else {
+                    // bytes b of tokens 2u and 2u + 1 side by side: b = 0, 1 and b = 2, 3
+                    const uint32_t lo = __builtin_amdgcn_perm(v[2 * u + 1][w], v[2 * u][w], 0x05010400u);
+                    const uint32_t hi = __builtin_amdgcn_perm(v[2 * u + 1][w], v[2 * u][w], 0x07030602u);
+                    vf[0][u] = kv_to_bf16x2<FMT, 0>(lo);
+                    vf[1][u] = kv_to_bf16x2<FMT, 1>(lo);
+                    vf[2][u] = kv_to_bf16x2<FMT, 0>(hi);
+                    vf[3][u] = kv_to_bf16x2<FMT, 1>(hi);
+                }
             }
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
@@ -442,7 +449,7 @@ __device__ inline void attend_tile(const char* stage, const bool* ok, const void
                 for (int r = 0; r < RT; ++r)
                     st.o[4 * w + b][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[b]), pf[r],
                                                                                  st.o[4 * w + b][r], 0, 0, 0);
-                if constexpr (RT == 1)
+                if constexpr (FINE)
                     st.o[4 * w + b][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[b]), pl,
                                                                                  st.o[4 * w + b][0], 0, 0, 0);
             }
@@ -491,44 +498,28 @@ __device__ inline float row_lse(float m, float l) {
 template <int D>
 constexpr int OCC = D == 256 ? 1 : 2;
 
-template <bool BF, int D, int FMT, int RT, int NW>
-__global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const DraftArgs a, int items, int rb_n, int whole) {
+// What a workgroup's rows are attended to with: LDS for the codes' staging rows, then the waves' sums (in one place),
+// and for their maxima and sums
+template <int D, int NW>
+constexpr int SUMS = NW * 16 * (D + 4) * 4;
+template <int D, int RT, int NW>
+struct Shared {
+    __attribute__((aligned(16))) char mem[NW * STAGE<D> > SUMS<D, NW> ? NW * STAGE<D> : SUMS<D, NW>];
+    float m[NW][RT * 16], l[NW][RT * 16];
+};
+
+// rows row0 .. row0 + 16 RT - 1 (of `rows`) of key/value head kvh over tokens [t_lo, t_hi) of a sequence.  ALONE: no
+// other workgroup reads the codes
+template <bool BF, int D, int FMT, int RT, int NW, bool ALONE>
+__device__ inline __attribute__((always_inline)) void attend_rows(const DraftArgs& a, const SeqInfo& s, int item, int kvh, int row0,
+                                                                  int rows, int pieces, int t_lo, int t_hi, const int32_t* table,
+                                                                  char* s_mem, float (*s_m)[RT * 16], float (*s_l)[RT * 16]) {
     constexpr int LD = D + 4, ROUND = NW * DA_TILE;
-    constexpr int SUMS = NW * 16 * LD * 4;
-    __shared__ __attribute__((aligned(16))) char s_mem[NW * STAGE<D> > SUMS ? NW * STAGE<D> : SUMS];
     float (*const s_o)[16][LD] = (float (*)[16][LD])s_mem;
-    __shared__ float s_m[NW][RT * 16], s_l[NW][RT * 16];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
-    // the row blocks of one piece and head on one XCD, where its codes are in L2
-    const int idx = blockIdx.x, jx = idx >> 3;
-    const int unit = (jx / rb_n) * 8 + (idx & 7), rb = jx % rb_n;
     const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
-    if (unit >= items * n_kv) return;
-    const int item = unit / n_kv, kvh = unit - item * n_kv;
-    int piece = 1 << 30, b = item, j = 0;
-    SeqInfo s;
-    if (whole) {
-        s = sequence(a, b);                          // every sequence is one piece
-    } else {
-        SeqInfo mine = {0, 0, 0, 0};
-        if (lane < a.B) mine = sequence(a, lane);
-        // (the same in every lane, and in scalar registers from here on: addresses and branches below rest on it)
-        piece = __builtin_amdgcn_readfirstlane(piece_tokens(a, rb_n, RT, ROUND, mine, lane));
-        s = find_item(a, piece, item, lane, blockIdx.x == 0 && wave == 0, mine, b, j);
-    }
-    b = __builtin_amdgcn_readfirstlane(b);
-    j = __builtin_amdgcn_readfirstlane(j);
-    s = SeqInfo{__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.n), __builtin_amdgcn_readfirstlane(s.ctx),
-                __builtin_amdgcn_readfirstlane(s.len)};
-    if (b < 0) return;
-    const int rows = s.n * G, row0 = rb * 16 * RT;
-    if (row0 >= rows) return;
-    const int pieces = pieces_of(s, piece);
-    const int t_lo = j * piece, t_hi = s.len - t_lo < piece ? s.len : t_lo + piece;
-    const int32_t* table = a.page_table + (int64_t)b * a.max_pages;
-
     // query rows: row = token * G + head; rows past the end are zeros and see nothing
     constexpr int NQ = BF ? RT * D / 32 : 1;
     Queries<NQ> qb;
@@ -571,21 +562,20 @@ __global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const 
     }
     const float scale2 = a.scale * 1.44269504088896341f;        // scores in units of log 2
     // two tiles are on their way while one is attended to
-    constexpr bool NTL = RT == 1;                     // (with more row tiles, other row blocks may read the codes too)
     Tile<D> t[2];
     char* const stage = s_mem + wave * STAGE<D>;
     int p = t_lo + wave * DA_TILE;
     Pages pg = tile_pages(a, table, p, t_hi);
-    load_tile<D, NTL>(a, pg, kvh, p, lane, t[0]);
+    load_tile<D, ALONE>(a, pg, kvh, p, lane, t[0]);
     pg = tile_pages(a, table, p + ROUND, t_hi);
-    load_tile<D, NTL>(a, pg, kvh, p + ROUND, lane, t[1]);
+    load_tile<D, ALONE>(a, pg, kvh, p + ROUND, lane, t[1]);
     pg = tile_pages(a, table, p + 2 * ROUND, t_hi);
     auto step = [&](Tile<D>& u) __attribute__((always_inline)) {
         const bool ok[2] = {u.ok[0], u.ok[1]};
         stage_tile<D>(u, stage, lane, scale2);
-        load_tile<D, NTL>(a, pg, kvh, p + 2 * ROUND, lane, u);
+        load_tile<D, ALONE>(a, pg, kvh, p + 2 * ROUND, lane, u);
         pg = tile_pages(a, table, p + 3 * ROUND, t_hi);
-        attend_tile<BF, D, FMT, RT>(stage, ok, qv, word, p, s, lane, st);
+        attend_tile<BF, D, FMT, RT, ALONE>(stage, ok, qv, word, p, s, lane, st);
         p += ROUND;
     };
     while (p < t_hi) {
@@ -656,6 +646,50 @@ __global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const 
         }
         __syncthreads();
     }
+}
+
+template <bool BF, int D, int FMT, int RT, int NW>
+__global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const DraftArgs a, int items, int rb_n, int whole) {
+    constexpr int ROUND = NW * DA_TILE;
+    __shared__ Shared<D, RT, NW> sh;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // the row blocks of one piece and head on one XCD, where its codes are in L2
+    const int idx = blockIdx.x, jx = idx >> 3;
+    const int unit = (jx / rb_n) * 8 + (idx & 7), rb = jx % rb_n;
+    const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
+    if (unit >= items * n_kv) return;
+    const int item = unit / n_kv, kvh = unit - item * n_kv;
+    int piece = 1 << 30, b = item, j = 0;
+    SeqInfo s;
+    if (whole) {
+        s = sequence(a, b);                          // every sequence is one piece
+    } else {
+        SeqInfo mine = {0, 0, 0, 0};
+        if (lane < a.B) mine = sequence(a, lane);
+        // (the same in every lane, and in scalar registers from here on: addresses and branches below rest on it)
+        piece = __builtin_amdgcn_readfirstlane(piece_tokens(a, rb_n, RT, ROUND, mine, lane));
+        s = find_item(a, piece, item, lane, blockIdx.x == 0 && wave == 0, mine, b, j);
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    j = __builtin_amdgcn_readfirstlane(j);
+    s = SeqInfo{__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.n), __builtin_amdgcn_readfirstlane(s.ctx),
+                __builtin_amdgcn_readfirstlane(s.len)};
+    if (b < 0) return;
+    const int rows = s.n * G, row0 = rb * 16 * RT;
+    if (row0 >= rows) return;
+    const int pieces = pieces_of(s, piece);
+    const int t_lo = j * piece, t_hi = s.len - t_lo < piece ? s.len : t_lo + piece;
+    const int32_t* table = a.page_table + (int64_t)b * a.max_pages;
+    if constexpr (RT > 1) {
+        // a last block of up to 16 rows, or a sequence of no more (ragged trees of 33 44 -> 41 us, of 64 325 -> 312)
+        if (rows - row0 <= 16) {
+            attend_rows<BF, D, FMT, 1, NW, false>(a, s, item, kvh, row0, rows, pieces, t_lo, t_hi, table, sh.mem,
+                                                  (float (*)[16])sh.m, (float (*)[16])sh.l);
+            return;
+        }
+    }
+    attend_rows<BF, D, FMT, RT, NW, RT == 1>(a, s, item, kvh, row0, rows, pieces, t_lo, t_hi, table, sh.mem, sh.m, sh.l);
 }
 
 // 16 / S (token, head) rows of a sequence per workgroup, S sets of 16 lanes a row: set z

@@ -26,17 +26,18 @@ __device__ inline float kv_to_f32(uint32_t w) {
     else return __builtin_amdgcn_cvt_f32_fp8((int)w, B);
 }
 
+__device__ inline uint32_t kv_bf16_pair(float a, float b) {
+    kv_bf16x2 r;
+    r[0] = (__bf16)a;
+    r[1] = (__bf16)b;
+    return __builtin_bit_cast(uint32_t, r);
+}
+
 // bytes 2H and 2H + 1 of w as a pair of bf16 (every code is a bf16 value)
 template <int FMT, int H>
 __device__ inline uint32_t kv_to_bf16x2(uint32_t w) {
-    kv_bf16x2 r;
-    if constexpr (FMT == ORDERMOE_CACHE_INT8) {
-        r[0] = (__bf16)kv_to_f32<FMT, 2 * H>(w);
-        r[1] = (__bf16)kv_to_f32<FMT, 2 * H + 1>(w);
-    } else {
-        r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, H != 0);
-    }
-    return __builtin_bit_cast(uint32_t, r);
+    if constexpr (FMT == ORDERMOE_CACHE_INT8) return kv_bf16_pair(kv_to_f32<FMT, 2 * H>(w), kv_to_f32<FMT, 2 * H + 1>(w));
+    else return __builtin_bit_cast(uint32_t, (kv_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, H != 0));
 }
 
 // four values in [-max, max] to codes
