@@ -614,11 +614,12 @@ def make_heads(dtype: int, n_q: int, head_dim: int, q_norm=None, k_norm=None, co
 
 def _rows(t, dtype, T: int, heads: int, D: int):
     """(address, stride) of [T, heads, D] whose tokens may lie apart."""
-    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != (T, heads, D):
+    if not t.is_cuda or t.dtype != dtype or t.shape != (T, heads, D):
         raise ValueError("expected a %s device tensor [%d, %d, %d]" % (dtype, T, heads, D))
-    if T > 0 and (t.stride(2) != 1 or t.stride(1) != D):
+    apart, per_head, per_element = t.stride()                # (once: a call on a tensor costs a tenth of a microsecond)
+    if T > 0 and (per_element != 1 or per_head != D):
         raise ValueError("the heads of a token must lie side by side")
-    return t.data_ptr(), (t.stride(0) if T > 1 else heads * D)
+    return t.data_ptr(), (apart if T > 1 else heads * D)
 
 
 def ordermoe_cache_write(cache: Cache, heads: Heads, q, k, v, pos, slots, q_out, stream=None):
