@@ -24,6 +24,7 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 constexpr int CW_THREADS = 256;
 constexpr int CW_ROWS = CW_THREADS / 16;     // 16-lane groups per block
 constexpr int64_t CW_MANY = 1 << 16;         // head rows from which a group takes four: twice the chip's waves
+constexpr int64_t CW_STREAM_BYTES = (int64_t)32 << 20;   // bytes of queries from which rows go past the caches: all L2s together
 
 // reductions over the 16 lanes of a DPP row, by rotations of 8, 4, 2, 1; every
 // lane ends with the same bits (each step adds the same two values in both lanes)
@@ -50,14 +51,19 @@ template <typename T, int N>
 struct Raw {
     static constexpr int W = N * (int)sizeof(T) / 4;
     uint32_t w[W];
+    template <bool NTL = false>
     __device__ inline void load(const T* p) {
         if constexpr (W == 2) {
-            const u32x2 v = *(const u32x2*)p;
+            u32x2 v;
+            if constexpr (NTL) v = __builtin_nontemporal_load((const u32x2*)p);
+            else v = *(const u32x2*)p;
             w[0] = v[0]; w[1] = v[1];
         } else {
 #pragma unroll
             for (int i = 0; i < W / 4; ++i) {
-                const u32x4 v = ((const u32x4*)p)[i];
+                u32x4 v;
+                if constexpr (NTL) v = __builtin_nontemporal_load((const u32x4*)p + i);
+                else v = ((const u32x4*)p)[i];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
             }
@@ -151,7 +157,7 @@ __device__ inline float quotient(float x, float b, float r) {
 __device__ inline uint32_t divided(uint32_t row, const Divisor& n) { return __umulhi(row, n.mul) >> n.shift; }
 
 // One head row of N elements per lane, already read (x): all of its work.
-template <typename T, int D, int FMT>
+template <typename T, int D, int FMT, bool NTS>
 __device__ inline void write_head_row(const CacheWriteArgs& a, uint32_t t, int h, int pos, int64_t slot, float* x, int c) {
     constexpr int N = D / 16;                                   // elements per lane
     const int kind = h < a.n_q ? 0 : h < a.n_q + a.cache.n_kv ? 1 : 2;      // query, key, value
@@ -213,7 +219,7 @@ __device__ inline void write_head_row(const CacheWriteArgs& a, uint32_t t, int h
             for (int i = 0; i < N; ++i) x[i] = __builtin_nanf("");
     }
     if (kind == 0) {
-        store_f32<T, N>((T*)a.q_out + ((int64_t)t * a.n_q + h) * D + c * N, x);
+        store_f32<T, N, NTS>((T*)a.q_out + ((int64_t)t * a.n_q + h) * D + c * N, x);
         return;
     }
     // the largest magnitude on the bits, where a NaN is larger than infinity
@@ -242,9 +248,11 @@ __device__ inline void write_head_row(const CacheWriteArgs& a, uint32_t t, int h
 }
 
 // U rows per 16 lanes, all read before the first is worked on: one row a lane leaves
-// too few bytes on their way for a prompt's rows (16001 tokens of 16 + 16 + 16 heads of 128: one row 94 us, four 90);
-// a step's are too few to share four by four.
-template <typename T, int D, int FMT, int U>
+// too few bytes on their way for a prompt's rows (16001 tokens of 16 + 16 + 16 heads of 128: one
+// row 94 us, four 90, before other steps made it 79); a step's are too few to share four by
+// four.  NTS: rows are read, and queries stored, past the caches (the same rows 79 us, so 74; 16001
+// tokens of 32 query heads and one key head 71, 65; 8000 of 32 and 8 heads 51, 46.5).
+template <typename T, int D, int FMT, int U, bool NTS>
 __global__ void __launch_bounds__(CW_THREADS) cache_write_kernel(const CacheWriteArgs a) {
     constexpr int N = D / 16;
     const int c = threadIdx.x & 15;
@@ -263,7 +271,7 @@ __global__ void __launch_bounds__(CW_THREADS) cache_write_kernel(const CacheWrit
         const T* src = hk < 0 ? (const T*)a.q + (int64_t)t[u] * a.q_stride + h[u] * D
                        : hv < 0 ? (const T*)a.k + (int64_t)t[u] * a.k_stride + hk * D
                                 : (const T*)a.v + (int64_t)t[u] * a.v_stride + hv * D;
-        raw[u].load(src + c * N);
+        raw[u].template load<NTS>(src + c * N);
         pos[u] = hv < 0 && a.rot ? a.pos[t[u]] : 0;
         slot[u] = hk < 0 ? -1 : a.slots[t[u]];
     }
@@ -272,7 +280,7 @@ __global__ void __launch_bounds__(CW_THREADS) cache_write_kernel(const CacheWrit
         if (row0 + CW_ROWS * u >= rows) return;                 // whole rows leave together
         float x[N];
         raw[u].f32(x);
-        write_head_row<T, D, FMT>(a, t[u], h[u], pos[u], slot[u], x, c);
+        write_head_row<T, D, FMT, NTS>(a, t[u], h[u], pos[u], slot[u], x, c);
     }
 }
 
@@ -368,10 +376,12 @@ int launch_cache_write(const CacheWriteArgs& args, void* stream) {
         KernelTimer kt_("cache_write", stream);
         constexpr int D = decltype(d)::value, F = decltype(f)::value;
         auto blocks = [&](int u) { return dim3((unsigned)((rows + CW_ROWS * u - 1) / (CW_ROWS * u))); };
-        if (rows >= CW_MANY)
-            cache_write_kernel<decltype(t), D, F, 4><<<blocks(4), dim3(CW_THREADS), 0, (hipStream_t)stream>>>(a);
+        if (rows < CW_MANY)
+            cache_write_kernel<decltype(t), D, F, 1, false><<<blocks(1), dim3(CW_THREADS), 0, (hipStream_t)stream>>>(a);
+        else if (a.T * a.n_q * D * (int64_t)sizeof(t) < CW_STREAM_BYTES)
+            cache_write_kernel<decltype(t), D, F, 4, false><<<blocks(4), dim3(CW_THREADS), 0, (hipStream_t)stream>>>(a);
         else
-            cache_write_kernel<decltype(t), D, F, 1><<<blocks(1), dim3(CW_THREADS), 0, (hipStream_t)stream>>>(a);
+            cache_write_kernel<decltype(t), D, F, 4, true><<<blocks(4), dim3(CW_THREADS), 0, (hipStream_t)stream>>>(a);
         return (int)hipGetLastError();
     });
 }

@@ -155,6 +155,31 @@ def test_rows_without_a_slot_or_a_position_and_rows_that_are_no_numbers():
     assert np.isfinite(scale[0][[4, 5]]).all() and (codes[0] != 0x7F)[[2, 3, 4, 5, 6]].all()
 
 
+@pytest.mark.parametrize("dtype,D,hq,hkv,T", [("bf16", 128, 32, 8, 4201), ("f32", 64, 48, 4, 2801), ("bf16", 64, 64, 8, 4203)])
+def test_a_prompt_in_one_call_and_in_parts(dtype, D, hq, hkv, T):
+    """Rows of over 32 MiB go past the caches; the same rows in parts of a few hundred tokens have the same bits."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    qkv = torch.randn((T, hq + 2 * hkv, D), generator=g, device="cuda").to(DT[dtype])
+    q, k, v = qkv.split([hq, hkv, hkv], 1)
+    assert q.numel() * q.element_size() > 32 << 20
+    page, pages = 64, -(-T // 64)
+    w = [(1 + 0.1 * torch.randn(D, generator=g, device="cuda")).to(DT[dtype]) for _ in range(2)]
+    heads = om.make_heads(CODE[dtype], hq, D, *w, _dev(om.rotary_table(T, D)), 0)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    slots = torch.randperm(pages * page, generator=g, device="cuda")[:T]
+    res = []
+    for step in (T, 401):
+        ca, out = _Cache("int8", pages, hkv, page, D), torch.empty((T, hq, D), dtype=DT[dtype], device="cuda")
+        for i in range(0, T, step):
+            c = slice(i, i + step)
+            om.ordermoe_cache_write(ca.c, heads, q[c], k[c], v[c], pos[c], slots[c], out[c])
+        torch.cuda.synchronize()
+        res.append([out] + ca.codes + [s.nan_to_num(-1.0) for s in ca.scale])
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
+
+
 def test_slots_past_2_31_bytes():
     """A slot whose codes lie more than 2^31 bytes into the cache, written, read and attended."""
     n_kv, page, D = 16, 128, 256
