@@ -61,16 +61,15 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 constexpr int DA_WAVES = 4, DA_WAVES_WIDE = 8;       // waves of a workgroup (wide: see launch_type)
 constexpr int DA_TILE = 32;                          // tokens of a tile
 // Tokens of a piece.  DA_FULL at least, where that gives DA_ONE_EACH workgroups or more
-// (pieces of 512: trees of 33 over 1-5000, eight sequences, 47 us for 42); else as many
+// (pieces of 512: trees of 33 over 1-5000, eight sequences, 47 us for 40.5); else as many
 // fewer as give about that many, but DA_MIN_PIECE at least (one sequence of 8000 tokens:
 // 1024 19.8 us, 512 15.9, 256 15.3, with the second kernel; 128 is one round of the waves).
 constexpr int DA_FULL = 1024, DA_MIN_PIECE = 256, DA_ONE_EACH = 256;
 // Tokens of a table up to which sequences are not split: see launch_type
 constexpr int DA_WHOLE_WIDE = 1024, DA_WHOLE = 512;
 // Workgroups that a large batch is split into: two rounds of the 512 that run together
-// (64 tokens over 200-8000 cached: 512 111 us, 1024 100, 1536 99; trees of 33 over
-// 1-5000, with the second kernel: 1024 50, 1536 52, 2048 55; trees of 64 over
-// 30000-100000: 359, 356, 360)
+// (64 tokens over 200-8000 cached: 1024 101 us, 1536 102; trees of 33 over 1-5000: 1024 40.5,
+// 1536 43; trees of 64 over 30000-100000: 312, 312)
 constexpr int DA_TARGET = 1024;
 
 // 16-row tiles of query rows per workgroup
