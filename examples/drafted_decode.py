@@ -182,7 +182,8 @@ def drafted(model, prompts, n_tokens, fmt):
         take(u, logits)
     steps = 0
     while min(len(t) - len(p) for t, p in zip(texts, prompts)) < n_tokens:
-        trees = [draft(t) for t in texts]
+        # a user that has its tokens drafts no more: its row of the page table ends soon after them
+        trees = [draft(t) if len(t) - len(p) < n_tokens else ([], []) for t, p in zip(texts, prompts)]
         depths, words = [], []
         for tokens, parents in trees:
             d, w = [], []
@@ -194,6 +195,8 @@ def drafted(model, prompts, n_tokens, fmt):
         logits = s.forward([t for t, _ in trees], depths, words)
         first = 0
         for u, (tokens, parents) in enumerate(trees):
+            if not tokens:
+                continue
             path = [0]
             while True:
                 take(u, logits[first + path[-1]])
