@@ -498,7 +498,7 @@ int ordermoe_pack_down(int32_t dtype, int32_t n, int32_t d, int32_t f, const voi
 
 typedef struct {
     int32_t format;         /* ORDERMOE_CACHE_INT8 or ORDERMOE_CACHE_FP8 */
-    int32_t n_kv;           /* key/value heads, >= 1 */
+    int32_t n_kv;           /* key/value heads, 1 to 1024 */
     int32_t head_dim;       /* 64, 128 or 256 */
     int32_t page_size;      /* slots of a page: a power of two from 16 to 1024 */
     int64_t n_pages;
@@ -510,11 +510,11 @@ typedef struct {
 
 typedef struct {
     int32_t dtype;          /* storage of q, k, v, q_out and the norm weights */
-    int32_t n_q;            /* query heads, a multiple of the cache's n_kv */
+    int32_t n_q;            /* query heads, a multiple of the cache's n_kv, at most 1024 */
     int32_t rotary_dim;     /* leading elements of a head that are turned: 0 to head_dim, a multiple of head_dim / 8 */
     int32_t interleaved;    /* 1: elements 2i and 2i + 1 turn together; 0: i and i + rotary_dim / 2 */
     int64_t max_pos;        /* rows of cos_sin */
-    float eps;              /* of the norms, >= 0 */
+    float eps;              /* of the norms, finite and >= 0 */
     const void* q_norm;     /* dev [head_dim] weights of the query norm, or NULL: no query norm (all three 16-byte aligned) */
     const void* k_norm;     /* dev [head_dim] weights of the key norm, or NULL: no key norm */
     const float* cos_sin;   /* dev [max_pos][rotary_dim]: per position the cosines of the rotary_dim / 2
@@ -533,7 +533,8 @@ typedef struct {
  *             their own).  16-byte aligned, strides multiples of 16 bytes and
  *             at least the heads' elements.
  *   pos       dev [T] int32 position of each token (NULL if rotary_dim = 0); one
- *             outside [0, max_pos) makes the token's queries and keys NaN
+ *             outside [0, max_pos) makes the turned elements of the token's queries
+ *             NaN, and its key rows whole (codes 0, scale NaN, as above)
  *   slots     dev [T] int64 cache slot of each token, distinct; a token whose slot is
  *             outside [0, n_pages * page_size) is not written (its queries are)
  *   q_out     dev [T][n_q][head_dim], may not overlap the inputs
