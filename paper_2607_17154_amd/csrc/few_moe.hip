@@ -658,6 +658,7 @@ __global__ void __launch_bounds__(FW_THREADS) few_layer_kernel(const FewArgs a, 
             }
         };
         u32x4 vw[2][UD][8], va[2][UD][2];
+        bool runs[2][UD];                                    // the lane's token runs in the step's group
         Pos pw{0, lo + wave, ns}, pa = pw;
         auto load_w = [&](int b) {
 #pragma unroll
@@ -687,6 +688,7 @@ __global__ void __launch_bounds__(FW_THREADS) few_layer_kernel(const FewArgs a, 
                 const char* A = shared ? (const char*)a.act_s : (const char*)a.act_r + (size_t)(in ? grp : 0) * FW * a.f * ES;
                 const __amdgpu_buffer_rsrc_t ra = make_rsrc(A, (uint32_t)FW * (uint32_t)F * ES);
                 const bool has = in && ((s_msk[grp] >> r16) & 1);
+                runs[b][u] = has;
                 const uint32_t ao = has ? (uint32_t)r16 * (uint32_t)F * ES + 16u * g16 : OOR;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) va[b][u][h] = load16(ra, ao, (uint32_t)(in ? pa.s : 0) * 128u + 64u * h);
@@ -700,11 +702,17 @@ __global__ void __launch_bounds__(FW_THREADS) few_layer_kernel(const FewArgs a, 
             for (int u = 0; u < UD; ++u) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) *(u32x4*)(put + 8 * i * ROW_LD) = vw[b][u][i];
+                f32x4 sum[4] = {acc[0], acc[1], acc[2], acc[3]};
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        acc[r] = mma<BF>(*(const u32x4*)(get + 16 * r * ROW_LD + 64 * h), va[b][u][h], acc[r]);
+                        sum[r] = mma<BF>(*(const u32x4*)(get + 16 * r * ROW_LD + 64 * h), va[b][u][h], sum[r]);
+                // a group's weights reach its own tokens only (to the others' zeros one that is no number would add a NaN)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[r][i] = runs[b][u] ? sum[r][i] : acc[r][i];
             }
         };
         load_w(0);
