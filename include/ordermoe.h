@@ -563,7 +563,8 @@ int ordermoe_cache_read(const ordermoe_cache* C, int32_t dtype, const int64_t* s
  *   s_p = scale * q . k_p,   out = sum_p exp(s_p) v_p / sum_p exp(s_p),
  *   lse = log sum_p exp(s_p)                          over the seen positions;
  * a token that sees nothing gets out = 0 and lse = -infinity.  What the cache
- * holds at unseen positions, and past a sequence's end, has no effect.
+ * holds at unseen positions, and past a sequence's end, has no effect: a position
+ * that was never written spoils the outputs of the tokens that see it, and no others.
  * bf16: q times the codes with fp32 sums, statistics in fp32, the weights
  * exp(s - max) * v_scale rounded to bf16 for the product with the codes of V (in
  * two parts, 16 bits together, for head_dim 256 or max_q * n_q / n_kv <= 16 rows),

@@ -233,8 +233,11 @@ __device__ inline void load_tile(const DraftArgs& a, const Pages& pg, int kvh, i
     const float* sc = lane < 32 ? a.cache.k_scale : a.cache.v_scale;
     t.s = sc[(lane & 16 ? row[1] : row[0]) + (lane & 15)];
 }
-template <int D>
-__device__ inline void stage_tile(const Tile<D>& t, char* st, int lane, float scale2) {
+// edge: some row may not see some token.  A weight of 0 would not keep a code that is no number (e4m3; a place
+// that was never written may hold one) out of that row's sums, so V's become zeros and the token's scale a NaN:
+// the rows that see it are no numbers all the same.  (In other tiles every row sees every token.)
+template <int D, int FMT>
+__device__ inline void stage_tile(const Tile<D>& t, char* st, int lane, float scale2, bool edge) {
     constexpr int CH = D / 16;                       // 16-byte chunks of a row
     char* p = st + (lane / CH) * PITCH<D> + (lane % CH) * 16;
 #pragma unroll
@@ -245,6 +248,23 @@ __device__ inline void stage_tile(const Tile<D>& t, char* st, int lane, float sc
             *(u32x4*)(p + (32 + 16 * tb + 64 / CH * i) * PITCH<D>) = t.v[tb][i];
         }
     *(float*)(st + 64 * PITCH<D> + 4 * lane) = lane < 32 ? t.s * scale2 : t.s;   // (K's in units of the scores)
+    if constexpr (FMT == ORDERMOE_CACHE_FP8) {
+        if (edge) {
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) {
+                    uint32_t nan = 0u;                           // the top bits of the bytes that are 0x7F but for their sign
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) nan |= ~((~t.v[tb][i][w] & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) & 0x80808080u;
+                    if (nan) {
+                        const int row = 32 + 16 * tb + 64 / CH * i;
+                        *(u32x4*)(p + row * PITCH<D>) = u32x4{0u, 0u, 0u, 0u};
+                        *(float*)(st + 64 * PITCH<D> + 4 * (row + lane / CH)) = __builtin_nanf("");
+                    }
+                }
+        }
+    }
 }
 
 // The running state of a wave: per row tile, lane (c, g) has row c's maximum (in
@@ -263,15 +283,6 @@ constexpr float DA_LAG = 8.0f;
 
 template <int N>
 struct Queries { bf16x8 b[N]; };
-
-// and over the 16 lanes of a DPP row, by rotations of 8, 4, 2, 1
-__device__ inline uint32_t row_and(uint32_t v) {
-    v &= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xF, 0xF, false);
-    v &= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xF, 0xF, false);
-    v &= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xF, 0xF, false);
-    v &= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xF, 0xF, false);
-    return v;
-}
 
 // FINE: the second product takes what the rounding of the weights to bf16 leaves out as well
 template <bool BF, int D, int FMT, int RT, bool FINE>
@@ -399,18 +410,6 @@ __device__ inline __attribute__((always_inline)) void attend_tile(const char* st
             const u32x4 w = *(const u32x4*)r;
             v[u][0] = w[0]; v[u][1] = w[1]; v[u][2] = w[2]; v[u][3] = w[3];
         }
-    }
-    // tokens that no row sees, past the end, in no page or drafted, may never have been written: a
-    // weight of 0 would not keep codes that are no numbers out of the sums
-    if (edge) {
-        uint32_t none = hidden[0];
-#pragma unroll
-        for (int r = 1; r < RT; ++r) none &= hidden[r];
-        none = row_and(none);                                    // (the 16 lanes of a group have the same tokens)
-#pragma unroll
-        for (int u = 0; u < 8; ++u)
-#pragma unroll
-            for (int w = 0; w < D / 64; ++w) v[u][w] = (none >> u) & 1 ? 0u : v[u][w];
     }
     if constexpr (BF) {
         // a kernel of one row tile has the matrix unit's time for it (the codes' reads bound it)
@@ -571,7 +570,7 @@ __device__ inline __attribute__((always_inline)) void attend_rows(const DraftArg
     pg = tile_pages(a, table, p + 2 * ROUND, t_hi);
     auto step = [&](Tile<D>& u) __attribute__((always_inline)) {
         const bool ok[2] = {u.ok[0], u.ok[1]};
-        stage_tile<D>(u, stage, lane, scale2);
+        stage_tile<D, FMT>(u, stage, lane, scale2, p + DA_TILE > s.ctx || !ok[0] || !ok[1]);
         load_tile<D, ALONE>(a, pg, kvh, p + 2 * ROUND, lane, u);
         pg = tile_pages(a, table, p + 3 * ROUND, t_hi);
         attend_tile<BF, D, FMT, RT, ALONE>(stage, ok, qv, word, p, s, lane, st);
