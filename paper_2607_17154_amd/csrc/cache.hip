@@ -13,6 +13,7 @@
 #include <type_traits>
 
 #include "common.hpp"
+#include "grid.hpp"
 #include "kv_codes.hpp"
 
 namespace ordermoe {
@@ -257,7 +258,7 @@ __global__ void __launch_bounds__(CW_THREADS) cache_write_kernel(const CacheWrit
     constexpr int N = D / 16;
     const int c = threadIdx.x & 15;
     const uint32_t heads = (uint32_t)(a.n_q + 2 * a.cache.n_kv), rows = (uint32_t)a.T * heads;
-    const uint32_t row0 = blockIdx.x * (CW_ROWS * U) + (threadIdx.x >> 4);
+    const uint32_t row0 = block_number() * (CW_ROWS * U) + (threadIdx.x >> 4);
     uint32_t t[U];
     int h[U], pos[U];
     int64_t slot[U];
@@ -297,7 +298,7 @@ __global__ void __launch_bounds__(CW_THREADS) cache_read_kernel(const CacheReadA
     const int c = threadIdx.x & 15;
     const bool on = D >= 16 * N || c < D / N;                   // lanes with a part of the row
     const uint32_t nh = (uint32_t)a.cache.n_kv, per = 2 * nh, rows = (uint32_t)a.n * per;
-    const uint32_t row0 = blockIdx.x * (CW_ROWS * CR_U) + (threadIdx.x >> 4);
+    const uint32_t row0 = block_number() * (CW_ROWS * CR_U) + (threadIdx.x >> 4);
     uint32_t i[CR_U], r[CR_U];
     int64_t slot[CR_U];
 #pragma unroll
@@ -375,7 +376,7 @@ int launch_cache_write(const CacheWriteArgs& args, void* stream) {
     return by_type(a.dtype, a.cache, [&](auto t, auto d, auto f) {
         KernelTimer kt_("cache_write", stream);
         constexpr int D = decltype(d)::value, F = decltype(f)::value;
-        auto blocks = [&](int u) { return dim3((unsigned)((rows + CW_ROWS * u - 1) / (CW_ROWS * u))); };
+        auto blocks = [&](int u) { return grid_of((rows + CW_ROWS * u - 1) / (CW_ROWS * u)); };
         if (rows < CW_MANY)
             cache_write_kernel<decltype(t), D, F, 1, false><<<blocks(1), dim3(CW_THREADS), 0, (hipStream_t)stream>>>(a);
         else if (a.T * a.n_q * D * (int64_t)sizeof(t) < CW_STREAM_BYTES)
@@ -394,7 +395,7 @@ int launch_cache_read(const CacheReadArgs& args, void* stream) {
     return by_type(a.dtype, a.cache, [&](auto t, auto d, auto f) {
         KernelTimer kt_("cache_read", stream);
         constexpr int D = decltype(d)::value, F = decltype(f)::value;
-        const dim3 blocks((unsigned)((rows + CW_ROWS * CR_U - 1) / (CW_ROWS * CR_U)));
+        const dim3 blocks = grid_of((rows + CW_ROWS * CR_U - 1) / (CW_ROWS * CR_U));
         if (rows * D * (int64_t)sizeof(t) >= CR_STREAM_BYTES)
             cache_read_kernel<decltype(t), D, F, true><<<blocks, dim3(CW_THREADS), 0, (hipStream_t)stream>>>(a);
         else

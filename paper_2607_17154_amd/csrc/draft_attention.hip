@@ -47,6 +47,7 @@
 #include <type_traits>
 
 #include "common.hpp"
+#include "grid.hpp"
 #include "kv_codes.hpp"
 
 namespace ordermoe {
@@ -653,7 +654,7 @@ __global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // the row blocks of one piece and head on one XCD, where its codes are in L2
-    const int idx = blockIdx.x, jx = idx >> 3;
+    const int idx = (int)block_number(), jx = idx >> 3;
     const int unit = (jx / rb_n) * 8 + (idx & 7), rb = jx % rb_n;
     const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
     if (unit >= items * n_kv) return;
@@ -667,7 +668,7 @@ __global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const 
         if (lane < a.B) mine = sequence(a, lane);
         // (the same in every lane, and in scalar registers from here on: addresses and branches below rest on it)
         piece = __builtin_amdgcn_readfirstlane(piece_tokens(a, rb_n, RT, ROUND, mine, lane));
-        s = find_item(a, piece, item, lane, blockIdx.x == 0 && wave == 0, mine, b, j);
+        s = find_item(a, piece, item, lane, idx == 0 && wave == 0, mine, b, j);
     }
     b = __builtin_amdgcn_readfirstlane(b);
     j = __builtin_amdgcn_readfirstlane(j);
@@ -697,12 +698,13 @@ __global__ void __launch_bounds__(256) draft_join_kernel(const DraftArgs a, int 
     constexpr int R = 16 / S, U = 4;                             // rows; pieces whose reads are in flight
     __shared__ __attribute__((aligned(16))) float s_x[16][D + 4];
     __shared__ float s_m[16], s_l[16];
-    const int b = blockIdx.x / rows_n;
+    const int idx = (int)block_number(), b = idx / rows_n;
+    if (b >= a.B) return;
     const int pieces = a.plan[2 * b + 1];
     if (pieces <= 1) return;
     const SeqInfo s = sequence(a, b);
     const int slot = threadIdx.x >> 4, z = slot % S, rows = s.n * a.n_q;
-    const int r = (blockIdx.x - b * rows_n) * R + slot / S;
+    const int r = (idx - b * rows_n) * R + slot / S;
     const int item = a.plan[2 * b], n_kv = a.cache.n_kv, G = a.n_q / n_kv;
     const int i = r / a.n_q, h = r - i * a.n_q, kvh = h / G;
     const int64_t stride = (int64_t)n_kv * a.max_q * G;          // rows of a piece
@@ -780,7 +782,7 @@ int launch_rows(const DraftArgs& a, int rows, bool whole, hipStream_t st) {
     {
         KernelTimer kt_("draft_attention", st);
         draft_attention_kernel<BF, D, FMT, RT, NW>
-            <<<dim3((unsigned)(units * rb)), dim3(64 * NW), 0, st>>>(a, (int)items, rb, whole);
+            <<<grid_of(units * rb), dim3(64 * NW), 0, st>>>(a, (int)items, rb, whole);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return (int)e;
     }
@@ -790,7 +792,7 @@ int launch_rows(const DraftArgs& a, int rows, bool whole, hipStream_t st) {
     auto join = [&](auto sets) {
         constexpr int S = decltype(sets)::value;
         const int rows_n = (a.max_q * a.n_q + 16 / S - 1) / (16 / S);
-        draft_join_kernel<BF, D, S><<<dim3((unsigned)((int64_t)a.B * rows_n)), dim3(256), 0, st>>>(a, rows_n);
+        draft_join_kernel<BF, D, S><<<grid_of((int64_t)a.B * rows_n), dim3(256), 0, st>>>(a, rows_n);
     };
     if (all <= JOIN_16) join(std::integral_constant<int, 16>{});
     else if (all <= JOIN_4) join(std::integral_constant<int, 4>{});
