@@ -617,7 +617,7 @@ def _rows(t, dtype, T: int, heads: int, D: int):
     if not t.is_cuda or t.dtype != dtype or t.shape != (T, heads, D):
         raise ValueError("expected a %s device tensor [%d, %d, %d]" % (dtype, T, heads, D))
     apart, per_head, per_element = t.stride()                # (once: a call on a tensor costs a tenth of a microsecond)
-    if T > 0 and (per_element != 1 or per_head != D):
+    if T > 0 and (per_element != 1 or (heads > 1 and per_head != D)):
         raise ValueError("the heads of a token must lie side by side")
     return t.data_ptr(), (apart if T > 1 else heads * D)
 
