@@ -609,6 +609,7 @@ def make_heads(dtype: int, n_q: int, head_dim: int, q_norm=None, k_norm=None, co
               k_norm=_dev(k_norm, _torch_dtype(dtype), head_dim) or None,
               cos_sin=(_dev(cos_sin, torch.float32) or None) if rot else None)
     h._tensors = (q_norm, k_norm, cos_sin)
+    h._head_dim = head_dim
     return h
 
 
@@ -627,6 +628,8 @@ def ordermoe_cache_write(cache: Cache, heads: Heads, q, k, v, pos, slots, q_out,
     rows), pos int32 [T] (None without rotation), slots int64 [T], q_out [T, n_q, D]."""
     import torch
     T, D, dt = q.shape[0], cache.head_dim, _torch_dtype(heads.dtype)
+    if getattr(heads, "_head_dim", D) != D:                  # (the norm weights end there)
+        raise ValueError("heads of %d, the cache of %d" % (heads._head_dim, D))
     (qp, qs), (kp, ks), (vp, vs) = _rows(q, dt, T, heads.n_q, D), _rows(k, dt, T, cache.n_kv, D), _rows(v, dt, T, cache.n_kv, D)
     _check(lib().ordermoe_cache_write(ctypes.byref(cache), ctypes.byref(heads), qp, qs, kp, ks, vp, vs, T,
                                       _dev(pos, torch.int32, T), _dev(slots, torch.int64, T),
