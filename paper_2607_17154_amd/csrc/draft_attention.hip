@@ -208,7 +208,7 @@ __device__ inline Pages tile_pages(const DraftArgs& a, const int32_t* table, int
     return r;
 }
 
-// NTL: past the caches, where no other workgroup reads the codes
+// NTL: past the caches (see launch_rows)
 template <bool NTL>
 __device__ inline u32x4 load_codes(const uint8_t* p) {
     if constexpr (NTL) return __builtin_nontemporal_load((const u32x4*)p);
@@ -507,9 +507,9 @@ struct Shared {
     float m[NW][RT * 16], l[NW][RT * 16];
 };
 
-// rows row0 .. row0 + 16 RT - 1 (of `rows`) of key/value head kvh over tokens [t_lo, t_hi) of a sequence.  ALONE: no
-// other workgroup reads the codes
-template <bool BF, int D, int FMT, int RT, int NW, bool ALONE>
+// rows row0 .. row0 + 16 RT - 1 (of `rows`) of key/value head kvh over tokens [t_lo, t_hi) of a sequence.  NTL: see
+// load_codes, FINE: see attend_tile
+template <bool BF, int D, int FMT, int RT, int NW, bool FINE, bool NTL>
 __device__ inline __attribute__((always_inline)) void attend_rows(const DraftArgs& a, const SeqInfo& s, int item, int kvh, int row0,
                                                                   int rows, int pieces, int t_lo, int t_hi, const int32_t* table,
                                                                   char* s_mem, float (*s_m)[RT * 16], float (*s_l)[RT * 16]) {
@@ -565,16 +565,16 @@ __device__ inline __attribute__((always_inline)) void attend_rows(const DraftArg
     char* const stage = s_mem + wave * STAGE<D>;
     int p = t_lo + wave * DA_TILE;
     Pages pg = tile_pages(a, table, p, t_hi);
-    load_tile<D, ALONE>(a, pg, kvh, p, lane, t[0]);
+    load_tile<D, NTL>(a, pg, kvh, p, lane, t[0]);
     pg = tile_pages(a, table, p + ROUND, t_hi);
-    load_tile<D, ALONE>(a, pg, kvh, p + ROUND, lane, t[1]);
+    load_tile<D, NTL>(a, pg, kvh, p + ROUND, lane, t[1]);
     pg = tile_pages(a, table, p + 2 * ROUND, t_hi);
     auto step = [&](Tile<D>& u) __attribute__((always_inline)) {
         const bool ok[2] = {u.ok[0], u.ok[1]};
         stage_tile<D, FMT>(u, stage, lane, scale2, p + DA_TILE > s.ctx || !ok[0] || !ok[1]);
-        load_tile<D, ALONE>(a, pg, kvh, p + 2 * ROUND, lane, u);
+        load_tile<D, NTL>(a, pg, kvh, p + 2 * ROUND, lane, u);
         pg = tile_pages(a, table, p + 3 * ROUND, t_hi);
-        attend_tile<BF, D, FMT, RT, ALONE>(stage, ok, qv, word, p, s, lane, st);
+        attend_tile<BF, D, FMT, RT, FINE>(stage, ok, qv, word, p, s, lane, st);
         p += ROUND;
     };
     while (p < t_hi) {
@@ -647,7 +647,7 @@ __device__ inline __attribute__((always_inline)) void attend_rows(const DraftArg
     }
 }
 
-template <bool BF, int D, int FMT, int RT, int NW>
+template <bool BF, int D, int FMT, int RT, int NW, bool NTL>
 __global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const DraftArgs a, int items, int rb_n, int whole) {
     constexpr int ROUND = NW * DA_TILE;
     __shared__ Shared<D, RT, NW> sh;
@@ -683,12 +683,12 @@ __global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const 
     if constexpr (RT > 1) {
         // a last block of up to 16 rows, or a sequence of no more (ragged trees of 33 44 -> 41 us, of 64 325 -> 312)
         if (rows - row0 <= 16) {
-            attend_rows<BF, D, FMT, 1, NW, false>(a, s, item, kvh, row0, rows, pieces, t_lo, t_hi, table, sh.mem,
+            attend_rows<BF, D, FMT, 1, NW, false, false>(a, s, item, kvh, row0, rows, pieces, t_lo, t_hi, table, sh.mem,
                                                   (float (*)[16])sh.m, (float (*)[16])sh.l);
             return;
         }
     }
-    attend_rows<BF, D, FMT, RT, NW, RT == 1>(a, s, item, kvh, row0, rows, pieces, t_lo, t_hi, table, sh.mem, sh.m, sh.l);
+    attend_rows<BF, D, FMT, RT, NW, RT == 1, NTL>(a, s, item, kvh, row0, rows, pieces, t_lo, t_hi, table, sh.mem, sh.m, sh.l);
 }
 
 // 16 / S (token, head) rows of a sequence per workgroup, S sets of 16 lanes a row: set z
@@ -781,8 +781,18 @@ int launch_rows(const DraftArgs& a, int rows, bool whole, hipStream_t st) {
     const int64_t units = (items * a.cache.n_kv + 7) / 8 * 8;
     {
         KernelTimer kt_("draft_attention", st);
-        draft_attention_kernel<BF, D, FMT, RT, NW>
-            <<<grid_of(units * rb), dim3(64 * NW), 0, st>>>(a, (int)items, rb, whole);
+        auto attend = [&](auto ntl) {
+            draft_attention_kernel<BF, D, FMT, RT, NW, decltype(ntl)::value>
+                <<<grid_of(units * rb), dim3(64 * NW), 0, st>>>(a, (int)items, rb, whole);
+        };
+        // Codes are read past the caches unless several row blocks share them: with two row tiles, and with heads of 256
+        // (four sequences, trees of 16 and 64: 4000 tokens 48.3 -> 43.6 us and 89.7 -> 81.7, 30000 204 -> 194 and 419 -> 400).
+        // Not in fp32, whose blocks wait for the matrix unit (the same with heads of 128: 58.4, 58.7; 144, 142; 328, 330; 869, 869).
+        if constexpr (BF && D == 256)
+            if (rb > 1) attend(std::false_type{});
+            else attend(std::true_type{});
+        else
+            attend(std::bool_constant<RT == 1>{});
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return (int)e;
     }
