@@ -647,7 +647,7 @@ __global__ void __launch_bounds__(FW_THREADS) few_layer_kernel(const FewArgs a, 
         const int tile = item % tiles, sp = item / tiles;
         const int d0 = 64 * tile;
         const int lo = (int)((int64_t)total * sp / pieces), hi = (int)((int64_t)total * (sp + 1) / pieces);
-        const int ns = (hi - lo - wave + FW_WAVES - 1) / FW_WAVES;               // steps lo + wave, lo + wave + 4, ...
+        const int ns = (hi - lo - wave + FW_WAVES - 1) / FW_WAVES;               // steps lo + wave, lo + wave + 8, ...
         struct Pos { int q, s, left; };                      // group (of those in use), step in it, steps left
         auto norm = [&](Pos& p) {
             while (p.left > 0) {
