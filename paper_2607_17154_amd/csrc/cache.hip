@@ -291,8 +291,9 @@ __global__ void __launch_bounds__(CW_THREADS) cache_write_kernel(const CacheWrit
 
 // CR_U rows per 16 lanes, their reads in flight together; a store covers 256
 // neighbouring bytes of a row (lane: 16 bytes of every 256).  Outputs that outgrow the
-// caches are stored past them: 60001 rows as fp32 118 us (5.3 TB/s; 126 otherwise),
-// 16001 as bf16 38 (44).
+// caches are stored past them.  8 heads of 128, both outputs together, stored through and past:
+// bf16 48 MiB 13.7 us and 13.9, 64 MiB 22.5 and 17.7, 128 MiB 42.5 and 33.3; fp32 48 MiB 11.7 and
+// 11.1, 64 MiB 15.8 and 14.1, 128 MiB 37.1 and 26.8.
 constexpr int CR_U = 4;
 constexpr int64_t CR_STREAM_BYTES = (int64_t)64 << 20;
 template <typename T, int D, int FMT, bool NTS>
@@ -330,8 +331,7 @@ __global__ void __launch_bounds__(CW_THREADS) cache_read_kernel(const CacheReadA
         if (row0 + CW_ROWS * u >= rows) break;
         const bool is_v = r[u] >= nh;
         T* o = (T*)(is_v ? a.v_out : a.k_out) + ((int64_t)i[u] * nh + (is_v ? r[u] - nh : r[u])) * D + c * N;
-#pragma unroll
-        for (int k = 0; k < C; ++k) {
+        auto chunk = [&](int k) {
             float x[N];
 #pragma unroll
             for (int j = 0; j < N / 4; ++j) {
@@ -343,6 +343,13 @@ __global__ void __launch_bounds__(CW_THREADS) cache_read_kernel(const CacheReadA
 #pragma unroll
             for (int j = 0; j < N; ++j) x[j] = there[u] ? x[j] : 0.f;
             if (on) store_f32<T, N, NTS>(o + 16 * N * k, x);
+        };
+        // (a loop of one chunk would lose the hint that its store goes past the caches: the compiler moves the store out of it)
+        if constexpr (C == 1) {
+            chunk(0);
+        } else {
+#pragma unroll
+            for (int k = 0; k < C; ++k) chunk(k);
         }
     }
 }
