@@ -567,7 +567,8 @@ int ordermoe_cache_read(const ordermoe_cache* C, int32_t dtype, const int64_t* s
  * that was never written spoils the outputs of the tokens that see it, and no others.
  * bf16: q times the codes with fp32 sums, statistics in fp32, the weights
  * exp(s - max) * v_scale rounded to bf16 for the product with the codes of V (in
- * two parts, 16 bits together, for head_dim 256 or max_q * n_q / n_kv <= 16 rows),
+ * two parts, 16 bits together, for head_dim 256 and, of a sequence's n_b * n_q / n_kv
+ * rows for a key/value head, for up to 16 left over from whole blocks of 32),
  * fp32 sums, rounded once.  fp32: fp32 throughout.
  *   q        dev [T][n_q][head_dim] of storage `dtype`, 16-byte aligned (as out)
  *   q_start  dev [B + 1] int32, not decreasing, within [0, T]

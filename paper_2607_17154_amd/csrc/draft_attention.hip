@@ -681,9 +681,11 @@ __global__ void __launch_bounds__(64 * NW, OCC<D>) draft_attention_kernel(const 
     const int t_lo = j * piece, t_hi = s.len - t_lo < piece ? s.len : t_lo + piece;
     const int32_t* table = a.page_table + (int64_t)b * a.max_pages;
     if constexpr (RT > 1) {
-        // a last block of up to 16 rows, or a sequence of no more (ragged trees of 33 44 -> 41 us, of 64 325 -> 312)
+        // A last block of up to 16 rows, or a sequence of no more (ragged trees of 33 44 -> 41 us, of 64 325 -> 312).  FINE,
+        // as with one row tile: a token's bits do not go with how many its neighbours in the batch have drafted
+        // (trees of 33 40.0 -> 40.7 us, of 64 312 -> 317).
         if (rows - row0 <= 16) {
-            attend_rows<BF, D, FMT, 1, NW, false, false>(a, s, item, kvh, row0, rows, pieces, t_lo, t_hi, table, sh.mem,
+            attend_rows<BF, D, FMT, 1, NW, true, false>(a, s, item, kvh, row0, rows, pieces, t_lo, t_hi, table, sh.mem,
                                                   (float (*)[16])sh.m, (float (*)[16])sh.l);
             return;
         }
