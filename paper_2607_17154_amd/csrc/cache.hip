@@ -255,8 +255,11 @@ __device__ inline void write_head_row(const CacheWriteArgs& a, uint32_t t, int h
 // U rows per 16 lanes, all read before the first is worked on: one row a lane leaves
 // too few bytes on their way for a prompt's rows (16001 tokens of 16 + 16 + 16 heads of 128: one
 // row 94 us, four 90, before other steps made it 79); a step's are too few to share four by
-// four.  NTS: rows are read, and queries stored, past the caches (the same rows 79 us, so 74; 16001
-// tokens of 32 query heads and one key head 71, 65; 8000 of 32 and 8 heads 51, 46.5).
+// four.  NTS: rows are read, and queries stored in 16 bytes a lane, past the caches (the same rows
+// 79 us, so 74).  At the switch of 32 MiB of queries through and past, heads of 128: bf16 32 + 8 heads
+// 26.8 us and 26.0, 16 + 16 50.3 and 46.5, 32 + 1 20.0 and 19.6, fp32 21.6 and 23.0, 39.1 and 37.7,
+// 16.4 and 19.7; at 48 MiB bf16 40.8 and 37.0, 69.8 and 65.3, 32.9 and 28.0, fp32 33.4 and 32.5, 53.6
+// and 52.7, 27.7 and 26.3.
 template <typename T, int D, int FMT, int U, bool NTS>
 __global__ void __launch_bounds__(CW_THREADS) cache_write_kernel(const CacheWriteArgs a) {
     constexpr int N = D / 16;

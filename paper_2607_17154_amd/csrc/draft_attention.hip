@@ -29,17 +29,22 @@
 // straight from memory, 64 single tokens took 149 us for 119).
 // Keys' scales multiply the scores, values' scales the weights, so codes enter the
 // matrix unit as they are (8-bit codes are exact in bf16).  In bf16 the weights are
-// rounded to bf16 for the second product, as its operands are; with one row tile what the
-// rounding leaves out goes through it as well (one token over 777 cached: error 0.0028 of
-// the output's size without, 0.0017 with, which is the output's own rounding; 64 single
-// tokens 100 -> 101 us).  Sums stay in fp32.
+// rounded to bf16 for the second product, as its operands are; for blocks of up to 16 rows
+// and heads of 256 what the rounding leaves out goes through it as well (one token over 777
+// cached: error 0.0028 of the output's size without, 0.0017 with, which is the output's own
+// rounding; 64 single tokens 100 -> 101 us; for all rows trees of 64 would take 361 us for 317
+// and trees of 33 42.4 for 40.7, error 0.0024 as it is).  Sums stay in fp32.
 // fp32 runs the same tile with v_mfma_f32_16x16x4_f32.
 //
 // Bound: one query row block, the codes: 64 sequences of 200-8000 tokens, 32 query and 8
 // key/value heads of 128, 101 us with the join, 5.5 TB/s.  64 drafted tokens (16 rows
 // of 16 a head), the vector instructions of a tile (some 230 a wave next to 40 matrix
-// instructions): 4 sequences of 30000-100000 tokens 312 us, 570 TFLOP/s.  One sequence of 778
-// tokens 10.6 us: a launch, and a chain of five dependent reads.
+// instructions, hardly at the same time): 4 sequences of 30000-100000 tokens 317 us, 560
+// TFLOP/s.  Trees of 33 over 1-5000 tokens, eight sequences of 16 heads, 40.7 us: by the
+// workgroups' clocks 2.6 us of plan, 12 (3 to 21) of tiles, 1 to 4 of sums; those that do not
+// start with the first 512 start at 18 to 20 and the last ends at 35; then the join.  One
+// sequence of 778 tokens 10.5 us: by the same clocks 1 to the first read, 6.5 for up to four
+// tiles a wave one after the other, 2 for the waves' sums.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

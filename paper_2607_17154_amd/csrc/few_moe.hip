@@ -25,10 +25,17 @@
 // v_mfma_f32_16x16x4_f32), the weights its rows, read in whole cache lines and turned
 // into the operand's lane order through LDS.
 // Bound: the weights in use, read once; below some 100 MB of them the latency of router,
-// token stage and hand-over (about 5 + 5 + 3 us) and of the weight stream's start.  d 4096,
-// f 1536, bf16, both kernels: 16 tokens with 24 experts in use (906 MB) 167 us, 5.4 TB/s; 1
-// token with 2 (75 MB) 36.5 us: 2.6 router, 2.4 logits, 5.3 token stage, 16 the gate/up weights,
-// 4 to 8 the down weights.  route_select and local_moe_forward in turn: 180 and 50 us.
+// token stage and hand-over and of the weight stream's start.  d 4096, f 1536, bf16, both
+// kernels: 16 tokens with 24 experts in use (906 MB) 170 us, 5.3 TB/s; 1 token with 2 (75 MB)
+// 36.7 us.  The layer kernel's workgroups by their clocks, us from their start (the router's
+// kernel takes 2.6 before):
+//                                  logits  token stage  activations  all done  outputs  end
+//   1 token                          2.7       5.2        1 to 18       26      4.7-7     35
+//   16 tokens                        4.3       7.9       66 to 103     113      35-47    161
+//   5, f 1408, two shared experts    2.5       4.5       10 to 20       27      3.7-7     37
+//   8, fp32, d 512, f 1024           2.6       2.6        1 to 8        14      4.8-6     20
+// route_select and local_moe_forward in turn on the same card: 184 and 51 us (16 tokens, 1),
+// 57 for 36.9 and 45 for 24 (the last two).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
