@@ -584,7 +584,9 @@ int ordermoe_cache_read(const ordermoe_cache* C, int32_t dtype, const int64_t* s
  *            on every run); in use until the stream passes the call
  * 1 <= max_q <= ORDERMOE_MAX_DRAFT (an upper bound of n_b), 0 <= B <= 65535,
  * max_pages >= 1, max_pages * page_size <= 2^30, n_q <= 1024, scale finite.  The lengths are
- * read on the device; the call does not synchronise. */
+ * read on the device; the call does not synchronise.  (Where tables hold more than 1024 tokens
+ * every workgroup reads the lengths of all sequences: past about a thousand of them several
+ * calls take less time than one.) */
 size_t ordermoe_draft_attention_workspace_size(const ordermoe_cache* C, int32_t dtype, int32_t n_q, int32_t B,
                                                int32_t max_q);
 int ordermoe_draft_attention(const ordermoe_cache* C, int32_t dtype, int32_t n_q, const void* q, int64_t T, int32_t B,
