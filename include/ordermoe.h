@@ -603,7 +603,8 @@ int ordermoe_draft_attention(const ordermoe_cache* C, int32_t dtype, int32_t n_q
  *   - bf16 y: the activation times the row's gate weight is rounded to bf16 before
  *     the down projection, whose products over all of a token's rows are summed in
  *     fp32 and rounded once (instead of once per row and once more).
- * L and W must agree in dtype, d and E; 0 <= T <= ORDERMOE_MAX_FEW.  ws: dev, of the size
+ * L and W must agree in dtype, d and E; E*d elements must span fewer than 2^31 bytes;
+ * 0 <= T <= ORDERMOE_MAX_FEW.  ws: dev, of the size
  * below, in use until the stream passes the call; needs no initial contents. */
 #define ORDERMOE_MAX_FEW 16
 size_t ordermoe_few_workspace_size(const ordermoe_layer* L, const ordermoe_experts* W, int64_t T);

@@ -395,6 +395,9 @@ static int check_few(const ordermoe_layer* L, const ordermoe_experts* W, int64_t
         return fail(ORDERMOE_EINVAL, "few_moe_layer: layer and experts must agree in dtype, d and E");
     if (!operands_fit_31_bits(W, ORDERMOE_MAX_FEW))
         return fail(ORDERMOE_EINVAL, "few_moe_layer: 2*f*d and 2*n_shared*f*d elements must each span fewer than 2^31 bytes");
+    // (the router's weights are read through a buffer resource too)
+    if ((int64_t)W->E * W->d * (W->dtype == ORDERMOE_BF16 ? 2 : 4) > ((int64_t)1 << 31) - 1)
+        return fail(ORDERMOE_EINVAL, "few_moe_layer: E*d elements must span fewer than 2^31 bytes");
     return ORDERMOE_OK;
 }
 
