@@ -22,6 +22,10 @@
  *   ordermoe_cache_write, ordermoe_cache_read, ordermoe_draft_attention
  *                               the attention half of a decode step, over a
  *                               quantised paged cache
+ *   ordermoe_latent_write, ordermoe_latent_attention, ordermoe_latent_expand,
+ *   ordermoe_latent_evict       the same over a cache of one latent vector a
+ *                               token, and that cache cut to a budget
+ *   ordermoe_prompt_attention   attention of whole prompts
  *
  * Conventions
  *   - Every entry point returns ORDERMOE_OK (0) or a negative status code and
@@ -611,6 +615,150 @@ size_t ordermoe_few_workspace_size(const ordermoe_layer* L, const ordermoe_exper
 int ordermoe_few_moe_layer(const ordermoe_layer* L, const ordermoe_experts* W, const void* x, int64_t T,
                            const uint8_t* loc_in, const float* qhat_in, int32_t server,
                            const ordermoe_route_out* out, void* y, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Attention with keys and values from one latent vector a token.
+ *
+ * Token p is cached as one row of rank + rotary_dim elements, [c_p | r_p], that
+ * every head shares: head h has the key [W_k,h c_p | r_p] and the value W_v,h c_p,
+ * with W_k,h, W_v,h of head_dim x rank.  Since q . W_k,h c = (W_k,h^T q) . c, a few
+ * queries attend to the rows as they are (absorbed: ordermoe_latent_write takes the
+ * queries through W_k, ordermoe_latent_attention the sums through W_v); a prompt's
+ * many queries to keys and values made once (expanded: ordermoe_latent_expand, then
+ * ordermoe_prompt_attention).
+ */
+typedef struct {
+    int32_t dtype;          /* storage of the rows, and of everything that meets them */
+    int32_t rank;           /* 128, 256 or 512 */
+    int32_t rotary_dim;     /* 32 or 64 */
+    int32_t page_size;      /* slots of a page: a power of two from 16 to 1024 */
+    int64_t n_pages;
+    void* rows;             /* dev [n_pages][page_size][rank + rotary_dim], 16-byte aligned */
+} ordermoe_latent_cache;
+
+typedef struct {
+    int32_t n_q;            /* heads, 1 to 128 */
+    int32_t head_dim;       /* 64 or 128 */
+    int32_t interleaved;    /* 1: elements 2i and 2i + 1 of the rotary part turn together; 0: i and i + rotary_dim / 2 */
+    int64_t max_pos;        /* rows of cos_sin */
+    float eps;              /* of the norm, finite and >= 0 */
+    const void* norm;       /* dev [rank] weights of the latent vector's norm, or NULL: no norm (all pointers 16-byte aligned) */
+    const float* cos_sin;   /* dev [max_pos][rotary_dim], as in ordermoe_heads, or NULL: nothing is turned */
+    const void* w_k;        /* dev [n_q][head_dim][rank] */
+    const void* w_v;        /* dev [n_q][head_dim][rank] */
+} ordermoe_latent_heads;
+
+/* Rows of T new tokens into the cache, and their queries, in one pass; in fp32:
+ *   c = x / sqrt(mean(x^2) + eps) * norm over kv's first rank elements (x where norm is NULL)
+ *   (a, b) -> (a cos - b sin, b cos + a sin)  for the pairs of kv's last rotary_dim elements and of
+ *                                             every query head's
+ * each rounded once to the storage type.
+ *   q       dev: head h of token t starts at t * q_stride + h * (head_dim + rotary_dim) elements; or
+ *           NULL: rows only.  16-byte aligned, strides multiples of 16 bytes and at least a token's
+ *           elements (as kv)
+ *   kv      dev: token t at t * kv_stride, rank + rotary_dim elements
+ *   pos     dev [T] int32 (NULL if cos_sin is); a position outside [0, max_pos) makes the token's turned
+ *           elements NaN
+ *   slots   dev [T] int64, distinct; a token whose slot is outside the cache is not written (its queries are)
+ *   absorb  0: q_out dev [T][n_q][head_dim + rotary_dim], the turned queries
+ *           1: q_out dev [T][n_q][rank + rotary_dim], their first part through the key weights, q W_k,h
+ *           (bf16: exact products, fp32 sums), as ordermoe_latent_attention takes them
+ *   q_out may overlap no input.  T >= 0 with T * n_q < 2^31.  No workspace. */
+int ordermoe_latent_write(const ordermoe_latent_cache* C, const ordermoe_latent_heads* H, const void* q, int64_t q_stride,
+                          const void* kv, int64_t kv_stride, int64_t T, const int32_t* pos, const int64_t* slots,
+                          int32_t absorb, void* q_out, void* stream);
+
+/* Attention of drafted tokens over the latent cache: ordermoe_draft_attention's
+ * sequences, page tables, trees and unseen positions, with
+ *   s_p = scale * q_h . [c_p | r_p],   out_h = W_v,h (sum_p exp(s_p) c_p / sum_p exp(s_p)),
+ *   lse = log sum_p exp(s_p)
+ * for the absorbed query q_h.  A token that sees nothing gets out = 0 and lse =
+ * -infinity.  bf16: exact products and fp32 sums, the weights rounded to bf16 for the second
+ * product where a sequence may have over LATENT_FINE_ROWS rows (n_b * n_q; in two parts, 16 bits
+ * together, where not), its sums in two parts for the third, rounded once at the end.  fp32: fp32
+ * throughout.
+ *   q, q_start, ctx_len, page_table, tree, max_q, max_pages as there; q dev [T][n_q][rank + rotary_dim]
+ *   out      dev [T][n_q][head_dim]; lse dev [T][n_q] fp32, or NULL
+ *   mass     dev [B][mass_stride] fp32: the attention weight that each of the sequence's positions has
+ *            got so far; or NULL, as zeros
+ *   mass_out dev [B][mass_stride] fp32, or NULL: none of this.  With w the softmax weights that position p
+ *            gets, summed over the sequence's tokens (its first max_q) and heads:
+ *              p < ctx_len:                 decay * mass[b][p] + w
+ *              ctx_len <= p < ctx_len + n_b:  w
+ *            entries past these, or past mass_stride, are left as they are.  May be mass itself.
+ *   ws       dev, of the size below (weighs: 1 where mass_out will be given), in use until the stream
+ *            passes the call.  With weighs it holds the scores, 4 B max_q n_q max_pages page_size bytes of it.
+ * Limits as there, but n_q <= 128; 0 <= T * n_q < 2^31; decay finite. */
+#define ORDERMOE_LATENT_FINE_ROWS 64
+size_t ordermoe_latent_attention_workspace_size(const ordermoe_latent_cache* C, const ordermoe_latent_heads* H, int32_t B,
+                                                int32_t max_q, int32_t max_pages, int32_t weighs);
+int ordermoe_latent_attention(const ordermoe_latent_cache* C, const ordermoe_latent_heads* H, const void* q, int64_t T,
+                              int32_t B, int32_t max_q, const int32_t* q_start, const int32_t* ctx_len,
+                              const int32_t* page_table, int32_t max_pages, const uint64_t* tree, float scale, void* out,
+                              float* lse, const float* mass, float* mass_out, int64_t mass_stride, float decay, void* ws,
+                              size_t ws_bytes, void* stream);
+
+/* Rows of the latent cache as the keys and values of every head, row i from
+ * slots[i] (dev int64; any order, repeats allowed; zeros for a slot outside the cache):
+ *   k_out dev [n][n_q][head_dim] = W_k,h c,  v_out dev [n][n_q][head_dim] = W_v,h c  (bf16: exact
+ *   products, fp32 sums, rounded once),  r_out dev [n][rotary_dim] = r
+ * all 16-byte aligned, of the cache's storage type.  n >= 0 with n * n_q < 2^31.  No workspace. */
+int ordermoe_latent_expand(const ordermoe_latent_cache* C, const ordermoe_latent_heads* H, const int64_t* slots, int64_t n,
+                           void* k_out, void* r_out, void* v_out, void* stream);
+
+/* Causal attention of prompts over keys and values in rows.  Sequence b holds
+ * query tokens [q_start[b], q_start[b + 1]), n_b of them, and positions
+ * [kv_start[b], kv_start[b + 1]) of k and v, L_b of them; its queries are its last n_b
+ * positions (the positions before are a context): token i sees position p if
+ * p <= L_b - n_b + i.  Query head h reads key/value head g = h / (n_q / n_kv), and
+ *   s_p = scale * (q_h . [k_p,g | r_p]),  out_h = sum_p exp(s_p) v_p,g / sum_p exp(s_p),  lse = log sum_p exp(s_p).
+ * A token that sees nothing (L_b < n_b) gets out = 0 and lse = -infinity.  bf16: exact
+ * products, fp32 sums and statistics, the weights rounded to bf16 for the second product, rounded once
+ * at the end.  fp32: fp32 throughout.
+ *   head_dim   64 or 128;  rotary_dim 0, 32 or 64
+ *   q          dev [T][n_q][head_dim + rotary_dim] of storage `dtype`, 16-byte aligned (as all of that type)
+ *   k, v       dev [L][n_kv][head_dim] (ordermoe_cache_read's or ordermoe_latent_expand's);  a position in
+ *              no sequence, or seen by no token, has no effect, whatever it holds
+ *   r          dev [L][rotary_dim], a part of the key that all heads share; NULL if rotary_dim = 0
+ *   q_start, kv_start  dev [B + 1] int32, not decreasing, within [0, T] and [0, L]
+ *   out        dev [T][n_q][head_dim]; lse dev [T][n_q] fp32, or NULL.  Rows of tokens in no sequence are
+ *              not written.
+ *   ws         dev, of the size below: partial results of rows whose positions are split over workgroups
+ *              (joined in a fixed order); in use until the stream passes the call
+ * 1 <= n_kv, n_q <= 1024 a multiple of n_kv, 0 <= B <= 65535, 0 <= T, L < 2^31 with T * n_q < 2^31,
+ * scale finite. */
+size_t ordermoe_prompt_attention_workspace_size(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t head_dim,
+                                                int32_t rotary_dim, int64_t T, int32_t B);
+int ordermoe_prompt_attention(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t rotary_dim, const void* q,
+                              int64_t T, const void* k, const void* r, const void* v, int64_t L, int32_t B,
+                              const int32_t* q_start, const int32_t* kv_start, float scale, void* out, float* lse, void* ws,
+                              size_t ws_bytes, void* stream);
+
+/* Sequences of the latent cache cut to `keep` cached tokens, those that got the
+ * most weight.  Sequence b has ctx_len[b] of them, in places 0 .. ctx_len - 1 of its page table.  Up
+ * to keep of them: all stay.  Else those stay whose pos (the position that the token in this place
+ * was written at) is below `first` or is one of the sequence's last `recent`, pos >= seq_len[b] - recent;
+ * then those of largest mass (ties: the lower place; a mass that is NaN counts as the smallest), keep in
+ * all.  Kept tokens in places from keep on move, in order, into the places below it whose tokens
+ * went, in order: attention does not go by places.
+ *   ctx_len   dev [B] int32, >= 0;  seq_len dev [B] int32, tokens that the sequence has had in all
+ *   page_table dev [B][max_pages] int32, as in ordermoe_latent_attention; a page that rows move in or out of
+ *             belongs to this sequence alone.  A row from a page outside the cache becomes zeros, one to such a
+ *             page is dropped; places past the table do not exist.
+ *   mass      dev [B][stride] fp32;  pos dev [B][stride] int32.  Places from stride on do not exist.
+ *   kept      dev [B][keep] int32, out: the place that each place's token was in before, -1 from the new
+ *             length on
+ *   len_out   dev [B] int32, out: the new lengths
+ *   mass_out, pos_out dev [B][stride], out: entry i from kept[i]; entries from the new length on are left as
+ *             they are.  len_out, mass_out and pos_out may be ctx_len, mass and pos themselves.
+ *   ws        dev, of the size below, in use until the stream passes the call
+ * keep >= 1, first, recent >= 0 with first + recent <= keep, stride >= 1, 0 <= B <= 65535,
+ * B * stride, B * keep < 2^40, max_pages as in ordermoe_latent_attention. */
+size_t ordermoe_latent_evict_workspace_size(const ordermoe_latent_cache* C, int32_t B, int32_t max_pages, int32_t keep);
+int ordermoe_latent_evict(const ordermoe_latent_cache* C, int32_t B, const int32_t* ctx_len, const int32_t* seq_len,
+                          const int32_t* page_table, int32_t max_pages, int32_t keep, int32_t first, int32_t recent,
+                          const float* mass, const int32_t* pos, int64_t stride, int32_t* kept, int32_t* len_out,
+                          float* mass_out, int32_t* pos_out, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * Kernel timing (measurement support, off by default).

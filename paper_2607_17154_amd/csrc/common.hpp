@@ -246,6 +246,108 @@ struct DraftArgs {
 int64_t draft_items(int n_q, int n_kv, int head_dim, int dtype, int B, int max_q);
 int launch_draft_attention(const DraftArgs& a, void* stream);
 
+// latent cache: rows, projections (latent.hip), attention (latent_attention.hip), eviction (evict.hip)
+struct LatentArgs {
+    int dtype, rank, rot, page_shift;
+    int64_t n_pages;
+    char* rows;
+};
+struct LatentWriteArgs {
+    LatentArgs cache;
+    int n_q, head_dim, interleaved, absorb;
+    float eps;
+    int64_t max_pos;
+    const void* norm;
+    const float* cos_sin;
+    const void* w_k;
+    const void* q;
+    const void* kv;
+    int64_t q_stride, kv_stride, T;
+    const int32_t* pos;
+    const int64_t* slots;
+    void* q_out;
+};
+int launch_latent_write(const LatentWriteArgs& a, void* stream);
+struct LatentExpandArgs {
+    LatentArgs cache;
+    int n_q, head_dim;
+    const void* w_k;
+    const void* w_v;
+    const int64_t* slots;
+    int64_t n;
+    void* k_out;
+    void* r_out;
+    void* v_out;
+};
+int launch_latent_expand(const LatentExpandArgs& a, void* stream);
+struct LatentAttentionArgs {
+    LatentArgs cache;
+    int n_q, head_dim, B, max_q, max_pages;
+    int64_t T;
+    const void* q;
+    const void* w_v;
+    const int32_t* q_start;
+    const int32_t* ctx_len;
+    const int32_t* page_table;
+    const uint64_t* tree;
+    float scale, decay;
+    void* out;
+    float* lse;
+    const float* mass;
+    float* mass_out;
+    int64_t mass_stride;
+    // workspace
+    int32_t* plan;         // [B][2] first work item of each sequence, its pieces
+    float* part_ml;        // [items][max_q n_q][2] maximum and sum of each piece's rows
+    float* part_o;         // [items][max_q n_q][rank] its sums
+    float* stat;           // [B][max_q n_q][2] maximum of each row, and 1 / its sum (with mass_out)
+    float* score;          // [B][max_q n_q][max_pages page_size] scores in units of log 2 (with mass_out)
+};
+// work items (sequence, piece of its cache) that a batch has at most
+int64_t latent_items(int dtype, int n_q, int B, int max_q);
+int launch_latent_attention(const LatentAttentionArgs& a, void* stream);
+struct EvictArgs {
+    LatentArgs cache;
+    int B, max_pages, keep, first, recent;
+    const int32_t* ctx_len;
+    const int32_t* seq_len;
+    const int32_t* page_table;
+    const float* mass;
+    const int32_t* pos;
+    int64_t stride;
+    int32_t* kept;
+    int32_t* len_out;
+    float* mass_out;
+    int32_t* pos_out;
+    // workspace
+    int32_t* moves;        // [B] rows to move
+    int32_t* holes;        // [B][holes_max] their new places
+    int32_t* fills;        // [B][holes_max] their old ones
+    int64_t holes_max;
+};
+int launch_latent_evict(const EvictArgs& a, void* stream);
+
+// attention of prompts (prompt_attention.hip)
+struct PromptArgs {
+    int dtype, n_q, n_kv, head_dim, rot, B;
+    const void* q;
+    const void* k;
+    const void* r;
+    const void* v;
+    int64_t T, L;
+    const int32_t* q_start;
+    const int32_t* kv_start;
+    float scale;
+    void* out;
+    float* lse;
+    // workspace
+    float* part_ml;        // [items][rows of a block][2] maximum and sum of each piece's rows
+    float* part_o;         // [items][rows of a block][head_dim] its sums
+};
+// partial results (row block, piece of its positions) that a batch has at most: rows of them
+int64_t prompt_part_rows(int dtype, int n_q, int n_kv, int head_dim, int rot, int64_t T, int B);
+int launch_prompt_attention(const PromptArgs& a, void* stream);
+
 int launch_pack_gate_up(int dtype, int n, int f, int d, const void* g, const void* u, void* out,
                         void* stream);
 int launch_pack_down(int dtype, int n, int d, int f, const void* w, void* out, void* stream);

@@ -1,0 +1,355 @@
+// Rows of the latent cache: written (norm, rotation), and expanded to the keys and
+// values of every head; queries taken through the key weights.
+//
+//   latent_write_kernel   three kinds of workgroups: 64 tokens x 64 ranks of one head's
+//                         absorbed queries, qa[t][r] = sum_d q[t][d] W_k[d][r]; four tokens'
+//                         rows, a wave each; 256 pieces of the queries that are turned or copied
+//   latent_expand_kernel  Y = C W^T for the rows C of the cache at the given slots and all of
+//                         W_k and W_v: tiles of TN tokens x TN weight rows
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <type_traits>
+
+#include "common.hpp"
+#include "grid.hpp"
+#include "mfma.hpp"
+
+namespace ordermoe {
+namespace {
+
+template <bool BF>
+using Elem = std::conditional_t<BF, __bf16, float>;
+
+// 8 elements as fp32, and back
+template <bool BF>
+__device__ inline void load8(const Elem<BF>* p, float* x) {
+    if constexpr (BF) {
+        const bf16x8 v = *(const bf16x8*)p;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
+    } else {
+        const f32x4 a = ((const f32x4*)p)[0], b = ((const f32x4*)p)[1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
+    }
+}
+template <bool BF>
+__device__ inline void store8(Elem<BF>* p, const float* x) {
+    if constexpr (BF) {
+        *(u32x4*)p = u32x4{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7])};
+    } else {
+        ((f32x4*)p)[0] = f32x4{x[0], x[1], x[2], x[3]};
+        ((f32x4*)p)[1] = f32x4{x[4], x[5], x[6], x[7]};
+    }
+}
+
+// 16 elements of a rotary part turned: unit u of rot / 16, pairs 8u .. 8u + 7
+template <bool BF>
+__device__ inline void turn16(const LatentWriteArgs& a, int64_t t, const Elem<BF>* from, Elem<BF>* to, int u) {
+    const int half = a.cache.rot / 2;
+    const int at0 = a.interleaved ? 16 * u : 8 * u, at1 = a.interleaved ? 16 * u + 8 : half + 8 * u;
+    float x[16];
+    load8<BF>(from + at0, x);
+    load8<BF>(from + at1, x + 8);
+    if (a.cos_sin) {
+        const int64_t p = a.pos[t];
+        const bool in = p >= 0 && p < a.max_pos;
+        const float* cs = a.cos_sin + (in ? p : 0) * a.cache.rot + 8 * u;
+        float co[8], si[8];
+        load8<false>(cs, co);
+        load8<false>(cs + half, si);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float c = in ? co[i] : __builtin_nanf(""), s = in ? si[i] : __builtin_nanf("");
+            const float lo = a.interleaved ? x[2 * i] : x[i], hi = a.interleaved ? x[2 * i + 1] : x[8 + i];
+            co[i] = lo * c - hi * s;
+            si[i] = hi * c + lo * s;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (a.interleaved) {
+                x[2 * i] = co[i];
+                x[2 * i + 1] = si[i];
+            } else {
+                x[i] = co[i];
+                x[8 + i] = si[i];
+            }
+        }
+    }
+    store8<BF>(to + at0, x);
+    store8<BF>(to + at1, x + 8);
+}
+
+// One token's cache row, by one wave: 8 elements of the latent vector a lane.
+template <bool BF>
+__device__ inline void write_row(const LatentWriteArgs& a, int64_t t, int lane) {
+    const int R = a.cache.rank, rot = a.cache.rot, row = R + rot;
+    const int64_t slot = a.slots[t];
+    if (slot < 0 || slot >= a.cache.n_pages << a.cache.page_shift) return;
+    const Elem<BF>* from = (const Elem<BF>*)a.kv + t * a.kv_stride;
+    Elem<BF>* to = (Elem<BF>*)a.cache.rows + slot * row;
+    const bool in = lane < R / 8;
+    float x[8] = {};
+    if (in) load8<BF>(from + 8 * lane, x);
+    if (a.norm) {
+        float w[8] = {};
+        if (in) load8<BF>((const Elem<BF>*)a.norm + 8 * lane, w);
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += x[i] * x[i];
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o);
+        const float r = 1.0f / sqrtf(s / (float)R + a.eps);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = x[i] * r * w[i];
+    }
+    if (in) store8<BF>(to + 8 * lane, x);
+    if (lane < rot / 16) turn16<BF>(a, t, from + R, to + R, lane);
+}
+
+constexpr int LW_TOK = 64, LW_COLS = 64;             // tokens and ranks of an absorb workgroup
+
+// qa[t][r] for 64 tokens and 64 ranks of one head: the matrix unit's rows are ranks, its
+// columns tokens; a wave takes 16 ranks and every token.
+template <bool BF, int D>
+__device__ inline void absorb_tile(const LatentWriteArgs& a, int64_t t0, int h, int r0, char* mem) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    const int R = a.cache.rank, wide = R + a.cache.rot;
+    const int tiles = (int)std::min<int64_t>(LW_TOK / 16, (a.T - t0 + 15) / 16);
+    f32x4 acc[LW_TOK / 16] = {};
+    if constexpr (BF) {
+        // W_k[h]'s 64 ranks in LDS, D rows of 128 bytes; row d's pieces of 32 bytes are swapped by d % 4, so that the
+        // four rows of a turned read lie on distinct banks
+        const __bf16* w = (const __bf16*)a.w_k + (int64_t)h * D * R + r0;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            const int piece = wave * (D / 32) + i, d = piece * 8 + (lane >> 3), ch = (lane & 7) ^ ((d & 3) << 1);
+            load_lds16(w + (int64_t)d * R + ch * 8, mem + piece * 1024);
+        }
+        u32x4 q[LW_TOK / 16][D / 32];
+#pragma unroll
+        for (int m = 0; m < LW_TOK / 16; ++m) {
+            const int64_t t = t0 + 16 * m + c;
+#pragma unroll
+            for (int s = 0; s < D / 32; ++s) {
+                q[m][s] = u32x4{0u, 0u, 0u, 0u};
+                if (m < tiles && t < a.T)
+                    q[m][s] = *(const u32x4*)((const __bf16*)a.q + t * a.q_stride + h * (D + a.cache.rot) + 32 * s + 8 * g);
+            }
+        }
+        __syncthreads();
+        const int i = c >> 2, j = c & 3;
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+            u32x2 half[2];
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const int d = 32 * s + 8 * g + 4 * p + i;
+                half[p] = read_turned(mem + d * 128 + (((2 * wave + (j >> 1)) ^ ((d & 3) << 1)) * 16) + (j & 1) * 8);
+            }
+            const u32x4 wf = {half[0][0], half[0][1], half[1][0], half[1][1]};
+#pragma unroll
+            for (int m = 0; m < LW_TOK / 16; ++m) acc[m] = mma16<true>(wf, q[m][s], acc[m]);
+        }
+    } else {
+        const float* w = (const float*)a.w_k + (int64_t)h * D * R + r0 + 16 * wave + c;
+        for (int s = 0; s < D / 16; ++s) {
+            u32x4 wf;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) wf[e] = __float_as_uint(w[(int64_t)(16 * s + 4 * g + e) * R]);
+#pragma unroll
+            for (int m = 0; m < LW_TOK / 16; ++m) {
+                const int64_t t = t0 + 16 * m + c;
+                u32x4 q = {0u, 0u, 0u, 0u};
+                if (m < tiles && t < a.T)
+                    q = *(const u32x4*)((const float*)a.q + t * a.q_stride + h * (D + a.cache.rot) + 16 * s + 4 * g);
+                acc[m] = mma16<false>(wf, q, acc[m]);
+            }
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < LW_TOK / 16; ++m) {
+        const int64_t t = t0 + 16 * m + c;
+        if (m < tiles && t < a.T)
+            store4<BF>(a.q_out, (t * a.n_q + h) * wide + r0 + 16 * wave + 4 * g, acc[m][0], acc[m][1], acc[m][2], acc[m][3]);
+    }
+}
+
+// blocks: absorb tiles, then rows, then pieces of the queries
+template <bool BF, int D, int ROT>
+__global__ void __launch_bounds__(256) latent_write_kernel(const LatentWriteArgs a, int64_t n_absorb, int64_t n_rows, int64_t n_units) {
+    __shared__ __attribute__((aligned(16))) char mem[BF ? D * LW_COLS * 2 : 16];
+    int64_t blk = block_number();
+    if (blk < n_absorb) {
+        const int slices = a.cache.rank / LW_COLS;
+        const int64_t th = blk / slices;
+        const int r0 = (int)(blk - th * slices) * LW_COLS, h = (int)(th % a.n_q);
+        absorb_tile<BF, D>(a, th / a.n_q * LW_TOK, h, r0, mem);
+        return;
+    }
+    blk -= n_absorb;
+    if (blk < n_rows) {
+        const int64_t t = blk * 4 + (threadIdx.x >> 6);
+        if (t < a.T) write_row<BF>(a, t, threadIdx.x & 63);
+        return;
+    }
+    blk -= n_rows;
+    // per head row: D / 8 pieces to copy (not where they are absorbed), then ROT / 16 to turn
+    const int copies = a.absorb ? 0 : D / 8, per = copies + ROT / 16;
+    const int64_t u = blk * 256 + threadIdx.x;
+    if (u >= n_units) return;
+    const int64_t row = (uint32_t)u == u ? (uint32_t)u / (uint32_t)per : u / per;
+    const int k = (int)(u - row * per);
+    const int64_t t = (uint32_t)row / (uint32_t)a.n_q;
+    const int h = (int)(row - t * a.n_q);
+    const Elem<BF>* from = (const Elem<BF>*)a.q + t * a.q_stride + h * (D + ROT);
+    Elem<BF>* to = (Elem<BF>*)a.q_out + row * ((a.absorb ? a.cache.rank : D) + ROT);
+    if (k < copies) {
+        float x[8];
+        load8<BF>(from + 8 * k, x);
+        store8<BF>(to + 8 * k, x);
+    } else {
+        turn16<BF>(a, t, from + D, to + (a.absorb ? a.cache.rank : D), k - copies);
+    }
+}
+
+template <bool BF, int D, int ROT>
+int launch_write(const LatentWriteArgs& a, hipStream_t st) {
+    const int64_t absorb = a.q && a.absorb ? (a.T + LW_TOK - 1) / LW_TOK * a.n_q * (a.cache.rank / LW_COLS) : 0;
+    const int64_t rows = (a.T + 3) / 4, units = a.q ? a.T * a.n_q * ((a.absorb ? 0 : D / 8) + ROT / 16) : 0;
+    KernelTimer kt_("latent_write", st);
+    latent_write_kernel<BF, D, ROT><<<grid_of(absorb + rows + (units + 255) / 256), dim3(256), 0, st>>>(a, absorb, rows, units);
+    return (int)hipGetLastError();
+}
+template <bool BF>
+int launch_write_dim(const LatentWriteArgs& a, hipStream_t st) {
+    if (a.head_dim == 64) return a.cache.rot == 32 ? launch_write<BF, 64, 32>(a, st) : launch_write<BF, 64, 64>(a, st);
+    return a.cache.rot == 32 ? launch_write<BF, 128, 32>(a, st) : launch_write<BF, 128, 64>(a, st);
+}
+
+// ------------------------------------------------------------------ expansion
+constexpr int LE_SLAB = 128;                         // bytes of a row staged at a time
+
+// A tile of TN tokens (the matrix unit's columns) x TN weight rows, 2 x 2 waves.  Both come in
+// slabs of 128 bytes a row through LDS, two buffers; chunk c of row r lies at c ^ (r % 8), so that the
+// 16-byte reads of eight rows lie on distinct banks.
+template <bool BF, int TN>
+__global__ void __launch_bounds__(256) latent_expand_kernel(const LatentExpandArgs a, int64_t tok_tiles, int row_tiles, int spread) {
+    constexpr int ES = BF ? 2 : 4, W = TN / 2, F = W / 16, LOADS = TN / 32;     // a wave's rows, its tiles, its pieces of a slab
+    __shared__ __attribute__((aligned(16))) char mem[2][2][TN * LE_SLAB];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, g = lane >> 4, wm = wave >> 1, wn = wave & 1;
+    int64_t id = block_number(), tt;
+    int rt;
+    if (spread) {
+        // eight token tiles after one another on each XCD, which then go through all weights together
+        const int64_t x = id & 7, l = id >> 3, grp = l / (8 * row_tiles);
+        const int in = (int)(l - grp * (8 * row_tiles));
+        rt = in >> 3;
+        tt = (grp * 8 + (in & 7)) * 8 + x;
+    } else {
+        tt = id / row_tiles;
+        rt = (int)(id - tt * row_tiles);
+    }
+    if (tt >= tok_tiles) return;
+    const int R = a.cache.rank, wide = R + a.cache.rot, half = a.n_q * a.head_dim, r0 = rt * TN;
+    const int64_t n0 = tt * TN, slots = a.cache.n_pages << a.cache.page_shift;
+    const char* from[2][LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int r = (wave * LOADS + i) * 8 + (lane >> 3), ch = (lane & 7) ^ (r & 7);
+        int64_t s = n0 + r < a.n ? a.slots[n0 + r] : 0;
+        if (s < 0 || s >= slots) s = 0;
+        from[0][i] = a.cache.rows + s * wide * ES + ch * 16;
+        const int wr = r0 + r < 2 * half ? r0 + r : 0;
+        from[1][i] = (wr < half ? (const char*)a.w_k + (int64_t)wr * R * ES : (const char*)a.w_v + (int64_t)(wr - half) * R * ES) + ch * 16;
+    }
+    auto issue = [&](int buf, int s) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+#pragma unroll
+            for (int o = 0; o < 2; ++o) load_lds16(from[o][i] + s * LE_SLAB, &mem[buf][o][(wave * LOADS + i) * 1024]);
+    };
+    f32x4 acc[F][F] = {};                            // [weight tile][token tile]
+    const int slabs = R * ES / LE_SLAB;
+    issue(0, 0);
+    for (int s = 0; s < slabs; ++s) {
+        __syncthreads();                             // slab s has arrived, and slab s - 1 has been read
+        if (s + 1 < slabs) issue((s + 1) & 1, s + 1);
+        const char* tok = mem[s & 1][0];
+        const char* wei = mem[s & 1][1];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            u32x4 t[F], w[F];
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                const int rt_ = wn * W + 16 * i + c, rw = wm * W + 16 * i + c;
+                t[i] = *(const u32x4*)(tok + rt_ * LE_SLAB + (((4 * k + g) ^ (rt_ & 7)) * 16));
+                w[i] = *(const u32x4*)(wei + rw * LE_SLAB + (((4 * k + g) ^ (rw & 7)) * 16));
+            }
+#pragma unroll
+            for (int i = 0; i < F; ++i)
+#pragma unroll
+                for (int j = 0; j < F; ++j) acc[i][j] = mma16<BF>(w[i], t[j], acc[i][j]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < F; ++j) {
+        const int64_t n = n0 + wn * W + 16 * j + c;
+        if (n >= a.n) continue;
+        const int64_t s = a.slots[n];
+        const bool in = s >= 0 && s < slots;
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            const int wr = r0 + wm * W + 16 * i + 4 * g;
+            if (wr >= 2 * half) continue;
+            const f32x4 v = in ? acc[i][j] : f32x4{0.f, 0.f, 0.f, 0.f};
+            if (wr < half) store4<BF>(a.k_out, n * half + wr, v[0], v[1], v[2], v[3]);
+            else store4<BF>(a.v_out, n * half + wr - half, v[0], v[1], v[2], v[3]);
+        }
+    }
+    if (rt == 0) {
+        const int per = a.cache.rot * ES / 16;       // 16-byte pieces of the rotary part
+        for (int u = tid; u < TN * per; u += 256) {
+            const int r = u / per, k = u - r * per;
+            if (n0 + r >= a.n) break;
+            const int64_t s = a.slots[n0 + r];
+            u32x4 v = {0u, 0u, 0u, 0u};
+            if (s >= 0 && s < slots) v = *(const u32x4*)(a.cache.rows + (s * wide + R) * ES + 16 * k);
+            *(u32x4*)((char*)a.r_out + (n0 + r) * a.cache.rot * ES + 16 * k) = v;
+        }
+    }
+}
+
+template <bool BF, int TN>
+int launch_expand(const LatentExpandArgs& a, hipStream_t st) {
+    const int64_t tt = (a.n + TN - 1) / TN;
+    const int rt = (2 * a.n_q * a.head_dim + TN - 1) / TN;
+    const bool spread = tt >= 64;
+    const int64_t blocks = spread ? (tt + 63) / 64 * 64 * rt : tt * rt;
+    KernelTimer kt_("latent_expand", st);
+    latent_expand_kernel<BF, TN><<<grid_of(blocks), dim3(256), 0, st>>>(a, tt, rt, spread);
+    return (int)hipGetLastError();
+}
+
+}  // namespace
+
+int launch_latent_write(const LatentWriteArgs& a, void* stream) {
+    if (a.T == 0) return 0;
+    return a.cache.dtype == ORDERMOE_BF16 ? launch_write_dim<true>(a, (hipStream_t)stream)
+                                          : launch_write_dim<false>(a, (hipStream_t)stream);
+}
+
+int launch_latent_expand(const LatentExpandArgs& a, void* stream) {
+    if (a.n == 0) return 0;
+    // tiles of 128 where they give every CU one
+    const bool big = (a.n + 127) / 128 * (2 * a.n_q * a.head_dim / 128) >= 256;
+    if (a.cache.dtype == ORDERMOE_BF16)
+        return big ? launch_expand<true, 128>(a, (hipStream_t)stream) : launch_expand<true, 64>(a, (hipStream_t)stream);
+    return big ? launch_expand<false, 128>(a, (hipStream_t)stream) : launch_expand<false, 64>(a, (hipStream_t)stream);
+}
+
+}  // namespace ordermoe

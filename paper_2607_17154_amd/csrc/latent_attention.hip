@@ -1,0 +1,687 @@
+// Attention of drafted tokens over the latent cache: every head's absorbed query on the
+// same rows [c_p | r_p], of which the first part is the value too.
+//
+//   latent_attention_kernel  one workgroup per (work item, block of 16 RW query rows).  A work
+//                            item is a piece of one sequence's cache.  RW waves that take 16 rows
+//                            each share a tile of its tokens in LDS; the tiles go round the groups of
+//                            such waves, every group with a running maximum, sum and output of its
+//                            own, joined in LDS at the end -> partial sums (memory)
+//   latent_out_kernel        the pieces' sums added in order, relative to their largest maximum,
+//                            divided, and taken through W_v: 16 tokens of one head
+//   latent_mass_kernel       the weight that each position got, from the scores that the first
+//                            kernel wrote and the rows' final maximum and sum
+// The query rows of a sequence are its n_b tokens times the heads: row = token * n_q + head.
+//
+// A tile (bf16; c = lane % 16, g = lane / 16):
+//   S^T = K Q^T   v_mfma_f32_16x16x32_bf16; rows: 16 tokens, columns: 16 query rows.  Maximum and sum belong
+//                 to a column, that is to a lane.
+//   O^T = C^T P^T v_mfma_f32_16x16x32_bf16, or 16x16x16 where a tile has 16 tokens; rows: 16 elements of the latent
+//                 vector, columns: 16 query rows.  S^T leaves lane (c, g) the weights of query row c for tokens
+//                 4g .. 4g + 3 of each 16: the inner indexes of its P^T operand, when C^T's lanes hold the
+//                 same tokens, which turned reads of the rows in LDS give them.  So the weights never
+//                 leave their registers.
+// fp32 runs the same tile with v_mfma_f32_16x16x4_f32.  Rows go straight from memory into LDS, a group's next tile
+// while it attends to one.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <type_traits>
+
+#include "common.hpp"
+#include "grid.hpp"
+#include "mfma.hpp"
+
+namespace ordermoe {
+namespace {
+
+constexpr int LA_TARGET = 512;                       // workgroups that a large batch is split into
+constexpr int LA_MIN_PIECE = 64;                     // tokens
+constexpr float LA_LAG = 8.0f;                       // see attend_tile
+
+// waves that share a tile, for sequences of up to `rows` query rows: 16 rows each
+__host__ __device__ inline int row_waves(int dtype, int rows) {
+    return dtype != ORDERMOE_BF16 || rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8;
+}
+__host__ __device__ inline int row_blocks(int rows, int rw) { return (rows + 16 * rw - 1) / (16 * rw); }
+
+struct Seq {
+    int first, n, ctx, len;     // first token, drafted tokens, cached tokens before them, positions
+};
+__device__ inline Seq sequence(const LatentAttentionArgs& a, int b) {
+    Seq s;
+    const int T = (int)a.T, cap = a.max_pages << a.cache.page_shift;
+    int s0 = a.q_start[b], s1 = a.q_start[b + 1], ctx = a.ctx_len[b];
+    s0 = s0 < 0 ? 0 : s0 > T ? T : s0;
+    s1 = s1 < s0 ? s0 : s1 > T ? T : s1;
+    ctx = ctx < 0 ? 0 : ctx > cap ? cap : ctx;
+    s.first = s0;
+    s.n = s1 - s0 < a.max_q ? s1 - s0 : a.max_q;
+    s.ctx = ctx;
+    s.len = s.n < cap - ctx ? ctx + s.n : cap;
+    return s;
+}
+__device__ inline Seq uniform(const Seq& s, int l) {
+    return Seq{__builtin_amdgcn_readlane(s.first, l), __builtin_amdgcn_readlane(s.n, l), __builtin_amdgcn_readlane(s.ctx, l),
+               __builtin_amdgcn_readlane(s.len, l)};
+}
+
+// The tokens of a piece, by one wave: as many, a multiple of a round of the waves, as give about LA_TARGET
+// workgroups in all, but at least total * rb_n / (2 LA_TARGET): that bounds the pieces by 2 LA_TARGET / rb_n + B.
+__device__ inline int piece_tokens(const LatentAttentionArgs& a, int rb_n, int rw, int round, const Seq& mine, int lane) {
+    int64_t total = 0, blocks = 0;
+    for (int b = lane; b < a.B; b += 64) {
+        const Seq s = b < 64 ? mine : sequence(a, b);
+        total += s.n > 0 ? s.len : 0;
+        blocks += s.n > 0 ? (int64_t)s.len * row_blocks(s.n * a.n_q, rw) : 0;
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+        total += __shfl_xor(total, o);
+        blocks += __shfl_xor(blocks, o);
+    }
+    int64_t p = (blocks + LA_TARGET - 1) / LA_TARGET;
+    const int64_t least = (total * rb_n + 2 * LA_TARGET - 1) / (2 * LA_TARGET);
+    p = p < least ? least : p;
+    p = p < LA_MIN_PIECE ? LA_MIN_PIECE : p;
+    p = (p + round - 1) / round * round;
+    return (int)(p > (1 << 30) ? 1 << 30 : p);
+}
+__device__ inline int pieces_of(const Seq& s, int piece) {
+    // a sequence without positions still writes its rows (zeros)
+    return s.n <= 0 ? 0 : s.len <= piece ? 1 : (s.len + piece - 1) / piece;
+}
+// sequence (of number b, < 0: none) and piece j of a work item, by one wave.
+// write_plan: every sequence's first item and pieces to a.plan.
+__device__ inline Seq find_item(const LatentAttentionArgs& a, int piece, int item, int lane, bool write_plan, const Seq& mine, int& b,
+                                int& j) {
+    Seq found = {0, 0, 0, 0};
+    int base = 0;
+    b = -1;
+    j = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        Seq s = mine;
+        if (b0 > 0 && b0 + lane < a.B) s = sequence(a, b0 + lane);
+        const int cnt = b0 + lane < a.B ? pieces_of(s, piece) : 0;
+        int inc = cnt;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(inc, o);
+            if (lane >= o) inc += v;
+        }
+        const int first = base + inc - cnt;
+        if (write_plan && b0 + lane < a.B) {
+            a.plan[2 * (b0 + lane)] = first;
+            a.plan[2 * (b0 + lane) + 1] = cnt;
+        }
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(item >= first && item < first + cnt);
+        if (hit) {
+            const int l = __builtin_ctzll(hit);
+            b = b0 + l;
+            j = item - __builtin_amdgcn_readlane(first, l);
+            found = uniform(s, l);
+            if (!write_plan) break;
+        }
+        base += __builtin_amdgcn_readlane(inc, 63);
+    }
+    return found;
+}
+
+// Rows of RB bytes in LDS, side by side, as 16-byte chunks: chunk ch of row r lies at ch ^ swap(r), so that the reads of
+// one chunk of 16 rows lie on distinct banks.
+template <int RB>
+__device__ inline int swap_row(int r) {
+    constexpr int CH = RB / 16;
+    return CH % 16 == 0 ? r & 15 : CH % 8 == 0 ? (r >> 1) & 7 : (r >> 2) & 3;
+}
+
+template <bool BF, int R, int ROT, int RW>
+struct Config {
+    static constexpr int ES = BF ? 2 : 4, RB = (R + ROT) * ES, CH = RB / 16;
+    static constexpr int NW = RW > 1 ? 8 : BF ? 4 : 2, GROUPS = NW / RW;     // waves, groups of them
+    static constexpr int TILE = BF ? (RW > 1 ? 8 * RW : 16) : 16;            // tokens of a group's tile
+    static constexpr int SUB = TILE < 32 ? 16 : 32;                          // tokens that are attended to at a time
+    static constexpr int STAGE = TILE * RB, PIECES = STAGE / 1024;           // bytes of a tile, wave loads of it
+    static constexpr int MINE = (PIECES + RW - 1) / RW;                      // of them a wave's, at most
+    static constexpr int KS = RB / 64;                                       // steps of the first product
+    static constexpr int LD = R + 4;                                         // floats of a row of sums in LDS
+    static_assert(STAGE % 1024 == 0 && GROUPS * 16 * LD * 4 <= GROUPS * 2 * STAGE, "whole pieces, the sums fit");
+};
+
+// page of the tile at t0 (16 tokens never cross a page), -1: none; uniform, through the scalar cache
+__device__ inline int tile_page(const LatentAttentionArgs& a, const int32_t* table, int t0, int len) {
+    const __attribute__((address_space(4))) int32_t* t = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)table;
+    return t0 < len ? t[t0 >> a.cache.page_shift] : -1;
+}
+
+template <int N>
+__device__ inline void wait_loads() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// of N tokens' rows, those that hold an infinity or a NaN, a bit each, by one wave
+template <bool BF, int RB, int N>
+__device__ inline uint32_t not_finite(const char* st, int lane) {
+    uint32_t m = 0;
+#pragma unroll 4
+    for (int i = 0; i < N * RB / 1024; ++i) {
+        const u32x4 x = *(const u32x4*)(st + (i * 64 + lane) * 16);
+        bool bad = false;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            bad |= BF ? (x[w] & 0x7F80u) == 0x7F80u || (x[w] & 0x7F800000u) == 0x7F800000u : (x[w] & 0x7F800000u) == 0x7F800000u;
+        if (bad) m |= 1u << ((i * 64 + lane) / (RB / 16));
+    }
+    if (!__builtin_amdgcn_ballot_w64(m != 0)) return 0;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) m |= __shfl_xor(m, o);
+    return m;
+}
+
+// The running state of a wave: lane (c, g) has row c's maximum (in units of log 2; a shared reference that may
+// lag behind the true one) and its own tokens' share of the sum; o[j] holds row c's elements 16 j + 4 g + i, i = 0 .. 3.
+template <int R>
+struct State {
+    float m, l;
+    f32x4 o[R / 16];
+};
+
+__device__ inline u32x2 only_finite(u32x2 v) {
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        if ((v[w] & 0x7F80u) == 0x7F80u) v[w] &= 0xFFFF0000u;
+        if ((v[w] & 0x7F800000u) == 0x7F800000u) v[w] &= 0xFFFFu;
+    }
+    return v;
+}
+
+// SUB tokens from t0 on, staged at st.  A maximum is taken over only when some score passes it by LA_LAG (a factor of
+// 256 in the weights, which fp32 sums and bf16 weights hold as well as 1): most tiles then need no exchange
+// between lanes and no rescaling of the outputs.  FINE: the second product takes what the rounding of the weights to
+// bf16 leaves out as well.
+template <bool BF, int R, int RB, int SUB, bool FINE, bool WEIGHS>
+__device__ inline __attribute__((always_inline)) void attend_tile(const char* st, const u32x4* q, const bool* ok, int t0, const Seq& s,
+                                                                  uint64_t word, float scale2, float* score, int lane,
+                                                                  State<R>& state) {
+    constexpr int NB = SUB / 16, KS = RB / 64;
+    const int c = lane & 15, g = lane >> 4;
+    const float ninf = -__builtin_inff();
+    f32x4 sc[NB] = {};
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+            sc[n] = mma16<BF>(*(const u32x4*)(st + (16 * n + c) * RB + (((4 * k + g) ^ swap_row<RB>(16 * n + c)) * 16)), q[k], sc[n]);
+    bool edge = t0 + SUB > s.ctx;
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        edge |= !ok[n];
+        sc[n] = sc[n] * scale2;
+    }
+    uint32_t bad = 0;
+    if (edge) {
+        bad = not_finite<BF, RB, SUB>(st, lane);
+        uint32_t seen = 0;
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int p = t0 + 16 * n + 4 * g + i, j = p - s.ctx;
+                const bool see = ok[n] && p < s.len && (j < 0 || ((word >> (j & 63)) & 1));
+                seen |= (uint32_t)see << (16 * n + 4 * g + i);
+                sc[n][i] = see ? sc[n][i] : ninf;
+            }
+        if (bad & seen) state.l = __builtin_nanf("");        // (what is no number is taken as 0 below)
+    }
+    if constexpr (WEIGHS) {
+        if (score) {
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+                if (t0 + 16 * n < s.len) *(f32x4*)(score + t0 + 16 * n + 4 * g) = sc[n];     // (a table holds whole 16s)
+        }
+    }
+    float top = ninf;
+#pragma unroll
+    for (int n = 0; n < NB; ++n) top = fmaxf(top, fmaxf(fmaxf(sc[n][0], sc[n][1]), fmaxf(sc[n][2], sc[n][3])));
+    if (__builtin_amdgcn_ballot_w64(top > state.m + LA_LAG)) {
+        float x = fmaxf(top, __shfl_xor(top, 16));
+        x = fmaxf(x, __shfl_xor(x, 32));
+        const float m = x > state.m + LA_LAG ? x : state.m;      // by the row alone, whatever the others do
+        const float al = state.m == m ? 1.0f : __builtin_amdgcn_exp2f(state.m - m);
+        state.m = m;
+        state.l *= al;
+#pragma unroll
+        for (int j = 0; j < R / 16; ++j) state.o[j] = state.o[j] * al;
+    }
+    // weights exp2(score - maximum), 0 where nothing has been seen yet
+    const float m = state.m == ninf ? 0.f : state.m;
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            sc[n][i] = __builtin_amdgcn_exp2f(sc[n][i] - m);
+            state.l += sc[n][i];
+        }
+    if constexpr (BF) {
+        u32x2 pf[NB], pl[NB];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            bf16x4 hi, lo;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                hi[i] = (__bf16)sc[n][i];
+                if constexpr (FINE) lo[i] = (__bf16)(sc[n][i] - (float)hi[i]);
+            }
+            pf[n] = __builtin_bit_cast(u32x2, hi);
+            if constexpr (FINE) pl[n] = __builtin_bit_cast(u32x2, lo);
+        }
+        const int row = 4 * g + (c >> 2), sub = c & 3;
+        const char* at = st + row * RB + (sub & 1) * 8;
+#pragma unroll
+        for (int j = 0; j < R / 16; ++j) {
+            u32x2 v[NB];
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                v[n] = read_turned(at + 16 * n * RB + (((2 * j + (sub >> 1)) ^ swap_row<RB>(16 * n + row)) * 16));
+                if (bad) v[n] = only_finite(v[n]);
+            }
+            if constexpr (NB == 1) {
+                const s16x4 vf = __builtin_bit_cast(s16x4, v[0]);
+                state.o[j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf, __builtin_bit_cast(s16x4, pf[0]), state.o[j], 0, 0, 0);
+                if constexpr (FINE)
+                    state.o[j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf, __builtin_bit_cast(s16x4, pl[0]), state.o[j], 0, 0, 0);
+            } else {
+                const u32x4 vf = {v[0][0], v[0][1], v[1][0], v[1][1]};
+                state.o[j] = mma16<true>(vf, u32x4{pf[0][0], pf[0][1], pf[1][0], pf[1][1]}, state.o[j]);
+                if constexpr (FINE) state.o[j] = mma16<true>(vf, u32x4{pl[0][0], pl[0][1], pl[1][0], pl[1][1]}, state.o[j]);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = 4 * g + i, sw = swap_row<RB>(row);
+            const char* at = st + row * RB + (c & 3) * 4;
+#pragma unroll
+            for (int j = 0; j < R / 16; ++j) {
+                float v = *(const float*)(at + (((4 * j + (c >> 2)) ^ sw) * 16));
+                if (bad) v = (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u ? 0.f : v;
+                state.o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, sc[0][i], state.o[j], 0, 0, 0);
+            }
+        }
+    }
+}
+
+template <bool BF, int R, int ROT, int RW, bool FINE, bool WEIGHS>
+__global__ void __launch_bounds__((64 * Config<BF, R, ROT, RW>::NW), (BF || R < 512 ? 2 : 1))
+latent_attention_kernel(const LatentAttentionArgs a, int items, int rb_n) {
+    using Cf = Config<BF, R, ROT, RW>;
+    constexpr int NW = Cf::NW, GROUPS = Cf::GROUPS, ROUND = GROUPS * Cf::TILE, NB = Cf::TILE / 16;
+    __shared__ __attribute__((aligned(16))) char s_mem[GROUPS * 2 * Cf::STAGE];
+    __shared__ float s_m[NW][16], s_l[NW][16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, g = lane >> 4, rw = wave % RW, grp = wave / RW;
+    // the row blocks of one piece on one XCD, where its rows are in L2
+    const int idx = (int)block_number(), jx = idx >> 3;
+    const int item = (jx / rb_n) * 8 + (idx & 7), rb = jx % rb_n;
+    if (item >= items) return;
+    Seq mine = {0, 0, 0, 0};
+    if (lane < a.B) mine = sequence(a, lane);
+    const int piece = __builtin_amdgcn_readfirstlane(piece_tokens(a, rb_n, RW, ROUND, mine, lane));
+    int b, j;
+    const Seq s = find_item(a, piece, item, lane, idx == 0 && wave == 0, mine, b, j);
+    if (b < 0) return;
+    const int rows = s.n * a.n_q, row0 = rb * 16 * RW, rows_max = a.max_q * a.n_q;
+    if (row0 >= rows) return;
+    const int t_lo = j * piece, t_hi = s.len - t_lo < piece ? s.len : t_lo + piece;
+    const int32_t* table = a.page_table + (int64_t)b * a.max_pages;
+    const float scale2 = a.scale * LOG2E;            // scores in units of log 2
+    const int row = row0 + 16 * rw + c;
+    const bool in = row < rows;                      // rows past the end are zeros and see nothing
+    const int i_tok = in ? row / a.n_q : 0;
+    const uint64_t word = !in ? 0ull : a.tree ? a.tree[s.first + i_tok] : ~0ull >> (63 - i_tok);
+    float* const score = WEIGHS && in ? a.score + ((int64_t)b * rows_max + row) * ((int64_t)a.max_pages << a.cache.page_shift) : nullptr;
+    u32x4 q[Cf::KS];
+    {
+        const char* from = (const char*)a.q + ((int64_t)s.first * a.n_q + (in ? row : 0)) * Cf::RB + 16 * g;
+#pragma unroll
+        for (int k = 0; k < Cf::KS; ++k) {
+            q[k] = u32x4{0u, 0u, 0u, 0u};
+            if (in) q[k] = *(const u32x4*)(from + 64 * k);
+        }
+    }
+    State<R> st;
+    st.m = -__builtin_inff();
+    st.l = 0.f;
+#pragma unroll
+    for (int e = 0; e < R / 16; ++e) st.o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    char* const stage = s_mem + grp * 2 * Cf::STAGE;
+    const int sh = a.cache.page_shift;
+    // a tile's pages, 16 tokens each
+    struct Pages { int p[NB]; };
+    auto pages = [&](int t0) __attribute__((always_inline)) {
+        Pages r;
+#pragma unroll
+        for (int n = 0; n < NB; ++n) r.p[n] = tile_page(a, table, t0 + 16 * n, t_hi);
+        return r;
+    };
+    struct Ok { bool b[NB]; };
+    auto issue = [&](const Pages& pg, int t0, char* to) __attribute__((always_inline)) {
+        Ok ok;
+        const char* from[NB];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            // tokens without a page read page 0
+            ok.b[n] = pg.p[n] >= 0 && pg.p[n] < a.cache.n_pages;
+            from[n] = a.cache.rows + (ok.b[n] ? ((int64_t)pg.p[n] << sh) + ((t0 + 16 * n) & ((1 << sh) - 1)) : 0) * Cf::RB;
+        }
+#pragma unroll
+        for (int i = 0; i < Cf::MINE; ++i) {
+            // piece i * RW + rw of the tile; its 16 tokens' page, uniform
+            const int piece_ = i * RW + rw;
+            if (Cf::PIECES % RW != 0 && piece_ >= Cf::PIECES) break;
+            const char* base = from[0];
+#pragma unroll
+            for (int n = 1; n < NB; ++n) base = piece_ >= n * (Cf::PIECES / NB) ? from[n] : base;
+            const int u = piece_ % (Cf::PIECES / NB) * 64 + lane, r = u / Cf::CH, ch = u - r * Cf::CH;
+            load_lds16(base + (uint32_t)(r * Cf::RB + (ch ^ swap_row<Cf::RB>(r)) * 16), to + piece_ * 1024);
+        }
+        return ok;
+    };
+    int p = t_lo + grp * Cf::TILE;
+    const int rounds = (t_hi - t_lo + ROUND - 1) / ROUND;
+    Ok ok = {}, next = {};
+    Pages pg = pages(p);
+    if (p < t_hi) ok = issue(pg, p, stage);
+    pg = pages(p + ROUND);
+    for (int k = 0, buf = 0; k < rounds; ++k, p += ROUND, buf ^= 1) {
+        if constexpr (RW > 1) __syncthreads();       // the tile has arrived, and the one before has been read
+        if (p + ROUND < t_hi) {
+            next = issue(pg, p + ROUND, stage + (buf ^ 1) * Cf::STAGE);
+            pg = pages(p + 2 * ROUND);
+            if constexpr (RW == 1) wait_loads<Cf::PIECES>();     // all but the next tile's
+        } else {
+            if constexpr (RW == 1) wait_loads<0>();
+        }
+        if (p < t_hi) {
+#pragma unroll
+            for (int n = 0; n < Cf::TILE / Cf::SUB; ++n)
+                attend_tile<BF, R, Cf::RB, Cf::SUB, FINE, WEIGHS>(stage + buf * Cf::STAGE + n * Cf::SUB * Cf::RB, q, ok.b + n * (Cf::SUB / 16),
+                                                                  p + n * Cf::SUB, s, word, scale2, score, lane, st);
+        }
+        ok = next;
+    }
+    // the groups' states joined, the rows of one of their waves at a time
+    float l = st.l;
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (g == 0) { s_m[wave][c] = st.m; s_l[wave][c] = l; }
+    __syncthreads();                                 // the staged rows become the place of the sums
+    float(*const s_o)[16][Cf::LD] = (float(*)[16][Cf::LD])s_mem;
+    constexpr int PER = NW * 4, PART = R / PER;      // threads a row, their elements
+    const int64_t prow = (int64_t)item * rows_max;
+    float m = s_m[rw][c];
+#pragma unroll
+    for (int w = 1; w < GROUPS; ++w) m = fmaxf(m, s_m[w * RW + rw][c]);
+    const float f = st.m == m ? 1.0f : __builtin_amdgcn_exp2f(st.m - m);
+#pragma unroll 1
+    for (int r = 0; r < RW; ++r) {
+        if (row0 + 16 * r >= rows) break;
+        if (r == rw) {
+#pragma unroll
+            for (int e = 0; e < R / 16; ++e) *(f32x4*)&s_o[grp][c][16 * e + 4 * g] = st.o[e] * f;
+        }
+        __syncthreads();
+        const int rt = tid / PER, rr = row0 + 16 * r + rt, u = tid % PER;
+        if (rr < rows) {
+            float* po = a.part_o + (prow + rr) * R;
+#pragma unroll
+            for (int e = 0; e < PART; e += 4) {
+                f32x4 v = *(const f32x4*)&s_o[0][rt][4 * u + PER * e];
+#pragma unroll
+                for (int w = 1; w < GROUPS; ++w) v += *(const f32x4*)&s_o[w][rt][4 * u + PER * e];
+                *(f32x4*)(po + 4 * u + PER * e) = v;
+            }
+            if (u == 0) {
+                float mm = s_m[r][rt], ll = 0.f;
+#pragma unroll
+                for (int w = 1; w < GROUPS; ++w) mm = fmaxf(mm, s_m[w * RW + r][rt]);
+#pragma unroll
+                for (int w = 0; w < GROUPS; ++w) {
+                    const float mw = s_m[w * RW + r][rt];
+                    ll += s_l[w * RW + r][rt] * (mw == mm ? 1.0f : __builtin_amdgcn_exp2f(mw - mm));
+                }
+                a.part_ml[2 * (prow + rr)] = mm;
+                a.part_ml[2 * (prow + rr) + 1] = ll;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// 16 tokens (of the batch) of one head, DS of the head's elements: the rows' pieces added in order, divided, and
+// out = o W_v^T.  The matrix unit's rows are elements, its columns tokens.  DS / 32 pairs of element tiles go round the
+// waves; where they are fewer than the waves, the waves share the inner index.
+template <bool BF, int R, int D, int DS>
+__global__ void __launch_bounds__(256) latent_out_kernel(const LatentAttentionArgs a, int slices) {
+    constexpr int ES = BF ? 2 : 4, PITCH = R * ES + 16, U = 4;       // bytes of a row in LDS; pieces whose reads are in flight
+    constexpr int PAIRS = DS / 32, SHARE = 4 / PAIRS, KS = R * ES / 64 / SHARE;
+    __shared__ __attribute__((aligned(16))) char s_o[BF ? 2 : 1][16 * PITCH];
+    __shared__ f32x4 s_acc[SHARE > 1 ? 4 : 1][2][64];
+    __shared__ int s_in[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t id = block_number(), rest = id / slices;
+    const int d0 = (int)(id - rest * slices) * DS, h = (int)(rest % a.n_q);
+    const int64_t tb = rest / a.n_q * 16;
+    if (tb >= a.T) return;
+    // the token's sequence: the number of sequences that end at or before it
+    const int slot = tid >> 4, u = tid & 15, t = (int)std::min<int64_t>(tb + slot, a.T);
+    int b = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 16) {
+        const bool past = b0 + u < a.B && a.q_start[b0 + u + 1] <= t;
+        const uint32_t m = (uint32_t)(__builtin_amdgcn_ballot_w64(past) >> (lane & 48)) & 0xFFFFu;
+        b += __builtin_popcount(m);
+    }
+    bool in = tb + slot < a.T && b < a.B;
+    Seq s = {0, 0, 0, 0};
+    if (in) s = sequence(a, b);
+    const int i = t - s.first;
+    in = in && i >= 0 && i < s.n;
+    const int row = i * a.n_q + h, rows_max = a.max_q * a.n_q;
+    if (u == 0) s_in[slot] = in;
+    const int pieces = in ? a.plan[2 * b + 1] : 0;
+    const int64_t at = in ? (int64_t)a.plan[2 * b] * rows_max + row : 0;
+    const f32x2* ml = (const f32x2*)a.part_ml;
+    float m = -__builtin_inff(), l = 0.f, x[R / 16] = {};
+    for (int p = 0; p < pieces; p += U) {
+        f32x2 q[U];
+        f32x4 v[U][R / 64];
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int64_t pr = at + (int64_t)(p + k < pieces ? p + k : p) * rows_max;
+            q[k] = ml[pr];
+#pragma unroll
+            for (int e = 0; e < R / 64; ++e) v[k][e] = *(const f32x4*)(a.part_o + pr * R + 4 * u + 64 * e);
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) top = fmaxf(top, q[k][0]);
+        const float al = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+        m = top;
+        l *= al;
+#pragma unroll
+        for (int e = 0; e < R / 16; ++e) x[e] *= al;
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (p + k >= pieces) break;
+            const float f = q[k][0] == m ? 1.0f : __builtin_amdgcn_exp2f(q[k][0] - m);
+            l += q[k][1] * f;
+#pragma unroll
+            for (int e = 0; e < R / 16; ++e) x[e] += v[k][e / 4][e % 4] * f;
+        }
+    }
+    const float r = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+    for (int e = 0; e < R / 64; ++e) {
+        float y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] = x[4 * e + k] * r;
+        char* o = &s_o[0][slot * PITCH + (4 * u + 64 * e) * ES];
+        if constexpr (BF) {
+            float z[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) z[k] = y[k] - (float)(__bf16)y[k];
+            *(u32x2*)o = u32x2{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3])};
+            *(u32x2*)&s_o[BF ? 1 : 0][slot * PITCH + (4 * u + 64 * e) * ES] = u32x2{bf16_pair(z[0], z[1]), bf16_pair(z[2], z[3])};
+        } else {
+            *(f32x4*)o = f32x4{y[0], y[1], y[2], y[3]};
+        }
+    }
+    if (in && u == 0 && d0 == 0) {
+        if (a.lse) a.lse[(int64_t)t * a.n_q + h] = l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * LN2;
+        if (a.mass_out) {
+            f32x2* stat = (f32x2*)a.stat + (int64_t)b * rows_max + row;
+            *stat = f32x2{m == -__builtin_inff() ? 0.f : m, r};
+        }
+    }
+    __syncthreads();
+    const int c = lane & 15, g = lane >> 4, pair = wave % PAIRS, share = wave / PAIRS;
+    f32x4 acc[2] = {};
+    const char* w = (const char*)a.w_v + ((int64_t)(h * D + d0 + 32 * pair + c) * R) * ES + (share * KS * 4 + g) * 16;
+    const char* o = &s_o[0][c * PITCH + (share * KS * 4 + g) * 16];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+        const u32x4 w0 = *(const u32x4*)(w + 64 * k), w1 = *(const u32x4*)(w + 16 * R * ES + 64 * k);
+        const u32x4 hi = *(const u32x4*)(o + 64 * k);
+        acc[0] = mma16<BF>(w0, hi, acc[0]);
+        acc[1] = mma16<BF>(w1, hi, acc[1]);
+        if constexpr (BF) {
+            const u32x4 lo = *(const u32x4*)(o + 16 * PITCH + 64 * k);
+            acc[0] = mma16<BF>(w0, lo, acc[0]);
+            acc[1] = mma16<BF>(w1, lo, acc[1]);
+        }
+    }
+    if constexpr (SHARE > 1) {
+        s_acc[wave][0][lane] = acc[0];
+        s_acc[wave][1][lane] = acc[1];
+        __syncthreads();
+        if (share != 0) return;
+#pragma unroll
+        for (int k = 1; k < SHARE; ++k) {
+            acc[0] += s_acc[pair + k * PAIRS][0][lane];
+            acc[1] += s_acc[pair + k * PAIRS][1][lane];
+        }
+    }
+    // (a token of no sequence, or past its sequence's first max_q, is not written)
+    if (!s_in[c]) return;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        store4<BF>(a.out, ((tb + c) * a.n_q + h) * D + d0 + 32 * pair + 16 * k + 4 * g, acc[k][0], acc[k][1], acc[k][2], acc[k][3]);
+}
+
+// 256 positions of a sequence: the weights of its rows, exp2(score - maximum) / sum, added up; the waves share the rows
+__global__ void __launch_bounds__(256) latent_mass_kernel(const LatentAttentionArgs a, int per_seq) {
+    __shared__ f32x4 s_w[4][64];
+    const int64_t id = block_number();
+    const int b = (int)(id / per_seq), p0 = (int)(id - (int64_t)b * per_seq) * 256;
+    if (b >= a.B) return;
+    const Seq s = sequence(a, b);
+    if (s.n <= 0 || p0 >= s.len) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p = p0 + 4 * lane;
+    const int rows = s.n * a.n_q, rows_max = a.max_q * a.n_q;
+    const int64_t cap = (int64_t)a.max_pages << a.cache.page_shift;
+    const f32x2* stat = (const f32x2*)a.stat + (int64_t)b * rows_max;
+    f32x4 w = {0.f, 0.f, 0.f, 0.f};
+    if (p < s.len) {
+        const float* score = a.score + (int64_t)b * rows_max * cap + p;
+#pragma unroll 4
+        for (int r = wave; r < rows; r += 4) {
+            const f32x4 x = *(const f32x4*)(score + r * cap);
+            const f32x2 q = stat[r];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] += x[k] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(x[k] - q[0]) * q[1];
+        }
+    }
+    s_w[wave][lane] = w;
+    __syncthreads();
+    if (wave != 0) return;
+    w = s_w[0][lane] + s_w[1][lane] + s_w[2][lane] + s_w[3][lane];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (p + k >= s.len || p + k >= a.mass_stride) break;
+        const int64_t at = b * a.mass_stride + p + k;
+        a.mass_out[at] = p + k < s.ctx && a.mass ? a.decay * a.mass[at] + w[k] : w[k];
+    }
+}
+
+template <bool BF, int R, int ROT, int RW, bool FINE>
+int launch_rows(const LatentAttentionArgs& a, hipStream_t st) {
+    const int rb = row_blocks(a.max_q * a.n_q, RW);
+    const int64_t cap = (int64_t)a.max_pages << a.cache.page_shift;
+    {
+        const int64_t items = std::min<int64_t>(latent_items(a.cache.dtype, a.n_q, a.B, a.max_q),
+                                                a.B * ((cap + LA_MIN_PIECE - 1) / LA_MIN_PIECE));
+        const dim3 grid = grid_of((items + 7) / 8 * 8 * rb), block((64 * Config<BF, R, ROT, RW>::NW));
+        KernelTimer kt_("latent_attention", st);
+        if (a.mass_out) latent_attention_kernel<BF, R, ROT, RW, FINE, true><<<grid, block, 0, st>>>(a, (int)items, rb);
+        else latent_attention_kernel<BF, R, ROT, RW, FINE, false><<<grid, block, 0, st>>>(a, (int)items, rb);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return (int)e;
+    }
+    {
+        KernelTimer kt_("latent_out", st);
+        const int64_t blocks = (a.T + 15) / 16 * a.n_q;
+        auto go = [&](auto d, auto ds) {
+            constexpr int D = decltype(d)::value, DS = decltype(ds)::value;
+            latent_out_kernel<BF, R, D, DS><<<grid_of(blocks * (D / DS)), dim3(256), 0, st>>>(a, D / DS);
+        };
+        using std::integral_constant;
+        const bool few = blocks < 512;
+        if (a.head_dim == 64) few ? go(integral_constant<int, 64>{}, integral_constant<int, 32>{})
+                                  : go(integral_constant<int, 64>{}, integral_constant<int, 64>{});
+        else few ? go(integral_constant<int, 128>{}, integral_constant<int, 32>{})
+                 : go(integral_constant<int, 128>{}, integral_constant<int, 128>{});
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return (int)e;
+    }
+    if (!a.mass_out) return 0;
+    const int per = (int)((cap + 255) / 256);
+    KernelTimer kt_("latent_mass", st);
+    latent_mass_kernel<<<grid_of((int64_t)a.B * per), dim3(256), 0, st>>>(a, per);
+    return (int)hipGetLastError();
+}
+template <bool BF, int R, int ROT>
+int launch_tiles(const LatentAttentionArgs& a, hipStream_t st) {
+    if constexpr (BF) {
+        static_assert(ORDERMOE_LATENT_FINE_ROWS == 64, "the waves that share a tile where the weights keep 16 bits");
+        switch (row_waves(ORDERMOE_BF16, a.max_q * a.n_q)) {
+            case 2: return launch_rows<BF, R, ROT, 2, true>(a, st);
+            case 4: return launch_rows<BF, R, ROT, 4, true>(a, st);
+            case 8: return launch_rows<BF, R, ROT, 8, false>(a, st);
+        }
+    }
+    return launch_rows<BF, R, ROT, 1, BF>(a, st);
+}
+template <bool BF, int R>
+int launch_rot(const LatentAttentionArgs& a, hipStream_t st) {
+    return a.cache.rot == 32 ? launch_tiles<BF, R, 32>(a, st) : launch_tiles<BF, R, 64>(a, st);
+}
+template <bool BF>
+int launch_rank(const LatentAttentionArgs& a, hipStream_t st) {
+    return a.cache.rank == 128 ? launch_rot<BF, 128>(a, st) : a.cache.rank == 256 ? launch_rot<BF, 256>(a, st) : launch_rot<BF, 512>(a, st);
+}
+
+}  // namespace
+
+int64_t latent_items(int dtype, int n_q, int B, int max_q) {
+    const int rows = max_q * n_q, rb = row_blocks(rows, row_waves(dtype, rows));
+    return (2 * LA_TARGET + rb - 1) / rb + B;
+}
+
+int launch_latent_attention(const LatentAttentionArgs& a, void* stream) {
+    if (a.B == 0 || a.T == 0) return 0;
+    return a.cache.dtype == ORDERMOE_BF16 ? launch_rank<true>(a, (hipStream_t)stream) : launch_rank<false>(a, (hipStream_t)stream);
+}
+
+}  // namespace ordermoe

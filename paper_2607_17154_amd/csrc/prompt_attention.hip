@@ -1,0 +1,352 @@
+// Causal attention of prompts over keys and values in rows.
+//
+//   prompt_attention_kernel  one workgroup per (128 query rows of a sequence, key/value
+//                            head): its four waves take 32 rows each and go through the
+//                            positions together, a tile at a time
+// The query rows of a key/value head are its n_b tokens times the n_q / n_kv query heads
+// that share it (row = token * (n_q / n_kv) + head).
+//
+// A tile (v_mfma_f32_32x32x16_bf16, c = lane % 32, h = lane / 32; fp32 the same with
+// v_mfma_f32_32x32x2_f32):
+//   S^T = K Q^T   rows: 32 positions, columns: 32 query rows.  Maximum and sum belong to a
+//                 column, that is to two lanes.
+//   O^T = V^T P^T rows: 32 elements of the head, columns: the query rows.  S^T leaves lane (c, h)
+//                 the weights of query row c for positions 8 j + 4 h .. + 3, j = 0 .. 3: in pairs of
+//                 j the 8 inner indexes of its P^T operand, when V^T's lanes hold the same positions,
+//                 which a turned read of V's rows in LDS gives them.  So the weights never leave their
+//                 registers.
+// K, the shared rotary part and V go straight from memory into LDS, two tiles on their way.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <type_traits>
+
+#include "common.hpp"
+#include "grid.hpp"
+#include "mfma.hpp"
+
+namespace ordermoe {
+namespace {
+
+constexpr int PA_WAVES = 4, PA_ROWS = 32 * PA_WAVES;     // query rows of a workgroup
+template <bool BF>
+constexpr int PA_TILE = BF ? 64 : 32;                    // positions of a tile
+// A maximum is taken over only when some score passes it by 8 (a factor of 256 in the weights, which fp32 sums
+// and bf16 weights hold as well as 1): most tiles then need no exchange between lanes and no rescaling.
+constexpr float PA_LAG = 8.0f;
+
+__host__ __device__ inline int64_t row_blocks(int64_t rows) { return (rows + PA_ROWS - 1) / PA_ROWS; }
+
+struct Seq {
+    int q0, n, k0, len;      // first token, tokens, first position, positions
+};
+__device__ inline Seq sequence(const PromptArgs& a, int b) {
+    const int T = (int)a.T, L = (int)a.L;
+    int q0 = a.q_start[b], q1 = a.q_start[b + 1], k0 = a.kv_start[b], k1 = a.kv_start[b + 1];
+    q0 = q0 < 0 ? 0 : q0 > T ? T : q0;
+    q1 = q1 < q0 ? q0 : q1 > T ? T : q1;
+    k0 = k0 < 0 ? 0 : k0 > L ? L : k0;
+    k1 = k1 < k0 ? k0 : k1 > L ? L : k1;
+    return Seq{q0, q1 - q0, k0, k1 - k0};
+}
+
+// sequence and row block of an item, by one wave; false: there are not so many.  A sequence's last row blocks,
+// which see the most, come first.
+__device__ inline bool find_block(const PromptArgs& a, int64_t item, int lane, Seq& s, int& rb) {
+    const int G = a.n_q / a.n_kv;
+    int64_t base = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        Seq m = {0, 0, 0, 0};
+        if (b0 + lane < a.B) m = sequence(a, b0 + lane);
+        const int cnt = (int)row_blocks((int64_t)m.n * G);
+        int inc = cnt;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(inc, o);
+            if (lane >= o) inc += v;
+        }
+        const int64_t first = base + inc - cnt;
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(item >= first && item < first + cnt);
+        if (hit) {
+            const int l = __builtin_ctzll(hit);
+            s = Seq{__builtin_amdgcn_readlane(m.q0, l), __builtin_amdgcn_readlane(m.n, l), __builtin_amdgcn_readlane(m.k0, l),
+                    __builtin_amdgcn_readlane(m.len, l)};
+            rb = __builtin_amdgcn_readlane((int)(first + cnt - 1 - item), l);
+            return true;
+        }
+        base += __builtin_amdgcn_readlane(inc, 63);
+    }
+    return false;
+}
+
+// Rows of RB bytes in LDS, as 16-byte chunks: chunk c of row r lies at c ^ swap(r), so that what the lanes of a read
+// take lies on distinct banks.  K and the rotary part: eight rows of one chunk; V: four rows of two chunks (bf16, turned)
+// or two rows, four apart, of eight (fp32).
+template <int RB>
+__device__ inline int swap_k(int r) {
+    return RB >= 256 ? r & 15 : RB == 128 ? r & 7 : (r >> 1) & 3;
+}
+template <bool BF, int RB>
+__device__ inline int swap_v(int r) {
+    if constexpr (BF) return RB >= 256 ? (r & 3) << 2 : (r & 3) << 1;
+    else return ((r >> 2) & 1) << 3;
+}
+
+template <bool BF, int D, int ROT>
+struct Layout {
+    static constexpr int ES = BF ? 2 : 4, TILE = PA_TILE<BF>, RBD = D * ES, RBR = ROT * ES;
+    static constexpr int K = 0, R = TILE * RBD, V = R + TILE * RBR, STAGE = V + TILE * RBD;
+    static constexpr int QN = (D + ROT) * ES / 32;       // 16-byte pieces of a query that a lane holds
+};
+
+// TILE rows of RB bytes, `stride` bytes apart in memory, into LDS; rows past the resource's end arrive as zeros
+template <int RB, int TILE, int KIND, bool BF>
+__device__ inline void issue_rows(__amdgpu_buffer_rsrc_t rs, uint32_t stride, char* to, int wave, int lane) {
+    constexpr int CH = RB / 16, PIECES = TILE * RB / 1024 / PA_WAVES;
+    static_assert(TILE * RB % (1024 * PA_WAVES) == 0, "whole pieces a wave");
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int piece = wave * PIECES + i, row = piece * (64 / CH) + lane / CH;
+        const int ch = (lane % CH) ^ (KIND == 0 ? swap_k<RB>(row) : swap_v<BF, RB>(row));
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(to + piece * 1024), 16, row * stride + ch * 16, 0, 0, 0);
+    }
+}
+__device__ inline __amdgpu_buffer_rsrc_t make_rsrc(const void* base, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, (int)bytes, 0x00020000);
+}
+
+// Positions of a tile's V that hold an infinity or a NaN, a bit each, by one wave
+template <bool BF, int D>
+__device__ inline uint64_t not_finite(const char* v, int lane) {
+    constexpr int CH = D * (BF ? 2 : 4) / 16;
+    uint64_t m = 0;
+#pragma unroll 4
+    for (int i = 0; i < PA_TILE<BF> * CH / 64; ++i) {
+        const u32x4 x = *(const u32x4*)(v + (i * 64 + lane) * 16);
+        bool bad = false;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            bad |= BF ? (x[w] & 0x7F80u) == 0x7F80u || (x[w] & 0x7F800000u) == 0x7F800000u : (x[w] & 0x7F800000u) == 0x7F800000u;
+        if (bad) m |= 1ull << ((i * 64 + lane) / CH);
+    }
+    if (!__builtin_amdgcn_ballot_w64(m != 0)) return 0;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) m |= __shfl_xor((unsigned long long)m, o);
+    return m;
+}
+
+template <bool BF, int D, int ROT>
+struct State {
+    float m, l;                  // of the lane's query row: maximum in units of log 2 (may lag), its positions' share of the sum
+    f32x16 o[D / 32];
+};
+
+// One tile by one wave.  edge: some row of the workgroup does not see all of it; the lane's row sees positions up to
+// lim (of the tile's: lim - t0).
+template <bool BF, int D, int ROT>
+__device__ inline __attribute__((always_inline)) void attend_tile(const char* st, const u32x4* q, float scale2, bool edge, int see, int lane,
+                                                                  State<BF, D, ROT>& s) {
+    using Lay = Layout<BF, D, ROT>;
+    constexpr int NB = Lay::TILE / 32;
+    const int c = lane & 31, h = lane >> 5;
+    const float ninf = -__builtin_inff();
+    f32x16 sc[NB];
+#pragma unroll
+    for (int tb = 0; tb < NB; ++tb) {
+        sc[tb] = f32x16{};
+        const int row = 32 * tb + c;
+#pragma unroll
+        for (int k = 0; k < Lay::RBD / 32; ++k)
+            sc[tb] = mma32<BF>(*(const u32x4*)(st + Lay::K + row * Lay::RBD + (((2 * k + h) ^ swap_k<Lay::RBD>(row)) * 16)), q[k], sc[tb]);
+        if constexpr (ROT > 0) {
+#pragma unroll
+            for (int k = 0; k < Lay::RBR / 32; ++k)
+                sc[tb] = mma32<BF>(*(const u32x4*)(st + Lay::R + row * Lay::RBR + (((2 * k + h) ^ swap_k<Lay::RBR>(row)) * 16)),
+                                   q[Lay::RBD / 32 + k], sc[tb]);
+        }
+    }
+    uint64_t bad = 0;
+    if (edge) {
+        bad = not_finite<BF, D>(st + Lay::V, lane);
+#pragma unroll
+        for (int tb = 0; tb < NB; ++tb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int p = 32 * tb + 8 * (i >> 2) + 4 * h + (i & 3);
+                sc[tb][i] = p <= see ? sc[tb][i] : ninf;
+            }
+    }
+    float top = ninf;
+#pragma unroll
+    for (int tb = 0; tb < NB; ++tb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[tb][i]);
+    top *= scale2;                                       // (scale2 >= 0; -inf stays, 0 of it included, as no number)
+    top = top == top ? top : ninf;
+    if (__builtin_amdgcn_ballot_w64(top > s.m + PA_LAG)) {
+        const float x = fmaxf(top, __shfl_xor(top, 32));
+        const float m = x > s.m + PA_LAG ? x : s.m;
+        const float al = s.m == m ? 1.0f : __builtin_amdgcn_exp2f(s.m - m);
+        s.m = m;
+        s.l *= al;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) s.o[d] = s.o[d] * al;
+    }
+    const float m = s.m == ninf ? 0.f : s.m;
+#pragma unroll
+    for (int tb = 0; tb < NB; ++tb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[tb][i], scale2, -m));
+            if (edge) p = sc[tb][i] == ninf ? 0.f : p;
+            sc[tb][i] = p;
+            s.l += p;
+        }
+    if (bad) {
+        // a weight of 0 would not keep what is no number out of a row's sums: it is taken as 0 below, and the rows that
+        // see it become NaN here
+        const uint64_t seen = see < 0 ? 0ull : see >= 63 ? ~0ull : (2ull << see) - 1;
+        if (bad & seen) s.l = __builtin_nanf("");
+    }
+#pragma unroll
+    for (int tb = 0; tb < NB; ++tb) {
+        if constexpr (BF) {
+            const int x = lane & 15, i = x >> 2, j = x & 3, col = ((lane >> 4) & 1) * 16 + 4 * j;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                u32x4 pf;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) pf[e] = bf16_pair(sc[tb][8 * k + 2 * e], sc[tb][8 * k + 2 * e + 1]);
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d) {
+                    u32x4 vf;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int row = 32 * tb + 16 * k + 8 * u + 4 * h + i, e = 32 * d + col;
+                        const u32x2 t = read_turned(st + Lay::V + row * Lay::RBD + (((e >> 3) ^ swap_v<BF, Lay::RBD>(row)) * 16) + (e & 7) * 2);
+                        vf[2 * u] = t[0];
+                        vf[2 * u + 1] = t[1];
+                    }
+                    if (bad) {
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            if ((vf[w] & 0x7F80u) == 0x7F80u) vf[w] &= 0xFFFF0000u;
+                            if ((vf[w] & 0x7F800000u) == 0x7F800000u) vf[w] &= 0xFFFFu;
+                        }
+                    }
+                    s.o[d] = mma32<true>(vf, pf, s.o[d]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int row = 32 * tb + 8 * (i >> 2) + 4 * h + (i & 3);
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d) {
+                    const int e = 32 * d + c;
+                    float v = *(const float*)(st + Lay::V + row * Lay::RBD + (((e >> 2) ^ swap_v<BF, Lay::RBD>(row)) * 16) + (e & 3) * 4);
+                    if (bad) v = (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u ? 0.f : v;
+                    s.o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, sc[tb][i], s.o[d], 0, 0, 0);
+                }
+            }
+        }
+    }
+}
+
+template <bool BF, int D, int ROT>
+__global__ void __launch_bounds__(64 * PA_WAVES, 2) prompt_attention_kernel(const PromptArgs a, int64_t items, int64_t per_xcd) {
+    using Lay = Layout<BF, D, ROT>;
+    constexpr int ES = Lay::ES, TILE = Lay::TILE;
+    __shared__ __attribute__((aligned(16))) char mem[2 * Lay::STAGE];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 31, h = lane >> 5;
+    // a key/value head's row blocks after one another on one XCD, where its rows are in L2
+    const int64_t id = block_number(), unit = (id & 7) * per_xcd + (id >> 3);
+    if ((id >> 3) >= per_xcd || unit >= items * a.n_kv) return;
+    const int kvh = (int)(unit / items);
+    Seq s;
+    int rb;
+    if (!find_block(a, unit - kvh * items, lane, s, rb)) return;
+    const int G = a.n_q / a.n_kv;
+    const int64_t rows = (int64_t)s.n * G, row0 = (int64_t)rb * PA_ROWS, row = row0 + 32 * wave + c;
+    const bool in = row < rows;
+    const int i = in ? (int)(row / G) : 0, hq = kvh * G + (in ? (int)(row - (int64_t)i * G) : 0);
+    const int before = s.len - s.n;                      // (may be negative)
+    const int lim = in ? before + i : -1;                // the last position that the lane's row sees
+    // positions that some row of the workgroup sees, and that all of them do
+    const int last = (int)((std::min(rows, row0 + PA_ROWS) - 1) / G), end = std::max(0, std::min(s.len, before + last + 1));
+    const int all = before + (int)(row0 / G) + 1;
+    const float scale2 = std::fabs(a.scale) * LOG2E;
+    u32x4 q[Lay::QN];
+    {
+        const char* from = (const char*)a.q + ((int64_t)(s.q0 + i) * a.n_q + hq) * ((D + ROT) * ES) + 16 * h;
+        const uint32_t flip = a.scale < 0.f ? (BF ? 0x80008000u : 0x80000000u) : 0u;
+#pragma unroll
+        for (int k = 0; k < Lay::QN; ++k) {
+            q[k] = u32x4{0u, 0u, 0u, 0u};
+            if (in) q[k] = *(const u32x4*)(from + 32 * k);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) q[k][w] ^= flip;
+        }
+    }
+    State<BF, D, ROT> st;
+    st.m = -__builtin_inff();
+    st.l = 0.f;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) st.o[d] = f32x16{};
+    const uint32_t stride = (uint32_t)a.n_kv * D * ES;
+    auto issue = [&](int t0, char* to) __attribute__((always_inline)) {
+        const int64_t at = (int64_t)s.k0 + t0;
+        const uint32_t left = (uint32_t)std::min(TILE, s.len - t0);
+        const int64_t off = at * stride + kvh * (D * ES);
+        issue_rows<Lay::RBD, TILE, 0, BF>(make_rsrc((const char*)a.k + off, (left - 1) * stride + D * ES), stride, to + Lay::K, wave, lane);
+        if constexpr (ROT > 0)
+            issue_rows<Lay::RBR, TILE, 0, BF>(make_rsrc((const char*)a.r + at * Lay::RBR, left * Lay::RBR), Lay::RBR, to + Lay::R, wave, lane);
+        issue_rows<Lay::RBD, TILE, 1, BF>(make_rsrc((const char*)a.v + off, (left - 1) * stride + D * ES), stride, to + Lay::V, wave, lane);
+    };
+    if (end > 0) issue(0, mem);
+    for (int t0 = 0, buf = 0; t0 < end; t0 += TILE, buf ^= 1) {
+        __syncthreads();                                 // the tile has arrived, and the one before has been read
+        if (t0 + TILE < end) issue(t0 + TILE, mem + (buf ^ 1) * Lay::STAGE);
+        attend_tile<BF, D, ROT>(mem + buf * Lay::STAGE, q, scale2, t0 + TILE > all, lim - t0, lane, st);
+    }
+    if (!in) return;
+    const float l = st.l + __shfl_xor(st.l, 32);
+    const float r = l == 0.f ? 0.f : 1.0f / l;
+    const int64_t at = (int64_t)(s.q0 + i) * a.n_q + hq;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            store4<BF>(a.out, at * D + 32 * d + 8 * j + 4 * h, st.o[d][4 * j] * r, st.o[d][4 * j + 1] * r, st.o[d][4 * j + 2] * r,
+                       st.o[d][4 * j + 3] * r);
+    if (a.lse && h == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (st.m + __builtin_amdgcn_logf(l)) * LN2;
+}
+
+template <bool BF, int D, int ROT>
+int launch_rows(const PromptArgs& a, hipStream_t st) {
+    // row blocks: every sequence ends in one that is not full, at most
+    const int64_t items = std::min<int64_t>(a.T * (a.n_q / a.n_kv), a.T * (a.n_q / a.n_kv) / PA_ROWS + a.B);
+    const int64_t per = (items * a.n_kv + 7) / 8;
+    KernelTimer kt_("prompt_attention", st);
+    prompt_attention_kernel<BF, D, ROT><<<grid_of(per * 8), dim3(64 * PA_WAVES), 0, st>>>(a, items, per);
+    return (int)hipGetLastError();
+}
+template <bool BF, int D>
+int launch_rot(const PromptArgs& a, hipStream_t st) {
+    return a.rot == 0 ? launch_rows<BF, D, 0>(a, st) : a.rot == 32 ? launch_rows<BF, D, 32>(a, st) : launch_rows<BF, D, 64>(a, st);
+}
+
+}  // namespace
+
+int64_t prompt_part_rows(int, int, int, int, int, int64_t, int) { return 0; }
+
+int launch_prompt_attention(const PromptArgs& a, void* stream) {
+    if (a.B == 0 || a.T == 0) return 0;
+    hipStream_t st = (hipStream_t)stream;
+    if (a.dtype == ORDERMOE_BF16) return a.head_dim == 64 ? launch_rot<true, 64>(a, st) : launch_rot<true, 128>(a, st);
+    return a.head_dim == 64 ? launch_rot<false, 64>(a, st) : launch_rot<false, 128>(a, st);
+}
+
+}  // namespace ordermoe

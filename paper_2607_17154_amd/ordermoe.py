@@ -37,7 +37,10 @@ EXPORTS = ("ordermoe_last_error", "ordermoe_similarity_workspace_size", "ordermo
            "ordermoe_build_lookahead_device", "ordermoe_transitions_device_workspace_size",
            "ordermoe_estimate_transitions_device", "ordermoe_route_select_noalloc",
            "ordermoe_cache_write", "ordermoe_cache_read", "ordermoe_draft_attention_workspace_size",
-           "ordermoe_draft_attention", "ordermoe_few_workspace_size", "ordermoe_few_moe_layer")
+           "ordermoe_draft_attention", "ordermoe_few_workspace_size", "ordermoe_few_moe_layer",
+           "ordermoe_latent_write", "ordermoe_latent_attention_workspace_size", "ordermoe_latent_attention",
+           "ordermoe_latent_expand", "ordermoe_prompt_attention_workspace_size", "ordermoe_prompt_attention",
+           "ordermoe_latent_evict_workspace_size", "ordermoe_latent_evict")
 TIMING_NAME = 64
 
 
@@ -77,6 +80,15 @@ class Cache(ctypes.Structure):
 class Heads(ctypes.Structure):
     _fields_ = [("dtype", _I32), ("n_q", _I32), ("rotary_dim", _I32), ("interleaved", _I32), ("max_pos", _I64),
                 ("eps", _F32), ("q_norm", _P), ("k_norm", _P), ("cos_sin", _P)]
+
+
+class LatentCache(ctypes.Structure):
+    _fields_ = [("dtype", _I32), ("rank", _I32), ("rotary_dim", _I32), ("page_size", _I32), ("n_pages", _I64), ("rows", _P)]
+
+
+class LatentHeads(ctypes.Structure):
+    _fields_ = [("n_q", _I32), ("head_dim", _I32), ("interleaved", _I32), ("max_pos", _I64), ("eps", _F32), ("norm", _P),
+                ("cos_sin", _P), ("w_k", _P), ("w_v", _P)]
 
 
 _lib = None
@@ -159,6 +171,25 @@ def lib() -> ctypes.CDLL:
     L.ordermoe_few_moe_layer.restype = ctypes.c_int
     L.ordermoe_few_moe_layer.argtypes = [ctypes.POINTER(Layer), ctypes.POINTER(Experts), _P, _I64, _P, _P, _I32,
                                          ctypes.POINTER(RouteOut), _P, _P, _SZ, _P]
+    LC, LH = ctypes.POINTER(LatentCache), ctypes.POINTER(LatentHeads)
+    L.ordermoe_latent_write.restype = ctypes.c_int
+    L.ordermoe_latent_write.argtypes = [LC, LH, _P, _I64, _P, _I64, _I64, _P, _P, _I32, _P, _P]
+    L.ordermoe_latent_attention_workspace_size.restype = _SZ
+    L.ordermoe_latent_attention_workspace_size.argtypes = [LC, LH, _I32, _I32, _I32, _I32]
+    L.ordermoe_latent_attention.restype = ctypes.c_int
+    L.ordermoe_latent_attention.argtypes = [LC, LH, _P, _I64, _I32, _I32, _P, _P, _P, _I32, _P, _F32, _P, _P, _P, _P, _I64, _F32,
+                                            _P, _SZ, _P]
+    L.ordermoe_latent_expand.restype = ctypes.c_int
+    L.ordermoe_latent_expand.argtypes = [LC, LH, _P, _I64, _P, _P, _P, _P]
+    L.ordermoe_prompt_attention_workspace_size.restype = _SZ
+    L.ordermoe_prompt_attention_workspace_size.argtypes = [_I32, _I32, _I32, _I32, _I32, _I64, _I32]
+    L.ordermoe_prompt_attention.restype = ctypes.c_int
+    L.ordermoe_prompt_attention.argtypes = [_I32, _I32, _I32, _I32, _I32, _P, _I64, _P, _P, _P, _I64, _I32, _P, _P, _F32, _P, _P,
+                                            _P, _SZ, _P]
+    L.ordermoe_latent_evict_workspace_size.restype = _SZ
+    L.ordermoe_latent_evict_workspace_size.argtypes = [LC, _I32, _I32, _I32]
+    L.ordermoe_latent_evict.restype = ctypes.c_int
+    L.ordermoe_latent_evict.argtypes = [LC, _I32, _P, _P, _P, _I32, _I32, _I32, _I32, _P, _P, _I64, _P, _P, _P, _P, _P, _SZ, _P]
     L.ordermoe_timing_enable.restype = ctypes.c_int
     L.ordermoe_timing_enable.argtypes = [_I32]
     L.ordermoe_timing_read.restype = ctypes.c_int
@@ -687,6 +718,137 @@ def ordermoe_few_moe_layer(layer: Layer, experts: Experts, x, T: int, loc_in, qh
     _check(lib().ordermoe_few_moe_layer(ctypes.byref(layer), ctypes.byref(experts), ptr(x), T, ptr(loc_in), ptr(qhat_in),
                                         server, ctypes.byref(s), ptr(y), _dev(workspace), workspace.numel(),
                                         _stream(stream)))
+
+
+# ---------------------------------------------------------------- latent attention, prompts, eviction
+def make_latent_cache(rows, rank: int) -> LatentCache:
+    """ordermoe_latent_cache of rows [n_pages, page_size, rank + rotary_dim] (float32 or
+    bfloat16); keeps the tensor alive."""
+    n_pages, page, width = rows.shape
+    c = LatentCache(dtype=_dtype_code(rows), rank=rank, rotary_dim=width - rank, page_size=page, n_pages=n_pages, rows=_dev(rows))
+    c._tensors = (rows,)
+    return c
+
+
+def alloc_latent_cache(dtype: int, n_pages: int, page_size: int, rank: int, rotary_dim: int, device) -> LatentCache:
+    """An ordermoe_latent_cache with memory of its own (contents undefined)."""
+    import torch
+    return make_latent_cache(torch.empty((n_pages, page_size, rank + rotary_dim), dtype=_torch_dtype(dtype), device=device), rank)
+
+
+def make_latent_heads(cache: LatentCache, w_k, w_v, norm=None, cos_sin=None, interleaved: int = 0, eps: float = 1e-6) -> LatentHeads:
+    """ordermoe_latent_heads for the cache: w_k, w_v [n_q, head_dim, rank], norm [rank] of
+    its storage type, cos_sin float32 [max_pos, rotary_dim] (rotary_table); keeps the tensors alive."""
+    import torch
+    n_q, D, rank = w_k.shape
+    dt = _torch_dtype(cache.dtype)
+    if rank != cache.rank:
+        raise ValueError("weights of rank %d, the cache of %d" % (rank, cache.rank))
+    max_pos = cos_sin.shape[0] if cos_sin is not None else 0
+    h = LatentHeads(n_q=n_q, head_dim=D, interleaved=interleaved, max_pos=max_pos, eps=eps,
+                    norm=_dev(norm, dt, rank) or None, cos_sin=_dev(cos_sin, torch.float32, max_pos * cache.rotary_dim) or None,
+                    w_k=_dev(w_k, dt), w_v=_dev(w_v, dt, n_q * D * rank))
+    h._tensors = (norm, cos_sin, w_k, w_v)
+    h._made_for = (cache.dtype, cache.rank, cache.rotary_dim)
+    return h
+
+
+def _same_kind(cache: LatentCache, heads: LatentHeads):
+    kind = (cache.dtype, cache.rank, cache.rotary_dim)
+    if getattr(heads, "_made_for", kind) != kind:            # (weights, norm and table end with those sizes)
+        raise ValueError("heads made for (dtype, rank, rotary_dim) %s, the cache has %s" % (heads._made_for, kind))
+
+
+def ordermoe_latent_write(cache: LatentCache, heads: LatentHeads, q, kv, pos, slots, q_out, absorb: int, stream=None):
+    """q [T, n_q, head_dim + rotary_dim] (None: rows only), kv [T, rank + rotary_dim] (tokens
+    may lie apart, as in one array of projections), pos int32 [T] (None without rotation), slots int64
+    [T]; q_out [T, n_q, (rank if absorb else head_dim) + rotary_dim]."""
+    import torch
+    _same_kind(cache, heads)
+    T, dt, R, rot = kv.shape[0], _torch_dtype(cache.dtype), cache.rank, cache.rotary_dim
+    if not kv.is_cuda or kv.dtype != dt or kv.shape != (T, R + rot) or (T > 0 and kv.stride(1) != 1):
+        raise ValueError("expected a %s device tensor [%d, %d] of rows" % (dt, T, R + rot))
+    qp, qs = _rows(q, dt, T, heads.n_q, heads.head_dim + rot) if q is not None else (0, 0)
+    qo = _dev(q_out, dt, T * heads.n_q * ((R if absorb else heads.head_dim) + rot)) if q is not None else 0
+    _check(lib().ordermoe_latent_write(ctypes.byref(cache), ctypes.byref(heads), qp, qs, kv.data_ptr(),
+                                       kv.stride(0) if T > 1 else R + rot, T, _dev(pos, torch.int32, T),
+                                       _dev(slots, torch.int64, T), absorb, qo, _stream(stream)))
+
+
+def ordermoe_latent_attention_workspace_size(cache: LatentCache, heads: LatentHeads, B: int, max_q: int, max_pages: int,
+                                             weighs: int = 0) -> int:
+    return int(lib().ordermoe_latent_attention_workspace_size(ctypes.byref(cache), ctypes.byref(heads), B, max_q, max_pages, weighs))
+
+
+def ordermoe_latent_attention(cache: LatentCache, heads: LatentHeads, q, q_start, ctx_len, page_table, max_q: int, scale: float, out,
+                              workspace, tree=None, lse=None, mass=None, mass_out=None, decay: float = 1.0, stream=None):
+    """q [T, n_q, rank + rotary_dim] (absorbed), out [T, n_q, head_dim]; q_start int32 [B + 1],
+    ctx_len int32 [B], page_table int32 [B, max_pages]; tree int64 [T] or None for chains; lse float32
+    [T, n_q] or None; mass, mass_out float32 [B, stride] or None."""
+    import torch
+    _same_kind(cache, heads)
+    T, n_q, width = q.shape
+    B, max_pages = page_table.shape
+    dt = _torch_dtype(cache.dtype)
+    if n_q != heads.n_q or width != cache.rank + cache.rotary_dim:
+        raise ValueError("q is [%d, %d, %d], expected [T, %d, %d]" % (T, n_q, width, heads.n_q, cache.rank + cache.rotary_dim))
+    if mass_out is not None and (mass_out.dim() != 2 or mass_out.shape[0] != B):
+        raise ValueError("expected mass_out [%d, stride]" % B)
+    _check(lib().ordermoe_latent_attention(
+        ctypes.byref(cache), ctypes.byref(heads), _dev(q, dt), T, B, max_q, _dev(q_start, torch.int32, B + 1),
+        _dev(ctx_len, torch.int32, B), _dev(page_table, torch.int32), max_pages, _dev(tree, torch.int64, T), scale,
+        _dev(out, dt, T * n_q * heads.head_dim), _dev(lse, torch.float32, T * n_q),
+        _dev(mass, torch.float32, None if mass_out is None else mass_out.numel()), _dev(mass_out, torch.float32),
+        0 if mass_out is None else mass_out.shape[1], decay, _dev(workspace), workspace.numel(), _stream(stream)))
+
+
+def ordermoe_latent_expand(cache: LatentCache, heads: LatentHeads, slots, k_out, r_out, v_out, stream=None):
+    """k_out, v_out [n, n_q, head_dim], r_out [n, rotary_dim] from slots int64 [n]."""
+    import torch
+    _same_kind(cache, heads)
+    n, dt = slots.numel(), _torch_dtype(cache.dtype)
+    m = n * heads.n_q * heads.head_dim
+    _check(lib().ordermoe_latent_expand(ctypes.byref(cache), ctypes.byref(heads), _dev(slots, torch.int64, n), n, _dev(k_out, dt, m),
+                                        _dev(r_out, dt, n * cache.rotary_dim), _dev(v_out, dt, m), _stream(stream)))
+
+
+def ordermoe_prompt_attention_workspace_size(dtype: int, n_q: int, n_kv: int, head_dim: int, rotary_dim: int, T: int, B: int) -> int:
+    return int(lib().ordermoe_prompt_attention_workspace_size(dtype, n_q, n_kv, head_dim, rotary_dim, T, B))
+
+
+def ordermoe_prompt_attention(q, k, v, q_start, kv_start, scale: float, out, workspace, k_shared=None, lse=None, stream=None):
+    """q [T, n_q, head_dim + rotary_dim], k, v [L, n_kv, head_dim], k_shared [L, rotary_dim]
+    (None: rotary_dim 0), out [T, n_q, head_dim]; q_start, kv_start int32 [B + 1]; lse float32 [T, n_q] or
+    None."""
+    import torch
+    (T, n_q, width), (L, n_kv, D), B = q.shape, k.shape, q_start.numel() - 1
+    rot = k_shared.shape[1] if k_shared is not None else 0
+    if width != D + rot:
+        raise ValueError("q has heads of %d, k of %d and %d that are shared" % (width, D, rot))
+    code = _dtype_code(q)
+    _check(lib().ordermoe_prompt_attention(
+        code, n_q, n_kv, D, rot, _dev(q), T, _dev(k, q.dtype), _dev(k_shared, q.dtype, L * rot), _dev(v, q.dtype, L * n_kv * D), L, B,
+        _dev(q_start, torch.int32), _dev(kv_start, torch.int32, B + 1), scale, _dev(out, q.dtype, T * n_q * D),
+        _dev(lse, torch.float32, T * n_q), _dev(workspace), workspace.numel(), _stream(stream)))
+
+
+def ordermoe_latent_evict_workspace_size(cache: LatentCache, B: int, max_pages: int, keep: int) -> int:
+    return int(lib().ordermoe_latent_evict_workspace_size(ctypes.byref(cache), B, max_pages, keep))
+
+
+def ordermoe_latent_evict(cache: LatentCache, ctx_len, seq_len, page_table, keep: int, first: int, recent: int, mass, pos, kept, len_out,
+                          mass_out, pos_out, workspace, stream=None):
+    """ctx_len, seq_len, len_out int32 [B], page_table int32 [B, max_pages], mass, mass_out
+    float32 [B, stride], pos, pos_out int32 [B, stride], kept int32 [B, keep]."""
+    import torch
+    B, max_pages = page_table.shape
+    if mass.dim() != 2 or mass.shape[0] != B:
+        raise ValueError("expected mass [%d, stride]" % B)
+    n, i32 = mass.numel(), torch.int32
+    _check(lib().ordermoe_latent_evict(
+        ctypes.byref(cache), B, _dev(ctx_len, i32, B), _dev(seq_len, i32, B), _dev(page_table, i32), max_pages, keep, first, recent,
+        _dev(mass, torch.float32), _dev(pos, i32, n), mass.shape[1], _dev(kept, i32, B * keep), _dev(len_out, i32, B),
+        _dev(mass_out, torch.float32, n), _dev(pos_out, i32, n), _dev(workspace), workspace.numel(), _stream(stream)))
 
 
 def ordermoe_timing_enable(on: bool = True):
