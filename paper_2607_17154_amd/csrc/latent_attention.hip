@@ -127,25 +127,22 @@ __device__ inline Seq find_item(const LatentAttentionArgs& a, int piece, int ite
     return found;
 }
 
-// Rows of RB bytes in LDS, side by side, as 16-byte chunks: chunk ch of row r lies at ch ^ swap(r), so that the reads of
-// one chunk of 16 rows lie on distinct banks.
-template <int RB>
-__device__ inline int swap_row(int r) {
-    constexpr int CH = RB / 16;
-    return CH % 16 == 0 ? r & 15 : CH % 8 == 0 ? (r >> 1) & 7 : (r >> 2) & 3;
-}
-
+// A tile of TILE rows of RB bytes in LDS: panels of 128 bytes of every row, chunk (of 16 bytes) ch of row r at ch ^ r % 8, so
+// that the reads of one chunk of eight rows lie on distinct banks; and what is left over, 64 bytes, as rows of their own,
+// at ch ^ r / 2 % 4.  A wave's load of 1 KB is eight rows of a panel: one offset per lane serves all of them.
 template <bool BF, int R, int ROT, int RW>
 struct Config {
-    static constexpr int ES = BF ? 2 : 4, RB = (R + ROT) * ES, CH = RB / 16;
+    static constexpr int ES = BF ? 2 : 4, RB = (R + ROT) * ES;
     static constexpr int NW = RW > 1 ? 8 : BF ? 4 : 2, GROUPS = NW / RW;     // waves, groups of them
-    static constexpr int TILE = BF ? (RW > 1 ? 8 * RW : 16) : 16;            // tokens of a group's tile
+    static constexpr int TILE = RW > 1 ? 8 * RW : 16;                        // tokens of a group's tile
     static constexpr int SUB = TILE < 32 ? 16 : 32;                          // tokens that are attended to at a time
-    static constexpr int STAGE = TILE * RB, PIECES = STAGE / 1024;           // bytes of a tile, wave loads of it
-    static constexpr int MINE = (PIECES + RW - 1) / RW;                      // of them a wave's, at most
+    static constexpr int PANELS = RB / 128, TAIL = PANELS * TILE * 128;      // whole panels, where the rest begins
+    static constexpr bool HAS_TAIL = RB % 128 != 0;
+    static constexpr int STAGE = TILE * RB, OCTETS = TILE / 8 / RW;          // bytes of a tile, a wave's eights of its rows
+    static constexpr int LOADS = OCTETS * (PANELS + HAS_TAIL);               // of a wave for a tile
     static constexpr int KS = RB / 64;                                       // steps of the first product
     static constexpr int LD = R + 4;                                         // floats of a row of sums in LDS
-    static_assert(STAGE % 1024 == 0 && GROUPS * 16 * LD * 4 <= GROUPS * 2 * STAGE, "whole pieces, the sums fit");
+    static_assert(RB % 64 == 0 && R * ES % 128 == 0 && GROUPS * 16 * LD * 4 <= GROUPS * 2 * STAGE, "whole chunks, the sums fit");
 };
 
 // page of the tile at t0 (16 tokens never cross a page), -1: none; uniform, through the scalar cache
@@ -161,19 +158,25 @@ __device__ inline void wait_loads() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// of N tokens' rows, those that hold an infinity or a NaN, a bit each, by one wave
-template <bool BF, int RB, int N>
-__device__ inline uint32_t not_finite(const char* st, int lane) {
+// of SUB tokens from row r0 of a tile on, those whose row holds an infinity or a NaN, a bit each, by one wave
+template <bool BF, typename Cf>
+__device__ inline uint32_t not_finite(const char* st, int r0, int lane) {
     uint32_t m = 0;
-#pragma unroll 4
-    for (int i = 0; i < N * RB / 1024; ++i) {
-        const u32x4 x = *(const u32x4*)(st + (i * 64 + lane) * 16);
+    auto look = [&](const char* p, int row) {
+        const u32x4 x = *(const u32x4*)p;
         bool bad = false;
 #pragma unroll
         for (int w = 0; w < 4; ++w)
             bad |= BF ? (x[w] & 0x7F80u) == 0x7F80u || (x[w] & 0x7F800000u) == 0x7F800000u : (x[w] & 0x7F800000u) == 0x7F800000u;
-        if (bad) m |= 1u << ((i * 64 + lane) / (RB / 16));
-    }
+        if (bad) m |= 1u << row;
+    };
+#pragma unroll 2
+    for (int p = 0; p < Cf::PANELS; ++p)
+#pragma unroll
+        for (int o = 0; o < Cf::SUB; o += 8) look(st + p * (Cf::TILE * 128) + (r0 + o) * 128 + lane * 16, o + (lane >> 3));
+    if constexpr (Cf::HAS_TAIL)
+#pragma unroll
+        for (int o = 0; o < Cf::SUB; o += 16) look(st + Cf::TAIL + (r0 + o) * 64 + lane * 16, o + (lane >> 2));
     if (!__builtin_amdgcn_ballot_w64(m != 0)) return 0;
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) m |= __shfl_xor(m, o);
@@ -197,39 +200,100 @@ __device__ inline u32x2 only_finite(u32x2 v) {
     return v;
 }
 
-// SUB tokens from t0 on, staged at st.  A maximum is taken over only when some score passes it by LA_LAG (a factor of
-// 256 in the weights, which fp32 sums and bf16 weights hold as well as 1): most tiles then need no exchange
-// between lanes and no rescaling of the outputs.  FINE: the second product takes what the rounding of the weights to
-// bf16 leaves out as well.
-template <bool BF, int R, int RB, int SUB, bool FINE, bool WEIGHS>
-__device__ inline __attribute__((always_inline)) void attend_tile(const char* st, const u32x4* q, const bool* ok, int t0, const Seq& s,
+// O^T += C^T P^T over SUB tokens from row r0 of a tile on; CLEAN: what is no number counts as 0.  The reads of a few
+// elements' rows are on their way during the products of the ones before.
+template <int R, typename Cf, bool FINE, bool CLEAN>
+__device__ inline __attribute__((always_inline)) void add_weighted(const char* st, int r0, const u32x2* pf, const u32x2* pl, int lane,
+                                                                   State<R>& state) {
+    constexpr int NB = Cf::SUB / 16, PANEL = Cf::TILE * 128, AHEAD = 4 / NB, STEPS = R / 16 / AHEAD;
+    const int c = lane & 15, row = 4 * (lane >> 4) + (c >> 2);
+    const char* at[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) at[j] = st + (r0 + row) * 128 + (((2 * j + ((c >> 1) & 1)) ^ (row & 7)) * 16) + (c & 1) * 8;
+    u32x2 v[2][AHEAD][NB];
+    auto read = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                const int j = i * AHEAD + e;
+                v[i & 1][e][n] = read_turned(at[j % 4] + j / 4 * PANEL + 16 * n * 128);
+            }
+    };
+    read(0);
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+        if (i + 1 < STEPS) read(i + 1);
+        if constexpr (CLEAN)
+#pragma unroll
+            for (int e = 0; e < AHEAD; ++e)
+#pragma unroll
+                for (int n = 0; n < NB; ++n) v[i & 1][e][n] = only_finite(v[i & 1][e][n]);
+#pragma unroll
+        for (int part = 0; part < (FINE ? 2 : 1); ++part) {
+            const u32x2* p = part ? pl : pf;
+#pragma unroll
+            for (int e = 0; e < AHEAD; ++e) {
+                const int j = i * AHEAD + e;
+                const u32x2* x = v[i & 1][e];
+                if constexpr (NB == 1)
+                    state.o[j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, x[0]), __builtin_bit_cast(s16x4, p[0]),
+                                                                           state.o[j], 0, 0, 0);
+                else
+                    state.o[j] = mma16<true>(u32x4{x[0][0], x[0][1], x[1][0], x[1][1]}, u32x4{p[0][0], p[0][1], p[1][0], p[1][1]}, state.o[j]);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// SUB tokens from t0 on, rows r0 .. of the tile staged at st.  A maximum is taken over only when some score passes it by
+// LA_LAG (a factor of 256 in the weights, which fp32 sums and bf16 weights hold as well as 1): most tiles then need no
+// exchange between lanes and no rescaling of the outputs.  FINE: the second product takes what the rounding of the
+// weights to bf16 leaves out as well.
+template <bool BF, int R, typename Cf, bool FINE, bool WEIGHS>
+__device__ inline __attribute__((always_inline)) void attend_tile(const char* st, int r0, const u32x4* q, uint32_t ok, int t0, const Seq& s,
                                                                   uint64_t word, float scale2, float* score, int lane,
                                                                   State<R>& state) {
-    constexpr int NB = SUB / 16, KS = RB / 64;
+    constexpr int SUB = Cf::SUB, NB = SUB / 16, KS = Cf::KS, PANEL = Cf::TILE * 128;
     const int c = lane & 15, g = lane >> 4;
     const float ninf = -__builtin_inff();
     f32x4 sc[NB] = {};
+    {
+        constexpr int RING = NB == 1 ? 5 : 3;                    // steps whose reads are in registers or on their way
+        const char* at[2];
 #pragma unroll
-    for (int k = 0; k < KS; ++k)
+        for (int k = 0; k < 2; ++k) at[k] = st + (r0 + c) * 128 + (((4 * k + g) ^ (c & 7)) * 16);
+        const char* tail = st + Cf::TAIL + (r0 + c) * 64 + ((g ^ ((c >> 1) & 3)) * 16);
+        u32x4 x[RING][NB];
+        auto read = [&](int k) __attribute__((always_inline)) {
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
-            sc[n] = mma16<BF>(*(const u32x4*)(st + (16 * n + c) * RB + (((4 * k + g) ^ swap_row<RB>(16 * n + c)) * 16)), q[k], sc[n]);
-    bool edge = t0 + SUB > s.ctx;
+            for (int n = 0; n < NB; ++n)
+                x[k % RING][n] = *(const u32x4*)(k / 2 < Cf::PANELS ? at[k % 2] + k / 2 * PANEL + 16 * n * 128 : tail + 16 * n * 64);
+        };
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-        edge |= !ok[n];
-        sc[n] = sc[n] * scale2;
+        for (int k = 0; k < RING - 1; ++k) read(k);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            if (k + RING - 1 < KS) read(k + RING - 1);
+#pragma unroll
+            for (int n = 0; n < NB; ++n) sc[n] = mma16<BF>(x[k % RING][n], q[k], sc[n]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
+    const bool edge = t0 + SUB > s.ctx || (~ok & ((1u << NB) - 1u));
+#pragma unroll
+    for (int n = 0; n < NB; ++n) sc[n] = sc[n] * scale2;
     uint32_t bad = 0;
     if (edge) {
-        bad = not_finite<BF, RB, SUB>(st, lane);
+        bad = not_finite<BF, Cf>(st, r0, lane);
         uint32_t seen = 0;
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int p = t0 + 16 * n + 4 * g + i, j = p - s.ctx;
-                const bool see = ok[n] && p < s.len && (j < 0 || ((word >> (j & 63)) & 1));
+                const bool see = ((ok >> n) & 1) && p < s.len && (j < 0 || ((word >> (j & 63)) & 1));
                 seen |= (uint32_t)see << (16 * n + 4 * g + i);
                 sc[n][i] = see ? sc[n][i] : ninf;
             }
@@ -277,35 +341,18 @@ __device__ inline __attribute__((always_inline)) void attend_tile(const char* st
             pf[n] = __builtin_bit_cast(u32x2, hi);
             if constexpr (FINE) pl[n] = __builtin_bit_cast(u32x2, lo);
         }
-        const int row = 4 * g + (c >> 2), sub = c & 3;
-        const char* at = st + row * RB + (sub & 1) * 8;
-#pragma unroll
-        for (int j = 0; j < R / 16; ++j) {
-            u32x2 v[NB];
-#pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                v[n] = read_turned(at + 16 * n * RB + (((2 * j + (sub >> 1)) ^ swap_row<RB>(16 * n + row)) * 16));
-                if (bad) v[n] = only_finite(v[n]);
-            }
-            if constexpr (NB == 1) {
-                const s16x4 vf = __builtin_bit_cast(s16x4, v[0]);
-                state.o[j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf, __builtin_bit_cast(s16x4, pf[0]), state.o[j], 0, 0, 0);
-                if constexpr (FINE)
-                    state.o[j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf, __builtin_bit_cast(s16x4, pl[0]), state.o[j], 0, 0, 0);
-            } else {
-                const u32x4 vf = {v[0][0], v[0][1], v[1][0], v[1][1]};
-                state.o[j] = mma16<true>(vf, u32x4{pf[0][0], pf[0][1], pf[1][0], pf[1][1]}, state.o[j]);
-                if constexpr (FINE) state.o[j] = mma16<true>(vf, u32x4{pl[0][0], pl[0][1], pl[1][0], pl[1][1]}, state.o[j]);
-            }
-        }
+        if (bad) add_weighted<R, Cf, FINE, true>(st, r0, pf, pl, lane, state);
+        else add_weighted<R, Cf, FINE, false>(st, r0, pf, pl, lane, state);
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int row = 4 * g + i, sw = swap_row<RB>(row);
-            const char* at = st + row * RB + (c & 3) * 4;
+            const int row = 4 * g + i;
+            const char* at[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) at[j] = st + (r0 + row) * 128 + (((4 * j + (c >> 2)) ^ (row & 7)) * 16) + (c & 3) * 4;
 #pragma unroll
             for (int j = 0; j < R / 16; ++j) {
-                float v = *(const float*)(at + (((4 * j + (c >> 2)) ^ sw) * 16));
+                float v = *(const float*)(at[j % 2] + j / 2 * PANEL);
                 if (bad) v = (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u ? 0.f : v;
                 state.o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, sc[0][i], state.o[j], 0, 0, 0);
             }
@@ -366,32 +413,31 @@ latent_attention_kernel(const LatentAttentionArgs a, int items, int rb_n) {
         for (int n = 0; n < NB; ++n) r.p[n] = tile_page(a, table, t0 + 16 * n, t_hi);
         return r;
     };
-    struct Ok { bool b[NB]; };
+    const uint32_t voff = (lane >> 3) * Cf::RB + (((lane & 7) ^ (lane >> 3)) * 16);
+    const uint32_t voff_tail = ((lane >> 2) & 7) * Cf::RB + (((lane & 3) ^ ((lane >> 3) & 3)) * 16);
     auto issue = [&](const Pages& pg, int t0, char* to) __attribute__((always_inline)) {
-        Ok ok;
-        const char* from[NB];
+        uint32_t ok = 0;                             // a bit each
 #pragma unroll
-        for (int n = 0; n < NB; ++n) {
-            // tokens without a page read page 0
-            ok.b[n] = pg.p[n] >= 0 && pg.p[n] < a.cache.n_pages;
-            from[n] = a.cache.rows + (ok.b[n] ? ((int64_t)pg.p[n] << sh) + ((t0 + 16 * n) & ((1 << sh) - 1)) : 0) * Cf::RB;
-        }
+        for (int n = 0; n < NB; ++n) ok |= (uint32_t)(pg.p[n] >= 0 && pg.p[n] < a.cache.n_pages) << n;
 #pragma unroll
-        for (int i = 0; i < Cf::MINE; ++i) {
-            // piece i * RW + rw of the tile; its 16 tokens' page, uniform
-            const int piece_ = i * RW + rw;
-            if (Cf::PIECES % RW != 0 && piece_ >= Cf::PIECES) break;
-            const char* base = from[0];
+        for (int e = 0; e < Cf::OCTETS; ++e) {
+            // eight rows; tokens without a page read page 0
+            const int o = rw * Cf::OCTETS + e;
+            int pid = pg.p[0];
 #pragma unroll
-            for (int n = 1; n < NB; ++n) base = piece_ >= n * (Cf::PIECES / NB) ? from[n] : base;
-            const int u = piece_ % (Cf::PIECES / NB) * 64 + lane, r = u / Cf::CH, ch = u - r * Cf::CH;
-            load_lds16(base + (uint32_t)(r * Cf::RB + (ch ^ swap_row<Cf::RB>(r)) * 16), to + piece_ * 1024);
+            for (int n = 1; n < NB; ++n) pid = o >= 2 * n ? pg.p[n] : pid;
+            const bool there = (ok >> (o / 2)) & 1;
+            const char* base = a.cache.rows + ((there ? ((int64_t)pid << sh) + ((t0 + 8 * o) & ((1 << sh) - 1)) : 0) * Cf::RB);
+#pragma unroll
+            for (int i = 0; i < Cf::PANELS; ++i) load_lds16(base + i * 128 + voff, to + (i * Cf::TILE + 8 * o) * 128);
+            if constexpr (Cf::HAS_TAIL)
+                if (lane < 32) load_lds16(base + Cf::PANELS * 128 + voff_tail, to + Cf::TAIL + 8 * o * 64);
         }
         return ok;
     };
     int p = t_lo + grp * Cf::TILE;
     const int rounds = (t_hi - t_lo + ROUND - 1) / ROUND;
-    Ok ok = {}, next = {};
+    uint32_t ok = 0, next = 0;
     Pages pg = pages(p);
     if (p < t_hi) ok = issue(pg, p, stage);
     pg = pages(p + ROUND);
@@ -400,14 +446,14 @@ latent_attention_kernel(const LatentAttentionArgs a, int items, int rb_n) {
         if (p + ROUND < t_hi) {
             next = issue(pg, p + ROUND, stage + (buf ^ 1) * Cf::STAGE);
             pg = pages(p + 2 * ROUND);
-            if constexpr (RW == 1) wait_loads<Cf::PIECES>();     // all but the next tile's
+            if constexpr (RW == 1) wait_loads<Cf::LOADS>();     // all but the next tile's
         } else {
             if constexpr (RW == 1) wait_loads<0>();
         }
         if (p < t_hi) {
-#pragma unroll
+#pragma unroll 1
             for (int n = 0; n < Cf::TILE / Cf::SUB; ++n)
-                attend_tile<BF, R, Cf::RB, Cf::SUB, FINE, WEIGHS>(stage + buf * Cf::STAGE + n * Cf::SUB * Cf::RB, q, ok.b + n * (Cf::SUB / 16),
+                attend_tile<BF, R, Cf, FINE, WEIGHS>(stage + buf * Cf::STAGE, n * Cf::SUB, q, ok >> (n * (Cf::SUB / 16)),
                                                                   p + n * Cf::SUB, s, word, scale2, score, lane, st);
         }
         ok = next;
