@@ -1,9 +1,8 @@
 // Sequences of the latent cache cut to a budget of tokens.
 //
-//   evict_select_kernel  one workgroup per sequence: the keys of its places (mass, or above
-//                        all masses where the token is protected) in registers, the keep-th
-//                        largest by three histograms of their bits, then the places that
-//                        stay, go or move
+//   evict_select_kernel  one workgroup per sequence: the keep-th largest key of its places (mass,
+//                        or above all masses where the token is protected) by three histograms
+//                        of the keys' bits, then the places that stay, go or move
 //   evict_move_kernel    the i-th kept row past the budget into the i-th place that came free
 //                        before it: as few rows move as can
 #include <hip/hip_runtime.h>
@@ -19,10 +18,11 @@ namespace ordermoe {
 namespace {
 
 constexpr int EV_THREADS = 1024, EV_WAVES = EV_THREADS / 64;
-constexpr int EV_KEYS = 32;                          // keys a thread holds
-constexpr int EV_BLOCK = EV_THREADS * EV_KEYS;       // places whose keys the registers hold
-static_assert(EV_KEYS * EV_WAVES <= EV_THREADS && EV_KEYS <= 32, "a count a thread, a bit a key");
-constexpr int EV_BITS = 11, EV_BINS = 1 << EV_BITS;  // of a histogram; shifts 21, 10 and (10 bits) 0
+constexpr int EV_BLOCK = 32768;                      // places whose keys LDS holds; those of longer sequences are made again
+constexpr int EV_WORDS = EV_BLOCK / 64;
+static_assert(EV_WORDS <= EV_THREADS && EV_BLOCK <= 1 << 15, "a thread a word, two counts in 32 bits");
+constexpr int EV_AHEAD = 8;                          // places of a thread whose reads are in flight together
+constexpr int EV_BINS = 2048;                        // of a histogram: 11 bits, 11 bits, 10 bits
 constexpr uint32_t EV_SAFE = 0xFFFFFFFFu;
 
 // a mass as an integer of the same order; NaN below all
@@ -32,39 +32,46 @@ __device__ inline uint32_t mass_key(float m) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-struct Scan {
-    uint32_t cnt[EV_THREADS], wave[EV_WAVES];
-};
-// cnt[] becomes the sum before each entry; returns the sum of all
-__device__ inline uint32_t scan(Scan& s, int tid) {
-    __syncthreads();
-    const int lane = tid & 63;
-    const uint32_t own = s.cnt[tid];
+// the sum over the threads before this one; all: over every thread
+__device__ inline uint32_t sum_before(uint32_t own, uint32_t* s_wave, int tid, uint32_t& all) {
+    const int lane = tid & 63, wave = tid >> 6;
     uint32_t inc = own;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
         const uint32_t v = __shfl_up(inc, o);
         if (lane >= o) inc += v;
     }
-    if (lane == 63) s.wave[tid >> 6] = inc;
     __syncthreads();
-    uint32_t base = 0, all = 0;
+    if (lane == 63) s_wave[wave] = inc;
+    __syncthreads();
+    uint32_t base = 0;
+    all = 0;
 #pragma unroll
     for (int w = 0; w < EV_WAVES; ++w) {
-        base += w < (tid >> 6) ? s.wave[w] : 0u;
-        all += s.wave[w];
+        base += w < wave ? s_wave[w] : 0u;
+        all += s_wave[w];
     }
-    s.cnt[tid] = base + inc - own;
-    __syncthreads();
-    return all;
+    return base + inc - own;
 }
-__device__ inline uint32_t lanes_below(uint64_t m) {
+__device__ inline uint32_t bits_below(uint64_t m) {
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
 }
+// the lowest k set bits of m
+__device__ inline uint64_t lowest(uint64_t m, int k) {
+    if (k >= __builtin_popcountll(m)) return m;
+    uint64_t r = 0;
+    for (; k > 0; --k) {
+        r |= m & (0 - m);
+        m &= m - 1;
+    }
+    return r;
+}
+// bits of the 64 places from p on that lie below n
+__device__ inline uint64_t below(int p, int n) { return n <= p ? 0ull : n - p >= 64 ? ~0ull : (1ull << (n - p)) - 1; }
 
 __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictArgs a) {
-    __shared__ uint32_t s_hist[EV_BINS];
-    __shared__ Scan s_a, s_b;
+    __shared__ uint32_t s_key[EV_BLOCK], s_hist[EV_BINS], s_off[EV_WORDS], s_wave[EV_WAVES];
+    __shared__ uint64_t s_stay[EV_WORDS], s_equal[EV_WORDS];
     __shared__ uint32_t s_bin, s_more;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = (int)block_number();
     if (b >= a.B) return;
@@ -87,110 +94,100 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictArg
         return;
     }
     const int64_t recent = (int64_t)a.seq_len[b] - a.recent;
-    const int blocks = (n + EV_BLOCK - 1) / EV_BLOCK;
-    uint32_t key[EV_KEYS];
-    auto load = [&](int p0) {
-#pragma unroll
-        for (int j = 0; j < EV_KEYS; ++j) {
-            key[j] = 0u;
-            if (p0 + j * EV_THREADS >= n) continue;
-            const int p = p0 + j * EV_THREADS + tid;
-            if (p < n) {
-                const int q = pos[p];
-                key[j] = q < a.first || q >= recent ? EV_SAFE : mass_key(mass[p]);
-            }
-        }
-    };
-    if (blocks == 1) load(0);
+    const bool cached = n <= EV_BLOCK;
     // the keep-th largest key, a digit at a time: `prefix` its digits so far, `more` of the keys that share them to keep
     uint32_t prefix = 0u, more = (uint32_t)keep;
-#pragma unroll
+    for (int i = tid; i < EV_BINS; i += EV_THREADS) s_hist[i] = 0u;
+    __syncthreads();
     for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : EV_BITS;
-        for (int i = tid; i < EV_BINS; i += EV_THREADS) s_hist[i] = 0u;
-        __syncthreads();
-        for (int k = 0; k < blocks; ++k) {
-            const int p0 = k * EV_BLOCK;
-            if (blocks > 1) load(p0);
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+        const bool again = pass > 0 && cached;
+        for (int64_t p0 = tid; p0 < n; p0 += EV_THREADS * EV_AHEAD) {
+            uint32_t key[EV_AHEAD];
+            if (again) {
 #pragma unroll
-            for (int j = 0; j < EV_KEYS; ++j) {
-                if (p0 + j * EV_THREADS >= n) continue;
-                const bool in = p0 + j * EV_THREADS + tid < n && (pass == 0 || (key[j] >> (shift + bits)) == prefix);
-                if (in) atomicAdd(&s_hist[(key[j] >> shift) & ((1u << bits) - 1u)], 1u);
+                for (int e = 0; e < EV_AHEAD; ++e) key[e] = s_key[(p0 + e * EV_THREADS) & (EV_BLOCK - 1)];
+            } else {
+                int32_t q[EV_AHEAD];
+                float m[EV_AHEAD];
+#pragma unroll
+                for (int e = 0; e < EV_AHEAD; ++e) {
+                    const int64_t p = p0 + e * EV_THREADS < n ? p0 + e * EV_THREADS : p0;
+                    q[e] = pos[p];
+                    m[e] = mass[p];
+                }
+#pragma unroll
+                for (int e = 0; e < EV_AHEAD; ++e) {
+                    key[e] = q[e] < a.first || q[e] >= recent ? EV_SAFE : mass_key(m[e]);
+                    if (cached && p0 + e * EV_THREADS < n) s_key[p0 + e * EV_THREADS] = key[e];
+                }
             }
+#pragma unroll
+            for (int e = 0; e < EV_AHEAD; ++e)
+                if (p0 + e * EV_THREADS < n && (pass == 0 || (key[e] >> (shift + bits)) == prefix))
+                    atomicAdd(&s_hist[(key[e] >> shift) & ((1u << bits) - 1u)], 1u);
         }
         __syncthreads();
         // from the top: thread t holds bins 2 (1023 - t) and the one above
         const int hi = EV_BINS - 1 - 2 * tid;
         const uint32_t h1 = s_hist[hi], h0 = s_hist[hi - 1];
-        s_a.cnt[tid] = h1 + h0;
-        scan(s_a, tid);
-        const uint32_t above = s_a.cnt[tid];
+        s_hist[hi] = s_hist[hi - 1] = 0u;
+        uint32_t all;
+        const uint32_t above = sum_before(h1 + h0, s_wave, tid, all);
         if (above < more && above + h1 >= more) { s_bin = (uint32_t)hi; s_more = more - above; }
         else if (above + h1 < more && above + h1 + h0 >= more) { s_bin = (uint32_t)(hi - 1); s_more = more - above - h1; }
         __syncthreads();
         prefix = (prefix << bits) | s_bin;
         more = s_more;
-        __syncthreads();
     }
     // places stay whose key is larger, and the first `more` of those whose key is equal
     uint32_t equal = 0, holes = 0, fills = 0;
-    for (int k = 0; k < blocks; ++k) {
-        const int p0 = k * EV_BLOCK;
-        if (blocks > 1) load(p0);
-        s_a.cnt[tid] = 0u;
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < EV_KEYS; ++j) {
-            if (p0 + j * EV_THREADS >= n) continue;
-            const uint64_t m = __builtin_amdgcn_ballot_w64(p0 + j * EV_THREADS + tid < n && key[j] == prefix);
-            if (lane == 0) s_a.cnt[j * EV_WAVES + wave] = (uint32_t)__builtin_popcountll(m);
+    for (int64_t p0 = 0; p0 < n; p0 += EV_BLOCK) {
+        const int words = (int)std::min<int64_t>(EV_WORDS, (n - p0 + 63) / 64);
+        for (int w = wave; w < words; w += EV_WAVES) {
+            const int64_t p = p0 + w * 64 + lane;
+            uint32_t key = 0u;
+            if (p < n) {
+                if (cached) {
+                    key = s_key[p & (EV_BLOCK - 1)];
+                } else {
+                    const int q = pos[p];
+                    key = q < a.first || q >= recent ? EV_SAFE : mass_key(mass[p]);
+                }
+            }
+            const uint64_t gt = __builtin_amdgcn_ballot_w64(p < n && key > prefix), eq = __builtin_amdgcn_ballot_w64(p < n && key == prefix);
+            if (lane == 0) { s_stay[w] = gt; s_equal[w] = eq; }
         }
-        const uint32_t eq_all = scan(s_a, tid);
-        uint32_t stay_bits = 0;
-#pragma unroll
-        for (int j = 0; j < EV_KEYS; ++j) {
-            if (p0 + j * EV_THREADS >= n) continue;
-            const int p = p0 + j * EV_THREADS + tid;
-            const bool eq = p < n && key[j] == prefix;
-            const uint64_t m = __builtin_amdgcn_ballot_w64(eq);
-            const bool stay = p < n && (key[j] > prefix || (eq && equal + s_a.cnt[j * EV_WAVES + wave] + lanes_below(m) < more));
-            stay_bits |= (uint32_t)stay << j;
-        }
-        equal += eq_all;
-        __syncthreads();                             // s_a has been read
-        s_a.cnt[tid] = 0u;
-        s_b.cnt[tid] = 0u;
         __syncthreads();
-#pragma unroll
-        for (int j = 0; j < EV_KEYS; ++j) {
-            if (p0 + j * EV_THREADS >= n) continue;
-            const int p = p0 + j * EV_THREADS + tid;
-            const bool stay = (stay_bits >> j) & 1;
-            const uint64_t hm = __builtin_amdgcn_ballot_w64(p < keep && !stay), fm = __builtin_amdgcn_ballot_w64(p >= keep && stay);
-            if (lane == 0) {
-                s_a.cnt[j * EV_WAVES + wave] = (uint32_t)__builtin_popcountll(hm);
-                s_b.cnt[j * EV_WAVES + wave] = (uint32_t)__builtin_popcountll(fm);
+        uint32_t all;
+        const uint64_t eq = tid < words ? s_equal[tid] : 0ull;
+        const uint32_t before = equal + sum_before((uint32_t)__builtin_popcountll(eq), s_wave, tid, all);
+        equal += all;
+        const int p = (int)p0 + tid * 64;
+        uint64_t stay = 0ull;
+        if (tid < words) {
+            stay = s_stay[tid] | (before < more ? lowest(eq, (int)(more - before)) : 0ull);
+            s_stay[tid] = stay;
+        }
+        const uint64_t front = tid < words ? below(p, keep) : 0ull;
+        const uint32_t own = (uint32_t)__builtin_popcountll(front & ~stay) | (uint32_t)__builtin_popcountll(stay & ~front) << 16;
+        const uint32_t off = sum_before(own, s_wave, tid, all);
+        if (tid < words) s_off[tid] = off;
+        __syncthreads();
+        for (int w = wave; w < words; w += EV_WAVES) {
+            const int q = (int)p0 + w * 64 + lane;
+            const uint64_t st = s_stay[w], fr = below((int)p0 + w * 64, keep), hm = fr & ~st, fm = st & ~fr;
+            const uint32_t o = s_off[w];
+            if ((hm >> lane) & 1) a.holes[(int64_t)b * a.holes_max + holes + (o & 0xFFFFu) + bits_below(hm)] = q;
+            if ((fm >> lane) & 1) a.fills[(int64_t)b * a.holes_max + fills + (o >> 16) + bits_below(fm)] = q;
+            if ((fr & st) >> lane & 1) {
+                kept[q] = q;
+                if (mass_out != mass) mass_out[q] = mass[q];
+                if (pos_out != pos) pos_out[q] = pos[q];
             }
         }
-        const uint32_t h_all = scan(s_a, tid), f_all = scan(s_b, tid);
-#pragma unroll
-        for (int j = 0; j < EV_KEYS; ++j) {
-            if (p0 + j * EV_THREADS >= n) continue;
-            const int p = p0 + j * EV_THREADS + tid;
-            const bool stay = (stay_bits >> j) & 1, hole = p < keep && !stay, fill = p >= keep && stay;
-            const uint64_t hm = __builtin_amdgcn_ballot_w64(hole), fm = __builtin_amdgcn_ballot_w64(fill);
-            if (hole) a.holes[(int64_t)b * a.holes_max + holes + s_a.cnt[j * EV_WAVES + wave] + lanes_below(hm)] = p;
-            if (fill) a.fills[(int64_t)b * a.holes_max + fills + s_b.cnt[j * EV_WAVES + wave] + lanes_below(fm)] = p;
-            if (p < keep && stay) {
-                kept[p] = p;
-                if (mass_out != mass) mass_out[p] = mass[p];
-                if (pos_out != pos) pos_out[p] = pos[p];
-            }
-        }
-        holes += h_all;
-        fills += f_all;
-        __syncthreads();
+        holes += all & 0xFFFFu;
+        fills += all >> 16;
     }
     if (tid == 0) { a.moves[b] = (int32_t)holes; a.len_out[b] = keep; }
 }
