@@ -324,7 +324,13 @@ struct EvictArgs {
     int32_t* holes;        // [B][holes_max] their new places
     int32_t* fills;        // [B][holes_max] their old ones
     int64_t holes_max;
+    uint32_t* part;        // long tables: [3][B][slices][2048] histograms of the keys' digits
+    uint32_t* above;       // [2][B][slices] keys of a slice that are larger by a digit
+    uint32_t* found;       // [2][B][2] the digits of the last key that stays, so far, and its rank among those that share them
 };
+// slices of a sequence of so many places, at most, and the words per sequence of the last three
+int evict_slices(int64_t places);
+size_t evict_slice_words(int64_t places);
 int launch_latent_evict(const EvictArgs& a, void* stream);
 
 // attention of prompts (prompt_attention.hip)

@@ -74,7 +74,13 @@ size_t evict_ws(const ordermoe_latent_cache* C, int32_t B, int32_t max_pages, in
     int32_t* m = c.take<int32_t>((size_t)std::max(B, 1));
     int32_t* h = c.take<int32_t>((size_t)B * most);
     int32_t* f = c.take<int32_t>((size_t)B * most);
-    if (a) { a->moves = m; a->holes = h; a->fills = f; a->holes_max = most; }
+    // (one taking for the three of them: the sizes go with the places that there are, which may be fewer than the table's)
+    uint32_t* w = c.take<uint32_t>((size_t)B * evict_slice_words(cap));
+    if (a) {
+        a->moves = m; a->holes = h; a->fills = f; a->holes_max = most;
+        const size_t slices = (size_t)evict_slices(cap);
+        a->part = w; a->above = w + 3 * (size_t)B * slices * 2048; a->found = a->above + 2 * (size_t)B * slices;
+    }
     return c.size();
 }
 
