@@ -37,6 +37,7 @@ namespace {
 
 constexpr int LA_TARGET = 512;                       // workgroups that a large batch is split into
 constexpr int LA_MIN_PIECE = 64;                     // tokens
+constexpr int LO_GROUPS = 256;                       // workgroups of the last product wished for
 constexpr float LA_LAG = 8.0f;                       // see attend_tile
 
 // waves that share a tile, for sequences of up to `rows` query rows: 16 rows each
@@ -506,23 +507,33 @@ latent_attention_kernel(const LatentAttentionArgs a, int items, int rb_n) {
     }
 }
 
-// 16 tokens (of the batch) of one head, DS of the head's elements: the rows' pieces added in order, divided, and
-// out = o W_v^T.  The matrix unit's rows are elements, its columns tokens.  DS / 32 pairs of element tiles go round the
-// waves; where they are fewer than the waves, the waves share the inner index.
-template <bool BF, int R, int D, int DS>
+// 16 / S tokens (of the batch) of one head, DS of the head's elements: the rows' pieces added in order, divided, and
+// out = o W_v^T.  A row has S sets of 16 lanes: set z adds pieces z, z + S, .., then the sets' sums are added.  The matrix
+// unit's rows are elements, its columns tokens.  DS / 32 pairs of element tiles go round the waves; where they are fewer
+// than the waves, the waves share the inner index, and their weights are on their way during the additions.
+template <bool BF, int R, int D, int DS, int S>
 __global__ void __launch_bounds__(256) latent_out_kernel(const LatentAttentionArgs a, int slices) {
-    constexpr int ES = BF ? 2 : 4, PITCH = R * ES + 16, U = 4;       // bytes of a row in LDS; pieces whose reads are in flight
-    constexpr int PAIRS = DS / 32, SHARE = 4 / PAIRS, KS = R * ES / 64 / SHARE;
+    constexpr int ES = BF ? 2 : 4, PITCH = R * ES + 16, U = 4, TOK = 16 / S;     // bytes of a row in LDS; pieces whose reads are in flight; tokens
+    constexpr int PAIRS = DS / 32, SHARE = 4 / PAIRS, KS = R * ES / 64 / SHARE, EARLY = SHARE > 1 ? KS : 0;
     __shared__ __attribute__((aligned(16))) char s_o[BF ? 2 : 1][16 * PITCH];
     __shared__ f32x4 s_acc[SHARE > 1 ? 4 : 1][2][64];
+    __shared__ float s_x[S == 16 ? 4 : 1][S == 16 ? R : 1], s_m[4], s_l[4];
     __shared__ int s_in[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t id = block_number(), rest = id / slices;
     const int d0 = (int)(id - rest * slices) * DS, h = (int)(rest % a.n_q);
-    const int64_t tb = rest / a.n_q * 16;
+    const int64_t tb = rest / a.n_q * TOK;
     if (tb >= a.T) return;
+    const int c = lane & 15, g = lane >> 4, pair = wave % PAIRS, share = wave / PAIRS;
+    const char* w = (const char*)a.w_v + ((int64_t)(h * D + d0 + 32 * pair + c) * R) * ES + (share * KS * 4 + g) * 16;
+    u32x4 early[EARLY > 0 ? EARLY : 1][2];
+#pragma unroll
+    for (int k = 0; k < EARLY; ++k) {
+        early[k][0] = *(const u32x4*)(w + 64 * k);
+        early[k][1] = *(const u32x4*)(w + 16 * R * ES + 64 * k);
+    }
     // the token's sequence: the number of sequences that end at or before it
-    const int slot = tid >> 4, u = tid & 15, t = (int)std::min<int64_t>(tb + slot, a.T);
+    const int slot = (tid >> 4) / S, z = (tid >> 4) % S, u = tid & 15, t = (int)std::min<int64_t>(tb + slot, a.T);
     int b = 0;
     for (int b0 = 0; b0 < a.B; b0 += 16) {
         const bool past = b0 + u < a.B && a.q_start[b0 + u + 1] <= t;
@@ -535,18 +546,18 @@ __global__ void __launch_bounds__(256) latent_out_kernel(const LatentAttentionAr
     const int i = t - s.first;
     in = in && i >= 0 && i < s.n;
     const int row = i * a.n_q + h, rows_max = a.max_q * a.n_q;
-    if (u == 0) s_in[slot] = in;
+    if (tid < 16) s_in[tid] = 0;
     const int pieces = in ? a.plan[2 * b + 1] : 0;
     const int64_t at = in ? (int64_t)a.plan[2 * b] * rows_max + row : 0;
     const f32x2* ml = (const f32x2*)a.part_ml;
     float m = -__builtin_inff(), l = 0.f, x[R / 16] = {};
-    for (int p = 0; p < pieces; p += U) {
+    for (int p = z; p < pieces; p += U * S) {
         f32x2 q[U];
         f32x4 v[U][R / 64];
         float top = m;
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            const int64_t pr = at + (int64_t)(p + k < pieces ? p + k : p) * rows_max;
+            const int64_t pr = at + (int64_t)(p + k * S < pieces ? p + k * S : p) * rows_max;
             q[k] = ml[pr];
 #pragma unroll
             for (int e = 0; e < R / 64; ++e) v[k][e] = *(const f32x4*)(a.part_o + pr * R + 4 * u + 64 * e);
@@ -560,50 +571,91 @@ __global__ void __launch_bounds__(256) latent_out_kernel(const LatentAttentionAr
         for (int e = 0; e < R / 16; ++e) x[e] *= al;
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            if (p + k >= pieces) break;
+            if (p + k * S >= pieces) break;
             const float f = q[k][0] == m ? 1.0f : __builtin_amdgcn_exp2f(q[k][0] - m);
             l += q[k][1] * f;
 #pragma unroll
             for (int e = 0; e < R / 16; ++e) x[e] += v[k][e / 4][e % 4] * f;
         }
     }
-    const float r = l == 0.f ? 0.f : 1.0f / l;
+    // four sets of a wave, then (S = 16) the waves'
+    if constexpr (S > 1) {
+        float top = fmaxf(m, __shfl_xor(m, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float f = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+        m = top;
+        l *= f;
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
 #pragma unroll
-    for (int e = 0; e < R / 64; ++e) {
-        float y[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) y[k] = x[4 * e + k] * r;
-        char* o = &s_o[0][slot * PITCH + (4 * u + 64 * e) * ES];
-        if constexpr (BF) {
-            float z[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) z[k] = y[k] - (float)(__bf16)y[k];
-            *(u32x2*)o = u32x2{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3])};
-            *(u32x2*)&s_o[BF ? 1 : 0][slot * PITCH + (4 * u + 64 * e) * ES] = u32x2{bf16_pair(z[0], z[1]), bf16_pair(z[2], z[3])};
-        } else {
-            *(f32x4*)o = f32x4{y[0], y[1], y[2], y[3]};
+        for (int e = 0; e < R / 16; ++e) {
+            x[e] *= f;
+            x[e] += __shfl_xor(x[e], 16);
+            x[e] += __shfl_xor(x[e], 32);
         }
     }
-    if (in && u == 0 && d0 == 0) {
-        if (a.lse) a.lse[(int64_t)t * a.n_q + h] = l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * LN2;
-        if (a.mass_out) {
-            f32x2* stat = (f32x2*)a.stat + (int64_t)b * rows_max + row;
-            *stat = f32x2{m == -__builtin_inff() ? 0.f : m, r};
+    __syncthreads();                                 // s_in is clear
+    if constexpr (S == 16) {
+        if (lane < 16) {
+#pragma unroll
+            for (int e = 0; e < R / 64; ++e) *(f32x4*)&s_x[wave][4 * u + 64 * e] = f32x4{x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]};
+        }
+        if (lane == 0) { s_m[wave] = m; s_l[wave] = l; }
+        __syncthreads();
+        m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+        l = 0.f;
+#pragma unroll
+        for (int e = 0; e < R / 16; ++e) x[e] = 0.f;
+        if (tid < 16) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float f = s_m[k] == m ? 1.0f : __builtin_amdgcn_exp2f(s_m[k] - m);
+                l += s_l[k] * f;
+#pragma unroll
+                for (int e = 0; e < R / 16; ++e) x[e] += s_x[k][4 * u + 64 * (e / 4) + e % 4] * f;
+            }
+        }
+    }
+    if (z == 0) {
+        const float r = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+        for (int e = 0; e < R / 64; ++e) {
+            float y[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) y[k] = x[4 * e + k] * r;
+            char* o = &s_o[0][slot * PITCH + (4 * u + 64 * e) * ES];
+            if constexpr (BF) {
+                float d[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) d[k] = y[k] - (float)(__bf16)y[k];
+                *(u32x2*)o = u32x2{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3])};
+                *(u32x2*)&s_o[BF ? 1 : 0][slot * PITCH + (4 * u + 64 * e) * ES] = u32x2{bf16_pair(d[0], d[1]), bf16_pair(d[2], d[3])};
+            } else {
+                *(f32x4*)o = f32x4{y[0], y[1], y[2], y[3]};
+            }
+        }
+        if (in && u == 0) {
+            s_in[slot] = 1;
+            if (d0 == 0) {
+                if (a.lse) a.lse[(int64_t)t * a.n_q + h] = l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * LN2;
+                if (a.mass_out) ((f32x2*)a.stat)[(int64_t)b * rows_max + row] = f32x2{m == -__builtin_inff() ? 0.f : m, r};
+            }
         }
     }
     __syncthreads();
-    const int c = lane & 15, g = lane >> 4, pair = wave % PAIRS, share = wave / PAIRS;
     f32x4 acc[2] = {};
-    const char* w = (const char*)a.w_v + ((int64_t)(h * D + d0 + 32 * pair + c) * R) * ES + (share * KS * 4 + g) * 16;
-    const char* o = &s_o[0][c * PITCH + (share * KS * 4 + g) * 16];
+    // (tokens past TOK: a row that is there, for columns that nobody reads)
+    const char* o = &s_o[0][(c < TOK ? c : 0) * PITCH + (share * KS * 4 + g) * 16];
+    const char* o_lo = &s_o[BF ? 1 : 0][(c < TOK ? c : 0) * PITCH + (share * KS * 4 + g) * 16];
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
-        const u32x4 w0 = *(const u32x4*)(w + 64 * k), w1 = *(const u32x4*)(w + 16 * R * ES + 64 * k);
+        const u32x4 w0 = k < EARLY ? early[k < EARLY ? k : 0][0] : *(const u32x4*)(w + 64 * k);
+        const u32x4 w1 = k < EARLY ? early[k < EARLY ? k : 0][1] : *(const u32x4*)(w + 16 * R * ES + 64 * k);
         const u32x4 hi = *(const u32x4*)(o + 64 * k);
         acc[0] = mma16<BF>(w0, hi, acc[0]);
         acc[1] = mma16<BF>(w1, hi, acc[1]);
         if constexpr (BF) {
-            const u32x4 lo = *(const u32x4*)(o + 16 * PITCH + 64 * k);
+            const u32x4 lo = *(const u32x4*)(o_lo + 64 * k);
             acc[0] = mma16<BF>(w0, lo, acc[0]);
             acc[1] = mma16<BF>(w1, lo, acc[1]);
         }
@@ -677,17 +729,22 @@ int launch_rows(const LatentAttentionArgs& a, hipStream_t st) {
     }
     {
         KernelTimer kt_("latent_out", st);
-        const int64_t blocks = (a.T + 15) / 16 * a.n_q;
-        auto go = [&](auto d, auto ds) {
-            constexpr int D = decltype(d)::value, DS = decltype(ds)::value;
-            latent_out_kernel<BF, R, D, DS><<<grid_of(blocks * (D / DS)), dim3(256), 0, st>>>(a, D / DS);
+        // as few sets a row as give every CU a workgroup; few rows: slices of the head's elements too
+        auto go = [&](auto d, auto ds, auto sets) {
+            constexpr int D = decltype(d)::value, DS = decltype(ds)::value, S = decltype(sets)::value, TOK = 16 / S;
+            latent_out_kernel<BF, R, D, DS, S><<<grid_of((a.T + TOK - 1) / TOK * a.n_q * (D / DS)), dim3(256), 0, st>>>(a, D / DS);
         };
-        using std::integral_constant;
-        const bool few = blocks < 512;
-        if (a.head_dim == 64) few ? go(integral_constant<int, 64>{}, integral_constant<int, 32>{})
-                                  : go(integral_constant<int, 64>{}, integral_constant<int, 64>{});
-        else few ? go(integral_constant<int, 128>{}, integral_constant<int, 32>{})
-                 : go(integral_constant<int, 128>{}, integral_constant<int, 128>{});
+        auto of = [&](auto d) {
+            using N1 = std::integral_constant<int, 1>;
+            using N4 = std::integral_constant<int, 4>;
+            using N16 = std::integral_constant<int, 16>;
+            if ((a.T + 15) / 16 * a.n_q >= LO_GROUPS) go(d, d, N1{});
+            else if ((a.T + 3) / 4 * a.n_q >= LO_GROUPS) go(d, d, N4{});
+            else if (a.T * a.n_q >= LO_GROUPS) go(d, d, N16{});
+            else go(d, std::integral_constant<int, 32>{}, N16{});
+        };
+        if (a.head_dim == 64) of(std::integral_constant<int, 64>{});
+        else of(std::integral_constant<int, 128>{});
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return (int)e;
     }
