@@ -67,6 +67,10 @@ __device__ inline Seq uniform(const Seq& s, int l) {
                __builtin_amdgcn_readlane(s.len, l)};
 }
 
+__device__ inline int64_t first_lane(int64_t x) {
+    return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)x) | (int64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32;
+}
+
 // The tokens of a piece, by one wave: as many, a multiple of a round of the waves, as give about LA_TARGET
 // workgroups in all, but at least total * rb_n / (2 LA_TARGET): that bounds the pieces by 2 LA_TARGET / rb_n + B.
 __device__ inline int piece_tokens(const LatentAttentionArgs& a, int rb_n, int rw, int round, const Seq& mine, int lane) {
@@ -76,11 +80,15 @@ __device__ inline int piece_tokens(const LatentAttentionArgs& a, int rb_n, int r
         total += s.n > 0 ? s.len : 0;
         blocks += s.n > 0 ? (int64_t)s.len * row_blocks(s.n * a.n_q, rw) : 0;
     }
+    // (to lane 0, from as many lanes as there are sequences)
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) {
+        if (o >= a.B) continue;
         total += __shfl_xor(total, o);
-        blocks += __shfl_xor(blocks, o);
+        if (rb_n > 1) blocks += __shfl_xor(blocks, o);
     }
+    total = first_lane(total);
+    blocks = rb_n > 1 ? first_lane(blocks) : total;
     int64_t p = (blocks + LA_TARGET - 1) / LA_TARGET;
     const int64_t least = (total * rb_n + 2 * LA_TARGET - 1) / (2 * LA_TARGET);
     p = p < least ? least : p;
@@ -107,6 +115,7 @@ __device__ inline Seq find_item(const LatentAttentionArgs& a, int piece, int ite
         int inc = cnt;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
+            if (o >= a.B) continue;
             const int v = __shfl_up(inc, o);
             if (lane >= o) inc += v;
         }
@@ -158,6 +167,10 @@ __device__ inline void wait_loads() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
     __builtin_amdgcn_sched_barrier(0);
 }
+
+// The bare barrier: what waves have waited for themselves is there for all behind it (__syncthreads() would wait for
+// every load that is on its way)
+__device__ inline void lds_barrier() { asm volatile("s_barrier" ::: "memory"); }
 
 // of SUB tokens from row r0 of a tile on, those whose row holds an infinity or a NaN, a bit each, by one wave
 template <bool BF, typename Cf>
@@ -254,7 +267,7 @@ __device__ inline __attribute__((always_inline)) void add_weighted(const char* s
 // weights to bf16 leaves out as well.
 template <bool BF, int R, typename Cf, bool FINE, bool WEIGHS>
 __device__ inline __attribute__((always_inline)) void attend_tile(const char* st, int r0, const u32x4* q, uint32_t ok, int t0, const Seq& s,
-                                                                  uint64_t word, float scale2, float* score, int lane,
+                                                                  uint64_t word, bool in, float scale2, float* score, int lane,
                                                                   State<R>& state) {
     constexpr int SUB = Cf::SUB, NB = SUB / 16, KS = Cf::KS, PANEL = Cf::TILE * 128;
     const int c = lane & 15, g = lane >> 4;
@@ -287,8 +300,8 @@ __device__ inline __attribute__((always_inline)) void attend_tile(const char* st
     for (int n = 0; n < NB; ++n) sc[n] = sc[n] * scale2;
     uint32_t bad = 0;
     if (edge) {
-        bad = not_finite<BF, Cf>(st, r0, lane);
-        uint32_t seen = 0;
+        // (places past the end hold the last token's row, see issue: what all rows see keeps nothing from any)
+        uint32_t seen = 0, there = 0;
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -296,9 +309,13 @@ __device__ inline __attribute__((always_inline)) void attend_tile(const char* st
                 const int p = t0 + 16 * n + 4 * g + i, j = p - s.ctx;
                 const bool see = ((ok >> n) & 1) && p < s.len && (j < 0 || ((word >> (j & 63)) & 1));
                 seen |= (uint32_t)see << (16 * n + 4 * g + i);
+                there |= (uint32_t)(p < s.len) << (16 * n + 4 * g + i);
                 sc[n][i] = see ? sc[n][i] : ninf;
             }
-        if (bad & seen) state.l = __builtin_nanf("");        // (what is no number is taken as 0 below)
+        if (__builtin_amdgcn_ballot_w64(in && seen != there)) {
+            bad = not_finite<BF, Cf>(st, r0, lane);
+            if (bad & seen) state.l = __builtin_nanf("");    // (what is no number is taken as 0 below)
+        }
     }
     if constexpr (WEIGHS) {
         if (score) {
@@ -428,11 +445,28 @@ latent_attention_kernel(const LatentAttentionArgs a, int items, int rb_n) {
 #pragma unroll
             for (int n = 1; n < NB; ++n) pid = o >= 2 * n ? pg.p[n] : pid;
             const bool there = (ok >> (o / 2)) & 1;
-            const char* base = a.cache.rows + ((there ? ((int64_t)pid << sh) + ((t0 + 8 * o) & ((1 << sh) - 1)) : 0) * Cf::RB);
+            const char* base = a.cache.rows + (there ? ((int64_t)pid << sh) + ((t0 + 8 * o) & ((1 << sh) - 1)) : 0) * Cf::RB;
+            const int last = s.len - 1 - (t0 + 8 * o);
+            if (last >= 7) {
 #pragma unroll
-            for (int i = 0; i < Cf::PANELS; ++i) load_lds16(base + i * 128 + voff, to + (i * Cf::TILE + 8 * o) * 128);
-            if constexpr (Cf::HAS_TAIL)
-                if (lane < 32) load_lds16(base + Cf::PANELS * 128 + voff_tail, to + Cf::TAIL + 8 * o * 64);
+                for (int i = 0; i < Cf::PANELS; ++i) load_lds16(base + i * 128 + voff, to + (i * Cf::TILE + 8 * o) * 128);
+                if constexpr (Cf::HAS_TAIL)
+                    if (lane < 32) load_lds16(base + Cf::PANELS * 128 + voff_tail, to + Cf::TAIL + 8 * o * 64);
+            } else {
+                // places past the end, which nothing may have been written to, take the last token's row
+                const int end = s.len - 1 - t0, e16 = end >> 4;
+                int pe = pg.p[0];
+#pragma unroll
+                for (int n = 1; n < NB; ++n) pe = e16 == n ? pg.p[n] : pe;
+                const char* row = a.cache.rows + (((ok >> e16) & 1) ? ((int64_t)pe << sh) + ((s.len - 1) & ((1 << sh) - 1)) : 0) * Cf::RB;
+                const int r = lane >> 3, rt = (lane >> 2) & 7;
+                const char* f = r <= last ? base + voff : row + (voff - r * Cf::RB);
+                const char* ft = rt <= last ? base + voff_tail : row + (voff_tail - rt * Cf::RB);
+#pragma unroll
+                for (int i = 0; i < Cf::PANELS; ++i) load_lds16(f + i * 128, to + (i * Cf::TILE + 8 * o) * 128);
+                if constexpr (Cf::HAS_TAIL)
+                    if (lane < 32) load_lds16(ft + Cf::PANELS * 128, to + Cf::TAIL + 8 * o * 64);
+            }
         }
         return ok;
     };
@@ -443,19 +477,27 @@ latent_attention_kernel(const LatentAttentionArgs a, int items, int rb_n) {
     if (p < t_hi) ok = issue(pg, p, stage);
     pg = pages(p + ROUND);
     for (int k = 0, buf = 0; k < rounds; ++k, p += ROUND, buf ^= 1) {
-        if constexpr (RW > 1) __syncthreads();       // the tile has arrived, and the one before has been read
+        if constexpr (RW > 1)
+            if (k > 0) {
+                wait_loads<0>();
+                __syncthreads();                     // the tile has arrived, and the one before has been read
+            }
         if (p + ROUND < t_hi) {
             next = issue(pg, p + ROUND, stage + (buf ^ 1) * Cf::STAGE);
             pg = pages(p + 2 * ROUND);
-            if constexpr (RW == 1) wait_loads<Cf::LOADS>();     // all but the next tile's
-        } else {
-            if constexpr (RW == 1) wait_loads<0>();
+            if (RW == 1 || k == 0) wait_loads<Cf::LOADS>();      // all but the next tile's
+        } else if (RW == 1 || k == 0) {
+            wait_loads<0>();
         }
+        if constexpr (RW > 1)
+            if (k == 0) lds_barrier();               // the first tile has arrived
         if (p < t_hi) {
 #pragma unroll 1
-            for (int n = 0; n < Cf::TILE / Cf::SUB; ++n)
+            for (int n = 0; n < Cf::TILE / Cf::SUB; ++n) {
+                if (p + n * Cf::SUB >= t_hi) break;
                 attend_tile<BF, R, Cf, FINE, WEIGHS>(stage + buf * Cf::STAGE, n * Cf::SUB, q, ok >> (n * (Cf::SUB / 16)),
-                                                                  p + n * Cf::SUB, s, word, scale2, score, lane, st);
+                                                                  p + n * Cf::SUB, s, word, in, scale2, score, lane, st);
+            }
         }
         ok = next;
     }
@@ -514,7 +556,7 @@ latent_attention_kernel(const LatentAttentionArgs a, int items, int rb_n) {
 template <bool BF, int R, int D, int DS, int S>
 __global__ void __launch_bounds__(256) latent_out_kernel(const LatentAttentionArgs a, int slices) {
     constexpr int ES = BF ? 2 : 4, PITCH = R * ES + 16, U = 4, TOK = 16 / S;     // bytes of a row in LDS; pieces whose reads are in flight; tokens
-    constexpr int PAIRS = DS / 32, SHARE = 4 / PAIRS, KS = R * ES / 64 / SHARE, EARLY = SHARE > 1 ? KS : 0;
+    constexpr int PAIRS = DS / 32, SHARE = 4 / PAIRS, KS = R * ES / 64 / SHARE, EARLY = SHARE > 1 ? KS : 4;
     __shared__ __attribute__((aligned(16))) char s_o[BF ? 2 : 1][16 * PITCH];
     __shared__ f32x4 s_acc[SHARE > 1 ? 4 : 1][2][64];
     __shared__ float s_x[S == 16 ? 4 : 1][S == 16 ? R : 1], s_m[4], s_l[4];
@@ -526,7 +568,7 @@ __global__ void __launch_bounds__(256) latent_out_kernel(const LatentAttentionAr
     if (tb >= a.T) return;
     const int c = lane & 15, g = lane >> 4, pair = wave % PAIRS, share = wave / PAIRS;
     const char* w = (const char*)a.w_v + ((int64_t)(h * D + d0 + 32 * pair + c) * R) * ES + (share * KS * 4 + g) * 16;
-    u32x4 early[EARLY > 0 ? EARLY : 1][2];
+    u32x4 early[EARLY][2];
 #pragma unroll
     for (int k = 0; k < EARLY; ++k) {
         early[k][0] = *(const u32x4*)(w + 64 * k);
@@ -740,7 +782,7 @@ int launch_rows(const LatentAttentionArgs& a, hipStream_t st) {
             using N16 = std::integral_constant<int, 16>;
             if ((a.T + 15) / 16 * a.n_q >= LO_GROUPS) go(d, d, N1{});
             else if ((a.T + 3) / 4 * a.n_q >= LO_GROUPS) go(d, d, N4{});
-            else if (a.T * a.n_q >= LO_GROUPS) go(d, d, N16{});
+            else if ((a.T + 3) / 4 * a.n_q * (decltype(d)::value / 32) >= LO_GROUPS) go(d, std::integral_constant<int, 32>{}, N4{});
             else go(d, std::integral_constant<int, 32>{}, N16{});
         };
         if (a.head_dim == 64) of(std::integral_constant<int, 64>{});

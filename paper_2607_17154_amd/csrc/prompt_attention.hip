@@ -63,6 +63,7 @@ __device__ inline bool find_block(const PromptArgs& a, int64_t item, int lane, S
         int inc = cnt;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
+            if (o >= a.B) continue;
             const int v = __shfl_up(inc, o);
             if (lane >= o) inc += v;
         }
@@ -115,6 +116,16 @@ __device__ inline void issue_rows(__amdgpu_buffer_rsrc_t rs, uint32_t stride, ch
 __device__ inline __amdgpu_buffer_rsrc_t make_rsrc(const void* base, uint32_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, (int)bytes, 0x00020000);
 }
+
+template <int N>
+__device__ inline void wait_loads() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+// The bare barrier: what waves have waited for themselves is there for all behind it (__syncthreads() would wait for
+// every load that is on its way)
+__device__ inline void lds_barrier() { asm volatile("s_barrier" ::: "memory"); }
 
 // Positions of a tile's V that hold an infinity or a NaN, a bit each, by one wave
 template <bool BF, int D>
@@ -305,10 +316,19 @@ __global__ void __launch_bounds__(64 * PA_WAVES, 2) prompt_attention_kernel(cons
             issue_rows<Lay::RBR, TILE, 0, BF>(make_rsrc((const char*)a.r + at * Lay::RBR, left * Lay::RBR), Lay::RBR, to + Lay::R, wave, lane);
         issue_rows<Lay::RBD, TILE, 1, BF>(make_rsrc((const char*)a.v + off, (left - 1) * stride + D * ES), stride, to + Lay::V, wave, lane);
     };
+    // (the first two tiles are on their way together)
     if (end > 0) issue(0, mem);
     for (int t0 = 0, buf = 0; t0 < end; t0 += TILE, buf ^= 1) {
-        __syncthreads();                                 // the tile has arrived, and the one before has been read
+        if (t0 > 0) {
+            wait_loads<0>();
+            __syncthreads();                             // the tile has arrived, and the one before has been read
+        }
         if (t0 + TILE < end) issue(t0 + TILE, mem + (buf ^ 1) * Lay::STAGE);
+        if (t0 == 0) {
+            if (TILE < end) wait_loads<Lay::STAGE / 1024 / PA_WAVES>();
+            else wait_loads<0>();
+            lds_barrier();
+        }
         attend_tile<BF, D, ROT>(mem + buf * Lay::STAGE, q, scale2, t0 + TILE > all, lim - t0, lane, st);
     }
     if (!in) return;
