@@ -689,7 +689,7 @@ int ordermoe_latent_write(const ordermoe_latent_cache* C, const ordermoe_latent_
  *   ws       dev, of the size below (weighs: 1 where mass_out will be given), in use until the stream
  *            passes the call.  With weighs it holds the scores, 4 B max_q n_q max_pages page_size bytes of it.
  * Limits as there, but n_q <= 128; 0 <= T * n_q < 2^31; decay finite. */
-#define ORDERMOE_LATENT_FINE_ROWS 64
+#define ORDERMOE_LATENT_FINE_ROWS 32
 size_t ordermoe_latent_attention_workspace_size(const ordermoe_latent_cache* C, const ordermoe_latent_heads* H, int32_t B,
                                                 int32_t max_q, int32_t max_pages, int32_t weighs);
 int ordermoe_latent_attention(const ordermoe_latent_cache* C, const ordermoe_latent_heads* H, const void* q, int64_t T,

@@ -297,7 +297,8 @@ struct LatentAttentionArgs {
     float* mass_out;
     int64_t mass_stride;
     // workspace
-    int32_t* plan;         // [B][2] first work item of each sequence, its pieces
+    int64_t items;         // pieces that it holds
+    int32_t* plan;         // [B][2] first piece of each sequence, and how many
     float* part_ml;        // [items][max_q n_q][2] maximum and sum of each piece's rows
     float* part_o;         // [items][max_q n_q][rank] its sums
     float* stat;           // [B][max_q n_q][2] maximum of each row, and 1 / its sum (with mass_out)

@@ -59,13 +59,14 @@ int check_attention(const ordermoe_latent_cache* C, const ordermoe_latent_heads*
 }
 size_t attention_ws(const ordermoe_latent_cache* C, const ordermoe_latent_heads* H, int32_t B, int32_t max_q, int32_t max_pages,
                     bool weighs, Carver& c, LatentAttentionArgs* a) {
-    const size_t rows = (size_t)max_q * H->n_q, parts = (size_t)latent_items(C->dtype, H->n_q, B, max_q) * rows;
+    const int64_t items = latent_items(C->dtype, H->n_q, B, max_q);
+    const size_t rows = (size_t)max_q * H->n_q, parts = (size_t)items * rows;
     int32_t* pl = c.take<int32_t>((size_t)std::max(B, 1) * 2);
     float* ml = c.take<float>(parts * 2);
     float* po = c.take<float>(parts * C->rank);
     float* st = c.take<float>(weighs ? B * rows * 2 : 0);
     float* sc = c.take<float>(weighs ? B * rows * max_pages * C->page_size : 0);
-    if (a) { a->plan = pl; a->part_ml = ml; a->part_o = po; a->stat = st; a->score = sc; }
+    if (a) { a->items = items; a->plan = pl; a->part_ml = ml; a->part_o = po; a->stat = st; a->score = sc; }
     return c.size();
 }
 

@@ -1,27 +1,31 @@
 // Attention of drafted tokens over the latent cache: every head's absorbed query on the
 // same rows [c_p | r_p], of which the first part is the value too.
 //
-//   latent_attention_kernel  one workgroup per (work item, block of 16 RW query rows).  A work
-//                            item is a piece of one sequence's cache.  RW waves that take 16 rows
-//                            each share a tile of its tokens in LDS; the tiles go round the groups of
-//                            such waves, every group with a running maximum, sum and output of its
-//                            own, joined in LDS at the end -> partial sums (memory)
+//   latent_attention_kernel  one workgroup per (work item, block of 16 or 32 query rows).  A work
+//                            item is a piece of one sequence's cache, gone through in tiles that all
+//                            waves share -> sums relative to the piece's maximum (memory)
+//   latent_rows_kernel       the same for sequences of many query rows: blocks of 128, 16 of them
+//                            a wave
 //   latent_out_kernel        the pieces' sums added in order, relative to their largest maximum,
 //                            divided, and taken through W_v: 16 tokens of one head
 //   latent_mass_kernel       the weight that each position got, from the scores that the first
 //                            kernel wrote and the rows' final maximum and sum
 // The query rows of a sequence are its n_b tokens times the heads: row = token * n_q + head.
 //
-// A tile (bf16; c = lane % 16, g = lane / 16):
-//   S^T = K Q^T   v_mfma_f32_16x16x32_bf16; rows: 16 tokens, columns: 16 query rows.  Maximum and sum belong
-//                 to a column, that is to a lane.
-//   O^T = C^T P^T v_mfma_f32_16x16x32_bf16, or 16x16x16 where a tile has 16 tokens; rows: 16 elements of the latent
-//                 vector, columns: 16 query rows.  S^T leaves lane (c, g) the weights of query row c for tokens
-//                 4g .. 4g + 3 of each 16: the inner indexes of its P^T operand, when C^T's lanes hold the
-//                 same tokens, which turned reads of the rows in LDS give them.  So the weights never
-//                 leave their registers.
-// fp32 runs the same tile with v_mfma_f32_16x16x4_f32.  Rows go straight from memory into LDS, a group's next tile
-// while it attends to one.
+// A tile of 64 tokens (bf16; c = lane % 16, g = lane / 16; fp32: 32 tokens, v_mfma_f32_16x16x4_f32):
+//   S^T = K Q^T   v_mfma_f32_16x16x32_bf16; rows: 16 tokens, columns: 16 query rows.  Maximum and sum belong to a
+//                 column, that is to a lane.
+//   O^T = C^T P^T rows: 16 elements of the latent vector, columns: 16 query rows, tokens the inner index; C^T by turned
+//                 reads of the rows in LDS (where tokens lie apart).
+// latent_attention_kernel: a wave forms the scores of 16 tokens and 16 query rows, and the sums of its share of the
+// elements, so that every row in LDS is read once for them and the outputs take few registers.  The maxima of a tile
+// go through LDS, so that all waves come to the same reference, and so do the weights: three barriers a tile.
+// latent_rows_kernel: a wave has 16 rows and all elements; the weights of two score blocks (tokens 4g .. 4g + 3 of each in
+// lane (c, g)) are the inner indexes of its second product when C^T's lanes hold the same tokens, so they never leave their
+// registers: one barrier a tile.  It reads each row in LDS eight times for 128 query rows, which bounds it (128 bytes a
+// cycle); blocks of 64 rows in the first way read it less than half as often but waited for each other: trees of 64 over
+// 30000-100000 tokens 993 us for 513.
+// Rows go straight from memory into LDS, the next tile while one is attended to.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -37,14 +41,13 @@ namespace {
 
 constexpr int LA_TARGET = 512;                       // workgroups that a large batch is split into
 constexpr int LA_MIN_PIECE = 64;                     // tokens
+constexpr int LA_FEW = 32;                           // query rows up to which latent_attention_kernel takes a batch
 constexpr int LO_GROUPS = 256;                       // workgroups of the last product wished for
 constexpr float LA_LAG = 8.0f;                       // see attend_tile
 
-// waves that share a tile, for sequences of up to `rows` query rows: 16 rows each
-__host__ __device__ inline int row_waves(int dtype, int rows) {
-    return dtype != ORDERMOE_BF16 || rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8;
-}
-__host__ __device__ inline int row_blocks(int rows, int rw) { return (rows + 16 * rw - 1) / (16 * rw); }
+// 16-row tiles of query rows per workgroup, for sequences of up to `rows` query rows (8: latent_rows_kernel)
+__host__ __device__ inline int row_tiles(int dtype, int rows) { return rows <= 16 ? 1 : rows <= LA_FEW || dtype != ORDERMOE_BF16 ? 2 : 8; }
+__host__ __device__ inline int row_blocks(int rows, int mt) { return (rows + 16 * mt - 1) / (16 * mt); }
 
 struct Seq {
     int first, n, ctx, len;     // first token, drafted tokens, cached tokens before them, positions
@@ -73,12 +76,12 @@ __device__ inline int64_t first_lane(int64_t x) {
 
 // The tokens of a piece, by one wave: as many, a multiple of a round of the waves, as give about LA_TARGET
 // workgroups in all, but at least total * rb_n / (2 LA_TARGET): that bounds the pieces by 2 LA_TARGET / rb_n + B.
-__device__ inline int piece_tokens(const LatentAttentionArgs& a, int rb_n, int rw, int round, const Seq& mine, int lane) {
+__device__ inline int piece_tokens(const LatentAttentionArgs& a, int rb_n, int mt, int round, const Seq& mine, int lane) {
     int64_t total = 0, blocks = 0;
     for (int b = lane; b < a.B; b += 64) {
         const Seq s = b < 64 ? mine : sequence(a, b);
         total += s.n > 0 ? s.len : 0;
-        blocks += s.n > 0 ? (int64_t)s.len * row_blocks(s.n * a.n_q, rw) : 0;
+        blocks += s.n > 0 ? (int64_t)s.len * row_blocks(s.n * a.n_q, mt) : 0;
     }
     // (to lane 0, from as many lanes as there are sequences)
 #pragma unroll
@@ -140,26 +143,54 @@ __device__ inline Seq find_item(const LatentAttentionArgs& a, int piece, int ite
 // A tile of TILE rows of RB bytes in LDS: panels of 128 bytes of every row, chunk (of 16 bytes) ch of row r at ch ^ r % 8, so
 // that the reads of one chunk of eight rows lie on distinct banks; and what is left over, 64 bytes, as rows of their own,
 // at ch ^ r / 2 % 4.  A wave's load of 1 KB is eight rows of a panel: one offset per lane serves all of them.
-template <bool BF, int R, int ROT, int RW>
+template <bool BF, int R_, int ROT, int MT>
 struct Config {
-    static constexpr int ES = BF ? 2 : 4, RB = (R + ROT) * ES;
-    static constexpr int NW = RW > 1 ? 8 : BF ? 4 : 2, GROUPS = NW / RW;     // waves, groups of them
-    static constexpr int TILE = RW > 1 ? 8 * RW : 16;                        // tokens of a group's tile
-    static constexpr int SUB = TILE < 32 ? 16 : 32;                          // tokens that are attended to at a time
+    static constexpr int ES = BF ? 2 : 4, R = R_, RB = (R + ROT) * ES;
+    static constexpr int NW = BF && MT > 1 ? 8 : 4;                          // waves
+    static constexpr int QT = BF ? 4 : 2, TILE = 16 * QT;                    // 16-token blocks, tokens of a tile
+    static constexpr int CT = R / 16 / NW;                                   // 16-element tiles whose sums a wave holds
     static constexpr int PANELS = RB / 128, TAIL = PANELS * TILE * 128;      // whole panels, where the rest begins
     static constexpr bool HAS_TAIL = RB % 128 != 0;
-    static constexpr int STAGE = TILE * RB, OCTETS = TILE / 8 / RW;          // bytes of a tile, a wave's eights of its rows
-    static constexpr int LOADS = OCTETS * (PANELS + HAS_TAIL);               // of a wave for a tile
+    static constexpr int STAGE = TILE * RB, OCTETS = TILE / 8 / NW;          // bytes of a tile, a wave's eights of its rows
     static constexpr int KS = RB / 64;                                       // steps of the first product
+    static constexpr int PP = TILE * ES + 16;                                // bytes of a row of weights in LDS
     static constexpr int LD = R + 4;                                         // floats of a row of sums in LDS
-    static_assert(RB % 64 == 0 && R * ES % 128 == 0 && GROUPS * 16 * LD * 4 <= GROUPS * 2 * STAGE, "whole chunks, the sums fit");
+    static_assert(RB % 64 == 0 && R * ES % 128 == 0 && OCTETS * 8 * NW == TILE && (MT == 8 || CT * 16 * NW == R), "whole shares");
 };
 
-// page of the tile at t0 (16 tokens never cross a page), -1: none; uniform, through the scalar cache
-__device__ inline int tile_page(const LatentAttentionArgs& a, const int32_t* table, int t0, int len) {
-    const __attribute__((address_space(4))) int32_t* t = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)table;
-    return t0 < len ? t[t0 >> a.cache.page_shift] : -1;
-}
+// The pages of a piece's tiles, 16 tokens each (they never cross a page), -1: none.  Lane i holds the page of block 64 j + i,
+// so that the loop has no loads through the scalar cache: those return in no order with reads of LDS, which would all wait
+// for them.
+template <int QT>
+struct Pages {
+    const int32_t* table;
+    int t_lo, t_hi, shift, now, after;
+    __device__ int load(int j, int lane) const {
+        const int64_t t = t_lo + 16 * (64 * (int64_t)j + lane);
+        return t < t_hi ? table[t >> shift] : -1;
+    }
+    __device__ void start(const LatentAttentionArgs& a, int b, int lo, int hi, int lane) {
+        table = a.page_table + (int64_t)b * a.max_pages;
+        t_lo = lo;
+        t_hi = hi;
+        shift = a.cache.page_shift;
+        now = load(0, lane);
+        after = load(1, lane);
+    }
+    struct Tile { int p[QT]; };
+    // of tile k; to be called for one tile after the other
+    __device__ Tile tile(int k, int lane) {
+        const int i = k * QT;
+        if (i > 0 && (i & 63) == 0) {
+            now = after;
+            after = load(i / 64 + 1, lane);
+        }
+        Tile t;
+#pragma unroll
+        for (int n = 0; n < QT; ++n) t.p[n] = __builtin_amdgcn_readlane(now, (i & 63) + n);
+        return t;
+    }
+};
 
 template <int N>
 __device__ inline void wait_loads() {
@@ -168,384 +199,516 @@ __device__ inline void wait_loads() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// The bare barrier: what waves have waited for themselves is there for all behind it (__syncthreads() would wait for
-// every load that is on its way)
-__device__ inline void lds_barrier() { asm volatile("s_barrier" ::: "memory"); }
+// A barrier behind which the waves' LDS writes, and the loads that they have waited for, are there for all
+// (__syncthreads() would wait for every load that is on its way)
+__device__ inline void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// of SUB tokens from row r0 of a tile on, those whose row holds an infinity or a NaN, a bit each, by one wave
+// The wave's rows of the tile at t0 on their way into LDS; returns a bit for each 16 tokens: their page is in the cache
+template <typename Cf>
+__device__ inline __attribute__((always_inline)) uint32_t issue_tile(const LatentAttentionArgs& a, const Seq& s, const typename Pages<Cf::QT>::Tile& pg,
+                                                                     int t0, char* to, int wave, int lane) {
+    constexpr int QT = Cf::QT, TILE = Cf::TILE;
+    const uint32_t voff = (lane >> 3) * Cf::RB + (((lane & 7) ^ (lane >> 3)) * 16);
+    const uint32_t voff_tail = ((lane >> 2) & 7) * Cf::RB + (((lane & 3) ^ ((lane >> 3) & 3)) * 16);
+    const int sh = a.cache.page_shift;
+    uint32_t ok = 0;
+#pragma unroll
+    for (int n = 0; n < QT; ++n) ok |= (uint32_t)(pg.p[n] >= 0 && pg.p[n] < a.cache.n_pages) << n;
+#pragma unroll
+    for (int e = 0; e < Cf::OCTETS; ++e) {
+        // eight rows; tokens without a page read page 0
+        const int o = wave * Cf::OCTETS + e;
+        int pid = pg.p[0];
+#pragma unroll
+        for (int n = 1; n < QT; ++n) pid = o >= 2 * n ? pg.p[n] : pid;
+        const bool there = (ok >> (o / 2)) & 1;
+        const char* base = a.cache.rows + (there ? ((int64_t)pid << sh) + ((t0 + 8 * o) & ((1 << sh) - 1)) : 0) * Cf::RB;
+        const int last = s.len - 1 - (t0 + 8 * o);
+        if (last >= 7) {
+#pragma unroll
+            for (int i = 0; i < Cf::PANELS; ++i) load_lds16(base + i * 128 + voff, to + (i * TILE + 8 * o) * 128);
+            if constexpr (Cf::HAS_TAIL)
+                if (lane < 32) load_lds16(base + Cf::PANELS * 128 + voff_tail, to + Cf::TAIL + 8 * o * 64);
+        } else {
+            // places past the end, which nothing may have been written to, take the last token's row: what all rows see
+            // keeps nothing from any
+            const int e16 = (s.len - 1 - t0) >> 4;
+            int pe = pg.p[0];
+#pragma unroll
+            for (int n = 1; n < QT; ++n) pe = e16 == n ? pg.p[n] : pe;
+            const char* row = a.cache.rows + (((ok >> e16) & 1) ? ((int64_t)pe << sh) + ((s.len - 1) & ((1 << sh) - 1)) : 0) * Cf::RB;
+            const int r = lane >> 3, rt = (lane >> 2) & 7;
+            const char* f = r <= last ? base + voff : row + (voff - r * Cf::RB);
+            const char* ft = rt <= last ? base + voff_tail : row + (voff_tail - rt * Cf::RB);
+#pragma unroll
+            for (int i = 0; i < Cf::PANELS; ++i) load_lds16(f + i * 128, to + (i * TILE + 8 * o) * 128);
+            if constexpr (Cf::HAS_TAIL)
+                if (lane < 32) load_lds16(ft + Cf::PANELS * 128, to + Cf::TAIL + 8 * o * 64);
+        }
+    }
+    return ok;
+}
+
+// Eight rows of a tile, by the wave that has loaded them: 16 bytes of the latent part that hold an infinity or a NaN become
+// zeros (a weight of 0 would not keep them out of the sums of the tokens that do not see the row), and the row's rotary part
+// a NaN: its scores are no numbers, whatever else it holds, for the tokens that do.
 template <bool BF, typename Cf>
-__device__ inline uint32_t not_finite(const char* st, int r0, int lane) {
-    uint32_t m = 0;
-    auto look = [&](const char* p, int row) {
-        const u32x4 x = *(const u32x4*)p;
-        bool bad = false;
+__device__ inline void clean_rows(char* tile, int o, int lane) {
+    constexpr int LATENT = Cf::R * Cf::ES / 128;
+    bool bad = false;
+#pragma unroll 4
+    for (int p = 0; p < LATENT; ++p) {
+        u32x4* at = (u32x4*)(tile + (p * Cf::TILE + 8 * o) * 128 + lane * 16);
+        const u32x4 x = *at;
+        bool no = false;
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-            bad |= BF ? (x[w] & 0x7F80u) == 0x7F80u || (x[w] & 0x7F800000u) == 0x7F800000u : (x[w] & 0x7F800000u) == 0x7F800000u;
-        if (bad) m |= 1u << row;
-    };
-#pragma unroll 2
-    for (int p = 0; p < Cf::PANELS; ++p)
-#pragma unroll
-        for (int o = 0; o < Cf::SUB; o += 8) look(st + p * (Cf::TILE * 128) + (r0 + o) * 128 + lane * 16, o + (lane >> 3));
-    if constexpr (Cf::HAS_TAIL)
-#pragma unroll
-        for (int o = 0; o < Cf::SUB; o += 16) look(st + Cf::TAIL + (r0 + o) * 64 + lane * 16, o + (lane >> 2));
-    if (!__builtin_amdgcn_ballot_w64(m != 0)) return 0;
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) m |= __shfl_xor(m, o);
-    return m;
-}
-
-// The running state of a wave: lane (c, g) has row c's maximum (in units of log 2; a shared reference that may
-// lag behind the true one) and its own tokens' share of the sum; o[j] holds row c's elements 16 j + 4 g + i, i = 0 .. 3.
-template <int R>
-struct State {
-    float m, l;
-    f32x4 o[R / 16];
-};
-
-__device__ inline u32x2 only_finite(u32x2 v) {
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        if ((v[w] & 0x7F80u) == 0x7F80u) v[w] &= 0xFFFF0000u;
-        if ((v[w] & 0x7F800000u) == 0x7F800000u) v[w] &= 0xFFFFu;
+        for (int w = 0; w < 4; ++w) no |= (BF && (x[w] & 0x7F80u) == 0x7F80u) || (x[w] & 0x7F800000u) == 0x7F800000u;
+        if (no) *at = u32x4{0u, 0u, 0u, 0u};
+        bad |= no;
     }
-    return v;
-}
-
-// O^T += C^T P^T over SUB tokens from row r0 of a tile on; CLEAN: what is no number counts as 0.  The reads of a few
-// elements' rows are on their way during the products of the ones before.
-template <int R, typename Cf, bool FINE, bool CLEAN>
-__device__ inline __attribute__((always_inline)) void add_weighted(const char* st, int r0, const u32x2* pf, const u32x2* pl, int lane,
-                                                                   State<R>& state) {
-    constexpr int NB = Cf::SUB / 16, PANEL = Cf::TILE * 128, AHEAD = 4 / NB, STEPS = R / 16 / AHEAD;
-    const int c = lane & 15, row = 4 * (lane >> 4) + (c >> 2);
-    const char* at[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) at[j] = st + (r0 + row) * 128 + (((2 * j + ((c >> 1) & 1)) ^ (row & 7)) * 16) + (c & 1) * 8;
-    u32x2 v[2][AHEAD][NB];
-    auto read = [&](int i) __attribute__((always_inline)) {
-#pragma unroll
-        for (int e = 0; e < AHEAD; ++e)
-#pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                const int j = i * AHEAD + e;
-                v[i & 1][e][n] = read_turned(at[j % 4] + j / 4 * PANEL + 16 * n * 128);
-            }
-    };
-    read(0);
-#pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-        if (i + 1 < STEPS) read(i + 1);
-        if constexpr (CLEAN)
-#pragma unroll
-            for (int e = 0; e < AHEAD; ++e)
-#pragma unroll
-                for (int n = 0; n < NB; ++n) v[i & 1][e][n] = only_finite(v[i & 1][e][n]);
-#pragma unroll
-        for (int part = 0; part < (FINE ? 2 : 1); ++part) {
-            const u32x2* p = part ? pl : pf;
-#pragma unroll
-            for (int e = 0; e < AHEAD; ++e) {
-                const int j = i * AHEAD + e;
-                const u32x2* x = v[i & 1][e];
-                if constexpr (NB == 1)
-                    state.o[j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, x[0]), __builtin_bit_cast(s16x4, p[0]),
-                                                                           state.o[j], 0, 0, 0);
-                else
-                    state.o[j] = mma16<true>(u32x4{x[0][0], x[0][1], x[1][0], x[1][1]}, u32x4{p[0][0], p[0][1], p[1][0], p[1][1]}, state.o[j]);
-            }
-        }
-        __builtin_amdgcn_sched_barrier(0);
+    const uint64_t rows = __builtin_amdgcn_ballot_w64(bad);
+    if ((lane & 7) == 0 && ((rows >> lane) & 0xFF)) {
+        const uint32_t nan = BF ? 0x7FC07FC0u : 0x7FC00000u;
+        char* at = Cf::PANELS > LATENT ? tile + (LATENT * Cf::TILE + 8 * o) * 128 + lane * 16 : tile + Cf::TAIL + (8 * o + (lane >> 3)) * 64;
+        *(u32x4*)at = u32x4{nan, nan, nan, nan};
     }
 }
 
-// SUB tokens from t0 on, rows r0 .. of the tile staged at st.  A maximum is taken over only when some score passes it by
-// LA_LAG (a factor of 256 in the weights, which fp32 sums and bf16 weights hold as well as 1): most tiles then need no
-// exchange between lanes and no rescaling of the outputs.  FINE: the second product takes what the rounding of the
-// weights to bf16 leaves out as well.
-template <bool BF, int R, typename Cf, bool FINE, bool WEIGHS>
-__device__ inline __attribute__((always_inline)) void attend_tile(const char* st, int r0, const u32x4* q, uint32_t ok, int t0, const Seq& s,
-                                                                  uint64_t word, bool in, float scale2, float* score, int lane,
-                                                                  State<R>& state) {
-    constexpr int SUB = Cf::SUB, NB = SUB / 16, KS = Cf::KS, PANEL = Cf::TILE * 128;
-    const int c = lane & 15, g = lane >> 4;
-    const float ninf = -__builtin_inff();
-    f32x4 sc[NB] = {};
-    {
-        constexpr int RING = NB == 1 ? 5 : 3;                    // steps whose reads are in registers or on their way
-        const char* at[2];
+// Rows of a tile that hold what is no number and that some token may not see are cleaned by the wave that has loaded them.
+// careful: not a token alone that sees itself, which sees all that is there
+template <bool BF, typename Cf>
+__device__ inline void clean_tile(const Seq& s, char* tile, int t0, int t_hi, uint32_t ok, bool careful, int wave, int lane) {
+    const int blocks = t_hi - t0 < Cf::TILE ? (t_hi - t0 + 15) / 16 : Cf::QT;
+    if ((careful && t0 + Cf::TILE > s.ctx) || (~ok & ((1u << blocks) - 1u)))
 #pragma unroll
-        for (int k = 0; k < 2; ++k) at[k] = st + (r0 + c) * 128 + (((4 * k + g) ^ (c & 7)) * 16);
-        const char* tail = st + Cf::TAIL + (r0 + c) * 64 + ((g ^ ((c >> 1) & 3)) * 16);
-        u32x4 x[RING][NB];
-        auto read = [&](int k) __attribute__((always_inline)) {
-#pragma unroll
-            for (int n = 0; n < NB; ++n)
-                x[k % RING][n] = *(const u32x4*)(k / 2 < Cf::PANELS ? at[k % 2] + k / 2 * PANEL + 16 * n * 128 : tail + 16 * n * 64);
-        };
-#pragma unroll
-        for (int k = 0; k < RING - 1; ++k) read(k);
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-            if (k + RING - 1 < KS) read(k + RING - 1);
-#pragma unroll
-            for (int n = 0; n < NB; ++n) sc[n] = mma16<BF>(x[k % RING][n], q[k], sc[n]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    }
-    const bool edge = t0 + SUB > s.ctx || (~ok & ((1u << NB) - 1u));
-#pragma unroll
-    for (int n = 0; n < NB; ++n) sc[n] = sc[n] * scale2;
-    uint32_t bad = 0;
-    if (edge) {
-        // (places past the end hold the last token's row, see issue: what all rows see keeps nothing from any)
-        uint32_t seen = 0, there = 0;
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int p = t0 + 16 * n + 4 * g + i, j = p - s.ctx;
-                const bool see = ((ok >> n) & 1) && p < s.len && (j < 0 || ((word >> (j & 63)) & 1));
-                seen |= (uint32_t)see << (16 * n + 4 * g + i);
-                there |= (uint32_t)(p < s.len) << (16 * n + 4 * g + i);
-                sc[n][i] = see ? sc[n][i] : ninf;
-            }
-        if (__builtin_amdgcn_ballot_w64(in && seen != there)) {
-            bad = not_finite<BF, Cf>(st, r0, lane);
-            if (bad & seen) state.l = __builtin_nanf("");    // (what is no number is taken as 0 below)
-        }
-    }
-    if constexpr (WEIGHS) {
-        if (score) {
-#pragma unroll
-            for (int n = 0; n < NB; ++n)
-                if (t0 + 16 * n < s.len) *(f32x4*)(score + t0 + 16 * n + 4 * g) = sc[n];     // (a table holds whole 16s)
-        }
-    }
-    float top = ninf;
-#pragma unroll
-    for (int n = 0; n < NB; ++n) top = fmaxf(top, fmaxf(fmaxf(sc[n][0], sc[n][1]), fmaxf(sc[n][2], sc[n][3])));
-    if (__builtin_amdgcn_ballot_w64(top > state.m + LA_LAG)) {
-        float x = fmaxf(top, __shfl_xor(top, 16));
-        x = fmaxf(x, __shfl_xor(x, 32));
-        const float m = x > state.m + LA_LAG ? x : state.m;      // by the row alone, whatever the others do
-        const float al = state.m == m ? 1.0f : __builtin_amdgcn_exp2f(state.m - m);
-        state.m = m;
-        state.l *= al;
-#pragma unroll
-        for (int j = 0; j < R / 16; ++j) state.o[j] = state.o[j] * al;
-    }
-    // weights exp2(score - maximum), 0 where nothing has been seen yet
-    const float m = state.m == ninf ? 0.f : state.m;
-#pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            sc[n][i] = __builtin_amdgcn_exp2f(sc[n][i] - m);
-            state.l += sc[n][i];
-        }
-    if constexpr (BF) {
-        u32x2 pf[NB], pl[NB];
-#pragma unroll
-        for (int n = 0; n < NB; ++n) {
-            bf16x4 hi, lo;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                hi[i] = (__bf16)sc[n][i];
-                if constexpr (FINE) lo[i] = (__bf16)(sc[n][i] - (float)hi[i]);
-            }
-            pf[n] = __builtin_bit_cast(u32x2, hi);
-            if constexpr (FINE) pl[n] = __builtin_bit_cast(u32x2, lo);
-        }
-        if (bad) add_weighted<R, Cf, FINE, true>(st, r0, pf, pl, lane, state);
-        else add_weighted<R, Cf, FINE, false>(st, r0, pf, pl, lane, state);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = 4 * g + i;
-            const char* at[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) at[j] = st + (r0 + row) * 128 + (((4 * j + (c >> 2)) ^ (row & 7)) * 16) + (c & 3) * 4;
-#pragma unroll
-            for (int j = 0; j < R / 16; ++j) {
-                float v = *(const float*)(at[j % 2] + j / 2 * PANEL);
-                if (bad) v = (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u ? 0.f : v;
-                state.o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, sc[0][i], state.o[j], 0, 0, 0);
-            }
-        }
-    }
+        for (int e = 0; e < Cf::OCTETS; ++e) clean_rows<BF, Cf>(tile, wave * Cf::OCTETS + e, lane);
 }
 
-template <bool BF, int R, int ROT, int RW, bool FINE, bool WEIGHS>
-__global__ void __launch_bounds__((64 * Config<BF, R, ROT, RW>::NW), (BF || R < 512 ? 2 : 1))
+// whether a row with this word sees position p, whose page is there.  (No branches: with && and || in one of these loops the
+// compiler lost the score of one of the four places.)
+__device__ inline bool sees(const Seq& s, bool there, uint64_t word, int p) {
+    const int d = p - s.ctx;
+    return ((uint32_t)there & (uint32_t)(p < s.len) & ((uint32_t)(d < 0) | (uint32_t)(word >> (d & 63)))) & 1u;
+}
+
+// FINE: the second product takes what the rounding of the weights to bf16 leaves out as well
+template <bool BF, int R, int ROT, int MT, bool FINE, bool WEIGHS>
+__global__ void __launch_bounds__((64 * Config<BF, R, ROT, MT>::NW), (BF ? 2 : 1))
 latent_attention_kernel(const LatentAttentionArgs a, int items, int rb_n) {
-    using Cf = Config<BF, R, ROT, RW>;
-    constexpr int NW = Cf::NW, GROUPS = Cf::GROUPS, ROUND = GROUPS * Cf::TILE, NB = Cf::TILE / 16;
-    __shared__ __attribute__((aligned(16))) char s_mem[GROUPS * 2 * Cf::STAGE];
-    __shared__ float s_m[NW][16], s_l[NW][16];
+    using Cf = Config<BF, R, ROT, MT>;
+    constexpr int NW = Cf::NW, TILE = Cf::TILE, QT = Cf::QT, CT = Cf::CT, KS = Cf::KS, PANEL = TILE * 128;
+    constexpr int ROWS = 16 * MT, SUMS = ROWS * Cf::LD * 4, MEM = 2 * Cf::STAGE > SUMS ? 2 * Cf::STAGE : SUMS;
+    __shared__ __attribute__((aligned(16))) char s_mem[MEM];
+    __shared__ __attribute__((aligned(16))) char s_p[FINE ? 2 : 1][ROWS * Cf::PP];
+    __shared__ float s_top[QT][ROWS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int c = lane & 15, g = lane >> 4, rw = wave % RW, grp = wave / RW;
+    const int c = lane & 15, g = lane >> 4;
     // the row blocks of one piece on one XCD, where its rows are in L2
     const int idx = (int)block_number(), jx = idx >> 3;
     const int item = (jx / rb_n) * 8 + (idx & 7), rb = jx % rb_n;
     if (item >= items) return;
     Seq mine = {0, 0, 0, 0};
     if (lane < a.B) mine = sequence(a, lane);
-    const int piece = __builtin_amdgcn_readfirstlane(piece_tokens(a, rb_n, RW, ROUND, mine, lane));
+    const int piece = __builtin_amdgcn_readfirstlane(piece_tokens(a, rb_n, MT, TILE, mine, lane));
     int b, j;
     const Seq s = find_item(a, piece, item, lane, idx == 0 && wave == 0, mine, b, j);
     if (b < 0) return;
-    const int rows = s.n * a.n_q, row0 = rb * 16 * RW, rows_max = a.max_q * a.n_q;
+    const int rows = s.n * a.n_q, row0 = rb * ROWS, rows_max = a.max_q * a.n_q;
     if (row0 >= rows) return;
     const int t_lo = j * piece, t_hi = s.len - t_lo < piece ? s.len : t_lo + piece;
-    const int32_t* table = a.page_table + (int64_t)b * a.max_pages;
-    const float scale2 = a.scale * LOG2E;            // scores in units of log 2
-    const int row = row0 + 16 * rw + c;
-    const bool in = row < rows;                      // rows past the end are zeros and see nothing
-    const int i_tok = in ? row / a.n_q : 0;
-    const uint64_t word = !in ? 0ull : a.tree ? a.tree[s.first + i_tok] : ~0ull >> (63 - i_tok);
-    float* const score = WEIGHS && in ? a.score + ((int64_t)b * rows_max + row) * ((int64_t)a.max_pages << a.cache.page_shift) : nullptr;
-    u32x4 q[Cf::KS];
+    const float scale2 = a.scale * LOG2E, ninf = -__builtin_inff();      // scores in units of log 2
+    const int sh = a.cache.page_shift;
+    Pages<QT> pages;
+    pages.start(a, b, t_lo, t_hi, lane);
+    int p = t_lo, k_tile = 0;
+    uint32_t ok = 0, next = 0;
+    if (p < t_hi) ok = issue_tile<Cf>(a, s, pages.tile(0, lane), p, s_mem, wave, lane);
+    // the wave's tokens and query rows of the first product
+    const int tt = wave % QT, r0 = wave / QT;
+    const bool scores = r0 < MT;
+    u32x4 q[KS];
     {
+        const int row = row0 + 16 * r0 + c;
+        const bool in = scores && row < rows;        // rows past the end are zeros and see nothing
         const char* from = (const char*)a.q + ((int64_t)s.first * a.n_q + (in ? row : 0)) * Cf::RB + 16 * g;
 #pragma unroll
-        for (int k = 0; k < Cf::KS; ++k) {
+        for (int k = 0; k < KS; ++k) {
             q[k] = u32x4{0u, 0u, 0u, 0u};
             if (in) q[k] = *(const u32x4*)(from + 64 * k);
         }
     }
-    State<R> st;
-    st.m = -__builtin_inff();
-    st.l = 0.f;
+    const bool careful = s.n > 1 || (a.tree && !(a.tree[s.first] & 1));
+    // Lane (c, g): the reference of row c of every row tile, in units of log 2; its own tokens' share of the sum of its
+    // row tile; row c's elements 16 (CT wave + t) + 4 g + i of every row tile.  The reference is the maximum, taken
+    // over only when some score passes it by LA_LAG (a factor of 256 in the weights, which fp32 sums and bf16 weights
+    // hold as well as 1): most tiles need no rescaling.
+    float m[MT], l = 0.f;
+    f32x4 o[CT][MT] = {};
 #pragma unroll
-    for (int e = 0; e < R / 16; ++e) st.o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-    char* const stage = s_mem + grp * 2 * Cf::STAGE;
-    const int sh = a.cache.page_shift;
-    // a tile's pages, 16 tokens each
-    struct Pages { int p[NB]; };
-    auto pages = [&](int t0) __attribute__((always_inline)) {
-        Pages r;
+    for (int r = 0; r < MT; ++r) m[r] = ninf;
+    for (int buf = 0; p < t_hi; p += TILE, buf ^= 1) {
+        char* const tile = s_mem + buf * Cf::STAGE;
+        wait_loads<0>();
+        clean_tile<BF, Cf>(s, tile, p, t_hi, ok, careful, wave, lane);
+        lds_barrier();                               // the tile has arrived, the one before has been read
+        if (p + TILE < t_hi) next = issue_tile<Cf>(a, s, pages.tile(++k_tile, lane), p + TILE, s_mem + (buf ^ 1) * Cf::STAGE, wave, lane);
+        f32x4 sc = {};
+        if (scores) {
+            constexpr int RING = 6;    // steps whose reads are in registers or on their way
+            const char* at[2];
 #pragma unroll
-        for (int n = 0; n < NB; ++n) r.p[n] = tile_page(a, table, t0 + 16 * n, t_hi);
-        return r;
-    };
-    const uint32_t voff = (lane >> 3) * Cf::RB + (((lane & 7) ^ (lane >> 3)) * 16);
-    const uint32_t voff_tail = ((lane >> 2) & 7) * Cf::RB + (((lane & 3) ^ ((lane >> 3) & 3)) * 16);
-    auto issue = [&](const Pages& pg, int t0, char* to) __attribute__((always_inline)) {
-        uint32_t ok = 0;                             // a bit each
+            for (int k = 0; k < 2; ++k) at[k] = tile + (16 * tt + c) * 128 + (((4 * k + g) ^ (c & 7)) * 16);
+            const char* tail = tile + Cf::TAIL + (16 * tt + c) * 64 + ((g ^ ((c >> 1) & 3)) * 16);
+            u32x4 x[RING];
+            auto read = [&](int k) __attribute__((always_inline)) {
+                x[k % RING] = *(const u32x4*)(k / 2 < Cf::PANELS ? at[k % 2] + k / 2 * PANEL : tail);
+            };
 #pragma unroll
-        for (int n = 0; n < NB; ++n) ok |= (uint32_t)(pg.p[n] >= 0 && pg.p[n] < a.cache.n_pages) << n;
+            for (int k = 0; k < RING - 1; ++k) read(k);
 #pragma unroll
-        for (int e = 0; e < Cf::OCTETS; ++e) {
-            // eight rows; tokens without a page read page 0
-            const int o = rw * Cf::OCTETS + e;
-            int pid = pg.p[0];
+            for (int k = 0; k < KS; ++k) {
+                if (k + RING - 1 < KS) read(k + RING - 1);
+                sc = mma16<BF>(x[k % RING], q[k], sc);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            const int t0 = p + 16 * tt;              // the wave's tokens
+            const bool there = (ok >> tt) & 1, edge = t0 + 16 > s.ctx || !there;
+            sc = sc * scale2;
+            const int row = row0 + 16 * r0 + c;
+            if (edge) {
+                const int i_tok = row / a.n_q;
+                const uint64_t word = row >= rows ? 0ull : a.tree ? a.tree[s.first + i_tok] : ~0ull >> (63 - i_tok);
 #pragma unroll
-            for (int n = 1; n < NB; ++n) pid = o >= 2 * n ? pg.p[n] : pid;
-            const bool there = (ok >> (o / 2)) & 1;
-            const char* base = a.cache.rows + (there ? ((int64_t)pid << sh) + ((t0 + 8 * o) & ((1 << sh) - 1)) : 0) * Cf::RB;
-            const int last = s.len - 1 - (t0 + 8 * o);
-            if (last >= 7) {
+                for (int i = 0; i < 4; ++i) sc[i] = sees(s, there, word, t0 + 4 * g + i) ? sc[i] : ninf;
+            }
+            if constexpr (WEIGHS)
+                if (row < rows && t0 < s.len)        // (a table holds whole 16s)
+                    *(f32x4*)(a.score + ((int64_t)b * rows_max + row) * ((int64_t)a.max_pages << sh) + t0 + 4 * g) = sc;
+            float top = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            if (g == 0) s_top[tt][16 * r0 + c] = top;
+        }
+        lds_barrier();
+        // the same in all waves
+        float al[MT];
+        bool change = false;
 #pragma unroll
-                for (int i = 0; i < Cf::PANELS; ++i) load_lds16(base + i * 128 + voff, to + (i * Cf::TILE + 8 * o) * 128);
-                if constexpr (Cf::HAS_TAIL)
-                    if (lane < 32) load_lds16(base + Cf::PANELS * 128 + voff_tail, to + Cf::TAIL + 8 * o * 64);
+        for (int r = 0; r < MT; ++r) {
+            float top = s_top[0][16 * r + c];
+#pragma unroll
+            for (int k = 1; k < QT; ++k) top = fmaxf(top, s_top[k][16 * r + c]);
+            const float was = m[r];
+            m[r] = top > was + LA_LAG ? top : was;
+            al[r] = was == m[r] ? 1.0f : __builtin_amdgcn_exp2f(was - m[r]);
+            change |= was != m[r] && was != ninf;    // (nothing to rescale before the first weights)
+        }
+        if (scores) {
+            float mr = m[0], ar = al[0];             // of the wave's row tile
+            if (MT > 1 && r0 > 0) { mr = m[MT - 1]; ar = al[MT - 1]; }
+            mr = mr == ninf ? 0.f : mr;              // (weights of 0 where nothing has been seen yet)
+            l *= ar;
+            float w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[i] = __builtin_amdgcn_exp2f(sc[i] - mr);
+                l += w[i];
+            }
+            char* to = &s_p[0][(16 * r0 + c) * Cf::PP + (16 * tt + 4 * g) * Cf::ES];
+            if constexpr (BF) {
+                *(u32x2*)to = u32x2{bf16_pair(w[0], w[1]), bf16_pair(w[2], w[3])};
+                if constexpr (FINE) {
+                    float d[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) d[i] = w[i] - (float)(__bf16)w[i];
+                    *(u32x2*)(to + ROWS * Cf::PP) = u32x2{bf16_pair(d[0], d[1]), bf16_pair(d[2], d[3])};
+                }
             } else {
-                // places past the end, which nothing may have been written to, take the last token's row
-                const int end = s.len - 1 - t0, e16 = end >> 4;
-                int pe = pg.p[0];
-#pragma unroll
-                for (int n = 1; n < NB; ++n) pe = e16 == n ? pg.p[n] : pe;
-                const char* row = a.cache.rows + (((ok >> e16) & 1) ? ((int64_t)pe << sh) + ((s.len - 1) & ((1 << sh) - 1)) : 0) * Cf::RB;
-                const int r = lane >> 3, rt = (lane >> 2) & 7;
-                const char* f = r <= last ? base + voff : row + (voff - r * Cf::RB);
-                const char* ft = rt <= last ? base + voff_tail : row + (voff_tail - rt * Cf::RB);
-#pragma unroll
-                for (int i = 0; i < Cf::PANELS; ++i) load_lds16(f + i * 128, to + (i * Cf::TILE + 8 * o) * 128);
-                if constexpr (Cf::HAS_TAIL)
-                    if (lane < 32) load_lds16(ft + Cf::PANELS * 128, to + Cf::TAIL + 8 * o * 64);
+                *(f32x4*)to = f32x4{w[0], w[1], w[2], w[3]};
             }
         }
-        return ok;
-    };
-    int p = t_lo + grp * Cf::TILE;
-    const int rounds = (t_hi - t_lo + ROUND - 1) / ROUND;
-    uint32_t ok = 0, next = 0;
-    Pages pg = pages(p);
-    if (p < t_hi) ok = issue(pg, p, stage);
-    pg = pages(p + ROUND);
-    for (int k = 0, buf = 0; k < rounds; ++k, p += ROUND, buf ^= 1) {
-        if constexpr (RW > 1)
-            if (k > 0) {
-                wait_loads<0>();
-                __syncthreads();                     // the tile has arrived, and the one before has been read
-            }
-        if (p + ROUND < t_hi) {
-            next = issue(pg, p + ROUND, stage + (buf ^ 1) * Cf::STAGE);
-            pg = pages(p + 2 * ROUND);
-            if (RW == 1 || k == 0) wait_loads<Cf::LOADS>();      // all but the next tile's
-        } else if (RW == 1 || k == 0) {
-            wait_loads<0>();
+        if (__builtin_amdgcn_ballot_w64(change)) {
+#pragma unroll
+            for (int r = 0; r < MT; ++r)
+#pragma unroll
+                for (int t = 0; t < CT; ++t) o[t][r] = o[t][r] * al[r];
         }
-        if constexpr (RW > 1)
-            if (k == 0) lds_barrier();               // the first tile has arrived
-        if (p < t_hi) {
-#pragma unroll 1
-            for (int n = 0; n < Cf::TILE / Cf::SUB; ++n) {
-                if (p + n * Cf::SUB >= t_hi) break;
-                attend_tile<BF, R, Cf, FINE, WEIGHS>(stage + buf * Cf::STAGE, n * Cf::SUB, q, ok >> (n * (Cf::SUB / 16)),
-                                                                  p + n * Cf::SUB, s, word, in, scale2, score, lane, st);
+        lds_barrier();
+        if constexpr (BF) {
+            // inner indexes 8 g .. 8 g + 7 of each 32 tokens
+            constexpr int STEPS = 2 * CT, RING = 3;
+            const int row = 8 * g + (c >> 2);
+            const int e0 = (2 * CT * wave) & 7;      // the wave's first chunk of a panel
+            const char* base = tile + (2 * CT * wave) / 8 * PANEL + row * 128 + (c & 1) * 8;
+            const int half = (c >> 1) & 1;
+            u32x2 v[RING][2];
+            auto read = [&](int i) __attribute__((always_inline)) {
+                const int s2 = i / CT, t = i % CT;
+                const int ch = e0 + 2 * t;           // (a wave's elements end within a panel, or are whole panels)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    v[i % RING][u] = read_turned(base + (ch >> 3) * PANEL + (32 * s2 + 4 * u) * 128 +
+                                                 ((((ch & 7) + half) ^ ((row + 4 * u) & 7)) * 16));
+            };
+            u32x4 pf[MT], pl[MT];
+#pragma unroll
+            for (int i = 0; i < RING - 1; ++i) read(i);
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                if (i % CT == 0) {
+#pragma unroll
+                    for (int r = 0; r < MT; ++r) {
+                        const char* at = &s_p[0][(16 * r + c) * Cf::PP + i / CT * 64 + 16 * g];
+                        pf[r] = *(const u32x4*)at;
+                        if constexpr (FINE) pl[r] = *(const u32x4*)(at + ROWS * Cf::PP);
+                    }
+                }
+                if (i + RING - 1 < STEPS) read(i + RING - 1);
+                const u32x2* x = v[i % RING];
+                const u32x4 vf = {x[0][0], x[0][1], x[1][0], x[1][1]};
+#pragma unroll
+                for (int r = 0; r < MT; ++r) o[i % CT][r] = mma16<true>(vf, pf[r], o[i % CT][r]);
+                if constexpr (FINE)
+#pragma unroll
+                    for (int r = 0; r < MT; ++r) o[i % CT][r] = mma16<true>(vf, pl[r], o[i % CT][r]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < QT; ++n) {
+                f32x4 pf[MT];
+#pragma unroll
+                for (int r = 0; r < MT; ++r) pf[r] = *(const f32x4*)&s_p[0][(16 * r + c) * Cf::PP + (16 * n + 4 * g) * 4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int row = 16 * n + 4 * g + i;
+#pragma unroll
+                    for (int t = 0; t < CT; ++t) {
+                        const int ch = 4 * (CT * wave + t) + (c >> 2);       // (of 16 bytes)
+                        const float v = *(const float*)(tile + (ch >> 3) * PANEL + row * 128 + (((ch & 7) ^ (row & 7)) * 16) + (c & 3) * 4);
+#pragma unroll
+                        for (int r = 0; r < MT; ++r) o[t][r] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, pf[r][i], o[t][r], 0, 0, 0);
+                    }
+                }
             }
         }
         ok = next;
     }
-    // the groups' states joined, the rows of one of their waves at a time
-    float l = st.l;
+    // the sums in rows
+    __syncthreads();                                 // the staged rows become their place
+    int tid2 = tid;
+    asm volatile("" : "+v"(tid2));                   // (what follows needs no registers before)
+    const int c2 = tid2 & 15, g2 = (tid2 & 63) >> 4;
+    float(*const s_o)[Cf::LD] = (float(*)[Cf::LD])s_mem;
+#pragma unroll
+    for (int r = 0; r < MT; ++r)
+#pragma unroll
+        for (int t = 0; t < CT; ++t) *(f32x4*)&s_o[16 * r + c2][16 * (CT * wave + t) + 4 * g2] = o[t][r];
+    if (scores) {
+        float x = l;
+        x += __shfl_xor(x, 16);
+        x += __shfl_xor(x, 32);
+        if (g2 == 0) s_top[tt][16 * r0 + c2] = x;
+    }
+    __syncthreads();
+    const int64_t at = (int64_t)item * rows_max + row0;
+    const int here = rows - row0 < ROWS ? rows - row0 : ROWS;
+    for (int u = tid2; u < here * (R / 4); u += 64 * NW) {
+        const int r = u / (R / 4), e = u % (R / 4) * 4;
+        *(f32x4*)(a.part_o + (at + r) * R + e) = *(const f32x4*)&s_o[r][e];
+    }
+    if (wave == 0 && g2 == 0) {
+#pragma unroll
+        for (int r = 0; r < MT; ++r) {
+            if (16 * r + c2 >= here) continue;
+            float x = s_top[0][16 * r + c2];
+#pragma unroll
+            for (int k = 1; k < QT; ++k) x += s_top[k][16 * r + c2];
+            ((f32x2*)a.part_ml)[at + 16 * r + c2] = f32x2{m[r], x};
+        }
+    }
+}
+
+// Sequences of many query rows: blocks of 128.  The weights are rounded to bf16.
+template <int R, int ROT, bool WEIGHS>
+__global__ void __launch_bounds__(512, 2) latent_rows_kernel(const LatentAttentionArgs a, int items, int rb_n) {
+    using Cf = Config<true, R, ROT, 8>;
+    constexpr int TILE = Cf::TILE, QT = Cf::QT, KS = Cf::KS, PANEL = TILE * 128, ET = R / 16;    // elements' tiles
+    static_assert(Cf::NW == 8 && Cf::OCTETS == 1 && TILE == 64, "a wave an eight of a tile's rows");
+    __shared__ __attribute__((aligned(16))) char s_mem[2 * Cf::STAGE];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    const int idx = (int)block_number(), jx = idx >> 3;
+    const int item = (jx / rb_n) * 8 + (idx & 7), rb = jx % rb_n;
+    if (item >= items) return;
+    Seq mine = {0, 0, 0, 0};
+    if (lane < a.B) mine = sequence(a, lane);
+    const int piece = __builtin_amdgcn_readfirstlane(piece_tokens(a, rb_n, 8, TILE, mine, lane));
+    int b, j;
+    const Seq s = find_item(a, piece, item, lane, idx == 0 && wave == 0, mine, b, j);
+    if (b < 0) return;
+    const int rows = s.n * a.n_q, row0 = rb * 128, rows_max = a.max_q * a.n_q;
+    if (row0 >= rows) return;
+    const int t_lo = j * piece, t_hi = s.len - t_lo < piece ? s.len : t_lo + piece;
+    const float scale2 = a.scale * LOG2E, ninf = -__builtin_inff();      // scores in units of log 2
+    const int sh = a.cache.page_shift;
+    Pages<QT> pages;
+    pages.start(a, b, t_lo, t_hi, lane);
+    int p = t_lo, k_tile = 0;
+    uint32_t ok = 0, next = 0;
+    if (p < t_hi) ok = issue_tile<Cf>(a, s, pages.tile(0, lane), p, s_mem, wave, lane);
+    const int wrow = row0 + 16 * wave;
+    u32x4 q[KS];
+    {
+        const bool in = wrow + c < rows;             // rows past the end are zeros and see nothing
+        const char* from = (const char*)a.q + ((int64_t)s.first * a.n_q + (in ? wrow + c : 0)) * Cf::RB + 16 * g;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            q[k] = u32x4{0u, 0u, 0u, 0u};
+            if (in) q[k] = *(const u32x4*)(from + 64 * k);
+        }
+    }
+    // Lane (c, g): row c's maximum (a reference that may lag, as above) and its own tokens' share of the sum; row c's elements
+    // 16 j + 4 g + i
+    float m = ninf, l = 0.f;
+    f32x4 o[ET];
+#pragma unroll
+    for (int e = 0; e < ET; ++e) o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int buf = 0; p < t_hi; p += TILE, buf ^= 1) {
+        char* const tile = s_mem + buf * Cf::STAGE;
+        wait_loads<0>();
+        clean_tile<true, Cf>(s, tile, p, t_hi, ok, true, wave, lane);
+        lds_barrier();                               // the tile has arrived, the one before has been read
+        if (p + TILE < t_hi) next = issue_tile<Cf>(a, s, pages.tile(++k_tile, lane), p + TILE, s_mem + (buf ^ 1) * Cf::STAGE, wave, lane);
+#pragma unroll 1
+        for (int n0 = 0; n0 < 2; ++n0) {             // 32 tokens at a time
+            const int t0 = p + 32 * n0;
+            if (t0 >= t_hi) break;
+            f32x4 sc[2] = {};
+            {
+                constexpr int RING = 3;              // steps whose reads are in registers or on their way
+                const char* at[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) at[k] = tile + (32 * n0 + c) * 128 + (((4 * k + g) ^ (c & 7)) * 16);
+                const char* tail = tile + Cf::TAIL + (32 * n0 + c) * 64 + ((g ^ ((c >> 1) & 3)) * 16);
+                u32x4 x[RING][2];
+                auto read = [&](int k) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+                        x[k % RING][n] = *(const u32x4*)(k / 2 < Cf::PANELS ? at[k % 2] + k / 2 * PANEL + 16 * n * 128 : tail + 16 * n * 64);
+                };
+#pragma unroll
+                for (int k = 0; k < RING - 1; ++k) read(k);
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    if (k + RING - 1 < KS) read(k + RING - 1);
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) sc[n] = mma16<true>(x[k % RING][n], q[k], sc[n]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            const uint32_t there = (ok >> (2 * n0)) & 3u;
+#pragma unroll
+            for (int n = 0; n < 2; ++n) sc[n] = sc[n] * scale2;
+            if (WEIGHS || t0 + 32 > s.ctx || there != 3u) {
+                // (the row's number is made again here, not held in registers)
+                int lane2 = lane;
+                asm volatile("" : "+v"(lane2));
+                const int row = wrow + (lane2 & 15), g2 = lane2 >> 4;
+                if (t0 + 32 > s.ctx || there != 3u) {
+                    const int i_tok = row / a.n_q;
+                    const uint64_t word = row >= rows ? 0ull : a.tree ? a.tree[s.first + i_tok] : ~0ull >> (63 - i_tok);
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sc[n][i] = sees(s, (there >> n) & 1u, word, t0 + 16 * n + 4 * g2 + i) ? sc[n][i] : ninf;
+                }
+                if constexpr (WEIGHS) {
+                    if (row < rows) {
+                        float* to = a.score + ((int64_t)b * rows_max + row) * ((int64_t)a.max_pages << sh) + t0 + 4 * g2;
+#pragma unroll
+                        for (int n = 0; n < 2; ++n)
+                            if (t0 + 16 * n < s.len) *(f32x4*)(to + 16 * n) = sc[n];     // (a table holds whole 16s)
+                    }
+                }
+            }
+            float top = ninf;
+#pragma unroll
+            for (int n = 0; n < 2; ++n) top = fmaxf(top, fmaxf(fmaxf(sc[n][0], sc[n][1]), fmaxf(sc[n][2], sc[n][3])));
+            if (__builtin_amdgcn_ballot_w64(top > m + LA_LAG)) {
+                float x = fmaxf(top, __shfl_xor(top, 16));
+                x = fmaxf(x, __shfl_xor(x, 32));
+                x = x > m + LA_LAG ? x : m;          // by the row alone, whatever the others do
+                const float al = m == x ? 1.0f : __builtin_amdgcn_exp2f(m - x);
+                m = x;
+                l *= al;
+#pragma unroll
+                for (int e = 0; e < ET; ++e) o[e] = o[e] * al;
+            }
+            const float mr = m == ninf ? 0.f : m;    // (weights of 0 where nothing has been seen yet)
+            u32x4 pf;
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sc[n][i] = __builtin_amdgcn_exp2f(sc[n][i] - mr);
+                    l += sc[n][i];
+                }
+                pf[2 * n] = bf16_pair(sc[n][0], sc[n][1]);
+                pf[2 * n + 1] = bf16_pair(sc[n][2], sc[n][3]);
+            }
+            const int vrow = 4 * g + (c >> 2);
+            const char* at[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) at[e] = tile + (32 * n0 + vrow) * 128 + (((2 * e + ((c >> 1) & 1)) ^ (vrow & 7)) * 16) + (c & 1) * 8;
+            u32x2 v[2][2][2];
+            auto read = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        const int t = 2 * i + e;
+                        v[i & 1][e][n] = read_turned(at[t % 4] + t / 4 * PANEL + 16 * n * 128);
+                    }
+            };
+            read(0);
+#pragma unroll
+            for (int i = 0; i < ET / 2; ++i) {
+                if (i + 1 < ET / 2) read(i + 1);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const u32x2* x = v[i & 1][e];
+                    o[2 * i + e] = mma16<true>(u32x4{x[0][0], x[0][1], x[1][0], x[1][1]}, pf, o[2 * i + e]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        ok = next;
+    }
+    // the sums through LDS, so that they are written in whole cache lines: two waves' rows at a time
+    int tid2 = tid;
+    asm volatile("" : "+v"(tid2));                   // (what follows needs no registers before)
+    const int c2 = tid2 & 15, g2 = (tid2 & 63) >> 4;
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    if (g == 0) { s_m[wave][c] = st.m; s_l[wave][c] = l; }
-    __syncthreads();                                 // the staged rows become the place of the sums
-    float(*const s_o)[16][Cf::LD] = (float(*)[16][Cf::LD])s_mem;
-    constexpr int PER = NW * 4, PART = R / PER;      // threads a row, their elements
-    const int64_t prow = (int64_t)item * rows_max;
-    float m = s_m[rw][c];
-#pragma unroll
-    for (int w = 1; w < GROUPS; ++w) m = fmaxf(m, s_m[w * RW + rw][c]);
-    const float f = st.m == m ? 1.0f : __builtin_amdgcn_exp2f(st.m - m);
+    const int64_t at = (int64_t)item * rows_max;
+    if (g2 == 0 && wrow + c2 < rows) ((f32x2*)a.part_ml)[at + wrow + c2] = f32x2{m, l};
+    constexpr int AT_ONCE = 2 * Cf::STAGE / (16 * Cf::LD * 4) >= 4 ? 4 : 2;
+    float(*const s_o)[Cf::LD] = (float(*)[Cf::LD])s_mem;
 #pragma unroll 1
-    for (int r = 0; r < RW; ++r) {
-        if (row0 + 16 * r >= rows) break;
-        if (r == rw) {
+    for (int w0 = 0; w0 < 8; w0 += AT_ONCE) {
+        if (row0 + 16 * w0 >= rows) break;
+        __syncthreads();
+        if (wave / AT_ONCE * AT_ONCE == w0) {
 #pragma unroll
-            for (int e = 0; e < R / 16; ++e) *(f32x4*)&s_o[grp][c][16 * e + 4 * g] = st.o[e] * f;
+            for (int e = 0; e < ET; ++e) *(f32x4*)&s_o[16 * (wave - w0) + c2][16 * e + 4 * g2] = o[e];
         }
         __syncthreads();
-        const int rt = tid / PER, rr = row0 + 16 * r + rt, u = tid % PER;
-        if (rr < rows) {
-            float* po = a.part_o + (prow + rr) * R;
-#pragma unroll
-            for (int e = 0; e < PART; e += 4) {
-                f32x4 v = *(const f32x4*)&s_o[0][rt][4 * u + PER * e];
-#pragma unroll
-                for (int w = 1; w < GROUPS; ++w) v += *(const f32x4*)&s_o[w][rt][4 * u + PER * e];
-                *(f32x4*)(po + 4 * u + PER * e) = v;
-            }
-            if (u == 0) {
-                float mm = s_m[r][rt], ll = 0.f;
-#pragma unroll
-                for (int w = 1; w < GROUPS; ++w) mm = fmaxf(mm, s_m[w * RW + r][rt]);
-#pragma unroll
-                for (int w = 0; w < GROUPS; ++w) {
-                    const float mw = s_m[w * RW + r][rt];
-                    ll += s_l[w * RW + r][rt] * (mw == mm ? 1.0f : __builtin_amdgcn_exp2f(mw - mm));
-                }
-                a.part_ml[2 * (prow + rr)] = mm;
-                a.part_ml[2 * (prow + rr) + 1] = ll;
-            }
+        const int left = rows - row0 - 16 * w0, here = left < 16 * AT_ONCE ? left : 16 * AT_ONCE;
+        for (int u = tid2; u < here * (R / 4); u += 512) {
+            const int r = u / (R / 4), e = u % (R / 4) * 4;
+            *(f32x4*)(a.part_o + (at + row0 + 16 * w0 + r) * R + e) = *(const f32x4*)&s_o[r][e];
         }
-        __syncthreads();
     }
 }
 
@@ -755,17 +918,21 @@ __global__ void __launch_bounds__(256) latent_mass_kernel(const LatentAttentionA
     }
 }
 
-template <bool BF, int R, int ROT, int RW, bool FINE>
+template <bool BF, int R, int ROT, int MT, bool FINE>
 int launch_rows(const LatentAttentionArgs& a, hipStream_t st) {
-    const int rb = row_blocks(a.max_q * a.n_q, RW);
+    const int rb = row_blocks(a.max_q * a.n_q, MT);
     const int64_t cap = (int64_t)a.max_pages << a.cache.page_shift;
     {
-        const int64_t items = std::min<int64_t>(latent_items(a.cache.dtype, a.n_q, a.B, a.max_q),
-                                                a.B * ((cap + LA_MIN_PIECE - 1) / LA_MIN_PIECE));
-        const dim3 grid = grid_of((items + 7) / 8 * 8 * rb), block((64 * Config<BF, R, ROT, RW>::NW));
+        const int64_t items = std::min<int64_t>(a.items, a.B * ((cap + LA_MIN_PIECE - 1) / LA_MIN_PIECE));
+        const dim3 grid = grid_of((items + 7) / 8 * 8 * rb), block((64 * Config<BF, R, ROT, MT>::NW));
         KernelTimer kt_("latent_attention", st);
-        if (a.mass_out) latent_attention_kernel<BF, R, ROT, RW, FINE, true><<<grid, block, 0, st>>>(a, (int)items, rb);
-        else latent_attention_kernel<BF, R, ROT, RW, FINE, false><<<grid, block, 0, st>>>(a, (int)items, rb);
+        if constexpr (MT == 8) {
+            if (a.mass_out) latent_rows_kernel<R, ROT, true><<<grid, block, 0, st>>>(a, (int)items, rb);
+            else latent_rows_kernel<R, ROT, false><<<grid, block, 0, st>>>(a, (int)items, rb);
+        } else {
+            if (a.mass_out) latent_attention_kernel<BF, R, ROT, MT, FINE, true><<<grid, block, 0, st>>>(a, (int)items, rb);
+            else latent_attention_kernel<BF, R, ROT, MT, FINE, false><<<grid, block, 0, st>>>(a, (int)items, rb);
+        }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return (int)e;
     }
@@ -798,15 +965,11 @@ int launch_rows(const LatentAttentionArgs& a, hipStream_t st) {
 }
 template <bool BF, int R, int ROT>
 int launch_tiles(const LatentAttentionArgs& a, hipStream_t st) {
-    if constexpr (BF) {
-        static_assert(ORDERMOE_LATENT_FINE_ROWS == 64, "the waves that share a tile where the weights keep 16 bits");
-        switch (row_waves(ORDERMOE_BF16, a.max_q * a.n_q)) {
-            case 2: return launch_rows<BF, R, ROT, 2, true>(a, st);
-            case 4: return launch_rows<BF, R, ROT, 4, true>(a, st);
-            case 8: return launch_rows<BF, R, ROT, 8, false>(a, st);
-        }
-    }
-    return launch_rows<BF, R, ROT, 1, BF>(a, st);
+    static_assert(ORDERMOE_LATENT_FINE_ROWS == LA_FEW, "the batches whose weights keep 16 bits");
+    const int mt = row_tiles(a.cache.dtype, a.max_q * a.n_q);
+    if constexpr (BF)
+        if (mt == 8) return launch_rows<BF, R, ROT, 8, false>(a, st);
+    return mt == 2 ? launch_rows<BF, R, ROT, 2, BF>(a, st) : launch_rows<BF, R, ROT, 1, BF>(a, st);
 }
 template <bool BF, int R>
 int launch_rot(const LatentAttentionArgs& a, hipStream_t st) {
@@ -820,7 +983,7 @@ int launch_rank(const LatentAttentionArgs& a, hipStream_t st) {
 }  // namespace
 
 int64_t latent_items(int dtype, int n_q, int B, int max_q) {
-    const int rows = max_q * n_q, rb = row_blocks(rows, row_waves(dtype, rows));
+    const int rows = max_q * n_q, rb = row_blocks(rows, row_tiles(dtype, rows));
     return (2 * LA_TARGET + rb - 1) / rb + B;
 }
 

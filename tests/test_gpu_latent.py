@@ -198,7 +198,7 @@ class _Batch:
         out, lse, mo = got
         o, ls = _host(out), _host(lse)
         width = self.rows.shape[2]
-        fine = self.dtype == "bf16" and max_q * self.h <= 64
+        fine = self.dtype == "bf16" and max_q * self.h <= 32
         written = np.zeros(self.T, bool)
         for b in range(len(self.n)):
             n, s0 = min(int(self.n[b]), max_q), self.start[b]
