@@ -42,6 +42,7 @@ namespace {
 constexpr int LA_TARGET = 512;                       // workgroups that a large batch is split into
 constexpr int LA_MIN_PIECE = 64;                     // tokens
 constexpr int LA_FEW = 32;                           // query rows up to which latent_attention_kernel takes a batch
+constexpr int LO_PIECES = 32;                        // pieces of a sequence past which 16 sets of lanes add them
 constexpr int LO_GROUPS = 256;                       // workgroups of the last product wished for
 constexpr float LA_LAG = 8.0f;                       // see attend_tile
 
@@ -92,7 +93,10 @@ __device__ inline int piece_tokens(const LatentAttentionArgs& a, int rb_n, int m
     }
     total = first_lane(total);
     blocks = rb_n > 1 ? first_lane(blocks) : total;
-    int64_t p = (blocks + LA_TARGET - 1) / LA_TARGET;
+    // One round of the workgroups that run together, each sequence's short last piece counted in (64 sequences of 200 to 8000
+    // tokens: 32 heads 111 us without, 84); blocks of 128 rows take two rounds (157 us in one, 128 heads, 139)
+    const int64_t ends = mt == 8 ? 0 : (int64_t)a.B * rb_n, want = ends < LA_TARGET / 2 ? LA_TARGET - ends : LA_TARGET / 2;
+    int64_t p = (blocks + want - 1) / want;
     const int64_t least = (total * rb_n + 2 * LA_TARGET - 1) / (2 * LA_TARGET);
     p = p < least ? least : p;
     p = p < LA_MIN_PIECE ? LA_MIN_PIECE : p;
@@ -146,8 +150,8 @@ __device__ inline Seq find_item(const LatentAttentionArgs& a, int piece, int ite
 template <bool BF, int R_, int ROT, int MT>
 struct Config {
     static constexpr int ES = BF ? 2 : 4, R = R_, RB = (R + ROT) * ES;
-    static constexpr int NW = BF && MT > 1 ? 8 : 4;                          // waves
-    static constexpr int QT = BF ? 4 : 2, TILE = 16 * QT;                    // 16-token blocks, tokens of a tile
+    static constexpr int NW = MT == 8 ? 8 : 4;                               // waves
+    static constexpr int QT = MT == 8 ? 4 : 2, TILE = 16 * QT;               // 16-token blocks, tokens of a tile
     static constexpr int CT = R / 16 / NW;                                   // 16-element tiles whose sums a wave holds
     static constexpr int PANELS = RB / 128, TAIL = PANELS * TILE * 128;      // whole panels, where the rest begins
     static constexpr bool HAS_TAIL = RB % 128 != 0;
@@ -436,7 +440,7 @@ latent_attention_kernel(const LatentAttentionArgs a, int items, int rb_n) {
         lds_barrier();
         if constexpr (BF) {
             // inner indexes 8 g .. 8 g + 7 of each 32 tokens
-            constexpr int STEPS = 2 * CT, RING = 3;
+            constexpr int STEPS = TILE / 32 * CT, RING = 4;
             const int row = 8 * g + (c >> 2);
             const int e0 = (2 * CT * wave) & 7;      // the wave's first chunk of a panel
             const char* base = tile + (2 * CT * wave) / 8 * PANEL + row * 128 + (c & 1) * 8;
@@ -936,9 +940,12 @@ int launch_rows(const LatentAttentionArgs& a, hipStream_t st) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return (int)e;
     }
+    // pieces that a sequence may have
+    const bool many = std::min<int64_t>((cap + LA_MIN_PIECE - 1) / LA_MIN_PIECE, LA_TARGET / ((int64_t)a.B * rb) + 1) > LO_PIECES;
     {
         KernelTimer kt_("latent_out", st);
-        // as few sets a row as give every CU a workgroup; few rows: slices of the head's elements too
+        // As few sets a row as give every CU a workgroup, and all 16 for many pieces (two sequences of 8000, 128 heads: 47 us
+        // with 4 sets, 21 with 16); few rows: slices of the head's elements too
         auto go = [&](auto d, auto ds, auto sets) {
             constexpr int D = decltype(d)::value, DS = decltype(ds)::value, S = decltype(sets)::value, TOK = 16 / S;
             latent_out_kernel<BF, R, D, DS, S><<<grid_of((a.T + TOK - 1) / TOK * a.n_q * (D / DS)), dim3(256), 0, st>>>(a, D / DS);
@@ -947,10 +954,13 @@ int launch_rows(const LatentAttentionArgs& a, hipStream_t st) {
             using N1 = std::integral_constant<int, 1>;
             using N4 = std::integral_constant<int, 4>;
             using N16 = std::integral_constant<int, 16>;
-            if ((a.T + 15) / 16 * a.n_q >= LO_GROUPS) go(d, d, N1{});
-            else if ((a.T + 3) / 4 * a.n_q >= LO_GROUPS) go(d, d, N4{});
-            else if ((a.T + 3) / 4 * a.n_q * (decltype(d)::value / 32) >= LO_GROUPS) go(d, std::integral_constant<int, 32>{}, N4{});
-            else go(d, std::integral_constant<int, 32>{}, N16{});
+            using N32 = std::integral_constant<int, 32>;
+            const int64_t one = (a.T + 15) / 16 * a.n_q, four = (a.T + 3) / 4 * a.n_q;
+            if (many) a.T * a.n_q >= LO_GROUPS ? go(d, d, N16{}) : go(d, N32{}, N16{});
+            else if (one >= LO_GROUPS) go(d, d, N1{});
+            else if (four >= LO_GROUPS) go(d, d, N4{});
+            else if (four * (decltype(d)::value / 32) >= LO_GROUPS) go(d, N32{}, N4{});
+            else go(d, N32{}, N16{});
         };
         if (a.head_dim == 64) of(std::integral_constant<int, 64>{});
         else of(std::integral_constant<int, 128>{});
