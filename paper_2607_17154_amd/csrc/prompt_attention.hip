@@ -97,24 +97,37 @@ __device__ inline int swap_v(int r) {
 template <bool BF, int D, int ROT>
 struct Layout {
     static constexpr int ES = BF ? 2 : 4, TILE = PA_TILE<BF>, RBD = D * ES, RBR = ROT * ES;
-    static constexpr int K = 0, R = TILE * RBD, V = R + TILE * RBR, STAGE = V + TILE * RBD;
+    static constexpr int R = TILE * RBD, KEYS = R + TILE * RBR, VALUES = TILE * RBD;      // a tile's keys, rotary part behind them
+    static constexpr int V = 2 * KEYS, BYTES = V + 2 * VALUES;                           // two tiles' keys, two tiles' values
     static constexpr int QN = (D + ROT) * ES / 32;       // 16-byte pieces of a query that a lane holds
 };
 
-// TILE rows of RB bytes, `stride` bytes apart in memory, into LDS; rows past the resource's end arrive as zeros
-template <int RB, int TILE, int KIND, bool BF>
-__device__ inline void issue_rows(__amdgpu_buffer_rsrc_t rs, uint32_t stride, char* to, int wave, int lane) {
-    constexpr int CH = RB / 16, PIECES = TILE * RB / 1024 / PA_WAVES;
-    static_assert(TILE * RB % (1024 * PA_WAVES) == 0, "whole pieces a wave");
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-        const int piece = wave * PIECES + i, row = piece * (64 / CH) + lane / CH;
-        const int ch = (lane % CH) ^ (KIND == 0 ? swap_k<RB>(row) : swap_v<BF, RB>(row));
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(to + piece * 1024), 16, row * stride + ch * 16, 0, 0, 0);
-    }
+// TILE rows of RB bytes, `stride` bytes apart in memory, into LDS by pieces of 1024 bytes, N of them a wave; where a lane's
+// 16 bytes of a piece lie is kept.  Rows behind the last of `left` take the last one's.
+template <bool BF, int RB, int KIND>
+__device__ inline uint32_t lane_place(int row, int lane, uint32_t stride, int last) {
+    constexpr int CH = RB / 16;
+    const int swap = KIND == 0 ? swap_k<RB>(row) : swap_v<BF, RB>(row);
+    return std::min(row, last) * stride + ((lane % CH) ^ swap) * 16;
 }
-__device__ inline __amdgpu_buffer_rsrc_t make_rsrc(const void* base, uint32_t bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, (int)bytes, 0x00020000);
+template <bool BF, int RB, int KIND, int N>
+__device__ inline void lane_places(uint32_t (&o)[N], uint32_t stride, int wave, int lane) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        o[i] = lane_place<BF, RB, KIND>((wave * N + i) * (1024 / RB) + lane / (RB / 16), lane, stride, 0x7FFF);
+}
+template <bool BF, int RB, int KIND, int N>
+__device__ inline __attribute__((always_inline)) void issue_rows(const uint32_t (&o)[N], const char* from, int left, uint32_t stride, char* to,
+                                                                 int wave, int lane) {
+    if (left >= N * PA_WAVES * 1024 / RB) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) load_lds16(from + o[i], to + (wave * N + i) * 1024);
+    } else {
+#pragma unroll 1
+        for (int i = 0; i < N; ++i)
+            load_lds16(from + lane_place<BF, RB, KIND>((wave * N + i) * (1024 / RB) + lane / (RB / 16), lane, stride, left - 1),
+                       to + (wave * N + i) * 1024);
+    }
 }
 
 template <int N>
@@ -127,23 +140,30 @@ __device__ inline void wait_loads() {
 // every load that is on its way)
 __device__ inline void lds_barrier() { asm volatile("s_barrier" ::: "memory"); }
 
-// Positions of a tile's V that hold an infinity or a NaN, a bit each, by one wave
+// Positions of a tile's values that hold an infinity or a NaN, a bit each; every wave finds them all.  They become zeros: a
+// weight of 0 would not keep what is no number out of a row's sums.
 template <bool BF, int D>
-__device__ inline uint64_t not_finite(const char* v, int lane) {
-    constexpr int CH = D * (BF ? 2 : 4) / 16;
+__device__ inline uint64_t clean_values(char* v, int wave, int lane) {
+    constexpr int CH = D * (BF ? 2 : 4) / 16, PIECES = PA_TILE<BF> * CH / 64;
+    auto bad = [&](const u32x4& x) {
+        bool r = false;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) r |= (BF && (x[w] & 0x7F80u) == 0x7F80u) | ((x[w] & 0x7F800000u) == 0x7F800000u);
+        return r;
+    };
     uint64_t m = 0;
 #pragma unroll 4
-    for (int i = 0; i < PA_TILE<BF> * CH / 64; ++i) {
-        const u32x4 x = *(const u32x4*)(v + (i * 64 + lane) * 16);
-        bool bad = false;
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-            bad |= BF ? (x[w] & 0x7F80u) == 0x7F80u || (x[w] & 0x7F800000u) == 0x7F800000u : (x[w] & 0x7F800000u) == 0x7F800000u;
-        if (bad) m |= 1ull << ((i * 64 + lane) / CH);
-    }
-    if (!__builtin_amdgcn_ballot_w64(m != 0)) return 0;
+    for (int i = 0; i < PIECES; ++i)
+        if (bad(*(const u32x4*)(v + (i * 64 + lane) * 16))) m |= 1ull << ((i * 64 + lane) / CH);
+    if (!__builtin_amdgcn_ballot_w64(m != 0)) return 0;  // (alike in all waves)
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) m |= __shfl_xor((unsigned long long)m, o);
+    __syncthreads();
+    for (int i = wave; i < PIECES; i += PA_WAVES) {
+        u32x4* at = (u32x4*)(v + (i * 64 + lane) * 16);
+        if (bad(*at)) *at = u32x4{0u, 0u, 0u, 0u};
+    }
+    __syncthreads();
     return m;
 }
 
@@ -153,33 +173,29 @@ struct State {
     f32x16 o[D / 32];
 };
 
-// One tile by one wave.  edge: some row of the workgroup does not see all of it; the lane's row sees positions up to
-// lim (of the tile's: lim - t0).
+// A lane's chunk of keys for block tb, inner step k.  (2 k + h) ^ swap = (h ^ swap) ^ 2 k
 template <bool BF, int D, int ROT>
-__device__ inline __attribute__((always_inline)) void attend_tile(const char* st, const u32x4* q, float scale2, bool edge, int see, int lane,
-                                                                  State<BF, D, ROT>& s) {
+__device__ inline __attribute__((always_inline)) u32x4 key_part(const char* keys, int tb, int k, int lane) {
     using Lay = Layout<BF, D, ROT>;
-    constexpr int NB = Lay::TILE / 32;
+    constexpr int KN = Lay::RBD / 32, RBR = ROT ? Lay::RBR : 64;
+    const int c = lane & 31, h = lane >> 5;
+    if (k < KN) return *(const u32x4*)(keys + 32 * tb * Lay::RBD + ((c * Lay::RBD + (h ^ swap_k<Lay::RBD>(c)) * 16) ^ (32 * k)));
+    return *(const u32x4*)(keys + Lay::R + 32 * tb * RBR + ((c * RBR + (h ^ swap_k<RBR>(c)) * 16) ^ (32 * (k - KN))));
+}
+
+// One tile by one wave, its scores in sc; NEXT: the scores of the tile behind it are made meanwhile.  edge: some row of the
+// workgroup does not see all of the tile; the lane's row sees positions up to see; bad: positions whose values are no numbers.
+template <bool BF, int D, int ROT, bool NEXT, class Load>
+__device__ inline __attribute__((always_inline)) void attend_tile(char* __restrict k0, const char* __restrict keys,
+                                                                  const char* __restrict values, char* __restrict v1, const Load& load, const u32x4* q, float scale2, bool edge,
+                                                                  int see, uint64_t bad, int lane, f32x16 (&sc)[PA_TILE<BF> / 32],
+                                                                  f32x16 (&nx)[PA_TILE<BF> / 32], State<BF, D, ROT>& s) {
+    using Lay = Layout<BF, D, ROT>;
+    constexpr int NB = Lay::TILE / 32, QN = Lay::QN, STEPS = NB * QN;
+    if constexpr (NEXT) load(k0, v1);
     const int c = lane & 31, h = lane >> 5;
     const float ninf = -__builtin_inff();
-    f32x16 sc[NB];
-#pragma unroll
-    for (int tb = 0; tb < NB; ++tb) {
-        sc[tb] = f32x16{};
-        const int row = 32 * tb + c;
-#pragma unroll
-        for (int k = 0; k < Lay::RBD / 32; ++k)
-            sc[tb] = mma32<BF>(*(const u32x4*)(st + Lay::K + row * Lay::RBD + (((2 * k + h) ^ swap_k<Lay::RBD>(row)) * 16)), q[k], sc[tb]);
-        if constexpr (ROT > 0) {
-#pragma unroll
-            for (int k = 0; k < Lay::RBR / 32; ++k)
-                sc[tb] = mma32<BF>(*(const u32x4*)(st + Lay::R + row * Lay::RBR + (((2 * k + h) ^ swap_k<Lay::RBR>(row)) * 16)),
-                                   q[Lay::RBD / 32 + k], sc[tb]);
-        }
-    }
-    uint64_t bad = 0;
     if (edge) {
-        bad = not_finite<BF, D>(st + Lay::V, lane);
 #pragma unroll
         for (int tb = 0; tb < NB; ++tb)
 #pragma unroll
@@ -187,14 +203,19 @@ __device__ inline __attribute__((always_inline)) void attend_tile(const char* st
                 const int p = 32 * tb + 8 * (i >> 2) + 4 * h + (i & 3);
                 sc[tb][i] = p <= see ? sc[tb][i] : ninf;
             }
+        // a weight of 0 would not keep what is no number out of a row's sums: it lies as 0 in LDS, and the rows that
+        // see it become NaN here
+        if (bad) {
+            const uint64_t seen = see < 0 ? 0ull : see >= 63 ? ~0ull : (2ull << see) - 1;
+            if (bad & seen) s.l = __builtin_nanf("");
+        }
     }
     float top = ninf;
 #pragma unroll
     for (int tb = 0; tb < NB; ++tb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[tb][i]);
-    top *= scale2;                                       // (scale2 >= 0; -inf stays, 0 of it included, as no number)
-    top = top == top ? top : ninf;
+    top *= scale2;                                       // (scale2 > 0)
     if (__builtin_amdgcn_ballot_w64(top > s.m + PA_LAG)) {
         const float x = fmaxf(top, __shfl_xor(top, 32));
         const float m = x > s.m + PA_LAG ? x : s.m;
@@ -205,25 +226,38 @@ __device__ inline __attribute__((always_inline)) void attend_tile(const char* st
         for (int d = 0; d < D / 32; ++d) s.o[d] = s.o[d] * al;
     }
     const float m = s.m == ninf ? 0.f : s.m;
+    constexpr int AHEAD = 4;
+    u32x4 kf[AHEAD];
+    if constexpr (NEXT) {
 #pragma unroll
-    for (int tb = 0; tb < NB; ++tb)
+        for (int i = 0; i < AHEAD; ++i) kf[i] = key_part<BF, D, ROT>(keys, i % NB, i / NB, lane);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[tb][i], scale2, -m));
-            if (edge) p = sc[tb][i] == ninf ? 0.f : p;
-            sc[tb][i] = p;
+        for (int tb = 0; tb < NB; ++tb) nx[tb] = f32x16{};
+    }
+    int done = 0;
+#pragma unroll
+    for (int i = 0; i < (NEXT ? STEPS : 1); ++i) {
+        if constexpr (NEXT) {
+            nx[i % NB] = mma32<BF>(kf[i % AHEAD], q[i / NB], nx[i % NB]);
+            if (i + AHEAD < STEPS) kf[i % AHEAD] = key_part<BF, D, ROT>(keys, (i + AHEAD) % NB, (i + AHEAD) / NB, lane);
+        }
+        const int to = NEXT ? 16 * NB * (i + 1) / STEPS : 16 * NB;
+#pragma unroll
+        for (int e = 0; e < 16 * NB; ++e) {
+            if (e < done || e >= to) continue;
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e / 16][e % 16], scale2, -m));   // (of -infinity: 0)
+            sc[e / 16][e % 16] = p;
             s.l += p;
         }
-    if (bad) {
-        // a weight of 0 would not keep what is no number out of a row's sums: it is taken as 0 below, and the rows that
-        // see it become NaN here
-        const uint64_t seen = see < 0 ? 0ull : see >= 63 ? ~0ull : (2ull << see) - 1;
-        if (bad & seen) s.l = __builtin_nanf("");
+        done = to;
     }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int tb = 0; tb < NB; ++tb) {
         if constexpr (BF) {
-            const int x = lane & 15, i = x >> 2, j = x & 3, col = ((lane >> 4) & 1) * 16 + 4 * j;
+            // row 4 h + i of eight, elements col .. col + 3 of 32
+            const int i = (lane >> 2) & 3, col = ((lane >> 4) & 1) * 16 + 4 * (lane & 3);
+            const int at = (4 * h + i) * Lay::RBD + (((col >> 3) ^ swap_v<BF, Lay::RBD>(i)) * 16) + (col & 7) * 2;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 u32x4 pf;
@@ -234,17 +268,9 @@ __device__ inline __attribute__((always_inline)) void attend_tile(const char* st
                     u32x4 vf;
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
-                        const int row = 32 * tb + 16 * k + 8 * u + 4 * h + i, e = 32 * d + col;
-                        const u32x2 t = read_turned(st + Lay::V + row * Lay::RBD + (((e >> 3) ^ swap_v<BF, Lay::RBD>(row)) * 16) + (e & 7) * 2);
+                        const u32x2 t = read_turned(values + (32 * tb + 16 * k + 8 * u) * Lay::RBD + (at ^ (64 * d)));
                         vf[2 * u] = t[0];
                         vf[2 * u + 1] = t[1];
-                    }
-                    if (bad) {
-#pragma unroll
-                        for (int w = 0; w < 4; ++w) {
-                            if ((vf[w] & 0x7F80u) == 0x7F80u) vf[w] &= 0xFFFF0000u;
-                            if ((vf[w] & 0x7F800000u) == 0x7F800000u) vf[w] &= 0xFFFFu;
-                        }
                     }
                     s.o[d] = mma32<true>(vf, pf, s.o[d]);
                 }
@@ -256,8 +282,7 @@ __device__ inline __attribute__((always_inline)) void attend_tile(const char* st
 #pragma unroll
                 for (int d = 0; d < D / 32; ++d) {
                     const int e = 32 * d + c;
-                    float v = *(const float*)(st + Lay::V + row * Lay::RBD + (((e >> 2) ^ swap_v<BF, Lay::RBD>(row)) * 16) + (e & 3) * 4);
-                    if (bad) v = (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u ? 0.f : v;
+                    const float v = *(const float*)(values + row * Lay::RBD + (((e >> 2) ^ swap_v<BF, Lay::RBD>(row)) * 16) + (e & 3) * 4);
                     s.o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, sc[tb][i], s.o[d], 0, 0, 0);
                 }
             }
@@ -269,16 +294,16 @@ template <bool BF, int D, int ROT>
 __global__ void __launch_bounds__(64 * PA_WAVES, 2) prompt_attention_kernel(const PromptArgs a, int64_t items, int64_t per_xcd) {
     using Lay = Layout<BF, D, ROT>;
     constexpr int ES = Lay::ES, TILE = Lay::TILE;
-    __shared__ __attribute__((aligned(16))) char mem[2 * Lay::STAGE];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int c = lane & 31, h = lane >> 5;
+    __shared__ __attribute__((aligned(16))) char mem[Lay::BYTES];
+    const int tid = threadIdx.x, lane_ = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane_ & 31, h = lane_ >> 5;
     // a key/value head's row blocks after one another on one XCD, where its rows are in L2
     const int64_t id = block_number(), unit = (id & 7) * per_xcd + (id >> 3);
     if ((id >> 3) >= per_xcd || unit >= items * a.n_kv) return;
     const int kvh = (int)(unit / items);
     Seq s;
     int rb;
-    if (!find_block(a, unit - kvh * items, lane, s, rb)) return;
+    if (!find_block(a, unit - kvh * items, lane_, s, rb)) return;
     const int G = a.n_q / a.n_kv;
     const int64_t rows = (int64_t)s.n * G, row0 = (int64_t)rb * PA_ROWS, row = row0 + 32 * wave + c;
     const bool in = row < rows;
@@ -288,17 +313,18 @@ __global__ void __launch_bounds__(64 * PA_WAVES, 2) prompt_attention_kernel(cons
     // positions that some row of the workgroup sees, and that all of them do
     const int last = (int)((std::min(rows, row0 + PA_ROWS) - 1) / G), end = std::max(0, std::min(s.len, before + last + 1));
     const int all = before + (int)(row0 / G) + 1;
-    const float scale2 = std::fabs(a.scale) * LOG2E;
+    // scores times scale2 > 0: a negative scale's sign goes to the query, a scale of 0 makes it zeros
+    const float scale2 = a.scale == 0.f ? 1.0f : std::fabs(a.scale) * LOG2E;
     u32x4 q[Lay::QN];
     {
         const char* from = (const char*)a.q + ((int64_t)(s.q0 + i) * a.n_q + hq) * ((D + ROT) * ES) + 16 * h;
-        const uint32_t flip = a.scale < 0.f ? (BF ? 0x80008000u : 0x80000000u) : 0u;
+        const uint32_t flip = a.scale < 0.f ? (BF ? 0x80008000u : 0x80000000u) : 0u, keep = a.scale == 0.f ? 0u : ~0u;
 #pragma unroll
         for (int k = 0; k < Lay::QN; ++k) {
             q[k] = u32x4{0u, 0u, 0u, 0u};
             if (in) q[k] = *(const u32x4*)(from + 32 * k);
 #pragma unroll
-            for (int w = 0; w < 4; ++w) q[k][w] ^= flip;
+            for (int w = 0; w < 4; ++w) q[k][w] = (q[k][w] & keep) ^ flip;
         }
     }
     State<BF, D, ROT> st;
@@ -307,29 +333,67 @@ __global__ void __launch_bounds__(64 * PA_WAVES, 2) prompt_attention_kernel(cons
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) st.o[d] = f32x16{};
     const uint32_t stride = (uint32_t)a.n_kv * D * ES;
-    auto issue = [&](int t0, char* to) __attribute__((always_inline)) {
-        const int64_t at = (int64_t)s.k0 + t0;
-        const uint32_t left = (uint32_t)std::min(TILE, s.len - t0);
-        const int64_t off = at * stride + kvh * (D * ES);
-        issue_rows<Lay::RBD, TILE, 0, BF>(make_rsrc((const char*)a.k + off, (left - 1) * stride + D * ES), stride, to + Lay::K, wave, lane);
-        if constexpr (ROT > 0)
-            issue_rows<Lay::RBR, TILE, 0, BF>(make_rsrc((const char*)a.r + at * Lay::RBR, left * Lay::RBR), Lay::RBR, to + Lay::R, wave, lane);
-        issue_rows<Lay::RBD, TILE, 1, BF>(make_rsrc((const char*)a.v + off, (left - 1) * stride + D * ES), stride, to + Lay::V, wave, lane);
+    constexpr int NK = TILE * Lay::RBD / 1024 / PA_WAVES, NR = ROT ? TILE * Lay::RBR / 1024 / PA_WAVES : 1;
+    static_assert(NK * 1024 * PA_WAVES == TILE * Lay::RBD && (!ROT || NR * 1024 * PA_WAVES == TILE * Lay::RBR), "whole pieces a wave");
+    uint32_t ko[NK], ro[NR], vo[NK];
+    lane_places<BF, Lay::RBD, 0>(ko, stride, wave, lane_);
+    lane_places<BF, Lay::RBD, 1>(vo, stride, wave, lane_);
+    if constexpr (ROT > 0) lane_places<BF, Lay::RBR, 0>(ro, Lay::RBR, wave, lane_);
+    const char *const kb = (const char*)a.k + (int64_t)s.k0 * stride + kvh * (D * ES), *const vb = (const char*)a.v + (kb - (const char*)a.k),
+               *const rb_ = ROT ? (const char*)a.r + (int64_t)s.k0 * Lay::RBR : nullptr;
+    auto keys = [&](int t0, char* to, int lane) __attribute__((always_inline)) {
+        issue_rows<BF, Lay::RBD, 0>(ko, kb + (int64_t)t0 * stride, s.len - t0, stride, to, wave, lane);
+        if constexpr (ROT > 0) issue_rows<BF, Lay::RBR, 0>(ro, rb_ + (int64_t)t0 * Lay::RBR, s.len - t0, Lay::RBR, to + Lay::R, wave, lane);
     };
-    // (the first two tiles are on their way together)
-    if (end > 0) issue(0, mem);
-    for (int t0 = 0, buf = 0; t0 < end; t0 += TILE, buf ^= 1) {
-        if (t0 > 0) {
-            wait_loads<0>();
-            __syncthreads();                             // the tile has arrived, and the one before has been read
+    auto values = [&](int t0, char* to, int lane) __attribute__((always_inline)) {
+        issue_rows<BF, Lay::RBD, 1>(vo, vb + (int64_t)t0 * stride, s.len - t0, stride, to, wave, lane);
+    };
+    // Tile t's weights and its product with V run beside tile t + 1's scores: the keys are a tile ahead of the values.
+    // What lies in k0 and v1 has been read, k1 and v0 are on their way.
+    auto step = [&](auto next, int t0, char* k0, char* k1, char* v0, char* v1, f32x16 (&sc)[TILE / 32],
+                    f32x16 (&nx)[TILE / 32]) __attribute__((always_inline)) {
+        const bool edge = t0 + TILE > all;
+        uint64_t bad = 0;
+        int lane = lane_;
+        asm volatile("" : "+v"(lane));                   // (addresses made anew for each tile: kept, they would take the sums' registers)
+        wait_loads<0>();
+        __syncthreads();
+        if (edge) bad = clean_values<BF, D>(v0, wave, lane);
+        auto load = [&](char* k, char* v) __attribute__((always_inline)) {
+            if (t0 + 2 * TILE < end) keys(t0 + 2 * TILE, k, lane);
+            values(t0 + TILE, v, lane);
+        };
+        attend_tile<BF, D, ROT, decltype(next)::value>(k0, k1, v0, v1, load, q, scale2, edge, lim - t0, bad, lane, sc, nx, st);
+    };
+    if (end > 0) {
+        char *const k0 = mem, *const k1 = mem + Lay::KEYS, *const v0 = mem + Lay::V, *const v1 = v0 + Lay::VALUES;
+        f32x16 s0[TILE / 32], s1[TILE / 32];
+        keys(0, k0, lane_);
+        if (TILE < end) keys(TILE, k1, lane_);
+        values(0, v0, lane_);
+        if (TILE < end) wait_loads<(Lay::KEYS + Lay::VALUES) / 1024 / PA_WAVES>();
+        else wait_loads<Lay::VALUES / 1024 / PA_WAVES>();
+        lds_barrier();
+#pragma unroll
+        for (int tb = 0; tb < TILE / 32; ++tb) {
+            s0[tb] = f32x16{};
+#pragma unroll
+            for (int k = 0; k < Lay::QN; ++k) s0[tb] = mma32<BF>(key_part<BF, D, ROT>(k0, tb, k, lane_), q[k], s0[tb]);
         }
-        if (t0 + TILE < end) issue(t0 + TILE, mem + (buf ^ 1) * Lay::STAGE);
-        if (t0 == 0) {
-            if (TILE < end) wait_loads<Lay::STAGE / 1024 / PA_WAVES>();
-            else wait_loads<0>();
-            lds_barrier();
+        int t0 = 0;
+        for (; t0 + 2 * TILE < end; t0 += 2 * TILE) {
+            step(std::true_type{}, t0, k0, k1, v0, v1, s0, s1);
+            step(std::true_type{}, t0 + TILE, k1, k0, v1, v0, s1, s0);
         }
-        attend_tile<BF, D, ROT>(mem + buf * Lay::STAGE, q, scale2, t0 + TILE > all, lim - t0, lane, st);
+        char* v = v0;
+        if (t0 + TILE < end) {
+            step(std::true_type{}, t0, k0, k1, v0, v1, s0, s1);
+#pragma unroll
+            for (int tb = 0; tb < TILE / 32; ++tb) s0[tb] = s1[tb];
+            v = v1;
+            t0 += TILE;
+        }
+        step(std::false_type{}, t0, k0, k1, v, v1, s0, s1);
     }
     if (!in) return;
     const float l = st.l + __shfl_xor(st.l, 32);
