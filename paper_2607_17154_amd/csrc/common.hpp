@@ -348,11 +348,11 @@ struct PromptArgs {
     void* out;
     float* lse;
     // workspace
-    float* part_ml;        // [items][rows of a block][2] maximum and sum of each piece's rows
-    float* part_o;         // [items][rows of a block][head_dim] its sums
+    float* part_ml;        // [pieces][T][n_q][2] maximum and sum of each piece of a row's positions
+    float* part_o;         // [pieces][T][n_q][head_dim] its sums
 };
-// partial results (row block, piece of its positions) that a batch has at most: rows of them
-int64_t prompt_part_rows(int dtype, int n_q, int n_kv, int head_dim, int rot, int64_t T, int B);
+// pieces into which a batch's positions are split, at most
+int prompt_pieces(int n_q, int n_kv, int64_t T, int B);
 int launch_prompt_attention(const PromptArgs& a, void* stream);
 
 int launch_pack_gate_up(int dtype, int n, int f, int d, const void* g, const void* u, void* out,

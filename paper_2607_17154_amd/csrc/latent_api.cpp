@@ -95,9 +95,8 @@ int check_prompt(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t head_dim, int
     if (T < 0 || T > (INT_LIMIT - 1) / n_q) return bad(who, "T * n_q must lie in [0, 2^31)");
     return ORDERMOE_OK;
 }
-size_t prompt_ws(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t rotary_dim, int64_t T, int32_t B, Carver& c,
-                 PromptArgs* a) {
-    const size_t rows = (size_t)prompt_part_rows(dtype, n_q, n_kv, head_dim, rotary_dim, T, B);
+size_t prompt_ws(int32_t n_q, int32_t n_kv, int32_t head_dim, int64_t T, int32_t B, Carver& c, PromptArgs* a) {
+    const size_t pieces = prompt_pieces(n_q, n_kv, T, B), rows = pieces > 1 ? pieces * T * n_q : 0;
     float* ml = c.take<float>(rows * 2);
     float* po = c.take<float>(rows * head_dim);
     if (a) { a->part_ml = ml; a->part_o = po; }
@@ -197,7 +196,7 @@ extern "C" size_t ordermoe_prompt_attention_workspace_size(int32_t dtype, int32_
                                                            int32_t rotary_dim, int64_t T, int32_t B) {
     if (check_prompt(dtype, n_q, n_kv, head_dim, rotary_dim, T, B, "prompt_attention") != ORDERMOE_OK) return 0;
     Carver c(nullptr);
-    return prompt_ws(dtype, n_q, n_kv, head_dim, rotary_dim, T, B, c, nullptr);
+    return prompt_ws(n_q, n_kv, head_dim, T, B, c, nullptr);
 }
 
 extern "C" int ordermoe_prompt_attention(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t rotary_dim, const void* q,
@@ -220,7 +219,7 @@ extern "C" int ordermoe_prompt_attention(int32_t dtype, int32_t n_q, int32_t n_k
     a.q = q; a.k = k; a.r = r; a.v = v; a.T = T; a.L = L; a.q_start = q_start; a.kv_start = kv_start;
     a.scale = scale; a.out = out; a.lse = lse;
     Carver c(ws);
-    prompt_ws(dtype, n_q, n_kv, head_dim, rotary_dim, T, B, c, &a);
+    prompt_ws(n_q, n_kv, head_dim, T, B, c, &a);
     const int e = launch_prompt_attention(a, stream);
     if (e) return hip_fail(e, "prompt_attention launch");
     clear_error();

@@ -3,6 +3,8 @@
 //   prompt_attention_kernel  one workgroup per (128 query rows of a sequence, key/value
 //                            head): its four waves take 32 rows each and go through the
 //                            positions together, a tile at a time
+//   prompt_join_kernel       few rows: their positions are split over workgroups, and this
+//                            adds up the pieces in order
 // The query rows of a key/value head are its n_b tokens times the n_q / n_kv query heads
 // that share it (row = token * (n_q / n_kv) + head).
 //
@@ -35,6 +37,11 @@ constexpr int PA_TILE = BF ? 64 : 32;                    // positions of a tile
 // A maximum is taken over only when some score passes it by 8 (a factor of 256 in the weights, which fp32 sums
 // and bf16 weights hold as well as 1): most tiles then need no exchange between lanes and no rescaling.
 constexpr float PA_LAG = 8.0f;
+
+// Blocks of rows that leave the card empty: their positions are split into pieces, so many that the workgroups fill it, of
+// PA_LEAST tiles or more of the longest sequence there can be.  (16 tokens behind 8000, 8 key heads: 152 us whole, 27 in
+// pieces of 8 tiles or more, 28 of 4, 33 of 16; 300 tokens of 16 heads: 18 whole or of 8, 20 of 4.)
+constexpr int PA_FEW = 128, PA_FILL = 512, PA_LEAST = 8;
 
 __host__ __device__ inline int64_t row_blocks(int64_t rows) { return (rows + PA_ROWS - 1) / PA_ROWS; }
 
@@ -290,15 +297,21 @@ __device__ inline __attribute__((always_inline)) void attend_tile(char* __restri
     }
 }
 
-template <bool BF, int D, int ROT>
-__global__ void __launch_bounds__(64 * PA_WAVES, 2) prompt_attention_kernel(const PromptArgs a, int64_t items, int64_t per_xcd) {
+template <bool BF, int D, int ROT, bool SPLIT>
+__global__ void __launch_bounds__(64 * PA_WAVES, 2) prompt_attention_kernel(const PromptArgs a, int64_t items, int64_t per_xcd, int pieces) {
     using Lay = Layout<BF, D, ROT>;
     constexpr int ES = Lay::ES, TILE = Lay::TILE;
     __shared__ __attribute__((aligned(16))) char mem[Lay::BYTES];
     const int tid = threadIdx.x, lane_ = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane_ & 31, h = lane_ >> 5;
     // a key/value head's row blocks after one another on one XCD, where its rows are in L2
-    const int64_t id = block_number(), unit = (id & 7) * per_xcd + (id >> 3);
+    const int64_t id = block_number();
+    int64_t unit = (id & 7) * per_xcd + (id >> 3);
+    int piece = 0;
+    if constexpr (SPLIT) {
+        piece = (int)(unit % pieces);
+        unit /= pieces;
+    }
     if ((id >> 3) >= per_xcd || unit >= items * a.n_kv) return;
     const int kvh = (int)(unit / items);
     Seq s;
@@ -311,7 +324,13 @@ __global__ void __launch_bounds__(64 * PA_WAVES, 2) prompt_attention_kernel(cons
     const int before = s.len - s.n;                      // (may be negative)
     const int lim = in ? before + i : -1;                // the last position that the lane's row sees
     // positions that some row of the workgroup sees, and that all of them do
-    const int last = (int)((std::min(rows, row0 + PA_ROWS) - 1) / G), end = std::max(0, std::min(s.len, before + last + 1));
+    const int last = (int)((std::min(rows, row0 + PA_ROWS) - 1) / G);
+    int start = 0, end = std::max(0, std::min(s.len, before + last + 1));
+    if constexpr (SPLIT) {
+        const int tiles = (end + TILE - 1) / TILE;
+        start = (int)((int64_t)tiles * piece / pieces) * TILE;
+        end = std::min(end, (int)((int64_t)tiles * (piece + 1) / pieces) * TILE);
+    }
     const int all = before + (int)(row0 / G) + 1;
     // scores times scale2 > 0: a negative scale's sign goes to the query, a scale of 0 makes it zeros
     const float scale2 = a.scale == 0.f ? 1.0f : std::fabs(a.scale) * LOG2E;
@@ -365,13 +384,13 @@ __global__ void __launch_bounds__(64 * PA_WAVES, 2) prompt_attention_kernel(cons
         };
         attend_tile<BF, D, ROT, decltype(next)::value>(k0, k1, v0, v1, load, q, scale2, edge, lim - t0, bad, lane, sc, nx, st);
     };
-    if (end > 0) {
+    if (start < end) {
         char *const k0 = mem, *const k1 = mem + Lay::KEYS, *const v0 = mem + Lay::V, *const v1 = v0 + Lay::VALUES;
         f32x16 s0[TILE / 32], s1[TILE / 32];
-        keys(0, k0, lane_);
-        if (TILE < end) keys(TILE, k1, lane_);
-        values(0, v0, lane_);
-        if (TILE < end) wait_loads<(Lay::KEYS + Lay::VALUES) / 1024 / PA_WAVES>();
+        keys(start, k0, lane_);
+        if (start + TILE < end) keys(start + TILE, k1, lane_);
+        values(start, v0, lane_);
+        if (start + TILE < end) wait_loads<(Lay::KEYS + Lay::VALUES) / 1024 / PA_WAVES>();
         else wait_loads<Lay::VALUES / 1024 / PA_WAVES>();
         lds_barrier();
 #pragma unroll
@@ -380,7 +399,7 @@ __global__ void __launch_bounds__(64 * PA_WAVES, 2) prompt_attention_kernel(cons
 #pragma unroll
             for (int k = 0; k < Lay::QN; ++k) s0[tb] = mma32<BF>(key_part<BF, D, ROT>(k0, tb, k, lane_), q[k], s0[tb]);
         }
-        int t0 = 0;
+        int t0 = start;
         for (; t0 + 2 * TILE < end; t0 += 2 * TILE) {
             step(std::true_type{}, t0, k0, k1, v0, v1, s0, s1);
             step(std::true_type{}, t0 + TILE, k1, k0, v1, v0, s1, s0);
@@ -397,8 +416,19 @@ __global__ void __launch_bounds__(64 * PA_WAVES, 2) prompt_attention_kernel(cons
     }
     if (!in) return;
     const float l = st.l + __shfl_xor(st.l, 32);
-    const float r = l == 0.f ? 0.f : 1.0f / l;
     const int64_t at = (int64_t)(s.q0 + i) * a.n_q + hq;
+    if constexpr (SPLIT) {
+        const int64_t pr = (int64_t)piece * a.T * a.n_q + at;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                *(f32x4*)(a.part_o + pr * D + 32 * d + 8 * j + 4 * h) =
+                    f32x4{st.o[d][4 * j], st.o[d][4 * j + 1], st.o[d][4 * j + 2], st.o[d][4 * j + 3]};
+        if (h == 0) ((f32x2*)a.part_ml)[pr] = f32x2{st.m, l};
+        return;
+    }
+    const float r = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -408,13 +438,74 @@ __global__ void __launch_bounds__(64 * PA_WAVES, 2) prompt_attention_kernel(cons
     if (a.lse && h == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (st.m + __builtin_amdgcn_logf(l)) * LN2;
 }
 
+// The pieces of a row's positions, in order: a workgroup has 1024 / D rows of a block, a thread four elements
+template <bool BF, int D>
+__global__ void __launch_bounds__(256) prompt_join_kernel(const PromptArgs a, int64_t items, int pieces) {
+    constexpr int ROWS = 1024 / D, PER = PA_ROWS / ROWS;
+    const int tid = threadIdx.x;
+    const int64_t id = block_number(), unit = id / PER;
+    if (unit >= items * a.n_kv) return;
+    const int kvh = (int)(unit / items);
+    Seq s;
+    int rb;
+    if (!find_block(a, unit - kvh * items, tid & 63, s, rb)) return;
+    const int G = a.n_q / a.n_kv, e = tid % (D / 4) * 4;
+    const int64_t row = (int64_t)rb * PA_ROWS + (id % PER) * ROWS + tid / (D / 4);
+    if (row >= (int64_t)s.n * G) return;
+    const int i = (int)(row / G), hq = kvh * G + (int)(row - (int64_t)i * G);
+    const int64_t at = (int64_t)(s.q0 + i) * a.n_q + hq, step = a.T * a.n_q;
+    constexpr int U = 4;
+    float m = -__builtin_inff(), l = 0.f;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < pieces; p += U) {
+        f32x2 q[U];
+        f32x4 v[U];
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int64_t pr = at + std::min(p + k, pieces - 1) * step;
+            q[k] = ((const f32x2*)a.part_ml)[pr];
+            v[k] = *(const f32x4*)(a.part_o + pr * D + e);
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) top = fmaxf(top, q[k][0]);
+        const float al = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+        m = top;
+        l *= al;
+        x = x * al;
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (p + k >= pieces) break;
+            const float f = q[k][0] == m ? 1.0f : __builtin_amdgcn_exp2f(q[k][0] - m);
+            l += q[k][1] * f;
+            x = x + v[k] * f;
+        }
+    }
+    const float r = l == 0.f ? 0.f : 1.0f / l;
+    store4<BF>(a.out, at * D + e, x[0] * r, x[1] * r, x[2] * r, x[3] * r);
+    if (a.lse && e == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * LN2;
+}
+
+// row blocks: every sequence ends in one that is not full, at most
+int64_t blocks_at_most(int n_q, int n_kv, int64_t T, int B) {
+    const int64_t rows = T * (n_q / n_kv);
+    return std::min(rows, rows / PA_ROWS + B);
+}
+
 template <bool BF, int D, int ROT>
 int launch_rows(const PromptArgs& a, hipStream_t st) {
-    // row blocks: every sequence ends in one that is not full, at most
-    const int64_t items = std::min<int64_t>(a.T * (a.n_q / a.n_kv), a.T * (a.n_q / a.n_kv) / PA_ROWS + a.B);
-    const int64_t per = (items * a.n_kv + 7) / 8;
-    KernelTimer kt_("prompt_attention", st);
-    prompt_attention_kernel<BF, D, ROT><<<grid_of(per * 8), dim3(64 * PA_WAVES), 0, st>>>(a, items, per);
+    const int64_t items = blocks_at_most(a.n_q, a.n_kv, a.T, a.B), least = (int64_t)PA_LEAST * PA_TILE<BF>;
+    const int pieces = (int)std::min<int64_t>(prompt_pieces(a.n_q, a.n_kv, a.T, a.B), (a.L + least - 1) / least);
+    const int64_t per = (items * a.n_kv * std::max(pieces, 1) + 7) / 8;
+    {
+        KernelTimer kt_("prompt_attention", st);
+        if (pieces > 1) prompt_attention_kernel<BF, D, ROT, true><<<grid_of(per * 8), dim3(64 * PA_WAVES), 0, st>>>(a, items, per, pieces);
+        else prompt_attention_kernel<BF, D, ROT, false><<<grid_of(per * 8), dim3(64 * PA_WAVES), 0, st>>>(a, items, per, 1);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || pieces <= 1) return (int)e;
+    }
+    KernelTimer kt_("prompt_join", st);
+    prompt_join_kernel<BF, D><<<grid_of(items * a.n_kv * (PA_ROWS * D / 1024)), dim3(256), 0, st>>>(a, items, pieces);
     return (int)hipGetLastError();
 }
 template <bool BF, int D>
@@ -424,7 +515,10 @@ int launch_rot(const PromptArgs& a, hipStream_t st) {
 
 }  // namespace
 
-int64_t prompt_part_rows(int, int, int, int, int, int64_t, int) { return 0; }
+int prompt_pieces(int n_q, int n_kv, int64_t T, int B) {
+    const int64_t blocks = blocks_at_most(n_q, n_kv, T, B) * n_kv;
+    return blocks == 0 || blocks > PA_FEW ? 1 : (int)(PA_FILL / blocks);
+}
 
 int launch_prompt_attention(const PromptArgs& a, void* stream) {
     if (a.B == 0 || a.T == 0) return 0;
