@@ -233,6 +233,43 @@ int launch_write_dim(const LatentWriteArgs& a, hipStream_t st) {
 // ------------------------------------------------------------------ expansion
 constexpr int LE_SLAB = 128;                         // bytes of a row staged at a time
 
+// The workgroup's tile; false: there is none.  spread: eight token tiles after one another on each XCD, which then go
+// through all weights together
+__device__ inline bool find_tile(int64_t tok_tiles, int row_tiles, int spread, int64_t& tt, int& rt) {
+    const int64_t id = block_number();
+    if (spread) {
+        const int64_t x = id & 7, l = id >> 3, grp = l / (8 * row_tiles);
+        const int in = (int)(l - grp * (8 * row_tiles));
+        rt = in >> 3;
+        tt = (grp * 8 + (in & 7)) * 8 + x;
+    } else {
+        tt = id / row_tiles;
+        rt = (int)(id - tt * row_tiles);
+    }
+    return tt < tok_tiles;
+}
+// The rotary parts of a tile's tokens
+template <int ES>
+__device__ inline void rotary_out(const LatentExpandArgs& a, int64_t n0, int tokens, int tid) {
+    const int wide = a.cache.rank + a.cache.rot, per = a.cache.rot * ES / 16;
+    const int64_t slots = a.cache.n_pages << a.cache.page_shift;
+    for (int u = tid; u < tokens * per; u += 256) {
+        const int r = u / per, k = u - r * per;
+        if (n0 + r >= a.n) break;
+        const int64_t s = a.slots[n0 + r];
+        u32x4 v = {0u, 0u, 0u, 0u};
+        if (s >= 0 && s < slots) v = *(const u32x4*)(a.cache.rows + (s * wide + a.cache.rank) * ES + 16 * k);
+        *(u32x4*)((char*)a.r_out + (n0 + r) * a.cache.rot * ES + 16 * k) = v;
+    }
+}
+template <int N>
+__device__ inline void wait_vmem() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+__device__ inline void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\ns_barrier" ::: "memory"); }
+
 // A tile of TN tokens (the matrix unit's columns) x TN weight rows, 2 x 2 waves.  Both come in
 // slabs of 128 bytes a row through LDS, two buffers; chunk c of row r lies at c ^ (r % 8), so that the
 // 16-byte reads of eight rows lie on distinct banks.
@@ -242,19 +279,9 @@ __global__ void __launch_bounds__(256) latent_expand_kernel(const LatentExpandAr
     __shared__ __attribute__((aligned(16))) char mem[2][2][TN * LE_SLAB];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4, wm = wave >> 1, wn = wave & 1;
-    int64_t id = block_number(), tt;
+    int64_t tt;
     int rt;
-    if (spread) {
-        // eight token tiles after one another on each XCD, which then go through all weights together
-        const int64_t x = id & 7, l = id >> 3, grp = l / (8 * row_tiles);
-        const int in = (int)(l - grp * (8 * row_tiles));
-        rt = in >> 3;
-        tt = (grp * 8 + (in & 7)) * 8 + x;
-    } else {
-        tt = id / row_tiles;
-        rt = (int)(id - tt * row_tiles);
-    }
-    if (tt >= tok_tiles) return;
+    if (!find_tile(tok_tiles, row_tiles, spread, tt, rt)) return;
     const int R = a.cache.rank, wide = R + a.cache.rot, half = a.n_q * a.head_dim, r0 = rt * TN;
     const int64_t n0 = tt * TN, slots = a.cache.n_pages << a.cache.page_shift;
     const char* from[2][LOADS];
@@ -311,17 +338,98 @@ __global__ void __launch_bounds__(256) latent_expand_kernel(const LatentExpandAr
             else store4<BF>(a.v_out, n * half + wr - half, v[0], v[1], v[2], v[3]);
         }
     }
-    if (rt == 0) {
-        const int per = a.cache.rot * ES / 16;       // 16-byte pieces of the rotary part
-        for (int u = tid; u < TN * per; u += 256) {
-            const int r = u / per, k = u - r * per;
-            if (n0 + r >= a.n) break;
-            const int64_t s = a.slots[n0 + r];
-            u32x4 v = {0u, 0u, 0u, 0u};
-            if (s >= 0 && s < slots) v = *(const u32x4*)(a.cache.rows + (s * wide + R) * ES + 16 * k);
-            *(u32x4*)((char*)a.r_out + (n0 + r) * a.cache.rot * ES + 16 * k) = v;
+    if (rt == 0) rotary_out<ES>(a, n0, TN, tid);
+}
+
+// The same in tiles of 256 tokens x 128 weight rows, 2 x 2 waves of 128 x 64: a wave reads 12 pieces of LDS for 32 matrix
+// instructions, where 64 x 64 reads 8 for 16 and LDS is what bounds it.  Slabs of 64 bytes a row, three
+// buffers, two slabs on their way; chunk c of row r lies at c ^ (r / 4 % 4), so that the reads of 16 rows lie on
+// distinct banks.  The results go through LDS, in whole lines to memory.
+constexpr int LX_TOK = 256, LX_W = 128, LX_SLAB = 64, LX_STAGE = (LX_TOK + LX_W) * LX_SLAB;
+
+// (The loads' buffer and the one that is read never overlap: told so, the compiler does not wait for the loads first.)
+template <class Issue>
+__device__ inline __attribute__((always_inline)) void expand_slab(char* __restrict behind, const char* __restrict tok,
+                                                                  const char* __restrict wei, const Issue& issue, bool there, f32x4 (&acc)[4][8]) {
+    issue(behind);
+    if (!there) return;
+    u32x4 w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = *(const u32x4*)(wei + 16 * i * LX_SLAB);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const u32x4 t = *(const u32x4*)(tok + 16 * j * LX_SLAB);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i][j] = mma16<true>(w[i], t, acc[i][j]);
+    }
+}
+
+__global__ void __launch_bounds__(256, 2) latent_expand_wide_kernel(const LatentExpandArgs a, int64_t tok_tiles, int row_tiles, int spread) {
+    constexpr int PIECES = LX_STAGE / 1024 / 4;          // of a slab, a wave: 16 rows each, the tokens' first
+    __shared__ __attribute__((aligned(16))) char mem[3 * LX_STAGE];
+    __shared__ uint8_t s_in[LX_TOK];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, g = lane >> 4, wm = wave >> 1, wn = wave & 1;
+    int64_t tt;
+    int rt;
+    if (!find_tile(tok_tiles, row_tiles, spread, tt, rt)) return;
+    const int R = a.cache.rank, wide = R + a.cache.rot, half = a.n_q * a.head_dim, r0 = rt * LX_W;
+    const int64_t n0 = tt * LX_TOK, slots = a.cache.n_pages << a.cache.page_shift;
+    const char* from[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int r = (i * 4 + wave) * 16 + (lane >> 2), ch = (lane & 3) ^ ((lane >> 4) & 3);
+        if (i < LX_TOK / 64) {
+            int64_t s = n0 + r < a.n ? a.slots[n0 + r] : 0;
+            const bool in = s >= 0 && s < slots;
+            if ((lane & 3) == 0) s_in[r] = in;
+            from[i] = a.cache.rows + (in ? s : 0) * wide * 2 + ch * 16;
+        } else {
+            const int wr = r0 + r - LX_TOK < 2 * half ? r0 + r - LX_TOK : 0;
+            from[i] = (wr < half ? (const char*)a.w_k + (int64_t)wr * R * 2 : (const char*)a.w_v + (int64_t)(wr - half) * R * 2) + ch * 16;
         }
     }
+    auto issue = [&](char* to, int s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) load_lds16(from[i] + s * LX_SLAB, to + (i * 4 + wave) * 1024);
+    };
+    f32x4 acc[4][8] = {};                                // [weight tile][token tile]
+    const int slabs = R * 2 / LX_SLAB, place = c * LX_SLAB + (g ^ ((c >> 2) & 3)) * 16;
+    for (int s = -2, at = LX_STAGE; s < slabs; ++s) {
+        if (s >= 0) {
+            if (s + 1 < slabs) wait_vmem<PIECES>();
+            else wait_vmem<0>();
+            lds_barrier();                               // slab s has arrived, and slab s - 1 has been read
+        }
+        expand_slab(mem + (at == 0 ? 2 * LX_STAGE : at - LX_STAGE), mem + at + wn * (128 * LX_SLAB) + place,
+                    mem + at + (LX_TOK + wm * 64) * LX_SLAB + place,
+                    [&](char* to) __attribute__((always_inline)) { if (s + 2 < slabs) issue(to, s + 2); }, s >= 0, acc);
+        at = at == 2 * LX_STAGE ? 0 : at + LX_STAGE;
+    }
+    __syncthreads();
+    // token n: 256 bytes, chunk of 16 bytes ch at ch ^ (n % 16)
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int n = wn * 128 + 16 * j + c, col = wm * 64 + 16 * i + 4 * g;
+            *(u32x2*)(mem + n * 256 + (((col >> 3) ^ c) * 16) + (col & 7) * 2) =
+                u32x2{bf16_pair(acc[i][j][0], acc[i][j][1]), bf16_pair(acc[i][j][2], acc[i][j][3])};
+        }
+    __syncthreads();
+    const int ch = tid & 15, wr = r0 + 8 * ch;
+    if (wr < 2 * half) {
+        __bf16* to = wr < half ? (__bf16*)a.k_out + wr : (__bf16*)a.v_out + (wr - half);
+#pragma unroll 4
+        for (int i = 0; i < LX_TOK / 16; ++i) {
+            const int n = 16 * i + (tid >> 4);
+            if (n0 + n >= a.n) break;
+            u32x4 v = *(const u32x4*)(mem + n * 256 + ((ch ^ (n & 15)) * 16));
+            if (!s_in[n]) v = u32x4{0u, 0u, 0u, 0u};
+            *(u32x4*)(to + (n0 + n) * half) = v;
+        }
+    }
+    if (rt == 0) rotary_out<2>(a, n0, LX_TOK, tid);
 }
 
 template <bool BF, int TN>
@@ -332,6 +440,16 @@ int launch_expand(const LatentExpandArgs& a, hipStream_t st) {
     const int64_t blocks = spread ? (tt + 63) / 64 * 64 * rt : tt * rt;
     KernelTimer kt_("latent_expand", st);
     latent_expand_kernel<BF, TN><<<grid_of(blocks), dim3(256), 0, st>>>(a, tt, rt, spread);
+    return (int)hipGetLastError();
+}
+
+int launch_expand_wide(const LatentExpandArgs& a, hipStream_t st) {
+    const int64_t tt = (a.n + LX_TOK - 1) / LX_TOK;
+    const int rt = (2 * a.n_q * a.head_dim + LX_W - 1) / LX_W;
+    const bool spread = tt >= 64;
+    const int64_t blocks = spread ? (tt + 63) / 64 * 64 * rt : tt * rt;
+    KernelTimer kt_("latent_expand", st);
+    latent_expand_wide_kernel<<<grid_of(blocks), dim3(256), 0, st>>>(a, tt, rt, spread);
     return (int)hipGetLastError();
 }
 
@@ -347,6 +465,8 @@ int launch_latent_expand(const LatentExpandArgs& a, void* stream) {
     if (a.n == 0) return 0;
     // tiles of 128 where they give every CU one
     const bool big = (a.n + 127) / 128 * (2 * a.n_q * a.head_dim / 128) >= 256;
+    if (a.cache.dtype == ORDERMOE_BF16 && (a.n + LX_TOK - 1) / LX_TOK * (2 * a.n_q * a.head_dim / LX_W) >= 512)
+        return launch_expand_wide(a, (hipStream_t)stream);
     if (a.cache.dtype == ORDERMOE_BF16)
         return big ? launch_expand<true, 128>(a, (hipStream_t)stream) : launch_expand<true, 64>(a, (hipStream_t)stream);
     return big ? launch_expand<false, 128>(a, (hipStream_t)stream) : launch_expand<false, 64>(a, (hipStream_t)stream);

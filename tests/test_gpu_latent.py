@@ -125,7 +125,8 @@ def test_rows_without_a_slot_a_position_a_rotation_or_queries():
 # ------------------------------------------------------------------ expand
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n,h,D,R,rot,page", [(1, 1, 64, 128, 32, 16), (63, 3, 64, 256, 64, 32), (130, 2, 128, 512, 32, 16), (300, 40, 128, 128, 64, 16),
-                                              (4200, 1, 64, 128, 32, 64), (8200, 8, 64, 128, 32, 1024)])
+                                              (4200, 1, 64, 128, 32, 64), (8200, 8, 64, 128, 32, 1024), (1100, 127, 64, 128, 32, 64), (4400, 30, 128, 512, 64, 64),
+                                              (16500, 8, 64, 256, 64, 16)])
 def test_expanded_rows(dtype, n, h, D, R, rot, page):
     rng = np.random.default_rng(n)
     n_pages = max(2, -(-n // page) // 2)
