@@ -344,92 +344,129 @@ __global__ void __launch_bounds__(256) latent_expand_kernel(const LatentExpandAr
 // The same in tiles of 256 tokens x 128 weight rows, 2 x 2 waves of 128 x 64: a wave reads 12 pieces of LDS for 32 matrix
 // instructions, where 64 x 64 reads 8 for 16 and LDS is what bounds it.  Slabs of 64 bytes a row, three
 // buffers, two slabs on their way; chunk c of row r lies at c ^ (r / 4 % 4), so that the reads of 16 rows lie on
-// distinct banks.  The results go through LDS, in whole lines to memory.
-constexpr int LX_TOK = 256, LX_W = 128, LX_SLAB = 64, LX_STAGE = (LX_TOK + LX_W) * LX_SLAB;
+// distinct banks.  A workgroup takes some weight tiles of its tokens after one another: the next tile's loads are on
+// their way while a tile's results go, through LDS of the wave's own, in whole lines to memory.
+constexpr int LX_TOK = 256, LX_W = 128, LX_SLAB = 64, LX_STAGE = (LX_TOK + LX_W) * LX_SLAB, LX_OUT = 16 * 128;
+constexpr int LX_CHUNK = 4;                          // weight tiles of a workgroup, at most
 
 // (The loads' buffer and the one that is read never overlap: told so, the compiler does not wait for the loads first.)
 template <class Issue>
 __device__ inline __attribute__((always_inline)) void expand_slab(char* __restrict behind, const char* __restrict tok,
-                                                                  const char* __restrict wei, const Issue& issue, bool there, f32x4 (&acc)[4][8]) {
+                                                                  const char* __restrict wei, const Issue& issue, f32x4 (&acc)[4][8]) {
     issue(behind);
-    if (!there) return;
-    u32x4 w[4];
+    __builtin_amdgcn_sched_barrier(0);
+    u32x4 w[4], t[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = *(const u32x4*)(wei + 16 * i * LX_SLAB);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const u32x4 t = *(const u32x4*)(tok + 16 * j * LX_SLAB);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i][j] = mma16<true>(w[i], t, acc[i][j]);
-    }
-}
-
-__global__ void __launch_bounds__(256, 2) latent_expand_wide_kernel(const LatentExpandArgs a, int64_t tok_tiles, int row_tiles, int spread) {
-    constexpr int PIECES = LX_STAGE / 1024 / 4;          // of a slab, a wave: 16 rows each, the tokens' first
-    __shared__ __attribute__((aligned(16))) char mem[3 * LX_STAGE];
-    __shared__ uint8_t s_in[LX_TOK];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int c = lane & 15, g = lane >> 4, wm = wave >> 1, wn = wave & 1;
-    int64_t tt;
-    int rt;
-    if (!find_tile(tok_tiles, row_tiles, spread, tt, rt)) return;
-    const int R = a.cache.rank, wide = R + a.cache.rot, half = a.n_q * a.head_dim, r0 = rt * LX_W;
-    const int64_t n0 = tt * LX_TOK, slots = a.cache.n_pages << a.cache.page_shift;
-    const char* from[PIECES];
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-        const int r = (i * 4 + wave) * 16 + (lane >> 2), ch = (lane & 3) ^ ((lane >> 4) & 3);
-        if (i < LX_TOK / 64) {
-            int64_t s = n0 + r < a.n ? a.slots[n0 + r] : 0;
-            const bool in = s >= 0 && s < slots;
-            if ((lane & 3) == 0) s_in[r] = in;
-            from[i] = a.cache.rows + (in ? s : 0) * wide * 2 + ch * 16;
-        } else {
-            const int wr = r0 + r - LX_TOK < 2 * half ? r0 + r - LX_TOK : 0;
-            from[i] = (wr < half ? (const char*)a.w_k + (int64_t)wr * R * 2 : (const char*)a.w_v + (int64_t)(wr - half) * R * 2) + ch * 16;
-        }
-    }
-    auto issue = [&](char* to, int s) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) load_lds16(from[i] + s * LX_SLAB, to + (i * 4 + wave) * 1024);
-    };
-    f32x4 acc[4][8] = {};                                // [weight tile][token tile]
-    const int slabs = R * 2 / LX_SLAB, place = c * LX_SLAB + (g ^ ((c >> 2) & 3)) * 16;
-    for (int s = -2, at = LX_STAGE; s < slabs; ++s) {
-        if (s >= 0) {
-            if (s + 1 < slabs) wait_vmem<PIECES>();
-            else wait_vmem<0>();
-            lds_barrier();                               // slab s has arrived, and slab s - 1 has been read
-        }
-        expand_slab(mem + (at == 0 ? 2 * LX_STAGE : at - LX_STAGE), mem + at + wn * (128 * LX_SLAB) + place,
-                    mem + at + (LX_TOK + wm * 64) * LX_SLAB + place,
-                    [&](char* to) __attribute__((always_inline)) { if (s + 2 < slabs) issue(to, s + 2); }, s >= 0, acc);
-        at = at == 2 * LX_STAGE ? 0 : at + LX_STAGE;
-    }
-    __syncthreads();
-    // token n: 256 bytes, chunk of 16 bytes ch at ch ^ (n % 16)
+    for (int j = 0; j < 8; ++j) t[j] = *(const u32x4*)(tok + 16 * j * LX_SLAB);
 #pragma unroll
     for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int n = wn * 128 + 16 * j + c, col = wm * 64 + 16 * i + 4 * g;
-            *(u32x2*)(mem + n * 256 + (((col >> 3) ^ c) * 16) + (col & 7) * 2) =
-                u32x2{bf16_pair(acc[i][j][0], acc[i][j][1]), bf16_pair(acc[i][j][2], acc[i][j][3])};
+        for (int i = 0; i < 4; ++i) acc[i][j] = mma16<true>(w[i], t[j], acc[i][j]);
+    // three pieces of the tokens are read ahead of their products
+    __builtin_amdgcn_sched_group_barrier(0x100, 7, 0);
+#pragma unroll
+    for (int j = 0; j < 5; ++j) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 12, 0);
+}
+
+__global__ void __launch_bounds__(256, 2) latent_expand_wide_kernel(const LatentExpandArgs a, int64_t tok_tiles, int row_tiles, int chunk,
+                                                                    int spread) {
+    constexpr int PIECES = LX_STAGE / 1024 / 4;          // of a slab, a wave: 16 rows each, the tokens' first
+    constexpr int TP = LX_TOK / 64, STORES = 16;         // the tokens' pieces; a wave's stores of a whole tile
+    __shared__ __attribute__((aligned(16))) char mem[3 * LX_STAGE + 4 * LX_OUT];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, g = lane >> 4, wm = wave >> 1, wn = wave & 1;
+    int64_t tt;
+    int rc;
+    if (!find_tile(tok_tiles, (row_tiles + chunk - 1) / chunk, spread, tt, rc)) return;
+    const int rt0 = rc * chunk, rt1 = std::min(row_tiles, rt0 + chunk);
+    const int R = a.cache.rank, wide = R + a.cache.rot, half = a.n_q * a.head_dim;
+    const int64_t n0 = tt * LX_TOK, slots = a.cache.n_pages << a.cache.page_shift;
+    const int row = lane >> 2, ch = (lane & 3) ^ ((lane >> 4) & 3);
+    const char *tok_at[TP], *wei_at[PIECES - TP];
+#pragma unroll
+    for (int i = 0; i < TP; ++i) {
+        const int r = (i * 4 + wave) * 16 + row;
+        int64_t s = n0 + r < a.n ? a.slots[n0 + r] : 0;
+        tok_at[i] = a.cache.rows + (s >= 0 && s < slots ? s : 0) * wide * 2 + ch * 16;
+    }
+    uint32_t there = 0;                                  // bit j: the lane's token 16 j + c of the wave's 128 lies in the cache
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int64_t n = n0 + wn * 128 + 16 * j + c, s = n < a.n ? a.slots[n] : -1;
+        there |= (uint32_t)(s >= 0 && s < slots) << j;
+    }
+    auto weights = [&](int rt) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < PIECES - TP; ++i) {
+            int wr = rt * LX_W + (i * 4 + wave) * 16 + row;
+            wr = wr < 2 * half ? wr : 0;
+            wei_at[i] = (wr < half ? (const char*)a.w_k + (int64_t)wr * R * 2 : (const char*)a.w_v + (int64_t)(wr - half) * R * 2) + ch * 16;
         }
-    __syncthreads();
-    const int ch = tid & 15, wr = r0 + 8 * ch;
-    if (wr < 2 * half) {
-        __bf16* to = wr < half ? (__bf16*)a.k_out + wr : (__bf16*)a.v_out + (wr - half);
-#pragma unroll 4
-        for (int i = 0; i < LX_TOK / 16; ++i) {
-            const int n = 16 * i + (tid >> 4);
-            if (n0 + n >= a.n) break;
-            u32x4 v = *(const u32x4*)(mem + n * 256 + ((ch ^ (n & 15)) * 16));
-            if (!s_in[n]) v = u32x4{0u, 0u, 0u, 0u};
-            *(u32x4*)(to + (n0 + n) * half) = v;
+    };
+    const int slabs = R * 2 / LX_SLAB, place = c * LX_SLAB + (g ^ ((c >> 2) & 3)) * 16;
+    const bool whole = n0 + LX_TOK <= a.n;
+    char* const out = mem + 3 * LX_STAGE + wave * LX_OUT;
+    int ls = 0, lt = rt0, at = 0;                        // the slab and the tile to load next; the buffer to read
+    weights(lt);
+    auto issue = [&](char* to) __attribute__((always_inline)) {
+        if (lt >= rt1) return;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+            load_lds16((i < TP ? tok_at[i] : wei_at[i < TP ? 0 : i - TP]) + ls * LX_SLAB, to + (i * 4 + wave) * 1024);
+        if (++ls == slabs) {
+            ls = 0;
+            weights(++lt);
+        }
+    };
+    issue(mem);
+    issue(mem + LX_STAGE);
+    __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0), in a form that the compiler takes into account
+    for (int rt = rt0; rt < rt1; ++rt) {
+        f32x4 acc[4][8] = {};                            // [weight tile][token tile]
+        for (int s = 0; s < slabs; ++s) {
+            // what was issued behind slab s may still be on its way: slab s + 1 and, before it, a tile's stores
+            if (s + 1 == slabs && rt + 1 == rt1) wait_vmem<0>();
+            else if (s < 2 && rt > rt0 && whole) wait_vmem<PIECES + STORES>();
+            else wait_vmem<PIECES>();
+            lds_barrier();                               // slab s has arrived, and slab s - 1 has been read
+            expand_slab(mem + (at == 0 ? 2 * LX_STAGE : at - LX_STAGE), mem + at + wn * (128 * LX_SLAB) + place,
+                        mem + at + (LX_TOK + wm * 64) * LX_SLAB + place, issue, acc);
+            at = at == 2 * LX_STAGE ? 0 : at + LX_STAGE;
+        }
+        // 16 tokens at a time: token n's 128 bytes in the wave's own LDS, chunk of 16 bytes k at k ^ (n % 8)
+        int l = lane;
+        asm volatile("" : "+v"(l));                      // (places made anew: kept, they would take the sums' registers)
+        const int oc = l & 7, on = l >> 3, wr = rt * LX_W + wm * 64 + 8 * oc;
+        const int64_t first = n0 + wn * 128 + on;
+        __bf16* to = (wr < half ? (__bf16*)a.k_out + wr : (__bf16*)a.v_out + (wr - half)) + first * half;
+        int left = wr < 2 * half ? (int)std::min<int64_t>(a.n - first, LX_TOK) : 0;
+        char* const put = out + (l & 15) * 128 + ((l >> 4) & 1) * 8;
+        const int swap = ((l >> 5) ^ (l & 7)) * 16;      // (2 i + g / 2) ^ (c % 8) = 2 i ^ (g / 2 ^ c % 8)
+        const char* const get = out + on * 128 + (oc ^ on) * 16;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t keep = there >> j & 1 ? ~0u : 0u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *(u32x2*)(put + (swap ^ (32 * i))) =
+                    u32x2{bf16_pair(acc[i][j][0], acc[i][j][1]) & keep, bf16_pair(acc[i][j][2], acc[i][j][3]) & keep};
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const u32x4 x = *(const u32x4*)(get + 1024 * k);
+                if (left > 0) *(u32x4*)to = x;
+                to += (int64_t)8 * half;
+                left -= 8;
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
-    if (rt == 0) rotary_out<2>(a, n0, LX_TOK, tid);
+    if (rt0 == 0) rotary_out<2>(a, n0, LX_TOK, tid);
 }
 
 template <bool BF, int TN>
@@ -446,10 +483,12 @@ int launch_expand(const LatentExpandArgs& a, hipStream_t st) {
 int launch_expand_wide(const LatentExpandArgs& a, hipStream_t st) {
     const int64_t tt = (a.n + LX_TOK - 1) / LX_TOK;
     const int rt = (2 * a.n_q * a.head_dim + LX_W - 1) / LX_W;
+    const int chunk = (int)std::min<int64_t>(LX_CHUNK, std::max<int64_t>(1, tt * rt / 1024));
+    const int chunks = (rt + chunk - 1) / chunk;
     const bool spread = tt >= 64;
-    const int64_t blocks = spread ? (tt + 63) / 64 * 64 * rt : tt * rt;
+    const int64_t blocks = spread ? (tt + 63) / 64 * 64 * chunks : tt * chunks;
     KernelTimer kt_("latent_expand", st);
-    latent_expand_wide_kernel<<<grid_of(blocks), dim3(256), 0, st>>>(a, tt, rt, spread);
+    latent_expand_wide_kernel<<<grid_of(blocks), dim3(256), 0, st>>>(a, tt, rt, chunk, spread);
     return (int)hipGetLastError();
 }
 
