@@ -178,9 +178,12 @@ __device__ inline void absorb_tile(const LatentWriteArgs& a, int64_t t0, int h, 
     }
 }
 
-// blocks: absorb tiles, then rows, then pieces of the queries
+constexpr int LW_COPIES = 4, LW_TURNS = 2;           // of a thread: pieces on their way together
+
+// blocks: absorb tiles, then rows, then the queries' pieces of 8 elements that are copied (not where they are absorbed), then
+// those of 16 that are turned
 template <bool BF, int D, int ROT>
-__global__ void __launch_bounds__(256) latent_write_kernel(const LatentWriteArgs a, int64_t n_absorb, int64_t n_rows, int64_t n_units) {
+__global__ void __launch_bounds__(256) latent_write_kernel(const LatentWriteArgs a, int64_t n_absorb, int64_t n_rows, int64_t n_copies) {
     __shared__ __attribute__((aligned(16))) char mem[BF ? D * LW_COLS * 2 : 16];
     int64_t blk = block_number();
     if (blk < n_absorb) {
@@ -197,31 +200,46 @@ __global__ void __launch_bounds__(256) latent_write_kernel(const LatentWriteArgs
         return;
     }
     blk -= n_rows;
-    // per head row: D / 8 pieces to copy (not where they are absorbed), then ROT / 16 to turn
-    const int copies = a.absorb ? 0 : D / 8, per = copies + ROT / 16;
-    const int64_t u = blk * 256 + threadIdx.x;
-    if (u >= n_units) return;
-    const int64_t row = (uint32_t)u == u ? (uint32_t)u / (uint32_t)per : u / per;
-    const int k = (int)(u - row * per);
-    const int64_t t = (uint32_t)row / (uint32_t)a.n_q;
-    const int h = (int)(row - t * a.n_q);
-    const Elem<BF>* from = (const Elem<BF>*)a.q + t * a.q_stride + h * (D + ROT);
-    Elem<BF>* to = (Elem<BF>*)a.q_out + row * ((a.absorb ? a.cache.rank : D) + ROT);
-    if (k < copies) {
-        float x[8];
-        load8<BF>(from + 8 * k, x);
-        store8<BF>(to + 8 * k, x);
-    } else {
-        turn16<BF>(a, t, from + D, to + (a.absorb ? a.cache.rank : D), k - copies);
+    const uint32_t heads = (uint32_t)(a.T * a.n_q), n_q = (uint32_t)a.n_q;       // (fewer than 2^31)
+    if (blk < n_copies) {
+        constexpr int PER = D / 8;
+        float x[LW_COPIES][8];
+        const int k = threadIdx.x % PER;
+        const int64_t first = blk * (256 / PER * LW_COPIES) + threadIdx.x / PER;
+#pragma unroll
+        for (int i = 0; i < LW_COPIES; ++i) {
+            const int64_t r = first + i * (256 / PER);
+            if (r >= heads) continue;
+            const uint32_t t = (uint32_t)r / n_q, h = (uint32_t)r - t * n_q;
+            load8<BF>((const Elem<BF>*)a.q + t * a.q_stride + h * (D + ROT) + 8 * k, x[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < LW_COPIES; ++i) {
+            const int64_t r = first + i * (256 / PER);
+            if (r < heads) store8<BF>((Elem<BF>*)a.q_out + r * (D + ROT) + 8 * k, x[i]);
+        }
+        return;
+    }
+    blk -= n_copies;
+    constexpr int PER = ROT / 16;
+    const int wide = a.absorb ? a.cache.rank : D, k = threadIdx.x % PER;
+#pragma unroll
+    for (int i = 0; i < LW_TURNS; ++i) {
+        const int64_t r = (blk * LW_TURNS + i) * (256 / PER) + threadIdx.x / PER;
+        if (r >= heads) break;
+        const uint32_t t = (uint32_t)r / n_q, h = (uint32_t)r - t * n_q;
+        turn16<BF>(a, t, (const Elem<BF>*)a.q + t * a.q_stride + h * (D + ROT) + D, (Elem<BF>*)a.q_out + r * (wide + ROT) + wide, k);
     }
 }
 
 template <bool BF, int D, int ROT>
 int launch_write(const LatentWriteArgs& a, hipStream_t st) {
     const int64_t absorb = a.q && a.absorb ? (a.T + LW_TOK - 1) / LW_TOK * a.n_q * (a.cache.rank / LW_COLS) : 0;
-    const int64_t rows = (a.T + 3) / 4, units = a.q ? a.T * a.n_q * ((a.absorb ? 0 : D / 8) + ROT / 16) : 0;
+    const int64_t rows = (a.T + 3) / 4, heads = a.q ? a.T * a.n_q : 0;
+    const int64_t per_copy = 256 / (D / 8) * LW_COPIES, per_turn = 256 / (ROT / 16) * LW_TURNS;
+    const int64_t copies = a.absorb ? 0 : (heads + per_copy - 1) / per_copy, turns = (heads + per_turn - 1) / per_turn;
     KernelTimer kt_("latent_write", st);
-    latent_write_kernel<BF, D, ROT><<<grid_of(absorb + rows + (units + 255) / 256), dim3(256), 0, st>>>(a, absorb, rows, units);
+    latent_write_kernel<BF, D, ROT><<<grid_of(absorb + rows + copies + turns), dim3(256), 0, st>>>(a, absorb, rows, copies);
     return (int)hipGetLastError();
 }
 template <bool BF>
