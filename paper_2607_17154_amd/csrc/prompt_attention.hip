@@ -147,22 +147,45 @@ __device__ inline void wait_loads() {
 // every load that is on its way)
 __device__ inline void lds_barrier() { asm volatile("s_barrier" ::: "memory"); }
 
+// The largest exponents of 16 bytes, taken up in `top`
+template <bool BF>
+__device__ inline void exponents(const u32x4& x, u32x4& top) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if constexpr (BF) {
+            const uint32_t now = x[w] & 0x7F807F80u, was = top[w];      // (a cast of a vector's element would take its first)
+            top[w] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, now), __builtin_bit_cast(u16x2, was)));
+        } else {
+            top[w] = std::max<uint32_t>(x[w] & 0x7F800000u, top[w]);
+        }
+    }
+}
+template <bool BF>
+__device__ inline bool no_number(const u32x4& top) {
+    bool r = false;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) r |= (top[w] >= 0x7F800000u) | (BF && (top[w] & 0xFFFFu) >= 0x7F80u);
+    return r;
+}
 // Positions of a tile's values that hold an infinity or a NaN, a bit each; every wave finds them all.  They become zeros: a
 // weight of 0 would not keep what is no number out of a row's sums.
 template <bool BF, int D>
 __device__ inline uint64_t clean_values(char* v, int wave, int lane) {
     constexpr int CH = D * (BF ? 2 : 4) / 16, PIECES = PA_TILE<BF> * CH / 64;
-    auto bad = [&](const u32x4& x) {
-        bool r = false;
+    u32x4 top = {0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int w = 0; w < 4; ++w) r |= (BF && (x[w] & 0x7F80u) == 0x7F80u) | ((x[w] & 0x7F800000u) == 0x7F800000u);
-        return r;
+    for (int i = 0; i < PIECES; ++i) exponents<BF>(*(const u32x4*)(v + (i * 64 + lane) * 16), top);
+    if (!__builtin_amdgcn_ballot_w64(no_number<BF>(top))) return 0;     // (alike in all waves)
+    auto bad = [&](const u32x4& x) {
+        u32x4 t = {0u, 0u, 0u, 0u};
+        exponents<BF>(x, t);
+        return no_number<BF>(t);
     };
     uint64_t m = 0;
-#pragma unroll 4
+#pragma unroll 1
     for (int i = 0; i < PIECES; ++i)
         if (bad(*(const u32x4*)(v + (i * 64 + lane) * 16))) m |= 1ull << ((i * 64 + lane) / CH);
-    if (!__builtin_amdgcn_ballot_w64(m != 0)) return 0;  // (alike in all waves)
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) m |= __shfl_xor((unsigned long long)m, o);
     __syncthreads();
