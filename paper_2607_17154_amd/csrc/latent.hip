@@ -288,13 +288,39 @@ __device__ inline void wait_vmem() {
 }
 __device__ inline void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\ns_barrier" ::: "memory"); }
 
+// One slab's products, the loads of a later one beside them.  (Their buffers never overlap: told so, the compiler does not
+// wait for the loads before the first read.)
+template <bool BF, int W, class Issue>
+__device__ inline __attribute__((always_inline)) void expand_step(char* __restrict behind, const char* __restrict tok, const char* __restrict wei,
+                                                                  int wm, int wn, int lane, const Issue& issue, f32x4 (&acc)[W / 16][W / 16]) {
+    constexpr int F = W / 16;
+    const int c = lane & 15, g = lane >> 4;
+    issue(behind);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        u32x4 t[F], w[F];
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            const int rt_ = wn * W + 16 * i + c, rw = wm * W + 16 * i + c;
+            t[i] = *(const u32x4*)(tok + rt_ * LE_SLAB + (((4 * k + g) ^ (rt_ & 7)) * 16));
+            w[i] = *(const u32x4*)(wei + rw * LE_SLAB + (((4 * k + g) ^ (rw & 7)) * 16));
+        }
+#pragma unroll
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+            for (int j = 0; j < F; ++j) acc[i][j] = mma16<BF>(w[i], t[j], acc[i][j]);
+    }
+}
+
 // A tile of TN tokens (the matrix unit's columns) x TN weight rows, 2 x 2 waves.  Both come in
-// slabs of 128 bytes a row through LDS, two buffers; chunk c of row r lies at c ^ (r % 8), so that the
-// 16-byte reads of eight rows lie on distinct banks.
+// slabs of 128 bytes a row through LDS, two buffers, or four of fewer rows, all but one on their way; chunk c of row r
+// lies at c ^ (r % 8), so that the 16-byte reads of eight rows lie on distinct banks.  (300 tokens x 40 heads, rank 128,
+// fp32: 8.0 us in tiles of 64, 5.9 of 32.)
 template <bool BF, int TN>
 __global__ void __launch_bounds__(256) latent_expand_kernel(const LatentExpandArgs a, int64_t tok_tiles, int row_tiles, int spread) {
     constexpr int ES = BF ? 2 : 4, W = TN / 2, F = W / 16, LOADS = TN / 32;     // a wave's rows, its tiles, its pieces of a slab
-    __shared__ __attribute__((aligned(16))) char mem[2][2][TN * LE_SLAB];
+    constexpr int BUFS = TN < 128 ? 4 : 2, SLAB = TN * LE_SLAB;
+    __shared__ __attribute__((aligned(16))) char mem[BUFS][2][SLAB];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4, wm = wave >> 1, wn = wave & 1;
     int64_t tt;
@@ -312,34 +338,24 @@ __global__ void __launch_bounds__(256) latent_expand_kernel(const LatentExpandAr
         const int wr = r0 + r < 2 * half ? r0 + r : 0;
         from[1][i] = (wr < half ? (const char*)a.w_k + (int64_t)wr * R * ES : (const char*)a.w_v + (int64_t)(wr - half) * R * ES) + ch * 16;
     }
-    auto issue = [&](int buf, int s) {
+    auto issue = [&](char* to, int s) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i)
 #pragma unroll
-            for (int o = 0; o < 2; ++o) load_lds16(from[o][i] + s * LE_SLAB, &mem[buf][o][(wave * LOADS + i) * 1024]);
+            for (int o = 0; o < 2; ++o) load_lds16(from[o][i] + s * LE_SLAB, to + o * SLAB + (wave * LOADS + i) * 1024);
     };
     f32x4 acc[F][F] = {};                            // [weight tile][token tile]
-    const int slabs = R * ES / LE_SLAB;
-    issue(0, 0);
+    const int slabs = R * ES / LE_SLAB;              // (2 or more)
+    issue(mem[0][0], 0);
+    __builtin_amdgcn_s_waitcnt(0x0F70);              // vmcnt(0), in a form that the compiler takes into account
     for (int s = 0; s < slabs; ++s) {
-        __syncthreads();                             // slab s has arrived, and slab s - 1 has been read
-        if (s + 1 < slabs) issue((s + 1) & 1, s + 1);
-        const char* tok = mem[s & 1][0];
-        const char* wei = mem[s & 1][1];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            u32x4 t[F], w[F];
-#pragma unroll
-            for (int i = 0; i < F; ++i) {
-                const int rt_ = wn * W + 16 * i + c, rw = wm * W + 16 * i + c;
-                t[i] = *(const u32x4*)(tok + rt_ * LE_SLAB + (((4 * k + g) ^ (rt_ & 7)) * 16));
-                w[i] = *(const u32x4*)(wei + rw * LE_SLAB + (((4 * k + g) ^ (rw & 7)) * 16));
-            }
-#pragma unroll
-            for (int i = 0; i < F; ++i)
-#pragma unroll
-                for (int j = 0; j < F; ++j) acc[i][j] = mma16<BF>(w[i], t[j], acc[i][j]);
-        }
+        if (s + BUFS - 2 < slabs) wait_vmem<(BUFS - 2) * 2 * LOADS>();
+        else wait_vmem<0>();
+        lds_barrier();                               // slab s has arrived, and slab s - 1 has been read
+        expand_step<BF, W>(mem[0][0], mem[s % BUFS][0], mem[s % BUFS][1], wm, wn, lane, [&](char* to) __attribute__((always_inline)) {
+            const int last = std::min(s + BUFS, slabs);
+            for (int x = s == 0 ? 1 : s + BUFS - 1; x < last; ++x) issue(to + x % BUFS * (2 * SLAB), x);
+        }, acc);
     }
 #pragma unroll
     for (int j = 0; j < F; ++j) {
@@ -520,13 +536,15 @@ int launch_latent_write(const LatentWriteArgs& a, void* stream) {
 
 int launch_latent_expand(const LatentExpandArgs& a, void* stream) {
     if (a.n == 0) return 0;
-    // tiles of 128 where they give every CU one
-    const bool big = (a.n + 127) / 128 * (2 * a.n_q * a.head_dim / 128) >= 256;
+    // the largest tiles that give every CU one
+    auto enough = [&](int tile) { return (a.n + tile - 1) / tile * (2 * a.n_q * a.head_dim / tile) >= 256; };
     if (a.cache.dtype == ORDERMOE_BF16 && (a.n + LX_TOK - 1) / LX_TOK * (2 * a.n_q * a.head_dim / LX_W) >= 512)
         return launch_expand_wide(a, (hipStream_t)stream);
     if (a.cache.dtype == ORDERMOE_BF16)
-        return big ? launch_expand<true, 128>(a, (hipStream_t)stream) : launch_expand<true, 64>(a, (hipStream_t)stream);
-    return big ? launch_expand<false, 128>(a, (hipStream_t)stream) : launch_expand<false, 64>(a, (hipStream_t)stream);
+        return enough(128) ? launch_expand<true, 128>(a, (hipStream_t)stream)
+               : enough(64) ? launch_expand<true, 64>(a, (hipStream_t)stream) : launch_expand<true, 32>(a, (hipStream_t)stream);
+    return enough(128) ? launch_expand<false, 128>(a, (hipStream_t)stream)
+           : enough(64) ? launch_expand<false, 64>(a, (hipStream_t)stream) : launch_expand<false, 32>(a, (hipStream_t)stream);
 }
 
 }  // namespace ordermoe
