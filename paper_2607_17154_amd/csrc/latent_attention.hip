@@ -768,13 +768,18 @@ __global__ void __launch_bounds__(256) latent_out_kernel(const LatentAttentionAr
     }
     bool in = tb + slot < a.T && b < a.B;
     Seq s = {0, 0, 0, 0};
-    if (in) s = sequence(a, b);
+    int first = 0, pieces = 0;
+    if (in) {
+        s = sequence(a, b);
+        first = a.plan[2 * b];
+        pieces = a.plan[2 * b + 1];
+    }
     const int i = t - s.first;
     in = in && i >= 0 && i < s.n;
+    pieces = in ? pieces : 0;
     const int row = i * a.n_q + h, rows_max = a.max_q * a.n_q;
     if (tid < 16) s_in[tid] = 0;
-    const int pieces = in ? a.plan[2 * b + 1] : 0;
-    const int64_t at = in ? (int64_t)a.plan[2 * b] * rows_max + row : 0;
+    const int64_t at = in ? (int64_t)first * rows_max + row : 0;
     const f32x2* ml = (const f32x2*)a.part_ml;
     float m = -__builtin_inff(), l = 0.f, x[R / 16] = {};
     for (int p = z; p < pieces; p += U * S) {
