@@ -2,7 +2,7 @@
 //
 //   evict_select_kernel  one workgroup per sequence: the keep-th largest key of its places (mass,
 //                        or above all masses where the token is protected) by three histograms
-//                        of the keys' bits, then the places that stay, go or move
+//                        of the keys' bits, then the places that stay, go or move; few rows move here
 //   evict_digit_kernel, evict_mark_kernel  the same where tables are long, a workgroup per slice of a
 //                        sequence: a slice's histogram of the next digit (three launches; every
 //                        workgroup finds the digits before from all the slices' histograms), then its places
@@ -23,6 +23,7 @@ namespace {
 constexpr int EV_CHUNK = 8192, EV_WORDS = EV_CHUNK / 64;      // places gone through together
 constexpr int EV_BINS = 2048;                        // of a histogram: digits of 11, 11 and 10 bits
 constexpr int EV_SLICES = 64;                        // of a sequence, at most, and one more
+constexpr int EV_MOVES = 256;                        // rows of a sequence that the workgroup which finds them moves
 constexpr uint32_t EV_SAFE = 0xFFFFFFFFu;
 __device__ inline int digit_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
 __device__ inline int digit_bits(int pass) { return pass == 2 ? 10 : 11; }
@@ -205,9 +206,36 @@ __device__ inline void count_key(uint32_t* s_hist, uint32_t key, int pass, uint3
     if (pass == 0 || (key >> (shift + bits)) == prefix) atomicAdd(&s_hist[(key >> shift) & ((1u << bits) - 1u)], 1u);
 }
 
+// Up to ROWS moves of a sequence from the x0-th on, by a workgroup
+template <int NT, int ROWS>
+struct Move { const char* from[ROWS]; char* to[ROWS]; };
+template <int NT, int ROWS>
+__device__ inline void move_rows(const EvictArgs& a, int b, int64_t x0, int rows, int chunks, Move<NT, ROWS>& s, int tid) {
+    if (tid < rows) {
+        const int to = a.holes[(int64_t)b * a.holes_max + x0 + tid], from = a.fills[(int64_t)b * a.holes_max + x0 + tid];
+        a.kept[(int64_t)b * a.keep + to] = from;
+        a.mass_out[b * a.stride + to] = a.mass[b * a.stride + from];
+        a.pos_out[b * a.stride + to] = a.pos[b * a.stride + from];
+        const int sh = a.cache.page_shift, in = (1 << sh) - 1;
+        const int32_t* table = a.page_table + (int64_t)b * a.max_pages;
+        const int64_t pt = table[to >> sh], pf = table[from >> sh], row = (int64_t)chunks * 16;
+        s.from[tid] = pf >= 0 && pf < a.cache.n_pages ? a.cache.rows + ((pf << sh) + (from & in)) * row : nullptr;
+        s.to[tid] = pt >= 0 && pt < a.cache.n_pages ? a.cache.rows + ((pt << sh) + (to & in)) * row : nullptr;
+    }
+    __syncthreads();
+    for (int u = tid; u < rows * chunks; u += NT) {
+        const int r = u / chunks, c = u - r * chunks;
+        u32x4 v = {0u, 0u, 0u, 0u};
+        if (s.from[r]) v = *(const u32x4*)(s.from[r] + 16 * c);
+        if (s.to[r]) *(u32x4*)(s.to[r] + 16 * c) = v;
+    }
+}
+
 // tables of up to EV_CHUNK places: a sequence in registers
-__global__ void __launch_bounds__(1024) evict_select_kernel(const EvictArgs a) {
+// chunks > 0: the rows, of so many pieces of 16 bytes, move here too
+__global__ void __launch_bounds__(1024) evict_select_kernel(const EvictArgs a, int chunks) {
     constexpr int NT = 1024;
+    __shared__ Move<NT, EV_MOVES> s_move;
     __shared__ uint32_t s_hist[EV_BINS], s_wave[NT / 64], s_found[2];
     __shared__ Marks s_marks;
     const int tid = threadIdx.x, b = (int)block_number();
@@ -238,6 +266,10 @@ __global__ void __launch_bounds__(1024) evict_select_kernel(const EvictArgs a) {
     uint32_t equal = 0, holes = 0, fills = 0;
     mark_chunk<NT>(a, pl, b, 0, pl.n, ch, prefix, more, equal, holes, fills, s_marks, s_wave, tid);
     if (tid == 0) a.moves[b] = (int32_t)holes;
+    if (chunks == 0) return;
+    __syncthreads();                                 // the places are written
+    if (tid == 0) a.len_out[b] = a.keep;
+    move_rows<NT, EV_MOVES>(a, b, 0, (int)holes, chunks, s_move, tid);
 }
 
 // Slices of `slice` places: those before the budget, then those from it on, so that a slice is all front or all back.
@@ -361,32 +393,13 @@ __global__ void __launch_bounds__(ES_THREADS) evict_mark_kernel(const EvictArgs 
 constexpr int EM_ROWS = 32;                          // rows that a workgroup moves
 
 __global__ void __launch_bounds__(256) evict_move_kernel(const EvictArgs a, int per_seq, int chunks) {
-    __shared__ const char* s_from[EM_ROWS];
-    __shared__ char* s_to[EM_ROWS];
+    __shared__ Move<256, EM_ROWS> s_move;
     const int64_t id = block_number();
     const int b = (int)(id / per_seq), x0 = (int)(id - (int64_t)b * per_seq) * EM_ROWS, tid = threadIdx.x;
     if (b >= a.B) return;
     const int moves = a.moves[b], rows = std::min(EM_ROWS, moves - x0);
     if (x0 == 0 && tid == 0 && moves >= 0) a.len_out[b] = a.keep;        // (it may be ctx_len: read by no kernel from here on)
-    if (rows <= 0) return;
-    if (tid < rows) {
-        const int to = a.holes[(int64_t)b * a.holes_max + x0 + tid], from = a.fills[(int64_t)b * a.holes_max + x0 + tid];
-        a.kept[(int64_t)b * a.keep + to] = from;
-        a.mass_out[b * a.stride + to] = a.mass[b * a.stride + from];
-        a.pos_out[b * a.stride + to] = a.pos[b * a.stride + from];
-        const int sh = a.cache.page_shift, in = (1 << sh) - 1;
-        const int32_t* table = a.page_table + (int64_t)b * a.max_pages;
-        const int64_t pt = table[to >> sh], pf = table[from >> sh], row = (int64_t)chunks * 16;
-        s_from[tid] = pf >= 0 && pf < a.cache.n_pages ? a.cache.rows + ((pf << sh) + (from & in)) * row : nullptr;
-        s_to[tid] = pt >= 0 && pt < a.cache.n_pages ? a.cache.rows + ((pt << sh) + (to & in)) * row : nullptr;
-    }
-    __syncthreads();
-    for (int u = tid; u < rows * chunks; u += 256) {
-        const int r = u / chunks, c = u - r * chunks;
-        u32x4 v = {0u, 0u, 0u, 0u};
-        if (s_from[r]) v = *(const u32x4*)(s_from[r] + 16 * c);
-        if (s_to[r]) *(u32x4*)(s_to[r] + 16 * c) = v;
-    }
+    if (rows > 0) move_rows<256, EM_ROWS>(a, b, x0, rows, chunks, s_move, tid);
 }
 
 }  // namespace
@@ -398,13 +411,16 @@ int launch_latent_evict(const EvictArgs& a, void* stream) {
     if (a.B == 0) return 0;
     hipStream_t st = (hipStream_t)stream;
     const int64_t cap = most_places(a);
+    const int chunks = (a.cache.rank + a.cache.rot) * (a.cache.dtype == ORDERMOE_BF16 ? 2 : 4) / 16;
     // One workgroup per sequence goes through a thousand places a microsecond; slices take four more launches (one sequence of
-    // 8000 places 18 us in one kernel).
+    // 8000 places 18 us in one kernel).  Few rows move there and then (16 of 1016 places: 12.0 us with a kernel for them, 10.0; 128
+    // of 1128 in 64 sequences: 15.9 and 14.2).
     if (cap <= EV_CHUNK) {
+        const bool here = a.holes_max <= EV_MOVES;
         KernelTimer kt_("evict_select", st);
-        evict_select_kernel<<<grid_of(a.B), dim3(1024), 0, st>>>(a);
+        evict_select_kernel<<<grid_of(a.B), dim3(1024), 0, st>>>(a, here ? chunks : 0);
         const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return (int)e;
+        if (e != hipSuccess || here) return (int)e;
     } else {
         const int64_t slice = std::max<int64_t>(EV_CHUNK, (cap + EV_SLICES - 2) / (EV_SLICES - 1));
         const int slices = (int)std::min<int64_t>(evict_slices(cap), cap / slice + 2);
@@ -422,7 +438,6 @@ int launch_latent_evict(const EvictArgs& a, void* stream) {
     }
     if (a.holes_max == 0) return 0;
     const int per = (int)((a.holes_max + EM_ROWS - 1) / EM_ROWS);
-    const int chunks = (a.cache.rank + a.cache.rot) * (a.cache.dtype == ORDERMOE_BF16 ? 2 : 4) / 16;
     KernelTimer kt_("evict_move", st);
     evict_move_kernel<<<grid_of((int64_t)a.B * per), dim3(256), 0, st>>>(a, per, chunks);
     return (int)hipGetLastError();
