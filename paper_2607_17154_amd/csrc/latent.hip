@@ -377,8 +377,8 @@ __global__ void __launch_bounds__(256) latent_expand_kernel(const LatentExpandAr
 
 // The same in tiles of 256 tokens x 128 weight rows, 2 x 2 waves of 128 x 64: a wave reads 12 pieces of LDS for 32 matrix
 // instructions, where 64 x 64 reads 8 for 16 and LDS is what bounds it.  Slabs of 64 bytes a row, three
-// buffers, two slabs on their way; chunk c of row r lies at c ^ (r / 4 % 4), so that the reads of 16 rows lie on
-// distinct banks.  A workgroup takes some weight tiles of its tokens after one another: the next tile's loads are on
+// buffers, two slabs on their way; chunk c of row r lies at c ^ (r / 2 % 4), so that lanes read together (0 - 3, 12 - 15,
+// 20 - 27, the others of each 32) do so on distinct banks.  A workgroup takes some weight tiles of its tokens after one another: the next tile's loads are on
 // their way while a tile's results go, through LDS of the wave's own, in whole lines to memory.
 constexpr int LX_TOK = 256, LX_W = 128, LX_SLAB = 64, LX_STAGE = (LX_TOK + LX_W) * LX_SLAB, LX_OUT = 16 * 128;
 constexpr int LX_CHUNK = 4;                          // weight tiles of a workgroup, at most
@@ -421,7 +421,7 @@ __global__ void __launch_bounds__(256, 2) latent_expand_wide_kernel(const Latent
     const int rt0 = rc * chunk, rt1 = std::min(row_tiles, rt0 + chunk);
     const int R = a.cache.rank, wide = R + a.cache.rot, half = a.n_q * a.head_dim;
     const int64_t n0 = tt * LX_TOK, slots = a.cache.n_pages << a.cache.page_shift;
-    const int row = lane >> 2, ch = (lane & 3) ^ ((lane >> 4) & 3);
+    const int row = lane >> 2, ch = (lane & 3) ^ ((lane >> 3) & 3);
     const char *tok_at[TP], *wei_at[PIECES - TP];
 #pragma unroll
     for (int i = 0; i < TP; ++i) {
@@ -443,7 +443,7 @@ __global__ void __launch_bounds__(256, 2) latent_expand_wide_kernel(const Latent
             wei_at[i] = (wr < half ? (const char*)a.w_k + (int64_t)wr * R * 2 : (const char*)a.w_v + (int64_t)(wr - half) * R * 2) + ch * 16;
         }
     };
-    const int slabs = R * 2 / LX_SLAB, place = c * LX_SLAB + (g ^ ((c >> 2) & 3)) * 16;
+    const int slabs = R * 2 / LX_SLAB, place = c * LX_SLAB + (g ^ ((c >> 1) & 3)) * 16;
     const bool whole = n0 + LX_TOK <= a.n;
     char* const out = mem + 3 * LX_STAGE + wave * LX_OUT;
     int ls = 0, lt = rt0, at = 0;                        // the slab and the tile to load next; the buffer to read

@@ -12,7 +12,7 @@
 //                            kernel wrote and the rows' final maximum and sum
 // The query rows of a sequence are its n_b tokens times the heads: row = token * n_q + head.
 //
-// A tile of 64 tokens (bf16; c = lane % 16, g = lane / 16; fp32: 32 tokens, v_mfma_f32_16x16x4_f32):
+// A tile of 32 tokens (latent_rows_kernel: 64; c = lane % 16, g = lane / 16; fp32 v_mfma_f32_16x16x4_f32 for each):
 //   S^T = K Q^T   v_mfma_f32_16x16x32_bf16; rows: 16 tokens, columns: 16 query rows.  Maximum and sum belong to a
 //                 column, that is to a lane.
 //   O^T = C^T P^T rows: 16 elements of the latent vector, columns: 16 query rows, tokens the inner index; C^T by turned
@@ -24,7 +24,7 @@
 // lane (c, g)) are the inner indexes of its second product when C^T's lanes hold the same tokens, so they never leave their
 // registers: one barrier a tile.  It reads each row in LDS eight times for 128 query rows, which bounds it (128 bytes a
 // cycle); blocks of 64 rows in the first way read it less than half as often but waited for each other: trees of 64 over
-// 30000-100000 tokens 993 us for 513.
+// 30000-100000 tokens 993 us for 482.
 // Rows go straight from memory into LDS, the next tile while one is attended to.
 #include <hip/hip_runtime.h>
 
@@ -44,7 +44,7 @@ constexpr int LA_MIN_PIECE = 64;                     // tokens
 constexpr int LA_FEW = 32;                           // query rows up to which latent_attention_kernel takes a batch
 constexpr int LO_PIECES = 32;                        // pieces of a sequence past which 16 sets of lanes add them
 constexpr int LO_GROUPS = 256;                       // workgroups of the last product wished for
-constexpr float LA_LAG = 8.0f;                       // see attend_tile
+constexpr float LA_LAG = 8.0f;                       // see latent_attention_kernel
 
 // 16-row tiles of query rows per workgroup, for sequences of up to `rows` query rows (8: latent_rows_kernel)
 __host__ __device__ inline int row_tiles(int dtype, int rows) { return rows <= 16 ? 1 : rows <= LA_FEW || dtype != ORDERMOE_BF16 ? 2 : 8; }

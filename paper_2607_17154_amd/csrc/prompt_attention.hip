@@ -89,11 +89,11 @@ __device__ inline bool find_block(const PromptArgs& a, int64_t item, int lane, S
 }
 
 // Rows of RB bytes in LDS, as 16-byte chunks: chunk c of row r lies at c ^ swap(r), so that what the lanes of a read
-// take lies on distinct banks.  K and the rotary part: eight rows of one chunk; V: four rows of two chunks (bf16, turned)
-// or two rows, four apart, of eight (fp32).
+// take together lies on distinct banks: lanes 0 - 3, 12 - 15, 20 - 27 and the others of each 32, 256 bytes.  K and the rotary
+// part: one chunk of 16 rows; V: four rows of two chunks (bf16, turned) or two rows, four apart, of eight (fp32).
 template <int RB>
 __device__ inline int swap_k(int r) {
-    return RB >= 256 ? r & 15 : RB == 128 ? r & 7 : (r >> 1) & 3;
+    return RB >= 256 ? r & 15 : RB == 128 ? (r >> 1) & 7 : (r >> 2) & 3;
 }
 template <bool BF, int RB>
 __device__ inline int swap_v(int r) {
