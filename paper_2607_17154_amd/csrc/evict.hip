@@ -8,6 +8,8 @@
 //                        workgroup finds the digits before from all the slices' histograms), then its places
 //   evict_move_kernel    the i-th kept row past the budget into the i-th place that came free
 //                        before it: as few rows move as can
+// Masses and positions are 8 bytes a place, little beside a row: barriers and launches bound the selection (16 of 1016 places
+// 10 us, of which 7 to 8 select; 20000 to 60000 places of 8 sequences 40), what the card copies the moves (5.5 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

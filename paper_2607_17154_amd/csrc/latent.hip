@@ -3,9 +3,11 @@
 //
 //   latent_write_kernel   three kinds of workgroups: 64 tokens x 64 ranks of one head's
 //                         absorbed queries, qa[t][r] = sum_d q[t][d] W_k[d][r]; four tokens'
-//                         rows, a wave each; 256 pieces of the queries that are turned or copied
-//   latent_expand_kernel  Y = C W^T for the rows C of the cache at the given slots and all of
-//                         W_k and W_v: tiles of TN tokens x TN weight rows
+//                         rows, a wave each; pieces of the queries of 16 or 8 elements that are
+//                         turned or copied.  Reads and writes bound it: 16001 tokens x 32 heads of
+//                         192, copied, 99 us, 4.4 TB/s
+//   latent_expand_kernel, latent_expand_wide_kernel  Y = C W^T for the rows C of the cache at the
+//                         given slots and all of W_k and W_v, in tiles
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -178,7 +180,8 @@ __device__ inline void absorb_tile(const LatentWriteArgs& a, int64_t t0, int h, 
     }
 }
 
-constexpr int LW_COPIES = 4, LW_TURNS = 2;           // of a thread: pieces on their way together
+// pieces of a thread that are on their way together, in workgroups of one kind (one each, mixed in a wave: 152 us for 99)
+constexpr int LW_COPIES = 4, LW_TURNS = 2;
 
 // blocks: absorb tiles, then rows, then the queries' pieces of 8 elements that are copied (not where they are absorbed), then
 // those of 16 that are turned
@@ -314,8 +317,8 @@ __device__ inline __attribute__((always_inline)) void expand_step(char* __restri
 
 // A tile of TN tokens (the matrix unit's columns) x TN weight rows, 2 x 2 waves.  Both come in
 // slabs of 128 bytes a row through LDS, two buffers, or four of fewer rows, all but one on their way; chunk c of row r
-// lies at c ^ (r % 8), so that the 16-byte reads of eight rows lie on distinct banks.  (300 tokens x 40 heads, rank 128,
-// fp32: 8.0 us in tiles of 64, 5.9 of 32.)
+// lies at c ^ (r % 8), so that the 16-byte reads of eight rows lie on distinct banks.  (300 tokens x 8 heads of 64,
+// rank 256, fp32: 8.0 us in tiles of 64, 5.9 of 32.)
 template <bool BF, int TN>
 __global__ void __launch_bounds__(256) latent_expand_kernel(const LatentExpandArgs a, int64_t tok_tiles, int row_tiles, int spread) {
     constexpr int ES = BF ? 2 : 4, W = TN / 2, F = W / 16, LOADS = TN / 32;     // a wave's rows, its tiles, its pieces of a slab
@@ -378,10 +381,12 @@ __global__ void __launch_bounds__(256) latent_expand_kernel(const LatentExpandAr
 // The same in tiles of 256 tokens x 128 weight rows, 2 x 2 waves of 128 x 64: a wave reads 12 pieces of LDS for 32 matrix
 // instructions, where 64 x 64 reads 8 for 16 and LDS is what bounds it.  Slabs of 64 bytes a row, three
 // buffers, two slabs on their way; chunk c of row r lies at c ^ (r / 2 % 4), so that lanes read together (0 - 3, 12 - 15,
-// 20 - 27, the others of each 32) do so on distinct banks.  A workgroup takes some weight tiles of its tokens after one another: the next tile's loads are on
-// their way while a tile's results go, through LDS of the wave's own, in whole lines to memory.
+// 20 - 27, the others of each 32) do so on distinct banks.  A workgroup takes some weight tiles of its tokens after one
+// another: the next tile's loads are on their way while a tile's results go, through LDS of the wave's own, in whole
+// lines to memory.  30001 tokens x 32 heads of 128, rank 512: 383 us in tiles of 128, 294 to 327 on different cards (770 to
+// 857 TFLOP/s); the matrix unit is busy 39% of the time, LDS 36%, each waiting for the other at a slab's end.
 constexpr int LX_TOK = 256, LX_W = 128, LX_SLAB = 64, LX_STAGE = (LX_TOK + LX_W) * LX_SLAB, LX_OUT = 16 * 128;
-constexpr int LX_CHUNK = 4;                          // weight tiles of a workgroup, at most
+constexpr int LX_CHUNK = 4;                          // weight tiles of a workgroup, at most (one 332 us, two 327, four 324, eight 338)
 
 // (The loads' buffer and the one that is read never overlap: told so, the compiler does not wait for the loads first.)
 template <class Issue>

@@ -25,7 +25,8 @@
 // registers: one barrier a tile.  It reads each row in LDS eight times for 128 query rows, which bounds it (128 bytes a
 // cycle); blocks of 64 rows in the first way read it less than half as often but waited for each other: trees of 64 over
 // 30000-100000 tokens 993 us for 482.
-// Rows go straight from memory into LDS, the next tile while one is attended to.
+// Rows go straight from memory into LDS, the next tile while one is attended to.  64 sequences of 200 to 8000 tokens, one token
+// of 32 heads, rank 512: 67 us, 4.6 TB/s, by the rows on their way; trees of 64 482 (790 TFLOP/s).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

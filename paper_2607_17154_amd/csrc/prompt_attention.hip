@@ -17,7 +17,11 @@
 //                 j the 8 inner indexes of its P^T operand, when V^T's lanes hold the same positions,
 //                 which a turned read of V's rows in LDS gives them.  So the weights never leave their
 //                 registers.
-// K, the shared rotary part and V go straight from memory into LDS, two tiles on their way.
+// K, the shared rotary part and V go straight from memory into LDS, keys two tiles ahead, values one: a tile's weights are
+// made beside the scores of the next.  Two waves a SIMD share the matrix unit and the vector instructions of the softmax,
+// which are busy 51% and 43% of the time: 12001 tokens x 32 heads of 128 + 64 1390 to 1510 us on different cards (970 to 1060
+// TFLOP/s of the part that is seen), 8 prompts of up to 4000 tokens, 32 heads over 8 of 128, 474 to 523.  A comparison and a
+// selection more per weight cost 7%.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
