@@ -685,7 +685,8 @@ int ordermoe_latent_write(const ordermoe_latent_cache* C, const ordermoe_latent_
  *            gets, summed over the sequence's tokens (its first max_q) and heads:
  *              p < ctx_len:                 decay * mass[b][p] + w
  *              ctx_len <= p < ctx_len + n_b:  w
- *            entries past these, or past mass_stride, are left as they are.  May be mass itself.
+ *            entries past these, or past mass_stride, and those of a sequence without tokens are left as they
+ *            are.  May be mass itself.
  *   ws       dev, of the size below (weighs: 1 where mass_out will be given), in use until the stream
  *            passes the call.  With weighs it holds the scores, 4 B max_q n_q max_pages page_size bytes of it.
  * Limits as there, but n_q <= 128; 0 <= T * n_q < 2^31; decay finite. */

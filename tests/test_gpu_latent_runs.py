@@ -294,3 +294,88 @@ def test_keys_and_values_past_32_bit_offsets():
     e = ol.prompt_attention(_host(q), _host(k[L - n0:]), _host(v[L - n0:]), None, 0.09)
     ew = 2 * e["score"] * (D + 4) * U + (8 + n0) * U + 2.0 ** -8
     _within(_host(out), e["out"], ew * e["size"] + (2.0 ** -8 + 2 * U) * np.abs(e["out"]), "out")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,h,g,rot", [(150, 4, 4, 32), (100, 2, 1, 0), (70, 40, 5, 0)])
+def test_many_prompts_with_gaps_between_them(dtype, B, h, g, rot):
+    """More sequences than a wave looks through at a time, in one piece and in several; tokens before the first."""
+    rng = np.random.default_rng(B)
+    n = rng.integers(0, 9, B)
+    n[rng.integers(0, B, 5)] = 0
+    n[B // 2] = 140
+    p = _prompt(rng, dtype, n, rng.integers(0, 40, B), h, g, 64, rot)
+    d = DT[dtype]
+    # the same sequences, five tokens and seven positions later
+    ahead = lambda x, c: torch.cat([torch.full((c,) + x.shape[1:], float("nan"), dtype=d, device="cuda"), x])  # noqa: E731
+    want = _run_prompt(p)
+    later = dict(p, q=ahead(p["q"], 5), k=ahead(p["k"], 7), v=ahead(p["v"], 7), r=None if p["r"] is None else ahead(p["r"], 7),
+                 qs=p["qs"] + 5, ks=p["ks"] + 7)
+    got = _run_prompt(later)
+    for x, y in zip(want, got):
+        assert torch.equal(x, y[5:]) and (y[:5] == 7).all()
+    q, k, v, r = (None if p[c] is None else _host(p[c]) for c in "qkvr")
+    qs, ks = p["qs"], p["ks"]
+    for b in range(B):
+        t, kk = slice(qs[b], qs[b + 1]), slice(ks[b], ks[b + 1])
+        if t.start == t.stop:
+            continue
+        e = ol.prompt_attention(q[t], k[kk], v[kk], None if r is None else r[kk], p["scale"])
+        es = e["score"] * (64 + rot + 4) * U
+        ew = 2 * es + (8 + kk.stop - kk.start) * U + (2.0 ** -8 if dtype == "bf16" else 0)
+        _within(_host(want[0])[t], e["out"], ew * e["size"] + (2 * U + HALF[dtype]) * np.abs(e["out"]), "out of %d" % b)
+
+
+def test_prompts_without_positions_and_a_scale_of_nothing():
+    rng = np.random.default_rng(8)
+    p = _prompt(rng, "bf16", [3, 70], [-3, -70], 4, 2, 64, 0)
+    p["k"], p["v"] = p["k"][:0], p["v"][:0]
+    out, lse = _run_prompt(p)
+    assert (out[:73] == 0).all() and torch.isneginf(lse[:73]).all() and (out[73:] == 7).all()
+    p = _prompt(rng, "f32", [5, 66], [2, 0], 2, 2, 64, 32)
+    p["scale"] = 0.0                                         # the mean of what a token sees
+    out, lse = _run_prompt(p)
+    v = _host(p["v"])
+    for t, (lo, seen) in {0: (0, 3), 4: (0, 7), 5: (7, 1), 70: (7, 66)}.items():
+        some = v[lo:lo + seen]
+        _within(_host(out)[t], some.mean(0), (8 + seen) * U * np.abs(some).mean(0), "mean of %d" % seen)
+        _within(_host(lse)[t], np.full(2, np.log(seen)), (8 + seen) * U * (1 + np.log(seen)), "lse")
+
+
+def test_a_thousand_short_sequences():
+    rng = np.random.default_rng(9)
+    n = rng.integers(0, 3, 1000)
+    ba = _Batch(rng, "bf16", rng.integers(0, 40, 1000), n, 4, 64, 128, 32, 16)
+    got = ba.run(2, stride=50)
+    ba.check(got, 2)
+    stays = _host(got[2])[n == 0]                            # entries of sequences without tokens
+    assert (stays == 7).all()
+
+
+def test_evictions_of_few_and_of_many_rows_and_one_after_another():
+    """Tables whose rows move in the kernel that finds them, or in one of their own; the second cut starts from the first."""
+    rng = np.random.default_rng(10)
+    for places, keep, first, recent in ((288, 40, 4, 8), (288, 30, 30, 0), (320, 200, 0, 200), (16, 15, 0, 0), (544, 280, 3, 7)):
+        s = _Server(11, "bf16", B=5, places=places, keep=keep)
+        n = np.array([0, places, keep, min(places, keep + 1), places - 3])
+        s.ctx.copy_(_dev(n.astype(np.int32)))
+        s.rows.copy_(_dev(rng.normal(size=s.rows.shape), torch.bfloat16))
+        s.mass.copy_(_dev(np.round(rng.random((5, places)) * 9) / 4, torch.float32))
+        s.pos.copy_(_dev(np.stack([rng.permutation(places) for _ in range(5)]).astype(np.int32)))
+        seq, ctx = np.full(5, places), n
+        for cut in (keep, max(1, keep // 2)):
+            f, r = min(first, cut), min(recent, cut - min(first, cut))
+            mass, pos, rows = _host(s.mass), _host(s.pos), [s.cached(b, ctx[b]) for b in range(5)]
+            kept = torch.full((5, cut), 99, dtype=torch.int32, device="cuda")
+            ws = torch.full((om.ordermoe_latent_evict_workspace_size(s.cache, 5, s.pages, cut),), 0x7F, dtype=torch.uint8, device="cuda")
+            om.ordermoe_latent_evict(s.cache, s.ctx, _dev(seq.astype(np.int32)), s.d_table, cut, f, r, s.mass, s.pos, kept, s.ctx, s.mass,
+                                     s.pos, ws)
+            for b in range(5):
+                want = ol.evict(int(ctx[b]), int(seq[b]), cut, f, r, mass[b], pos[b])
+                np.testing.assert_array_equal(_host(kept)[b], want)
+                new = min(int(ctx[b]), cut)
+                np.testing.assert_array_equal(s.cached(b, new), rows[b][want[:new]])
+                np.testing.assert_array_equal(_host(s.mass)[b, :new], mass[b][want[:new]])
+                np.testing.assert_array_equal(_host(s.pos)[b, :new], pos[b][want[:new]])
+            ctx = np.minimum(ctx, cut)
+            np.testing.assert_array_equal(_host(s.ctx), ctx)
