@@ -744,7 +744,8 @@ __global__ void __launch_bounds__(256) latent_out_kernel(const LatentAttentionAr
     constexpr int PAIRS = DS / 32, SHARE = 4 / PAIRS, KS = R * ES / 64 / SHARE, EARLY = SHARE > 1 ? KS : 4;
     __shared__ __attribute__((aligned(16))) char s_o[BF ? 2 : 1][16 * PITCH];
     __shared__ f32x4 s_acc[SHARE > 1 ? 4 : 1][2][64];
-    __shared__ float s_x[S == 16 ? 4 : 1][S == 16 ? R : 1], s_m[4], s_l[4];
+    __shared__ __attribute__((aligned(16))) float s_x[S > 1 ? 16 : 1][S > 1 ? R + 4 : 4];
+    __shared__ float s_m[16], s_l[16];
     __shared__ int s_in[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t id = block_number(), rest = id / slices;
@@ -810,68 +811,59 @@ __global__ void __launch_bounds__(256) latent_out_kernel(const LatentAttentionAr
             for (int e = 0; e < R / 16; ++e) x[e] += v[k][e / 4][e % 4] * f;
         }
     }
-    // four sets of a wave, then (S = 16) the waves'
+    // Four elements of a token's sums, relative to its maximum, divided and put into the operand's two parts
+    auto put = [&](int to, int e, const f32x4& sum, float r) __attribute__((always_inline)) {
+        const f32x4 y = sum * r;
+        char* o = &s_o[0][to * PITCH + e * ES];
+        if constexpr (BF) {
+            float d[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) d[k] = y[k] - (float)(__bf16)y[k];
+            *(u32x2*)o = u32x2{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3])};
+            *(u32x2*)&s_o[BF ? 1 : 0][to * PITCH + e * ES] = u32x2{bf16_pair(d[0], d[1]), bf16_pair(d[2], d[3])};
+        } else {
+            *(f32x4*)o = y;
+        }
+    };
     if constexpr (S > 1) {
-        float top = fmaxf(m, __shfl_xor(m, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float f = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
-        m = top;
-        l *= f;
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
+        // the sets of a token through LDS, in order.  (By exchanges between the lanes that hold them 6500 cycles, of 13000 in
+        // all for one token over 777.)
 #pragma unroll
-        for (int e = 0; e < R / 16; ++e) {
-            x[e] *= f;
-            x[e] += __shfl_xor(x[e], 16);
-            x[e] += __shfl_xor(x[e], 32);
-        }
-    }
-    __syncthreads();                                 // s_in is clear
-    if constexpr (S == 16) {
-        if (lane < 16) {
-#pragma unroll
-            for (int e = 0; e < R / 64; ++e) *(f32x4*)&s_x[wave][4 * u + 64 * e] = f32x4{x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]};
-        }
-        if (lane == 0) { s_m[wave] = m; s_l[wave] = l; }
+        for (int e = 0; e < R / 64; ++e) *(f32x4*)&s_x[tid >> 4][4 * u + 64 * e] = f32x4{x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]};
+        if (u == 0) { s_m[tid >> 4] = m; s_l[tid >> 4] = l; }
         __syncthreads();
-        m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-        l = 0.f;
+        auto whole = [&](int to, float (&f)[S]) __attribute__((always_inline)) {        // m, l and the sets' factors
+            m = s_m[to * S];
 #pragma unroll
-        for (int e = 0; e < R / 16; ++e) x[e] = 0.f;
-        if (tid < 16) {
+            for (int k = 1; k < S; ++k) m = fmaxf(m, s_m[to * S + k]);
+            l = 0.f;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float f = s_m[k] == m ? 1.0f : __builtin_amdgcn_exp2f(s_m[k] - m);
-                l += s_l[k] * f;
-#pragma unroll
-                for (int e = 0; e < R / 16; ++e) x[e] += s_x[k][4 * u + 64 * (e / 4) + e % 4] * f;
+            for (int k = 0; k < S; ++k) {
+                f[k] = s_m[to * S + k] == m ? 1.0f : __builtin_amdgcn_exp2f(s_m[to * S + k] - m);
+                l += s_l[to * S + k] * f[k];
             }
+        };
+        float f[S];
+        for (int v = tid; v < TOK * (R / 4); v += 256) {
+            const int to = v / (R / 4), e = v % (R / 4) * 4;
+            whole(to, f);
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < S; ++k) sum = sum + *(const f32x4*)&s_x[to * S + k][e] * f[k];
+            put(to, e, sum, l == 0.f ? 0.f : 1.0f / l);
         }
-    }
-    if (z == 0) {
+        if (z == 0) whole(slot, f);
+    } else {
+        __syncthreads();                             // s_in is clear
         const float r = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
-        for (int e = 0; e < R / 64; ++e) {
-            float y[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) y[k] = x[4 * e + k] * r;
-            char* o = &s_o[0][slot * PITCH + (4 * u + 64 * e) * ES];
-            if constexpr (BF) {
-                float d[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) d[k] = y[k] - (float)(__bf16)y[k];
-                *(u32x2*)o = u32x2{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3])};
-                *(u32x2*)&s_o[BF ? 1 : 0][slot * PITCH + (4 * u + 64 * e) * ES] = u32x2{bf16_pair(d[0], d[1]), bf16_pair(d[2], d[3])};
-            } else {
-                *(f32x4*)o = f32x4{y[0], y[1], y[2], y[3]};
-            }
-        }
-        if (in && u == 0) {
-            s_in[slot] = 1;
-            if (d0 == 0) {
-                if (a.lse) a.lse[(int64_t)t * a.n_q + h] = l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * LN2;
-                if (a.mass_out) ((f32x2*)a.stat)[(int64_t)b * rows_max + row] = f32x2{m == -__builtin_inff() ? 0.f : m, r};
-            }
+        for (int e = 0; e < R / 64; ++e) put(slot, 4 * u + 64 * e, f32x4{x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]}, r);
+    }
+    if (z == 0 && in && u == 0) {
+        s_in[slot] = 1;
+        if (d0 == 0) {
+            if (a.lse) a.lse[(int64_t)t * a.n_q + h] = l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * LN2;
+            if (a.mass_out) ((f32x2*)a.stat)[(int64_t)b * rows_max + row] = f32x2{m == -__builtin_inff() ? 0.f : m, l == 0.f ? 0.f : 1.0f / l};
         }
     }
     __syncthreads();
