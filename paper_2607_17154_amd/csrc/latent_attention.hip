@@ -746,7 +746,7 @@ template <bool BF, int R, int D, int DS, int S>
 __global__ void __launch_bounds__(256) latent_out_kernel(const LatentAttentionArgs a, int slices) {
     constexpr int ES = BF ? 2 : 4, PITCH = R * ES + 16, U = 4, TOK = 16 / S;     // bytes of a row in LDS; pieces whose reads are in flight; tokens
     constexpr int PAIRS = DS / 32, SHARE = 4 / PAIRS, KS = R * ES / 64 / SHARE, EARLY = SHARE > 1 ? KS : 4;
-    __shared__ __attribute__((aligned(16))) char s_o[BF ? 2 : 1][16 * PITCH];
+    __shared__ __attribute__((aligned(16))) char s_o[BF ? 2 : 1][TOK * PITCH];
     __shared__ f32x4 s_acc[SHARE > 1 ? 4 : 1][2][64];
     __shared__ __attribute__((aligned(16))) float s_x[S > 1 ? 16 : 1][S > 1 ? R + 4 : 4];
     __shared__ float s_m[16], s_l[16];
