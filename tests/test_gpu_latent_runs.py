@@ -379,3 +379,33 @@ def test_evictions_of_few_and_of_many_rows_and_one_after_another():
                 np.testing.assert_array_equal(_host(s.pos)[b, :new], pos[b][want[:new]])
             ctx = np.minimum(ctx, cut)
             np.testing.assert_array_equal(_host(s.ctx), ctx)
+
+
+@pytest.mark.parametrize("n,h,D,R", [(4400, 120, 64, 128), (6500, 127, 64, 256), (16500, 128, 64, 128), (16640, 64, 128, 512)])
+def test_large_expansions(n, h, D, R):
+    """Several weight tiles of a workgroup one after the other: all of them whole, the last one not, few tokens in the last tile."""
+    rng = np.random.default_rng(n)
+    page, rot = 64, 32
+    rows = _dev(rng.normal(size=(n // page // 2, page, R + rot)), torch.bfloat16)
+    cache = om.make_latent_cache(rows, R)
+    wk, wv = _weights(rng, h, D, R, "bf16")
+    slots = rng.integers(0, rows.shape[0] * page, n).astype(np.int64)
+    slots[[0, 300, n - 1]] = -1
+    k, v = (torch.full((n, h, D), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    r = torch.full((n, rot), 7.0, dtype=torch.bfloat16, device="cuda")
+    heads, d_slots = om.make_latent_heads(cache, wk, wv), _dev(slots)
+    om.ordermoe_latent_expand(cache, heads, d_slots, k, r, v)
+    x = torch.where(d_slots[:, None] >= 0, rows.flatten(0, 1)[d_slots.clamp(min=0)], torch.zeros((), dtype=torch.bfloat16, device="cuda"))
+    assert torch.equal(r, x[:, R:])
+    x = x[:, :R].float()
+    for got, w in ((k, wk), (v, wv)):
+        for lo in range(0, h, 32):                           # every output, in fp32 (its own error: as the kernel's sums')
+            w32 = w[lo:lo + 32].float().flatten(0, 1).t().contiguous()
+            want, size = x @ w32, x.abs() @ w32.abs()
+            off = (got[:, lo:lo + 32].flatten(1).float() - want).abs() > 2 * (R + 1) * U * size + 2.0 ** -8 * want.abs()
+            assert not off.any(), (lo, int(off.sum()))
+    again = [torch.empty_like(t) for t in (k, r, v)]
+    for _ in range(3):
+        om.ordermoe_latent_expand(cache, heads, d_slots, *again)
+        for a, b in zip((k, r, v), again):
+            assert torch.equal(a, b)
