@@ -17,6 +17,7 @@
 #include "common.hpp"
 #include "grid.hpp"
 #include "mfma.hpp"
+#include "write_blocks.hpp"
 
 namespace ordermoe {
 namespace {
@@ -111,8 +112,6 @@ __device__ inline void write_row(const LatentWriteArgs& a, int64_t t, int lane) 
     if (lane < rot / 16) turn16<BF>(a, t, from + R, to + R, lane);
 }
 
-constexpr int LW_TOK = 64, LW_COLS = 64;             // tokens and ranks of an absorb workgroup
-
 // qa[t][r] for 64 tokens and 64 ranks of one head: the matrix unit's rows are ranks, its
 // columns tokens; a wave takes 16 ranks and every token.
 template <bool BF, int D>
@@ -180,31 +179,28 @@ __device__ inline void absorb_tile(const LatentWriteArgs& a, int64_t t0, int h, 
     }
 }
 
-// pieces of a thread that are on their way together, in workgroups of one kind (one each, mixed in a wave: 152 us for 99)
-constexpr int LW_COPIES = 4, LW_TURNS = 2;
-
 // blocks: absorb tiles, then rows, then the queries' pieces of 8 elements that are copied (not where they are absorbed), then
 // those of 16 that are turned
 template <bool BF, int D, int ROT>
-__global__ void __launch_bounds__(256) latent_write_kernel(const LatentWriteArgs a, int64_t n_absorb, int64_t n_rows, int64_t n_copies) {
+__global__ void __launch_bounds__(256) latent_write_kernel(const LatentWriteArgs a, const WriteBlocks n) {
     __shared__ __attribute__((aligned(16))) char mem[BF ? D * LW_COLS * 2 : 16];
     int64_t blk = block_number();
-    if (blk < n_absorb) {
+    const WriteBlocks::Kind kind = n.kind(blk);
+    if (kind == WriteBlocks::ABSORB) {
         const int slices = a.cache.rank / LW_COLS;
         const int64_t th = blk / slices;
         const int r0 = (int)(blk - th * slices) * LW_COLS, h = (int)(th % a.n_q);
         absorb_tile<BF, D>(a, th / a.n_q * LW_TOK, h, r0, mem);
         return;
     }
-    blk -= n_absorb;
-    if (blk < n_rows) {
+    if (kind == WriteBlocks::ROWS) {
         const int64_t t = blk * 4 + (threadIdx.x >> 6);
         if (t < a.T) write_row<BF>(a, t, threadIdx.x & 63);
         return;
     }
-    blk -= n_rows;
+    if (kind == WriteBlocks::NONE) return;
     const uint32_t heads = (uint32_t)(a.T * a.n_q), n_q = (uint32_t)a.n_q;       // (fewer than 2^31)
-    if (blk < n_copies) {
+    if (kind == WriteBlocks::COPY) {
         constexpr int PER = D / 8;
         float x[LW_COPIES][8];
         const int k = threadIdx.x % PER;
@@ -223,7 +219,6 @@ __global__ void __launch_bounds__(256) latent_write_kernel(const LatentWriteArgs
         }
         return;
     }
-    blk -= n_copies;
     constexpr int PER = ROT / 16;
     const int wide = a.absorb ? a.cache.rank : D, k = threadIdx.x % PER;
 #pragma unroll
@@ -237,12 +232,9 @@ __global__ void __launch_bounds__(256) latent_write_kernel(const LatentWriteArgs
 
 template <bool BF, int D, int ROT>
 int launch_write(const LatentWriteArgs& a, hipStream_t st) {
-    const int64_t absorb = a.q && a.absorb ? (a.T + LW_TOK - 1) / LW_TOK * a.n_q * (a.cache.rank / LW_COLS) : 0;
-    const int64_t rows = (a.T + 3) / 4, heads = a.q ? a.T * a.n_q : 0;
-    const int64_t per_copy = 256 / (D / 8) * LW_COPIES, per_turn = 256 / (ROT / 16) * LW_TURNS;
-    const int64_t copies = a.absorb ? 0 : (heads + per_copy - 1) / per_copy, turns = (heads + per_turn - 1) / per_turn;
+    const WriteBlocks n = write_blocks(a.T, a.n_q, D, a.cache.rank, ROT, a.q != nullptr, a.absorb != 0);
     KernelTimer kt_("latent_write", st);
-    latent_write_kernel<BF, D, ROT><<<grid_of(absorb + rows + copies + turns), dim3(256), 0, st>>>(a, absorb, rows, copies);
+    latent_write_kernel<BF, D, ROT><<<grid_of(n.absorb + n.rows + n.copies + n.turns), dim3(256), 0, st>>>(a, n);
     return (int)hipGetLastError();
 }
 template <bool BF>

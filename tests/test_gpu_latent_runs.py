@@ -409,3 +409,20 @@ def test_large_expansions(n, h, D, R):
         om.ordermoe_latent_expand(cache, heads, d_slots, *again)
         for a, b in zip((k, r, v), again):
             assert torch.equal(a, b)
+
+
+def test_rows_alone_of_more_tokens_than_one_row_of_the_grid_takes():
+    """No queries, and more than 2^22 workgroups: the launch has some that find nothing to do."""
+    T, R, rot, page = (1 << 24) + 4, 128, 32, 1024
+    pages = -(-T // page)
+    kv = torch.empty((T, R + rot), dtype=torch.bfloat16, device="cuda")
+    kv.view(torch.int16).random_(0, 0x7000)                  # (finite numbers)
+    rows = torch.zeros((pages, page, R + rot), dtype=torch.bfloat16, device="cuda")
+    cache = om.make_latent_cache(rows, R)
+    wk, wv = _weights(np.random.default_rng(12), 1, 64, R, "bf16")
+    slots = torch.arange(T - 1, -1, -1, dtype=torch.int64, device="cuda")
+    for absorb in (0, 1):
+        rows.zero_()
+        om.ordermoe_latent_write(cache, om.make_latent_heads(cache, wk, wv), None, kv, None, slots, None, absorb)
+        flat = rows.flatten(0, 1)
+        assert torch.equal(flat[:T].view(torch.int16), kv.flip(0).view(torch.int16)) and not flat[T:].view(torch.int16).any()
