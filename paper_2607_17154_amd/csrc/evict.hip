@@ -62,13 +62,13 @@ __device__ inline Places places_of(const EvictArgs& a, int b) {
 // a sequence that keeps all of its tokens
 template <int NT>
 __device__ inline void keep_all(const EvictArgs& a, const Places& pl, int b, int tid) {
-    for (int p = tid; p < a.keep; p += NT) {
+    every(tid, a.keep, NT, [&](int p) {
         pl.kept[p] = p < pl.n ? p : -1;
         if (p < pl.n) {
             if (pl.mass_out != pl.mass) pl.mass_out[p] = pl.mass[p];
             if (pl.pos_out != pl.pos) pl.pos_out[p] = pl.pos[p];
         }
-    }
+    });
     if (tid == 0) { a.moves[b] = -1; a.len_out[b] = pl.n; }
 }
 

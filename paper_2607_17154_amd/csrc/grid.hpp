@@ -18,4 +18,10 @@ inline dim3 grid_of(int64_t n) {
 // reading gridDim costs a small kernel a memory access before its first address.
 __device__ inline uint32_t block_number() { return (blockIdx.y << GRID_ROW) + blockIdx.x; }
 
+// f(i) for i = first, first + step, .. below n, which may be the largest number that an int holds
+template <class F>
+__host__ __device__ inline void every(int first, int n, int step, const F& f) {
+    for (int64_t i = first; i < n; i += step) f((int)i);
+}
+
 }  // namespace ordermoe

@@ -426,3 +426,18 @@ def test_rows_alone_of_more_tokens_than_one_row_of_the_grid_takes():
         om.ordermoe_latent_write(cache, om.make_latent_heads(cache, wk, wv), None, kv, None, slots, None, absorb)
         flat = rows.flatten(0, 1)
         assert torch.equal(flat[:T].view(torch.int16), kv.flip(0).view(torch.int16)) and not flat[T:].view(torch.int16).any()
+
+
+@pytest.mark.parametrize("places", [160, 8320])              # tables that one kernel goes through, and longer ones
+def test_a_budget_of_the_largest_number(places):
+    keep = (1 << 31) - 1
+    s = _Server(13, "bf16", B=1, places=places, keep=1)
+    n = places - 3
+    s.ctx.fill_(n)
+    s.mass.copy_(_dev(s.rng.random((1, places)), torch.float32))
+    rows, mass = s.rows.clone(), s.mass.clone()
+    kept = torch.full((1, keep), 99, dtype=torch.int32, device="cuda")
+    ws = torch.full((om.ordermoe_latent_evict_workspace_size(s.cache, 1, s.pages, keep),), 0x7F, dtype=torch.uint8, device="cuda")
+    om.ordermoe_latent_evict(s.cache, s.ctx, s.ctx.clone(), s.d_table, keep, 5, keep - 5, s.mass, s.pos, kept, s.ctx, s.mass, s.pos, ws)
+    assert int(s.ctx) == n and torch.equal(s.rows, rows) and torch.equal(s.mass, mass)
+    assert torch.equal(kept[0, :n], torch.arange(n, dtype=torch.int32, device="cuda")) and bool((kept[0, n:] == -1).all())

@@ -1,5 +1,6 @@
-"""Workgroups of latent_write on the host: a launch of more than 2^22 of them is rounded up to whole
-rows of the grid, and those past the last one have nothing to do."""
+"""Numbers of workgroups and places on the host.  latent_write: a launch of more than 2^22 workgroups is
+rounded up to whole rows of the grid, and those past the last one have nothing to do.  latent_evict: a
+budget may be any positive int32."""
 import os
 import shutil
 import subprocess
@@ -39,20 +40,24 @@ int main(int, char** v) {
 """
 
 
-@pytest.fixture(scope="module")
-def blocks(tmp_path_factory):
+def _program(d, source):
     if not shutil.which(b.HIPCC):
         pytest.skip("no hipcc")
-    d = tmp_path_factory.mktemp("blocks")
-    src, exe = d / "blocks.hip", d / "blocks"
-    src.write_text(SOURCE)
-    subprocess.run([b.HIPCC] + b.FLAGS + ["-I", b.CSRC, str(src), "-o", str(exe)], check=True, capture_output=True)
+    src, exe = d / "host.hip", d / "host"
+    src.write_text(source)
+    # (-fwrapv: a count that outgrows its type is seen, not optimised away)
+    subprocess.run([b.HIPCC] + b.FLAGS + ["-fwrapv", "-I", b.CSRC, str(src), "-o", str(exe)], check=True, capture_output=True)
 
     def run(*args):
         r = subprocess.run([str(exe)] + [str(int(a)) for a in args], capture_output=True, text=True, timeout=100)
         assert r.returncode == 0, r.stdout + r.stderr
         return [int(x) for x in r.stdout.split()]
     return run
+
+
+@pytest.fixture(scope="module")
+def blocks(tmp_path_factory):
+    return _program(tmp_path_factory.mktemp("blocks"), SOURCE)
 
 
 @pytest.mark.parametrize("T,n_q,D,R,rot,queries,absorb", [
@@ -67,3 +72,36 @@ def test_every_workgroup_of_a_write_has_its_own_work_or_none(blocks, T, n_q, D, 
     assert n_rows == -(-T // 4) and n_turns == -(-heads // (256 // (rot // 16) * 2))
     assert n_absorb == (-(-T // 64) * n_q * (R // 64) if queries and absorb else 0)
     assert n_copies == (0 if absorb else -(-heads // (256 // (D // 8) * 4)))
+
+
+STRIDES = r"""
+#include <cstdio>
+#include <cstdlib>
+
+#include "grid.hpp"
+
+// first n step -> how many numbers, and the last one
+int main(int, char** v) {
+    int64_t count = 0, last = -1;
+    ordermoe::every(atoi(v[1]), atoi(v[2]), atoi(v[3]), [&](int i) {
+        if (i <= last) exit(1);
+        ++count;
+        last = i;
+    });
+    printf("%lld %lld\n", (long long)count, (long long)last);
+    return 0;
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def strides(tmp_path_factory):
+    return _program(tmp_path_factory.mktemp("strides"), STRIDES)
+
+
+@pytest.mark.parametrize("n", [1, 511, 512, 513, 5000, (1 << 30) + 1, (1 << 31) - 1024, (1 << 31) - 513, (1 << 31) - 2, (1 << 31) - 1])
+@pytest.mark.parametrize("step", [512, 1024])
+def test_a_thread_s_places_of_any_budget(strides, n, step):
+    for first in (0, 1, step - 1):
+        want = range(first, n, step)
+        assert strides(first, n, step) == [len(want), want[-1] if len(want) else -1]
