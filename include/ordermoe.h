@@ -728,8 +728,8 @@ int ordermoe_latent_expand(const ordermoe_latent_cache* C, const ordermoe_latent
  *              not written.
  *   ws         dev, of the size below: partial results of rows whose positions are split over workgroups
  *              (joined in a fixed order); in use until the stream passes the call
- * 1 <= n_kv, n_q <= 1024 a multiple of n_kv, 0 <= B <= 65535, 0 <= T, L < 2^31 with T * n_q < 2^31,
- * scale finite. */
+ * 1 <= n_kv, n_q <= 1024 a multiple of n_kv, 0 <= B <= 65535, 0 <= T with T * n_q < 2^31,
+ * 0 <= L <= 2^31 - 128, scale finite. */
 size_t ordermoe_prompt_attention_workspace_size(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t head_dim,
                                                 int32_t rotary_dim, int64_t T, int32_t B);
 int ordermoe_prompt_attention(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t rotary_dim, const void* q,

@@ -206,7 +206,8 @@ extern "C" int ordermoe_prompt_attention(int32_t dtype, int32_t n_q, int32_t n_k
     const char* who = "prompt_attention";
     const int rc = check_prompt(dtype, n_q, n_kv, head_dim, rotary_dim, T, B, who);
     if (rc) return rc;
-    if (L < 0 || L >= INT_LIMIT) return bad(who, "L must lie in [0, 2^31)");
+    // (the kernel counts positions in 32 bits and looks up to two tiles of 64 past the last one)
+    if (L < 0 || L > INT_LIMIT - 128) return bad(who, "L must lie in [0, 2^31 - 128]");
     if (!std::isfinite(scale)) return bad(who, "scale must be finite");
     if (T > 0 && B > 0 && (!good16(q) || !q_start || !kv_start || !good16(out) ||
                            (L > 0 && (!good16(k) || !good16(v) || (rotary_dim > 0 && !good16(r))))))

@@ -168,3 +168,10 @@ def test_oracle_forms_agree():
     mass, pos = np.array([0, 7, 9, 1, 7, 8, 2, 0, np.nan]), np.arange(9)
     assert ol.evict(9, 9, 6, 1, 2, mass, pos).tolist() == [0, 1, 2, 7, 8, 5]
     assert ol.evict(4, 9, 6, 1, 2, mass, pos).tolist() == [0, 1, 2, 3, -1, -1]
+
+
+@pytest.mark.parametrize("L", [(1 << 31) - 127, (1 << 31) - 64, (1 << 31) - 1])
+def test_positions_up_to_two_tiles_below_32_bits(L):
+    """The loop over tiles looks two of them ahead in 32 bits: so many positions have no room for that."""
+    assert _prompt(L=L) == om.EINVAL and "prompt_attention" in om.last_error()
+    assert _prompt(L=L, T=0, q=0) == om.EINVAL
