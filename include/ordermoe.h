@@ -714,8 +714,9 @@ int ordermoe_latent_expand(const ordermoe_latent_cache* C, const ordermoe_latent
  * positions (the positions before are a context): token i sees position p if
  * p <= L_b - n_b + i.  Query head h reads key/value head g = h / (n_q / n_kv), and
  *   s_p = scale * (q_h . [k_p,g | r_p]),  out_h = sum_p exp(s_p) v_p,g / sum_p exp(s_p),  lse = log sum_p exp(s_p).
- * A token that sees nothing (L_b < n_b) gets out = 0 and lse = -infinity; an infinity or a NaN in what a
- * token sees makes its outputs infinite or NaN, some of them or all.  bf16: exact
+ * A token that sees nothing (L_b < n_b) gets out = 0 and lse = -infinity.  An infinity or a NaN in a value
+ * that it sees makes this element of its outputs infinite or NaN, and nothing else; one in q or in a key that
+ * it sees makes its outputs infinite or NaN, some of them or all.  bf16: exact
  * products, fp32 sums and statistics, the weights rounded to bf16 for the second product, rounded once
  * at the end.  fp32: fp32 throughout.
  *   head_dim   64 or 128;  rotary_dim 0, 32 or 64

@@ -172,33 +172,70 @@ __device__ inline bool no_number(const u32x4& top) {
     for (int w = 0; w < 4; ++w) r |= (top[w] >= 0x7F800000u) | (BF && (top[w] & 0xFFFFu) >= 0x7F80u);
     return r;
 }
-// Positions of a tile's values that hold an infinity or a NaN, a bit each; every wave finds them all.  They become zeros: a
-// weight of 0 would not keep what is no number out of a row's sums.
+// the elements of 16 bytes that are no numbers, as they are (NUMBERS: those that are), the others as zeros
+template <bool BF, bool NUMBERS>
+__device__ inline uint32_t parted(uint32_t x) {
+    if constexpr (BF) {
+        const bool lo = (x & 0x7F80u) == 0x7F80u, hi = (x & 0x7F800000u) == 0x7F800000u;
+        return (lo == NUMBERS ? 0u : x & 0xFFFFu) | (hi == NUMBERS ? 0u : x & 0xFFFF0000u);
+    } else {
+        return ((x & 0x7F800000u) == 0x7F800000u) == NUMBERS ? 0u : x;
+    }
+}
+// Infinities and NaNs of a tile's values become zeros: a weight of 0 would not keep what is no number out of a row's sums.
+// A lane's row that sees such a value (positions of the tile up to `see`) gets it added to the sums of its own element here.
+// Every wave looks through the whole tile, so that they meet the barriers together.
 template <bool BF, int D>
-__device__ inline uint64_t clean_values(char* v, int wave, int lane) {
-    constexpr int CH = D * (BF ? 2 : 4) / 16, PIECES = PA_TILE<BF> * CH / 64;
+__device__ inline __attribute__((always_inline)) void clean_values(char* v, int see, int wave, int lane, f32x16 (&o)[D / 32]) {
+    constexpr int RB = D * (BF ? 2 : 4), CH = RB / 16, PIECES = PA_TILE<BF> * CH / 64;
     u32x4 top = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) exponents<BF>(*(const u32x4*)(v + (i * 64 + lane) * 16), top);
-    if (!__builtin_amdgcn_ballot_w64(no_number<BF>(top))) return 0;     // (alike in all waves)
-    auto bad = [&](const u32x4& x) {
-        u32x4 t = {0u, 0u, 0u, 0u};
-        exponents<BF>(x, t);
-        return no_number<BF>(t);
-    };
-    uint64_t m = 0;
+    if (!__builtin_amdgcn_ballot_w64(no_number<BF>(top))) return;       // (alike in all waves)
+    const int h = lane >> 5;
+    uint64_t m = 0;                                      // positions
 #pragma unroll 1
-    for (int i = 0; i < PIECES; ++i)
-        if (bad(*(const u32x4*)(v + (i * 64 + lane) * 16))) m |= 1ull << ((i * 64 + lane) / CH);
+    for (int i = 0; i < PIECES; ++i) {
+        u32x4 t = {0u, 0u, 0u, 0u};
+        exponents<BF>(*(const u32x4*)(v + (i * 64 + lane) * 16), t);
+        if (no_number<BF>(t)) m |= 1ull << ((i * 64 + lane) / CH);
+    }
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) m |= __shfl_xor((unsigned long long)m, o);
+    for (int x = 32; x >= 1; x >>= 1) m |= __shfl_xor((unsigned long long)m, x);
+    uint64_t left = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)m) |
+                    (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(m >> 32)) << 32;
+    for (; left; left &= left - 1) {
+        const int p = __builtin_ctzll(left);
+        const char* row = v + p * RB;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                // elements 32 d + 8 j + 4 h .. + 3
+                const int ch = (BF ? 4 * d + j : 8 * d + 2 * j + h) ^ swap_v<BF, RB>(p);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float x;
+                    if constexpr (BF) {
+                        const uint32_t w = parted<BF, false>(*(const uint32_t*)(row + ch * 16 + 8 * h + 4 * (e / 2)));
+                        x = __uint_as_float(e % 2 ? w & 0xFFFF0000u : w << 16);
+                    } else {
+                        x = __uint_as_float(parted<BF, false>(*(const uint32_t*)(row + ch * 16 + 4 * e)));
+                    }
+                    if (p <= see) o[d][4 * j + e] += x;
+                }
+                __builtin_amdgcn_sched_barrier(0);       // (few registers: most tiles hold numbers alone)
+            }
+    }
     __syncthreads();
     for (int i = wave; i < PIECES; i += PA_WAVES) {
         u32x4* at = (u32x4*)(v + (i * 64 + lane) * 16);
-        if (bad(*at)) *at = u32x4{0u, 0u, 0u, 0u};
+        u32x4 x = *at;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) x[w] = parted<BF, true>(x[w]);
+        *at = x;
     }
     __syncthreads();
-    return m;
 }
 
 template <bool BF, int D, int ROT>
@@ -218,11 +255,11 @@ __device__ inline __attribute__((always_inline)) u32x4 key_part(const char* keys
 }
 
 // One tile by one wave, its scores in sc; NEXT: the scores of the tile behind it are made meanwhile.  edge: some row of the
-// workgroup does not see all of the tile; the lane's row sees positions up to see; bad: positions whose values are no numbers.
+// workgroup does not see all of the tile; the lane's row sees positions up to see.
 template <bool BF, int D, int ROT, bool NEXT, class Load>
 __device__ inline __attribute__((always_inline)) void attend_tile(char* __restrict k0, const char* __restrict keys,
                                                                   const char* __restrict values, char* __restrict v1, const Load& load, const u32x4* q, float scale2, bool edge,
-                                                                  int see, uint64_t bad, int lane, f32x16 (&sc)[PA_TILE<BF> / 32],
+                                                                  int see, int lane, f32x16 (&sc)[PA_TILE<BF> / 32],
                                                                   f32x16 (&nx)[PA_TILE<BF> / 32], State<BF, D, ROT>& s) {
     using Lay = Layout<BF, D, ROT>;
     constexpr int NB = Lay::TILE / 32, QN = Lay::QN, STEPS = NB * QN;
@@ -237,12 +274,6 @@ __device__ inline __attribute__((always_inline)) void attend_tile(char* __restri
                 const int p = 32 * tb + 8 * (i >> 2) + 4 * h + (i & 3);
                 sc[tb][i] = p <= see ? sc[tb][i] : ninf;
             }
-        // a weight of 0 would not keep what is no number out of a row's sums: it lies as 0 in LDS, and the rows that
-        // see it become NaN here
-        if (bad) {
-            const uint64_t seen = see < 0 ? 0ull : see >= 63 ? ~0ull : (2ull << see) - 1;
-            if (bad & seen) s.l = __builtin_nanf("");
-        }
     }
     float top = ninf;
 #pragma unroll
@@ -399,17 +430,16 @@ __global__ void __launch_bounds__(64 * PA_WAVES, 2) prompt_attention_kernel(cons
     auto step = [&](auto next, int t0, char* k0, char* k1, char* v0, char* v1, f32x16 (&sc)[TILE / 32],
                     f32x16 (&nx)[TILE / 32]) __attribute__((always_inline)) {
         const bool edge = t0 + TILE > all;
-        uint64_t bad = 0;
         int lane = lane_;
         asm volatile("" : "+v"(lane));                   // (addresses made anew for each tile: kept, they would take the sums' registers)
         wait_loads<0>();
         __syncthreads();
-        if (edge) bad = clean_values<BF, D>(v0, wave, lane);
+        if (edge) clean_values<BF, D>(v0, lim - t0, wave, lane, st.o);
         auto load = [&](char* k, char* v) __attribute__((always_inline)) {
             if (t0 + 2 * TILE < end) keys(t0 + 2 * TILE, k, lane);
             values(t0 + TILE, v, lane);
         };
-        attend_tile<BF, D, ROT, decltype(next)::value>(k0, k1, v0, v1, load, q, scale2, edge, lim - t0, bad, lane, sc, nx, st);
+        attend_tile<BF, D, ROT, decltype(next)::value>(k0, k1, v0, v1, load, q, scale2, edge, lim - t0, lane, sc, nx, st);
     };
     if (start < end) {
         char *const k0 = mem, *const k1 = mem + Lay::KEYS, *const v0 = mem + Lay::V, *const v1 = v0 + Lay::VALUES;

@@ -509,3 +509,23 @@ def test_evict_past_the_table_and_with_a_page_outside_the_cache():
     _evict(rng, [500, 100], [100, 100], 40, 0, 5, mass, pos)                       # more tokens than places
     _evict(rng, [96, 90], [100, 100], 40, 2, 5, mass, pos, bad_page=1)             # rows into it are dropped
     _evict(rng, [96, 90], [100, 100], 40, 2, 5, mass, pos, bad_page=4, in_place=True)   # rows from it are zeros
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("n,ctx,h,g,D,rot", [([150, 40], [10, 0], 2, 2, 64, 32), ([16, 5], [2500, 700], 8, 2, 128, 0), ([300], [0], 4, 1, 128, 64)])
+def test_a_value_that_is_no_number_reaches_its_own_element_alone(dtype, value, n, ctx, h, g, D, rot):
+    """Of the tokens that see it, in tiles that all of a workgroup's tokens see and in others; the sums of the weights stay."""
+    rng = np.random.default_rng(n[0] + D)
+    p = _prompt(rng, dtype, n, ctx, h, g, D, rot)
+    want = _run_prompt(p)
+    hit = {(c, g - 1, e) for c, e in ((0, 3), (ctx[0] // 2, 9), (ctx[0] + 2, 5), (ctx[0] + 7, 5), (ctx[0] + 7, 6), (ctx[0] + n[0] - 1, D - 1))}
+    for at, kh, e in hit:                                    # positions of the first sequence
+        p["v"][at, kh, e] = value
+    got = _run_prompt(p)
+    assert torch.equal(want[1], got[1])
+    spoilt = np.zeros(got[0].shape, bool)
+    for at, kh, e in hit:
+        spoilt[max(0, at - ctx[0]):n[0], kh * (h // g):(kh + 1) * (h // g), e] = True
+    np.testing.assert_array_equal(_host(want[0])[~spoilt], _host(got[0])[~spoilt])
+    assert not np.isfinite(_host(got[0])[spoilt]).any()
