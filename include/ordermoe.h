@@ -676,8 +676,11 @@ int ordermoe_latent_write(const ordermoe_latent_cache* C, const ordermoe_latent_
  * -infinity.  bf16: exact products and fp32 sums, the weights rounded to bf16 for the second
  * product where a sequence may have over ORDERMOE_LATENT_FINE_ROWS rows (max_q * n_q; in two parts, 16 bits
  * together, where not), its sums in two parts for the third, rounded once at the end.  fp32: fp32
- * throughout.  A row that a token does not see has no effect on it, whatever it holds; an infinity or a
- * NaN in one that it sees makes its outputs NaN, some of them or all.
+ * throughout.  A row that a token does not see has no effect on it, whatever it holds.  What is no number
+ * in q, or in the rotary part of a row that it sees, acts through the score: +infinity or NaN makes out, lse and
+ * the weights of this token and head NaN; -infinity is as a position that is not seen (where there is no
+ * other: out = 0, lse = -infinity).  What is no number in the latent part of such a row makes the token's out NaN
+ * (its lse and weights NaN, or what the scores give).
  *   q, q_start, ctx_len, page_table, tree, max_q, max_pages as there; q dev [T][n_q][rank + rotary_dim]
  *   out      dev [T][n_q][head_dim]; lse dev [T][n_q] fp32, or NULL
  *   mass     dev [B][mass_stride] fp32: the attention weight that each of the sequence's positions has
@@ -714,9 +717,10 @@ int ordermoe_latent_expand(const ordermoe_latent_cache* C, const ordermoe_latent
  * positions (the positions before are a context): token i sees position p if
  * p <= L_b - n_b + i.  Query head h reads key/value head g = h / (n_q / n_kv), and
  *   s_p = scale * (q_h . [k_p,g | r_p]),  out_h = sum_p exp(s_p) v_p,g / sum_p exp(s_p),  lse = log sum_p exp(s_p).
- * A token that sees nothing (L_b < n_b) gets out = 0 and lse = -infinity.  An infinity or a NaN in a value
- * that it sees makes this element of its outputs infinite or NaN, and nothing else; one in q or in a key that
- * it sees makes its outputs infinite or NaN, some of them or all.  bf16: exact
+ * A token that sees nothing (L_b < n_b) gets out = 0 and lse = -infinity.  What is no number in a value that it
+ * sees makes this element of its outputs infinite or NaN, and nothing else.  What is none in q, or in a key or
+ * shared part that it sees, acts through the score: +infinity or NaN makes out and lse of this token and head
+ * NaN; -infinity is as a position that is not seen.  (scale = 0: q counts as zeros.)  bf16: exact
  * products, fp32 sums and statistics, the weights rounded to bf16 for the second product, rounded once
  * at the end.  fp32: fp32 throughout.
  *   head_dim   64 or 128;  rotary_dim 0, 32 or 64

@@ -529,3 +529,102 @@ def test_a_value_that_is_no_number_reaches_its_own_element_alone(dtype, value, n
         spoilt[max(0, at - ctx[0]):n[0], kh * (h // g):(kh + 1) * (h // g), e] = True
     np.testing.assert_array_equal(_host(want[0])[~spoilt], _host(got[0])[~spoilt])
     assert not np.isfinite(_host(got[0])[spoilt]).any()
+
+
+# ------------------------------------------------------------------ keys that are no numbers
+def _by_scores(got, e, lse, score, width, L, rounding, dtype, extra=0.0):
+    """out [n, h, D] and lse [n, h] against the oracle's, where a score of +infinity or NaN makes a row NaN whole, and one of
+    -infinity is as a place that is not seen."""
+    out, ls = got
+    spoilt = ~np.isfinite(e["out"]).all(-1)
+    assert np.isnan(out[spoilt]).all() and np.isnan(ls[spoilt]).all()
+    es = score * (width + 4) * U
+    tol = (2 * es + (8 + L) * U + rounding) * e["size"] + extra + (2 * U + HALF[dtype]) * np.abs(e["out"])
+    _within(out[~spoilt], e["out"][~spoilt], tol[~spoilt], "out")
+    fine = ~spoilt & np.isfinite(lse)
+    _within(ls[fine], lse[fine], es + (8 + L) * U + 2 * U * np.abs(lse[fine]), "lse")
+    nothing = ~spoilt & np.isneginf(lse)
+    assert np.isneginf(ls[nothing]).all() and (out[nothing] == 0).all()
+    return spoilt, nothing
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("n,ctx,h,g,D,rot,scale", [(150, 10, 2, 2, 64, 32, 0.1), (16, 2500, 8, 2, 128, 0, -0.08), (300, 0, 4, 1, 128, 64, 0.07)])
+def test_a_key_that_is_no_number_acts_through_its_score(dtype, value, n, ctx, h, g, D, rot, scale):
+    rng = np.random.default_rng(n + D)
+    p = _prompt(rng, dtype, [n], [ctx], h, g, D, rot, scale)
+    clean = ol.prompt_attention(*(None if p[c] is None else _host(p[c])[:k] for c, k in (("q", n), ("k", n + ctx), ("v", n + ctx), ("r", n + ctx))),
+                                scale)
+    # seen by the first token alone of all that it sees (or of a few), in tiles that all rows see, and late
+    for what, at in [("k", 0), ("k", ctx + 3), ("k", ctx + n - 2)] + ([("r", 0), ("r", ctx + 7)] if rot else []):
+        t = p[what]
+        keep = t[at].clone()
+        if what == "k":
+            t[at, g - 1, 5] = value
+        else:
+            t[at, 6] = value
+        q, k, v, r = (None if p[c] is None else _host(p[c]) for c in "qkvr")
+        L = n + ctx
+        with np.errstate(invalid="ignore"):
+            e = ol.prompt_attention(q[:n], k[:L], v[:L], None if r is None else r[:L], scale)
+        got = _run_prompt(p)
+        spoilt, _ = _by_scores((_host(got[0])[:n], _host(got[1])[:n]), e, e["lse"], clean["score"], D + rot, L,
+                               2.0 ** -8 if dtype == "bf16" else 0.0, dtype)
+        sees = np.arange(n)[:, None] + ctx >= at
+        x = q[:n, :, 5] if what == "k" else q[:n, :, D + 6]
+        reads = np.arange(h)[None, :] >= (h - h // g if what == "k" else 0)
+        want = sees & reads & (np.ones_like(x, bool) if np.isnan(value) else x * scale * value > 0)
+        np.testing.assert_array_equal(spoilt, want)
+        t[at] = keep
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("h,n", [(2, 1), (3, 6), (8, 4), (10, 6)])
+def test_a_cached_row_that_is_no_number(dtype, value, h, n):
+    """In its rotary part it acts through its score; in its latent part, which is the value too, it spoils the tokens that see it."""
+    rng = np.random.default_rng(h + n)
+    D, R, rot, ctx = 64, 128, 32, 130
+    ba = _Batch(rng, dtype, [ctx], [n], h, D, R, rot, 16)
+    words = [(2 << i) - 1 for i in range(n)]
+    seen = ol.tree_seen(n, ctx, words, ctx + n)
+    clean = ol.latent_attention(_host(ba.q)[:n], ba.cached(0, ctx + n), seen, _host(ba.wv), ba.scale)
+    for at in (3, ctx - 1, ctx + n - 1):                     # in a tile that all see; beside places that some do not
+        slot = ba.rows[int(ba.table[0, at // 16]), at % 16]
+        keep = slot.clone()
+        slot[R + 5] = value
+        with np.errstate(invalid="ignore"):
+            e = ol.latent_attention(_host(ba.q)[:n], ba.cached(0, ctx + n), seen, _host(ba.wv), ba.scale)
+        out, lse, mass = ba.run(n, stride=ctx + n)
+        rounding = 0.0 if dtype == "f32" else 2.0 ** -16 if n * h <= 32 else 2.0 ** -8
+        spoilt, _ = _by_scores((_host(out)[:n], _host(lse)[:n]), e, e["lse"], clean["score"], R + rot, ctx + n, rounding, dtype,
+                               (2.0 ** -16 + (R + 1) * U) * e["through"])
+        x = _host(ba.q)[:n, :, R + 5]
+        np.testing.assert_array_equal(spoilt, seen[:, None, at] & (np.ones_like(x, bool) if np.isnan(value) else x * value > 0))
+        if not spoilt.any():
+            assert torch.isfinite(mass).all() and float(mass[0, at]) == 0
+        slot.copy_(keep)
+        slot[7] = value
+        out, _, _ = ba.run(n, stride=ctx + n)
+        np.testing.assert_array_equal(np.isnan(_host(out)[:n]).all((1, 2)), seen[:, at])
+        assert np.isfinite(_host(out)[:n][~seen[:, at]]).all()
+        slot.copy_(keep)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_tokens_whose_every_score_is_minus_infinity(dtype):
+    """As tokens that see nothing."""
+    rng = np.random.default_rng(14)
+    p = _prompt(rng, dtype, [3, 70], [0, 0], 2, 2, 64, 0)
+    p["q"] = p["q"].abs()
+    p["k"][0, 1, 9] = -float("inf")                          # the only position of the first token
+    p["k"][3:73, 0, 9] = -float("inf")
+    out, lse = _run_prompt(p)
+    assert (out[0, 1] == 0).all() and torch.isneginf(lse[0, 1]) and torch.isfinite(lse[0, 0]) and torch.isfinite(lse[1:3]).all()
+    assert (out[3:73, 0] == 0).all() and torch.isneginf(lse[3:73, 0]).all() and torch.isfinite(lse[3:73, 1]).all()
+    ba = _Batch(rng, dtype, [0, 40], [1, 2], 3, 64, 128, 32, 16)
+    ba.q.abs_()
+    ba.rows[int(ba.table[0, 0]), 0, 128] = -float("inf")
+    out, lse, mass = ba.run(2, stride=50)
+    assert (out[0] == 0).all() and torch.isneginf(lse[0]).all() and torch.isfinite(lse[1:3]).all() and float(mass[0, 0]) == 0
