@@ -693,7 +693,8 @@ int ordermoe_latent_write(const ordermoe_latent_cache* C, const ordermoe_latent_
  *            are.  May be mass itself.
  *   ws       dev, of the size below (weighs: 1 where mass_out will be given), in use until the stream
  *            passes the call.  With weighs it holds the scores, 4 B max_q n_q max_pages page_size bytes of it.
- * Limits as there, but n_q <= 128; 0 <= T * n_q < 2^31; decay finite. */
+ * Limits as there, but n_q <= 128; 0 <= T * n_q < 2^31; decay finite.  The size does not fall where B, max_q, max_pages
+ * or weighs grow: one workspace of a server's largest call serves its smaller ones. */
 #define ORDERMOE_LATENT_FINE_ROWS 32
 size_t ordermoe_latent_attention_workspace_size(const ordermoe_latent_cache* C, const ordermoe_latent_heads* H, int32_t B,
                                                 int32_t max_q, int32_t max_pages, int32_t weighs);
@@ -734,7 +735,8 @@ int ordermoe_latent_expand(const ordermoe_latent_cache* C, const ordermoe_latent
  *   ws         dev, of the size below: partial results of rows whose positions are split over workgroups
  *              (joined in a fixed order); in use until the stream passes the call
  * 1 <= n_kv, n_q <= 1024 a multiple of n_kv, 0 <= B <= 65535, 0 <= T with T * n_q < 2^31,
- * 0 <= L <= 2^31 - 128, scale finite. */
+ * 0 <= L <= 2^31 - 128, scale finite.  The size does not fall where T or B grow (34 MB at most): one
+ * workspace of a server's largest call serves its smaller ones. */
 size_t ordermoe_prompt_attention_workspace_size(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t head_dim,
                                                 int32_t rotary_dim, int64_t T, int32_t B);
 int ordermoe_prompt_attention(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t rotary_dim, const void* q,
@@ -761,7 +763,8 @@ int ordermoe_prompt_attention(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t 
  *             they are.  len_out, mass_out and pos_out may be ctx_len, mass and pos themselves.
  *   ws        dev, of the size below, in use until the stream passes the call
  * keep >= 1, first, recent >= 0 with first + recent <= keep, stride >= 1, 0 <= B <= 65535,
- * B * stride, B * keep < 2^40, max_pages as in ordermoe_latent_attention. */
+ * B * stride, B * keep < 2^40, max_pages as in ordermoe_latent_attention.  The size does not fall where B, max_pages or
+ * keep grow: one workspace of a server's largest call serves its smaller ones. */
 size_t ordermoe_latent_evict_workspace_size(const ordermoe_latent_cache* C, int32_t B, int32_t max_pages, int32_t keep);
 int ordermoe_latent_evict(const ordermoe_latent_cache* C, int32_t B, const int32_t* ctx_len, const int32_t* seq_len,
                           const int32_t* page_table, int32_t max_pages, int32_t keep, int32_t first, int32_t recent,

@@ -304,8 +304,8 @@ struct LatentAttentionArgs {
     float* stat;           // [B][max_q n_q][2] maximum of each row, and 1 / its sum (with mass_out)
     float* score;          // [B][max_q n_q][max_pages page_size] scores in units of log 2 (with mass_out)
 };
-// work items (sequence, piece of its cache) that a batch has at most
-int64_t latent_items(int dtype, int n_q, int B, int max_q);
+// work items (sequence, piece of its cache) that a batch has at most, with tables of cap places
+int64_t latent_items(int dtype, int n_q, int B, int max_q, int64_t cap);
 int launch_latent_attention(const LatentAttentionArgs& a, void* stream);
 struct EvictArgs {
     LatentArgs cache;
@@ -351,8 +351,9 @@ struct PromptArgs {
     float* part_ml;        // [pieces][T][n_q][2] maximum and sum of each piece of a row's positions
     float* part_o;         // [pieces][T][n_q][head_dim] its sums
 };
-// pieces into which a batch's positions are split, at most
+// pieces into which a batch's positions are split, at most; rows of all pieces in any batch of up to T tokens
 int prompt_pieces(int n_q, int n_kv, int64_t T, int B);
+int64_t prompt_rows_at_most(int n_q, int n_kv, int64_t T);
 int launch_prompt_attention(const PromptArgs& a, void* stream);
 
 int launch_pack_gate_up(int dtype, int n, int f, int d, const void* g, const void* u, void* out,

@@ -57,21 +57,27 @@ int check_attention(const ordermoe_latent_cache* C, const ordermoe_latent_heads*
         return fail(ORDERMOE_EINVAL, who + ": max_q must lie in [1, " + std::to_string(ORDERMOE_MAX_DRAFT) + "]");
     return ORDERMOE_OK;
 }
+// Each workspace is carved by the call's own sizes; its size function asks for the most that a call of the same or of smaller
+// sizes carves, so that one buffer serves them all.
+int64_t attention_rows(const ordermoe_latent_cache* C, const ordermoe_latent_heads* H, int32_t B, int32_t max_q, int32_t max_pages) {
+    return latent_items(C->dtype, H->n_q, B, max_q, (int64_t)max_pages * C->page_size) * max_q * H->n_q;
+}
 size_t attention_ws(const ordermoe_latent_cache* C, const ordermoe_latent_heads* H, int32_t B, int32_t max_q, int32_t max_pages,
-                    bool weighs, Carver& c, LatentAttentionArgs* a) {
-    const int64_t items = latent_items(C->dtype, H->n_q, B, max_q);
-    const size_t rows = (size_t)max_q * H->n_q, parts = (size_t)items * rows;
+                    int64_t parts, bool weighs, Carver& c, LatentAttentionArgs* a) {
+    const size_t rows = (size_t)max_q * H->n_q;
     int32_t* pl = c.take<int32_t>((size_t)std::max(B, 1) * 2);
-    float* ml = c.take<float>(parts * 2);
-    float* po = c.take<float>(parts * C->rank);
+    float* ml = c.take<float>((size_t)parts * 2);
+    float* po = c.take<float>((size_t)parts * C->rank);
     float* st = c.take<float>(weighs ? B * rows * 2 : 0);
     float* sc = c.take<float>(weighs ? B * rows * max_pages * C->page_size : 0);
-    if (a) { a->items = items; a->plan = pl; a->part_ml = ml; a->part_o = po; a->stat = st; a->score = sc; }
+    if (a) { a->items = parts / (int64_t)rows; a->plan = pl; a->part_ml = ml; a->part_o = po; a->stat = st; a->score = sc; }
     return c.size();
 }
 
-size_t evict_ws(const ordermoe_latent_cache* C, int32_t B, int32_t max_pages, int32_t keep, Carver& c, EvictArgs* a) {
-    const int64_t cap = (int64_t)max_pages * C->page_size, most = std::max<int64_t>(0, std::min<int64_t>(keep, cap - keep));
+// rows of a sequence that move at most, out of the places past the budget into those before it
+int64_t evict_moves(int64_t cap, int32_t keep) { return std::max<int64_t>(0, std::min<int64_t>(keep, cap - keep)); }
+size_t evict_ws(const ordermoe_latent_cache* C, int32_t B, int32_t max_pages, int64_t most, Carver& c, EvictArgs* a) {
+    const int64_t cap = (int64_t)max_pages * C->page_size;
     int32_t* m = c.take<int32_t>((size_t)std::max(B, 1));
     int32_t* h = c.take<int32_t>((size_t)B * most);
     int32_t* f = c.take<int32_t>((size_t)B * most);
@@ -95,10 +101,9 @@ int check_prompt(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t head_dim, int
     if (T < 0 || T > (INT_LIMIT - 1) / n_q) return bad(who, "T * n_q must lie in [0, 2^31)");
     return ORDERMOE_OK;
 }
-size_t prompt_ws(int32_t n_q, int32_t n_kv, int32_t head_dim, int64_t T, int32_t B, Carver& c, PromptArgs* a) {
-    const size_t pieces = prompt_pieces(n_q, n_kv, T, B), rows = pieces > 1 ? pieces * T * n_q : 0;
-    float* ml = c.take<float>(rows * 2);
-    float* po = c.take<float>(rows * head_dim);
+size_t prompt_ws(int32_t head_dim, int64_t rows, Carver& c, PromptArgs* a) {
+    float* ml = c.take<float>((size_t)rows * 2);
+    float* po = c.take<float>((size_t)rows * head_dim);
     if (a) { a->part_ml = ml; a->part_o = po; }
     return c.size();
 }
@@ -141,8 +146,10 @@ extern "C" int ordermoe_latent_write(const ordermoe_latent_cache* C, const order
 extern "C" size_t ordermoe_latent_attention_workspace_size(const ordermoe_latent_cache* C, const ordermoe_latent_heads* H, int32_t B,
                                                            int32_t max_q, int32_t max_pages, int32_t weighs) {
     if (check_attention(C, H, B, max_q, max_pages, "latent_attention") != ORDERMOE_OK) return 0;
+    int64_t parts = 0;
+    for (int32_t q = 1; q <= max_q; ++q) parts = std::max(parts, attention_rows(C, H, B, q, max_pages));
     Carver c(nullptr);
-    return attention_ws(C, H, B, max_q, max_pages, weighs != 0, c, nullptr);
+    return attention_ws(C, H, B, max_q, max_pages, parts, weighs != 0, c, nullptr);
 }
 
 extern "C" int ordermoe_latent_attention(const ordermoe_latent_cache* C, const ordermoe_latent_heads* H, const void* q, int64_t T,
@@ -159,7 +166,9 @@ extern "C" int ordermoe_latent_attention(const ordermoe_latent_cache* C, const o
         return bad(who, "null pointer, or q or out not 16-byte aligned");
     if (mass_out ? mass_stride < 1 || (B > 0 && mass_stride > ((int64_t)1 << 40) / B) : mass != nullptr)
         return bad(who, "mass_stride must lie in [1, 2^40 / B] where mass_out is given; mass needs mass_out");
-    const size_t need = ordermoe_latent_attention_workspace_size(C, H, B, max_q, max_pages, mass_out != nullptr);
+    const int64_t parts = attention_rows(C, H, B, max_q, max_pages);
+    Carver sized(nullptr);
+    const size_t need = attention_ws(C, H, B, max_q, max_pages, parts, mass_out != nullptr, sized, nullptr);
     if (!ws || ws_bytes < need) return fail(ORDERMOE_EWORKSPACE, std::string(who) + ": workspace needs " + std::to_string(need) + " bytes");
     LatentAttentionArgs a{};
     a.cache = cache_args(C);
@@ -167,7 +176,7 @@ extern "C" int ordermoe_latent_attention(const ordermoe_latent_cache* C, const o
     a.q = q; a.w_v = H->w_v; a.q_start = q_start; a.ctx_len = ctx_len; a.page_table = page_table; a.tree = tree;
     a.scale = scale; a.decay = decay; a.out = out; a.lse = lse; a.mass = mass; a.mass_out = mass_out; a.mass_stride = mass_stride;
     Carver c(ws);
-    attention_ws(C, H, B, max_q, max_pages, mass_out != nullptr, c, &a);
+    attention_ws(C, H, B, max_q, max_pages, parts, mass_out != nullptr, c, &a);
     const int e = launch_latent_attention(a, stream);
     if (e) return hip_fail(e, "latent_attention launch");
     clear_error();
@@ -196,7 +205,7 @@ extern "C" size_t ordermoe_prompt_attention_workspace_size(int32_t dtype, int32_
                                                            int32_t rotary_dim, int64_t T, int32_t B) {
     if (check_prompt(dtype, n_q, n_kv, head_dim, rotary_dim, T, B, "prompt_attention") != ORDERMOE_OK) return 0;
     Carver c(nullptr);
-    return prompt_ws(n_q, n_kv, head_dim, T, B, c, nullptr);
+    return prompt_ws(head_dim, prompt_rows_at_most(n_q, n_kv, T), c, nullptr);
 }
 
 extern "C" int ordermoe_prompt_attention(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t rotary_dim, const void* q,
@@ -212,7 +221,9 @@ extern "C" int ordermoe_prompt_attention(int32_t dtype, int32_t n_q, int32_t n_k
     if (T > 0 && B > 0 && (!good16(q) || !q_start || !kv_start || !good16(out) ||
                            (L > 0 && (!good16(k) || !good16(v) || (rotary_dim > 0 && !good16(r))))))
         return bad(who, "null pointer, or q, k, r, v or out not 16-byte aligned");
-    const size_t need = ordermoe_prompt_attention_workspace_size(dtype, n_q, n_kv, head_dim, rotary_dim, T, B);
+    const int64_t pieces = prompt_pieces(n_q, n_kv, T, B), rows = pieces > 1 ? pieces * T * n_q : 0;
+    Carver sized(nullptr);
+    const size_t need = prompt_ws(head_dim, rows, sized, nullptr);
     if (need > 0 && (!ws || ws_bytes < need))
         return fail(ORDERMOE_EWORKSPACE, std::string(who) + ": workspace needs " + std::to_string(need) + " bytes");
     PromptArgs a{};
@@ -220,7 +231,7 @@ extern "C" int ordermoe_prompt_attention(int32_t dtype, int32_t n_q, int32_t n_k
     a.q = q; a.k = k; a.r = r; a.v = v; a.T = T; a.L = L; a.q_start = q_start; a.kv_start = kv_start;
     a.scale = scale; a.out = out; a.lse = lse;
     Carver c(ws);
-    prompt_ws(n_q, n_kv, head_dim, T, B, c, &a);
+    prompt_ws(head_dim, rows, c, &a);
     const int e = launch_prompt_attention(a, stream);
     if (e) return hip_fail(e, "prompt_attention launch");
     clear_error();
@@ -231,8 +242,9 @@ extern "C" size_t ordermoe_latent_evict_workspace_size(const ordermoe_latent_cac
     const char* who = "latent_evict";
     if (check_cache(C, who) != ORDERMOE_OK || check_table(C, B, max_pages, who) != ORDERMOE_OK) return 0;
     if (keep < 1) { bad(who, "keep must be at least 1"); return 0; }
+    const int64_t cap = (int64_t)max_pages * C->page_size;
     Carver c(nullptr);
-    return evict_ws(C, B, max_pages, keep, c, nullptr);
+    return evict_ws(C, B, max_pages, std::min<int64_t>(keep, cap / 2), c, nullptr);      // (the most moves of any budget up to keep)
 }
 
 extern "C" int ordermoe_latent_evict(const ordermoe_latent_cache* C, int32_t B, const int32_t* ctx_len, const int32_t* seq_len,
@@ -248,7 +260,9 @@ extern "C" int ordermoe_latent_evict(const ordermoe_latent_cache* C, int32_t B, 
         return bad(who, "stride must be at least 1, B * stride and B * keep at most 2^40");
     if (B > 0 && (!ctx_len || !seq_len || !page_table || !mass || !pos || !kept || !len_out || !mass_out || !pos_out))
         return bad(who, "null pointer");
-    const size_t need = ordermoe_latent_evict_workspace_size(C, B, max_pages, keep);
+    const int64_t most = evict_moves((int64_t)max_pages * C->page_size, keep);
+    Carver sized(nullptr);
+    const size_t need = evict_ws(C, B, max_pages, most, sized, nullptr);
     if (!ws || ws_bytes < need) return fail(ORDERMOE_EWORKSPACE, std::string(who) + ": workspace needs " + std::to_string(need) + " bytes");
     EvictArgs a{};
     a.cache = cache_args(C);
@@ -256,7 +270,7 @@ extern "C" int ordermoe_latent_evict(const ordermoe_latent_cache* C, int32_t B, 
     a.ctx_len = ctx_len; a.seq_len = seq_len; a.page_table = page_table; a.mass = mass; a.pos = pos; a.stride = stride;
     a.kept = kept; a.len_out = len_out; a.mass_out = mass_out; a.pos_out = pos_out;
     Carver c(ws);
-    evict_ws(C, B, max_pages, keep, c, &a);
+    evict_ws(C, B, max_pages, most, c, &a);
     const int e = launch_latent_evict(a, stream);
     if (e) return hip_fail(e, "latent_evict launch");
     clear_error();

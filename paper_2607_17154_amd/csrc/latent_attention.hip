@@ -946,7 +946,7 @@ int launch_rows(const LatentAttentionArgs& a, hipStream_t st) {
     const int rb = row_blocks(a.max_q * a.n_q, MT);
     const int64_t cap = (int64_t)a.max_pages << a.cache.page_shift;
     {
-        const int64_t items = std::min<int64_t>(a.items, a.B * ((cap + LA_MIN_PIECE / 2 - 1) / (LA_MIN_PIECE / 2)));
+        const int64_t items = a.items;
         const dim3 grid = grid_of((items + 7) / 8 * 8 * rb), block((64 * Config<BF, R, ROT, MT>::NW));
         KernelTimer kt_("latent_attention", st);
         if constexpr (MT == 8) {
@@ -1011,9 +1011,10 @@ int launch_rank(const LatentAttentionArgs& a, hipStream_t st) {
 
 }  // namespace
 
-int64_t latent_items(int dtype, int n_q, int B, int max_q) {
+int64_t latent_items(int dtype, int n_q, int B, int max_q, int64_t cap) {
     const int rows = max_q * n_q, rb = row_blocks(rows, row_tiles(dtype, rows));
-    return (2 * LA_TARGET + rb - 1) / rb + B;
+    constexpr int LEAST = LA_MIN_PIECE / 2;
+    return std::min<int64_t>((2 * LA_TARGET + rb - 1) / rb + B, B * ((cap + LEAST - 1) / LEAST));
 }
 
 int launch_latent_attention(const LatentAttentionArgs& a, void* stream) {

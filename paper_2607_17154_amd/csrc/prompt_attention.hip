@@ -574,7 +574,12 @@ int launch_rot(const PromptArgs& a, hipStream_t st) {
 
 int prompt_pieces(int n_q, int n_kv, int64_t T, int B) {
     const int64_t blocks = blocks_at_most(n_q, n_kv, T, B) * n_kv;
-    return blocks == 0 || blocks > PA_FEW ? 1 : (int)(PA_FILL / blocks);
+    return B == 0 || blocks == 0 || blocks > PA_FEW ? 1 : (int)(PA_FILL / blocks);
+}
+
+// `pieces` workgroups of a block hold PA_ROWS rows each, or what few tokens have, and there are PA_FILL of them at most
+int64_t prompt_rows_at_most(int n_q, int n_kv, int64_t T) {
+    return n_kv > PA_FEW ? 0 : std::min<int64_t>(PA_ROWS, T * (n_q / n_kv)) * PA_FILL;
 }
 
 int launch_prompt_attention(const PromptArgs& a, void* stream) {

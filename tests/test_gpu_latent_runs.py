@@ -441,3 +441,48 @@ def test_a_budget_of_the_largest_number(places):
     om.ordermoe_latent_evict(s.cache, s.ctx, s.ctx.clone(), s.d_table, keep, 5, keep - 5, s.mass, s.pos, kept, s.ctx, s.mass, s.pos, ws)
     assert int(s.ctx) == n and torch.equal(s.rows, rows) and torch.equal(s.mass, mass)
     assert torch.equal(kept[0, :n], torch.arange(n, dtype=torch.int32, device="cuda")) and bool((kept[0, n:] == -1).all())
+
+
+def _guarded(size):
+    """A workspace of this size, and the bytes behind it, which no call may touch."""
+    both = torch.full((size + 4096,), 0x7F, dtype=torch.uint8, device="cuda")
+    return both[:size], both[size:]
+
+
+def test_one_workspace_serves_smaller_calls():
+    rng = np.random.default_rng(15)
+    ba = _Batch(rng, "bf16", [3000, 40, 900, 7], [20, 1, 9, 17], 16, 64, 256, 32, 16)
+    ws, behind = _guarded(om.ordermoe_latent_attention_workspace_size(ba.cache, ba.heads, 4, 20, ba.table.shape[1], 1))
+    for max_q in (20, 17, 16, 9, 8, 3, 2, 1):
+        ws.fill_(0x7F)
+        got = ba.run(max_q, stride=3100, ws=ws)
+        ba.check(got, max_q)
+        for x, y in zip(got, ba.run(max_q, stride=3100)):
+            assert torch.equal(x, y)
+        ba.run(max_q, ws=ws)
+    assert (behind == 0x7F).all()
+    h, g, D = 8, 2, 128
+    ws, behind = _guarded(om.ordermoe_prompt_attention_workspace_size(om.BF16, h, g, D, 0, 2002, 5))
+    for n, ctx in (([2000], [0]), ([600], [100]), ([300, 7], [900, 4000]), ([127], [3000]), ([16, 16, 1], [2500, 1, 700]), ([33], [9000]), ([1], [5000])):
+        p = _prompt(rng, "bf16", n, ctx, h, g, D, 0)
+        want = _run_prompt(p)
+        out, lse = torch.full_like(want[0], 7.0), torch.full_like(want[1], 7.0)
+        ws.fill_(0x7F)
+        om.ordermoe_prompt_attention(p["q"], p["k"], p["v"], _dev(p["qs"]), _dev(p["ks"]), p["scale"], out, ws, lse=lse)
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    assert (behind == 0x7F).all()
+    s = _Server(16, "bf16", B=5, places=9600, keep=1)
+    ws, behind = _guarded(om.ordermoe_latent_evict_workspace_size(s.cache, 5, s.pages, 9000))
+    for keep in (9000, 5000, 4800, 100):
+        n = np.array([9600, 4801, keep, 7000, 9599])
+        s.ctx.copy_(_dev(n.astype(np.int32)))
+        mass = s.rng.random((5, 9600)).astype(np.float32)
+        s.mass.copy_(_dev(mass))
+        pos = np.tile(np.arange(9600, dtype=np.int32), (5, 1))
+        s.pos.copy_(_dev(pos))
+        kept = torch.full((5, keep), 99, dtype=torch.int32, device="cuda")
+        ws.fill_(0x7F)
+        om.ordermoe_latent_evict(s.cache, s.ctx, _dev(n.astype(np.int32)), s.d_table, keep, 2, 8, s.mass, s.pos, kept, s.ctx, s.mass, s.pos, ws)
+        for b in range(5):
+            np.testing.assert_array_equal(_host(kept)[b], ol.evict(int(n[b]), int(n[b]), keep, 2, 8, mass[b], pos[b]))
+    assert (behind == 0x7F).all()

@@ -175,3 +175,39 @@ def test_positions_up_to_two_tiles_below_32_bits(L):
     """The loop over tiles looks two of them ahead in 32 bits: so many positions have no room for that."""
     assert _prompt(L=L) == om.EINVAL and "prompt_attention" in om.last_error()
     assert _prompt(L=L, T=0, q=0) == om.EINVAL
+
+
+def _grows(size, grid):
+    """size over a grid of arguments: as large as at any arguments of which none is larger."""
+    s = np.array([[[size(x, y, z) for z in grid[2]] for y in grid[1]] for x in grid[0]], np.int64)
+    assert (s > 0).any()
+    for axis in range(3):
+        assert (np.diff(s, axis=axis) >= 0).all(), axis
+
+
+@pytest.mark.parametrize("dtype", [om.BF16, om.F32])
+@pytest.mark.parametrize("n_q,rank", [(1, 128), (3, 512), (16, 512), (40, 256), (128, 128)])
+@pytest.mark.parametrize("weighs", [0, 1])
+def test_attention_s_workspace_serves_every_smaller_call(dtype, n_q, rank, weighs):
+    c, h = _cache(dtype=dtype, rank=rank, page_size=64), _heads(n_q=n_q)
+    f = om.lib().ordermoe_latent_attention_workspace_size
+    _grows(lambda B, n, pages: f(ref(c), ref(h), B, n, pages, weighs),
+           ([1, 2, 3, 17, 64, 1000], list(range(1, 65)), [1, 2, 7, 40, 100, 3000, 1 << 20]))
+    assert f(ref(c), ref(h), 5, 9, 100, 1) >= f(ref(c), ref(h), 5, 9, 100, 0)
+
+
+@pytest.mark.parametrize("n_q,n_kv,D", [(1, 1, 128), (32, 8, 128), (16, 16, 64), (128, 1, 64), (128, 128, 128), (160, 160, 64), (1024, 16, 64)])
+def test_prompts_workspace_serves_every_smaller_call(n_q, n_kv, D):
+    f = om.lib().ordermoe_prompt_attention_workspace_size
+    T = sorted({1, 2, 3, 5, 16, 31, 32, 33, 64, 100, 127, 128, 129, 130, 250, 257, 300, 512, 600, 1000, 2049, 4000, 8000, 100000})
+    s = np.array([[f(om.BF16, n_q, n_kv, D, 0, t, B) for B in (1, 2, 3, 16, 100, 65535)] for t in [0] + T], np.int64)
+    assert (np.diff(s, axis=0) >= 0).all() and (np.diff(s, axis=1) >= 0).all()
+    assert s.max() <= 512 * 128 * (D + 2) * 4 + 512          # what 512 workgroups' rows take
+
+
+def test_eviction_s_workspace_serves_every_smaller_call():
+    c = _cache(page_size=64)
+    f = om.lib().ordermoe_latent_evict_workspace_size
+    _grows(lambda B, pages, keep: f(ref(c), B, pages, keep),
+           ([1, 2, 9, 500], [1, 2, 50, 100, 127, 128, 129, 200, 5000],
+            [1, 10, 64, 127, 129, 1000, 3199, 3200, 3201, 4000, 6000, 6399, 6400, 9000, 1 << 20, (1 << 31) - 1]))
