@@ -378,7 +378,7 @@ __global__ void __launch_bounds__(256) latent_expand_kernel(const LatentExpandAr
 // lines to memory.  30001 tokens x 32 heads of 128, rank 512: 383 us in tiles of 128, 294 to 327 on different cards (770 to
 // 857 TFLOP/s); the matrix unit is busy 39% of the time, LDS 36%, each waiting for the other at a slab's end.
 constexpr int LX_TOK = 256, LX_W = 128, LX_SLAB = 64, LX_STAGE = (LX_TOK + LX_W) * LX_SLAB, LX_OUT = 16 * 128;
-constexpr int LX_CHUNK = 4;                          // weight tiles of a workgroup, at most (one 332 us, two 327, four 324, eight 338)
+constexpr int LX_CHUNK = 4;                          // weight tiles of a workgroup, at most (one 332 us, two 322, four 319, eight 332)
 
 // (The loads' buffer and the one that is read never overlap: told so, the compiler does not wait for the loads first.)
 template <class Issue>

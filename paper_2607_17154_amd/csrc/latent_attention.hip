@@ -24,7 +24,7 @@
 // lane (c, g)) are the inner indexes of its second product when C^T's lanes hold the same tokens, so they never leave their
 // registers: one barrier a tile.  It reads each row in LDS eight times for 128 query rows, which bounds it (128 bytes a
 // cycle); blocks of 64 rows in the first way read it less than half as often but waited for each other: trees of 64 over
-// 30000-100000 tokens 993 us for 482.
+// 30000-100000 tokens 993 us for 513, before loads were told apart from reads (482).
 // Rows go straight from memory into LDS, the next tile while one is attended to.  64 sequences of 200 to 8000 tokens, one token
 // of 32 heads, rank 512: 67 us, 4.6 TB/s, by the rows on their way; trees of 64 482 (790 TFLOP/s).
 #include <hip/hip_runtime.h>
@@ -45,7 +45,7 @@ constexpr int LA_TARGET = 512;                       // workgroups that a large 
 // shortens (200 tokens 12.6 -> 11.6 us, two fp32 sequences of 800 22.4 -> 18.2; 4 of 1000 15.5 -> 17.1, 16 of 300 16.5 -> 19.3)
 constexpr int LA_MIN_PIECE = 64, LA_SHORT = 1024;
 constexpr int LA_FEW = 32;                           // query rows up to which latent_attention_kernel takes a batch
-constexpr int LO_PIECES = 32;                        // pieces of a sequence past which 16 sets of lanes add them
+constexpr int LO_PIECES = 32;                        // pieces of a sequence, as expected, past which 16 sets of lanes add them
 constexpr int LO_GROUPS = 256;                       // workgroups of the last product wished for
 constexpr float LA_LAG = 8.0f;                       // see latent_attention_kernel
 
@@ -959,7 +959,8 @@ int launch_rows(const LatentAttentionArgs& a, hipStream_t st) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return (int)e;
     }
-    // pieces that a sequence may have
+    // About how many pieces a sequence has where they are of like length.  (One long sequence among many short ones has more,
+    // up to 2 LA_TARGET / rb, and fewer sets to add them than it could use.)
     const bool many = std::min<int64_t>((cap + LA_MIN_PIECE - 1) / LA_MIN_PIECE, LA_TARGET / ((int64_t)a.B * rb) + 1) > LO_PIECES;
     {
         KernelTimer kt_("latent_out", st);

@@ -486,3 +486,18 @@ def test_one_workspace_serves_smaller_calls():
         for b in range(5):
             np.testing.assert_array_equal(_host(kept)[b], ol.evict(int(n[b]), int(n[b]), keep, 2, 8, mass[b], pos[b]))
     assert (behind == 0x7F).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,h,max_q", [(20, 8, 1), (64, 8, 1), (17, 32, 3)])
+def test_one_long_sequence_among_short_ones(dtype, B, h, max_q):
+    """Its pieces are far more than a sequence of the batch has on average."""
+    rng = np.random.default_rng(B)
+    ctx, n = rng.integers(0, 11, B), rng.integers(1, max_q + 1, B)
+    ctx[B // 2], n[B // 2] = 30011, max_q
+    ba = _Batch(rng, dtype, ctx, n, h, 64, 128, 32, 64)
+    first = ba.run(max_q, stride=100)
+    ba.check(first, max_q)
+    for _ in range(2):
+        for x, y in zip(first, ba.run(max_q, stride=100)):
+            assert torch.equal(x, y)
