@@ -693,7 +693,7 @@ int ordermoe_latent_write(const ordermoe_latent_cache* C, const ordermoe_latent_
  *            are.  May be mass itself.
  *   ws       dev, of the size below (weighs: 1 where mass_out will be given), in use until the stream
  *            passes the call.  With weighs it holds the scores, 4 B max_q n_q max_pages page_size bytes of it.
- * Limits as there, but n_q <= 128; 0 <= T * n_q < 2^31; decay finite.  The size does not fall where B, max_q, max_pages
+ * Limits as there, but n_q <= 128, |scale| <= 2^127; 0 <= T * n_q < 2^31; decay finite.  The size does not fall where B, max_q, max_pages
  * or weighs grow: one workspace of a server's largest call serves its smaller ones. */
 #define ORDERMOE_LATENT_FINE_ROWS 32
 size_t ordermoe_latent_attention_workspace_size(const ordermoe_latent_cache* C, const ordermoe_latent_heads* H, int32_t B,
@@ -735,7 +735,7 @@ int ordermoe_latent_expand(const ordermoe_latent_cache* C, const ordermoe_latent
  *   ws         dev, of the size below: partial results of rows whose positions are split over workgroups
  *              (joined in a fixed order); in use until the stream passes the call
  * 1 <= n_kv, n_q <= 1024 a multiple of n_kv, 0 <= B <= 65535, 0 <= T with T * n_q < 2^31,
- * 0 <= L <= 2^31 - 128, scale finite.  The size does not fall where T or B grow (34 MB at most): one
+ * 0 <= L <= 2^31 - 128, |scale| <= 2^127.  The size does not fall where T or B grow (34 MB at most): one
  * workspace of a server's largest call serves its smaller ones. */
 size_t ordermoe_prompt_attention_workspace_size(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t head_dim,
                                                 int32_t rotary_dim, int64_t T, int32_t B);

@@ -12,6 +12,8 @@ namespace ordermoe {
 namespace {
 
 constexpr int64_t INT_LIMIT = (int64_t)1 << 31;
+// (scores are taken in units of log 2: the factor has to be finite too)
+bool good_scale(float scale) { return std::isfinite(scale * 1.44269504f); }
 
 int hip_fail(int e, const char* where) {
     return fail(ORDERMOE_EHIP, std::string(where) + ": " + hipGetErrorString((hipError_t)e));
@@ -161,7 +163,7 @@ extern "C" int ordermoe_latent_attention(const ordermoe_latent_cache* C, const o
     const int rc = check_attention(C, H, B, max_q, max_pages, who);
     if (rc) return rc;
     if (T < 0 || T > (INT_LIMIT - 1) / H->n_q) return bad(who, "T * n_q must lie in [0, 2^31)");
-    if (!std::isfinite(scale) || !std::isfinite(decay)) return bad(who, "scale and decay must be finite");
+    if (!good_scale(scale) || !std::isfinite(decay)) return bad(who, "scale (times log2 e) and decay must be finite");
     if (T > 0 && B > 0 && (!good16(q) || !q_start || !ctx_len || !page_table || !good16(out)))
         return bad(who, "null pointer, or q or out not 16-byte aligned");
     if (mass_out ? mass_stride < 1 || (B > 0 && mass_stride > ((int64_t)1 << 40) / B) : mass != nullptr)
@@ -217,7 +219,7 @@ extern "C" int ordermoe_prompt_attention(int32_t dtype, int32_t n_q, int32_t n_k
     if (rc) return rc;
     // (the kernel counts positions in 32 bits and looks up to two tiles of 64 past the last one)
     if (L < 0 || L > INT_LIMIT - 128) return bad(who, "L must lie in [0, 2^31 - 128]");
-    if (!std::isfinite(scale)) return bad(who, "scale must be finite");
+    if (!good_scale(scale)) return bad(who, "scale (times log2 e) must be finite");
     if (T > 0 && B > 0 && (!good16(q) || !q_start || !kv_start || !good16(out) ||
                            (L > 0 && (!good16(k) || !good16(v) || (rotary_dim > 0 && !good16(r))))))
         return bad(who, "null pointer, or q, k, r, v or out not 16-byte aligned");

@@ -211,3 +211,10 @@ def test_eviction_s_workspace_serves_every_smaller_call():
     _grows(lambda B, pages, keep: f(ref(c), B, pages, keep),
            ([1, 2, 9, 500], [1, 2, 50, 100, 127, 128, 129, 200, 5000],
             [1, 10, 64, 127, 129, 1000, 3199, 3200, 3201, 4000, 6000, 6399, 6400, 9000, 1 << 20, (1 << 31) - 1]))
+
+
+@pytest.mark.parametrize("scale", [2.4e38, -3.4e38])
+def test_scales_whose_scores_in_units_of_log_2_have_no_factor(scale):
+    """scale * log2(e) is no finite number there: a score of 0 would be none either."""
+    assert _attend(_cache(), _heads(), scale=scale) == om.EINVAL and "latent_attention" in om.last_error()
+    assert _prompt(scale=scale) == om.EINVAL and "prompt_attention" in om.last_error()
