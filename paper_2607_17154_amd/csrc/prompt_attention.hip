@@ -20,7 +20,7 @@
 // K, the shared rotary part and V go straight from memory into LDS, keys two tiles ahead, values one: a tile's weights are
 // made beside the scores of the next.  Two waves a SIMD share the matrix unit and the vector instructions of the softmax,
 // which are busy 51% and 43% of the time: 12001 tokens x 32 heads of 128 + 64 1390 to 1510 us on different cards (970 to 1060
-// TFLOP/s of the part that is seen), 8 prompts of up to 4000 tokens, 32 heads over 8 of 128, 474 to 523.  A comparison and a
+// TFLOP/s of the part that is seen), 8 prompts of up to 4000 tokens, 32 heads over 8 of 128, 474 to 536.  A comparison and a
 // selection more per weight cost 7%.
 #include <hip/hip_runtime.h>
 
@@ -325,6 +325,8 @@ __device__ inline __attribute__((always_inline)) void attend_tile(char* __restri
             const int at = (4 * h + i) * Lay::RBD + (((col >> 3) ^ swap_v<BF, Lay::RBD>(i)) * 16) + (col & 7) * 2;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
+                // The weights in bf16: as large an error as the outputs' own rounding (0.0019 to 0.0023 of the outputs with both,
+                // 0.0017 with that alone); two parts of 16 bits together would double this product
                 u32x4 pf;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) pf[e] = bf16_pair(sc[tb][8 * k + 2 * e], sc[tb][8 * k + 2 * e + 1]);
