@@ -373,6 +373,7 @@ latent_attention_kernel(const LatentAttentionArgs a, int items, int rb_n) {
         auto work = [&](char* tile) __attribute__((always_inline)) {
         f32x4 sc = {};
         if (scores) {
+            LongSum<BF> dot;
             constexpr int RING = 6;    // steps whose reads are in registers or on their way
             const char* at[2];
 #pragma unroll
@@ -387,9 +388,10 @@ latent_attention_kernel(const LatentAttentionArgs a, int items, int rb_n) {
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
                 if (k + RING - 1 < KS) read(k + RING - 1);
-                sc = mma16<BF>(x[k % RING], q[k], sc);
+                dot.add(x[k % RING], q[k]);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            sc = dot.sum();
             const int t0 = p + 16 * tt;              // the wave's tokens
             const bool there = (ok >> tt) & 1, edge = t0 + 16 > s.ctx || !there;
             sc = sc * scale2;
@@ -873,7 +875,7 @@ __global__ void __launch_bounds__(256) latent_out_kernel(const LatentAttentionAr
         }
     }
     __syncthreads();
-    f32x4 acc[2] = {};
+    LongSum<BF> sums[2];
     // (tokens past TOK: a row that is there, for columns that nobody reads)
     const char* o = &s_o[0][(c < TOK ? c : 0) * PITCH + (share * KS * 4 + g) * 16];
     const char* o_lo = &s_o[BF ? 1 : 0][(c < TOK ? c : 0) * PITCH + (share * KS * 4 + g) * 16];
@@ -882,14 +884,15 @@ __global__ void __launch_bounds__(256) latent_out_kernel(const LatentAttentionAr
         const u32x4 w0 = k < EARLY ? early[k < EARLY ? k : 0][0] : *(const u32x4*)(w + 64 * k);
         const u32x4 w1 = k < EARLY ? early[k < EARLY ? k : 0][1] : *(const u32x4*)(w + 16 * R * ES + 64 * k);
         const u32x4 hi = *(const u32x4*)(o + 64 * k);
-        acc[0] = mma16<BF>(w0, hi, acc[0]);
-        acc[1] = mma16<BF>(w1, hi, acc[1]);
+        sums[0].add(w0, hi);
+        sums[1].add(w1, hi);
         if constexpr (BF) {
             const u32x4 lo = *(const u32x4*)(o_lo + 64 * k);
-            acc[0] = mma16<BF>(w0, lo, acc[0]);
-            acc[1] = mma16<BF>(w1, lo, acc[1]);
+            sums[0].add(w0, lo);
+            sums[1].add(w1, lo);
         }
     }
+    f32x4 acc[2] = {sums[0].sum(), sums[1].sum()};
     if constexpr (SHARE > 1) {
         s_acc[wave][0][lane] = acc[0];
         s_acc[wave][1][lane] = acc[1];

@@ -628,3 +628,20 @@ def test_tokens_whose_every_score_is_minus_infinity(dtype):
     ba.rows[int(ba.table[0, 0]), 0, 128] = -float("inf")
     out, lse, mass = ba.run(2, stride=50)
     assert (out[0] == 0).all() and torch.isneginf(lse[0]).all() and torch.isfinite(lse[1:3]).all() and float(mass[0, 0]) == 0
+
+
+def test_long_sums_in_fp32_keep_their_bits():
+    """Outputs' error against 64 bits, of their size.  A sum of n products of varying sign, in one sum, is off by u sqrt(n / 6) of its
+    size (partial sums grow with the square root of their terms, each rounding is u / sqrt(3) of one); in four sums by half of that.
+    A score's error is its weight's: with scores of size 2, 2 * u sqrt(544 / 6) / 2; then the last product's, u sqrt(512 / 6) / 2; half as much
+    again for the weights' sums and exponentials."""
+    rng = np.random.default_rng(20)
+    R, rot, h, D = 512, 32, 20, 128
+    ba = _Batch(rng, "f32", np.linspace(85, 686, 8).astype(int), [1] * 8, h, D, R, rot, 16)
+    out, _, _ = ba.run(1)
+    off = size = 0.0
+    for b in range(8):
+        L = int(ba.ctx[b]) + 1
+        e = ol.latent_attention(_host(ba.q)[b:b + 1], ba.cached(b, L), np.ones((1, L), bool), _host(ba.wv), ba.scale)["out"]
+        off, size = off + ((_host(out)[b] - e[0]) ** 2).sum(), size + (e ** 2).sum()
+    assert (off / size) ** 0.5 <= 1.5 * U * np.hypot((R + rot) ** 0.5, R ** 0.5 / 2) / 6 ** 0.5
