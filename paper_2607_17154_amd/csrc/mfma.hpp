@@ -37,7 +37,7 @@ __device__ inline f32x4 mma16(u32x4 a, u32x4 b, f32x4 acc) {
 
 // The same for long sums: fp32 in four of them, to be added at the end.  A sum of n products whose signs vary is off by about
 // n / 2.4 roundings of a product's size (it grows with the square root of its terms), in four sums by half of that.  fp32 attention
-// against 64 bits: 0.5 to 2.0e-6 of the outputs in one sum, 0.3 to 0.7e-6 in four, for 0 to 2% of the time.  (bf16: an
+// against 64 bits: 0.6 to 1.9e-6 of the outputs in one sum, 0.3 to 0.7e-6 in four, which take 0 to 3% longer.  (bf16: an
 // instruction rounds once for 32 products.)
 template <bool BF>
 struct LongSum {
